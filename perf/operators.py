@@ -89,7 +89,7 @@ def draw(rng):
     W, dtype = rng.randint(2, 12), rng.choice(("bf16", "bf16", "f32"))
     V = _log_int(rng, 1000, 160000)
     return dict(op=op, B=min(64, _log_int(rng, 1, max(2, int((7e7 if dtype == "bf16" else 3.5e7) / V / W)))), W=W, n=rng.choice((W, W, min(32, 2 * W))), V=V, dtype=dtype,
-                temperature=rng.choice((1.0, 1.0, 0.7, 1.3)), finished=rng.random() < 0.5)
+                temperature=rng.choice((1.0, 1.0, 0.75, 1.25)), finished=rng.random() < 0.5)
 
 
 # ---- inputs ----
