@@ -85,6 +85,9 @@ typedef enum { SAKI_F32 = 0, SAKI_BF16 = 1 } saki_dtype;
 #define SAKI_ROW_BAD_ID      16u  /* proposal id outside [0,V) */
 #define SAKI_ROW_TIMEOUT     32u  /* a bounded on-device wait expired; the row's outputs are void */
 #define SAKI_ROW_NOT_COMPUTED 64u /* block verification: position after the first rejection */
+#define SAKI_ROW_BAD_PAGE   128u  /* paged cache: a page id outside [0, n_pages) among the sequence's pages */
+#define SAKI_ROW_BAD_LENGTH 256u  /* paged cache: a length or count below 0 or beyond what the sequence's page table holds */
+#define SAKI_ROW_NO_PAGES   512u  /* paged cache: too few free pages */
 
 /* Inputs of one routing call over N positions. */
 typedef struct {
@@ -353,8 +356,86 @@ SAKI_API int saki_sample_proposal(const void* logits, int64_t ld, int64_t N, int
                          int32_t dtype, float temperature, uint64_t seed,
                          uint64_t row_offset, int32_t* out, void* cuda_stream);
 
+/* The pages of a key-value cache (Section 3.5, Appendix K: the engine drafts and verifies on caches of its own, and a block's
+ * verdict is committed to them; the paper gives no layout).  A cache is three arrays of the caller's:
+ *   page_table [B, max_pages]  the pages of sequence b in the order of its positions, row stride ld_table; position x lies in
+ *                              entry x / page_size, slot x % page_size.  Entries behind the last page are -1
+ *   length     [B]             positions of sequence b; it holds ceil(length / page_size) pages
+ *   ref_count  [n_pages]       how many sequences hold a page; 0: the page is free.  (Sequences share pages after a fork.)
+ * Keys and values lie in pools of n_pages pages, one pair per layer, that saki_cache_write and saki_cache_copy_pages are
+ * given: the tables are kept once for all layers.  New pages are the free pages of the lowest ids, dealt out in the order of
+ * the sequences and of their positions, so that results do not depend on how the work was spread.
+ * `scratch`: saki_cache_scratch_bytes(B, max_pages, n_pages) bytes, 16-byte aligned, for the call's own use (calls on one cache
+ * are ordered by their stream anyway; caches used at the same time have scratch of their own).  saki_cache_truncate and
+ * saki_cache_write need none.
+ * All calls are asynchronous on the stream.  row_status ([B], may be NULL) receives 0 or SAKI_ROW_* bits; every flagged
+ * sequence counts towards saki_check(). */
+typedef struct {
+  int32_t* page_table; int64_t ld_table;
+  int32_t* length;
+  int32_t* ref_count;
+  void* scratch; int64_t scratch_bytes;
+  int64_t B;                  /* >= 0, at most 2^20 */
+  int32_t max_pages;          /* >= 1 */
+  int32_t n_pages;            /* 1 .. 2^30 */
+  int32_t page_size;          /* >= 1; max_pages * page_size below 2^31 */
+} saki_cache;
+SAKI_API int64_t saki_cache_scratch_bytes(int64_t B, int32_t max_pages, int32_t n_pages);
+
+/* n_new[b] more positions (n_new NULL: n_all for every sequence): the lengths grow, pages are added.  A sequence that goes on
+ * writing into a partly filled last page which others hold too gets a page of its own in its place: page copy_src[b] is to be
+ * copied to page copy_dst[b] (both [B]; -1: nothing to copy) in every pool, before anything is written.  Where all holders of
+ * such a page go on in this call, the first of them keeps it.  A sequence for which there is no room (a page for each
+ * shared last page counted, kept or not; the sequences before it served first, and their wants counted even where they were
+ * not) is flagged NO_PAGES, one whose table is too short, or whose count is negative, BAD_LENGTH, one whose last page's id is
+ * outside the pool BAD_PAGE; none of them changes. */
+SAKI_API int saki_cache_reserve(const saki_cache* cache, const int32_t* n_new, int32_t n_all, int32_t* copy_src, int32_t* copy_dst,
+                                uint32_t* row_status, void* cuda_stream);
+
+/* Sequence b keeps the first keep[b] + keep_add of its last `of` positions, or, with of < 0, of all of them; pages behind them are
+ * given back and their entries become -1.  With `of` = K + 1, keep = n_accept of saki_spec_verify and keep_add = 1 this commits a
+ * verified block (the token in front of the draft and the accepted prefix).  A number to keep outside [0, of], or `of` beyond the
+ * length: BAD_LENGTH, unchanged.  An entry given back whose id is outside the pool: BAD_PAGE, and no count changes for it. */
+SAKI_API int saki_cache_truncate(const saki_cache* cache, const int32_t* keep, int32_t keep_add, int32_t of, uint32_t* row_status,
+                                 void* cuda_stream);
+
+/* Every sequence becomes what its parent was: row b takes pages and length of row parent[b] + b / group * group (group >= 1: parents
+ * are counted within groups of that many sequences, as saki_beam_select gives them).  Nothing is copied: pages are shared until
+ * saki_cache_reserve parts them.  parent -1: the sequence is emptied; other ids outside the group: emptied and BAD_ID.  An id
+ * outside the pool among the pages that a row had or takes: BAD_PAGE (it is taken as it is, and counted nowhere); a length
+ * outside the table: BAD_LENGTH, read as 0. */
+SAKI_API int saki_cache_fork(const saki_cache* cache, const int32_t* parent, int64_t group, uint32_t* row_status, void* cuda_stream);
+
+/* The used pages move to the lowest ids: with n used pages, page copy_src[i] (id >= n, ascending) goes to page copy_dst[i] (id < n,
+ * ascending), -1 behind the last move (both arrays n_pages / 2 long); tables and counts follow, n_moves[0] (may be NULL)
+ * receives the number of moves.  Copy the pages (saki_cache_copy_pages) before the cache is used again.  A length outside the
+ * table: BAD_LENGTH, its row is left as it was; an id outside the pool: BAD_PAGE, it stays. */
+SAKI_API int saki_cache_compact(const saki_cache* cache, int32_t* copy_src, int32_t* copy_dst, int32_t* n_moves, uint32_t* row_status,
+                                void* cuda_stream);
+
+/* Page src[i] to page dst[i], i < n, in every one of n_pools pools (HOST arrays of device pointers, byte strides between pages
+ * and bytes per page; a page is one run of bytes).  Pairs with an id outside [0, n_pages) are passed over.  No page may be
+ * both read and written, or written twice (the lists of saki_cache_reserve and saki_cache_compact never do). */
+SAKI_API int saki_cache_copy_pages(void* const* pools, const int64_t* page_stride, const int64_t* page_bytes, int32_t n_pools,
+                                   const int32_t* src, const int32_t* dst, int64_t n, int32_t n_pages, void* cuda_stream);
+
+/* The keys and values of new positions go into one layer's pools: row j < n_new[b] (n_new NULL: Q) of sequence b is position
+ * length[b] - n_new[b] + j (the lengths are those after saki_cache_reserve).  Sequences whose row_status (of that call; may be
+ * NULL) has a flag are passed over, and so are positions below 0, counts outside [0, Q], lengths beyond the table and ids outside the pool. */
+typedef struct {
+  const void* k; int64_t k_seq, k_pos, k_head;              /* [B, Q, H, D], strides in elements, unit stride along D */
+  const void* v; int64_t v_seq, v_pos, v_head;
+  void* k_pages; int64_t kp_page, kp_pos, kp_head;          /* [n_pages, page_size, H, D] */
+  void* v_pages; int64_t vp_page, vp_pos, vp_head;
+  int32_t Q, H, D;
+  int32_t dtype;                                            /* of k, v and the pools */
+  const int32_t* n_new;                                     /* [B] or NULL */
+  const uint32_t* row_status;                               /* [B] or NULL */
+} saki_cache_kv;
+SAKI_API int saki_cache_write(const saki_cache* cache, const saki_cache_kv* kv, void* cuda_stream);
+
 /* Synchronises the stream, then reports and clears the number of rows flagged
- * NONFINITE, BAD_ID or TIMEOUT by calls on this device since the last check.
+ * NONFINITE, BAD_ID, TIMEOUT, BAD_PAGE, BAD_LENGTH or NO_PAGES by calls on this device since the last check.
  * Returns SAKI_ERR_ROW_STATUS if that number is non-zero.  n_flagged may be NULL. */
 SAKI_API int saki_check(void* cuda_stream, uint64_t* n_flagged);
 

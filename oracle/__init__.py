@@ -16,3 +16,6 @@ from .saki_oracle import (  # noqa: F401
     STAGE_SELECT, SELECT_RANDOM, SELECT_TV_WEIGHTED, select_tm,
     lmhead_lse,
 )
+from .rollout_oracle import (  # noqa: F401
+    ST_BAD_PAGE, ST_BAD_LENGTH, ST_NO_PAGES, Cache, paged_attention, beam_select,
+)

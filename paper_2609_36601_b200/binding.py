@@ -17,16 +17,20 @@ LIB_PATH = os.path.join(_HERE, "libsaki.so")
 _lib = None
 _fast = None          # the module _saki_torch, bound to the library
 _BOUND = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc", "saki_route_bwd_from_meta", "saki_select_tm",
-          "saki_spec_verify", "saki_sample_proposal", "saki_vshard_stage", "saki_last_error")
+          "saki_spec_verify", "saki_sample_proposal", "saki_vshard_stage", "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate",
+          "saki_cache_fork", "saki_cache_compact", "saki_cache_copy_pages", "saki_cache_write", "saki_last_error")
 
 SAKI_F32, SAKI_BF16 = 0, 1
 ROW_SATURATED, ROW_EPS_ZERO, ROW_MASKED, ROW_NONFINITE, ROW_BAD_ID, ROW_TIMEOUT, ROW_NOT_COMPUTED = 1, 2, 4, 8, 16, 32, 64
+ROW_BAD_PAGE, ROW_BAD_LENGTH, ROW_NO_PAGES = 128, 256, 512
 
 _FLOAT_FIELDS = ("lambda", "kl", "tv", "accept_prob", "logp_x", "logq_x", "logT_x", "logp_y", "logq_y", "logT_y", "loss")
 EXPORTS = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc", "saki_route_host",
            "saki_route_bwd_from_meta", "saki_select_tm", "saki_spec_verify",
            "saki_vshard_partial", "saki_vshard_stage", "saki_vshard_combine", "saki_vshard_combine_host",
            "saki_lmhead_scratch_bytes", "saki_lmhead_lse",
+           "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate", "saki_cache_fork", "saki_cache_compact",
+           "saki_cache_copy_pages", "saki_cache_write",
            "saki_sample_proposal", "saki_check", "saki_set_kernel", "saki_last_kernel", "saki_last_layout", "saki_last_rowsm_layout", "saki_redo_count",
            "saki_set_spec_early_out", "saki_spec_positions_routed", "saki_solve_evaluations", "saki_set_wait_limit", "saki_set_phase_clock", "saki_phase_cycles",
            "saki_launch_count",
@@ -103,6 +107,21 @@ class SakiSpecOut(C.Structure):
                 ("per_pos", SakiOut)]
 
 
+class SakiCache(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("ld_table", C.c_int64), ("length", C.c_void_p), ("ref_count", C.c_void_p),
+                ("scratch", C.c_void_p), ("scratch_bytes", C.c_int64), ("B", C.c_int64),
+                ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
+class SakiCacheKv(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("k_seq", C.c_int64), ("k_pos", C.c_int64), ("k_head", C.c_int64),
+                ("v", C.c_void_p), ("v_seq", C.c_int64), ("v_pos", C.c_int64), ("v_head", C.c_int64),
+                ("k_pages", C.c_void_p), ("kp_page", C.c_int64), ("kp_pos", C.c_int64), ("kp_head", C.c_int64),
+                ("v_pages", C.c_void_p), ("vp_page", C.c_int64), ("vp_pos", C.c_int64), ("vp_head", C.c_int64),
+                ("Q", C.c_int32), ("H", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32),
+                ("n_new", C.c_void_p), ("row_status", C.c_void_p)]
+
+
 def load_library(path: str | None = None):
     """Loads libsaki.so (built in-tree by `python -m paper_2609_36601_b200.build`)."""
     global _lib, _fast
@@ -149,6 +168,18 @@ def load_library(path: str | None = None):
     lib.saki_lmhead_lse.argtypes = [C.POINTER(SakiLmheadIn), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
                                     C.c_int64, C.c_void_p]
     lib.saki_lmhead_lse.restype = C.c_int
+    lib.saki_cache_scratch_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32]
+    lib.saki_cache_scratch_bytes.restype = C.c_int64
+    for f, args in (("reserve", [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+                    ("truncate", [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
+                    ("fork", [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+                    ("compact", [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+                    ("write", [C.POINTER(SakiCacheKv), C.c_void_p])):
+        getattr(lib, "saki_cache_" + f).argtypes = [C.POINTER(SakiCache), *args]
+        getattr(lib, "saki_cache_" + f).restype = C.c_int
+    lib.saki_cache_copy_pages.argtypes = [C.POINTER(C.c_void_p), C.POINTER(C.c_int64), C.POINTER(C.c_int64), C.c_int32, C.c_void_p,
+                                          C.c_void_p, C.c_int64, C.c_int32, C.c_void_p]
+    lib.saki_cache_copy_pages.restype = C.c_int
     lib.saki_set_wait_limit.argtypes = [C.c_int64]
     lib.saki_set_wait_limit.restype = C.c_int64
     lib.saki_set_phase_clock.argtypes = [C.c_int]
@@ -390,6 +421,81 @@ def spec_verify(s, t, draft, eps, temperature=1.0, seed=0, seq_offset=0, stream=
 def sample_proposal(s, temperature=1.0, seed=0, row_offset=0, stream=None):
     """saki_sample_proposal: x_i ~ softmax(s_i / temperature) by Philox-keyed Gumbel-max."""
     return (_fast or _tensors()).propose(s, temperature, seed, row_offset, _handle(stream))
+
+
+class PageCache:
+    """Page tables, lengths and counts of holders of a paged key-value cache (saki_cache), in one int32 tensor `meta` on the GPU:
+    `page_table` [B, max_pages], `length` [B] and `ref_count` [n_pages] are views of it.  `PageCache.empty` makes one without
+    positions.  The pools that hold keys and values, [n_pages, page_size, H, D] each, are the caller's, a pair per layer."""
+    __slots__ = ("meta", "B", "max_pages", "n_pages", "page_size", "scratch")
+
+    def __init__(self, meta, B, max_pages, n_pages, page_size):
+        if meta.dtype != torch.int32 or not meta.is_contiguous() or meta.numel() != B * max_pages + B + n_pages:
+            raise ValueError("a cache's tables must be a contiguous int32 tensor of B * max_pages + B + n_pages elements")
+        self.meta, self.B, self.max_pages, self.n_pages, self.page_size = meta, B, max_pages, n_pages, page_size
+        # what the integer calls work in: made along with the tables, so that whatever orders a stream behind them covers it
+        self.scratch = torch.empty((_lib or load_library()).saki_cache_scratch_bytes(B, max_pages, n_pages), dtype=torch.uint8, device=meta.device)
+
+    @classmethod
+    def empty(cls, B, max_pages, n_pages, page_size, device):
+        meta = torch.zeros(B * max_pages + B + n_pages, dtype=torch.int32, device=device)
+        meta[:B * max_pages] = -1
+        return cls(meta, B, max_pages, n_pages, page_size)
+
+    @property
+    def page_table(self):
+        return self.meta[:self.B * self.max_pages].view(self.B, self.max_pages)
+
+    @property
+    def length(self):
+        return self.meta[self.B * self.max_pages:self.B * (self.max_pages + 1)]
+
+    @property
+    def ref_count(self):
+        return self.meta[self.B * (self.max_pages + 1):]
+
+    def clone(self):
+        """Another cache with the same tables, on the same pools."""
+        return PageCache(self.meta.clone(), self.B, self.max_pages, self.n_pages, self.page_size)
+
+    def _args(self):
+        return self.meta, self.B, self.max_pages, self.n_pages, self.page_size
+
+
+def cache_reserve(cache, n_new, stream=None):
+    """saki_cache_reserve: n_new (an int, or an int32 tensor [B]) more positions for every sequence of a PageCache.  Returns
+    (copy_src, copy_dst, row_status), int32 [B]: pass the lists to copy_pages before anything is written (where the cache was forked),
+    the status to cache_write."""
+    return (_fast or _tensors()).cache_reserve(*cache._args(), cache.scratch, n_new, _handle(stream))
+
+
+def cache_write(cache, k, v, k_pages, v_pages, row_status=None, n_new=None, stream=None):
+    """saki_cache_write: k, v [B, Q, H, D] become the last Q (n_new[b]) positions of the sequences in one layer's pools
+    [n_pages, page_size, H, D].  Sequences that row_status (of cache_reserve) flags are passed over."""
+    (_fast or _tensors()).cache_write(*cache._args(), k, v, k_pages, v_pages, row_status, n_new, _handle(stream))
+
+
+def cache_truncate(cache, keep, of=None, keep_add=0, stream=None):
+    """saki_cache_truncate: sequence b keeps the first keep[b] + keep_add (int32 [B]) of its last `of` positions, or of all of
+    them (None).  cache_truncate(cache, verdict["n_accept"], of=K + 1, keep_add=1) commits a verified block.  Returns row_status."""
+    return (_fast or _tensors()).cache_truncate(*cache._args(), keep, keep_add, -1 if of is None else of, _handle(stream))
+
+
+def cache_fork(cache, parent, group=None, stream=None):
+    """saki_cache_fork: every sequence takes the pages of its parent (int32, B elements), counted within groups of `group`
+    sequences (None: all of them).  Returns row_status."""
+    return (_fast or _tensors()).cache_fork(*cache._args(), cache.scratch, parent, max(1, cache.B) if group is None else group, _handle(stream))
+
+
+def cache_compact(cache, stream=None):
+    """saki_cache_compact: the used pages move to the lowest ids.  Returns (copy_src, copy_dst, n_moves): pass the lists to
+    copy_pages before the cache is used again."""
+    return (_fast or _tensors()).cache_compact(*cache._args(), cache.scratch, _handle(stream))[:3]
+
+
+def copy_pages(pools, copy_src, copy_dst, stream=None):
+    """saki_cache_copy_pages: page copy_src[i] to page copy_dst[i] (int32; -1: none) in every pool of the sequence `pools`."""
+    (_fast or _tensors()).copy_pages(pools, copy_src, copy_dst, _handle(stream))
 
 
 def check(stream=None) -> int:

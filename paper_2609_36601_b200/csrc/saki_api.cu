@@ -621,6 +621,112 @@ SAKI_API int saki_sample_proposal(const void* logits, int64_t ld, int64_t N, int
   return SAKI_OK;
 }
 
+// ---- the pages of a key-value cache ----
+static bool aligned(const void* q, uintptr_t a) { return ((uintptr_t)q & (a - 1)) == 0; }
+
+static int cache_check(const saki_cache* c) {
+  g_err[0] = 0;
+  if (!c) return fail(SAKI_ERR_INVALID_ARG, "NULL argument struct");
+  if (c->B < 0 || c->B > (1 << 20)) return fail(SAKI_ERR_INVALID_ARG, "B must be in [0, 2^20] (got %lld)", (long long)c->B);
+  if (c->max_pages < 1 || c->page_size < 1 || (int64_t)c->max_pages * c->page_size >= (1LL << 31))
+    return fail(SAKI_ERR_INVALID_ARG, "max_pages and page_size must be >= 1 and their product below 2^31 (got %d, %d)", c->max_pages, c->page_size);
+  if (c->n_pages < 1 || c->n_pages > (1 << 30)) return fail(SAKI_ERR_INVALID_ARG, "n_pages must be in [1, 2^30] (got %d)", c->n_pages);
+  if (c->ld_table < c->max_pages) return fail(SAKI_ERR_INVALID_ARG, "page table stride smaller than max_pages");
+  return SAKI_OK;
+}
+// arrays and, where the call has a use for it, scratch
+static int cache_ready(const saki_cache* c, bool scratch, unsigned long long** flagged) {
+  if ((c->B > 0 && (!c->page_table || !c->length)) || !c->ref_count) return fail(SAKI_ERR_INVALID_ARG, "NULL page_table, length or ref_count pointer");
+  if (scratch) {
+    const int64_t need = cache_scratch_bytes(c->B, c->max_pages, c->n_pages);
+    if (!c->scratch || c->scratch_bytes < need) return fail(SAKI_ERR_INVALID_ARG, "scratch too small: %lld bytes needed", (long long)need);
+    if (!aligned(c->scratch, 16)) return fail(SAKI_ERR_UNSUPPORTED, "scratch must be 16-byte aligned");
+  }
+  return device_ready(flagged);
+}
+static int launched(cudaError_t e, int n, const char* what) {
+  if (e != cudaSuccess) return cuda_fail(e, what);
+  g_launches += (uint64_t)n;
+  return SAKI_OK;
+}
+
+SAKI_API int64_t saki_cache_scratch_bytes(int64_t B, int32_t max_pages, int32_t n_pages) {
+  return B < 0 || B > (1 << 20) || max_pages < 1 || n_pages < 1 ? 0 : cache_scratch_bytes(B, max_pages, n_pages);
+}
+
+SAKI_API int saki_cache_reserve(const saki_cache* cache, const int32_t* n_new, int32_t n_all, int32_t* copy_src, int32_t* copy_dst,
+                                uint32_t* row_status, void* cuda_stream) {
+  int rc = cache_check(cache);
+  if (rc) return rc;
+  if (!n_new && n_all < 0) return fail(SAKI_ERR_INVALID_ARG, "negative number of positions");
+  if (cache->B == 0) return SAKI_OK;
+  if (!copy_src || !copy_dst) return fail(SAKI_ERR_INVALID_ARG, "copy_src and copy_dst are required");
+  unsigned long long* flagged = nullptr;
+  rc = cache_ready(cache, true, &flagged);
+  return rc ? rc : launched(launch_cache_reserve(*cache, n_new, n_all, copy_src, copy_dst, row_status, flagged, (cudaStream_t)cuda_stream), 1, "reservation kernel launch");
+}
+
+SAKI_API int saki_cache_truncate(const saki_cache* cache, const int32_t* keep, int32_t keep_add, int32_t of, uint32_t* row_status,
+                                 void* cuda_stream) {
+  int rc = cache_check(cache);
+  if (rc || cache->B == 0) return rc;
+  if (!keep) return fail(SAKI_ERR_INVALID_ARG, "NULL keep pointer");
+  unsigned long long* flagged = nullptr;
+  rc = cache_ready(cache, false, &flagged);
+  return rc ? rc : launched(launch_cache_truncate(*cache, keep, keep_add, of, row_status, flagged, (cudaStream_t)cuda_stream), 1, "truncation kernel launch");
+}
+
+SAKI_API int saki_cache_fork(const saki_cache* cache, const int32_t* parent, int64_t group, uint32_t* row_status, void* cuda_stream) {
+  int rc = cache_check(cache);
+  if (rc) return rc;
+  if (group < 1) return fail(SAKI_ERR_INVALID_ARG, "group must be >= 1");
+  if (cache->B == 0) return SAKI_OK;
+  if (!parent) return fail(SAKI_ERR_INVALID_ARG, "NULL parent pointer");
+  unsigned long long* flagged = nullptr;
+  rc = cache_ready(cache, true, &flagged);
+  return rc ? rc : launched(launch_cache_fork(*cache, parent, group, row_status, flagged, (cudaStream_t)cuda_stream), 2, "fork kernel launch");
+}
+
+SAKI_API int saki_cache_compact(const saki_cache* cache, int32_t* copy_src, int32_t* copy_dst, int32_t* n_moves, uint32_t* row_status,
+                                void* cuda_stream) {
+  int rc = cache_check(cache);
+  if (rc) return rc;
+  if (cache->n_pages > 1 && (!copy_src || !copy_dst)) return fail(SAKI_ERR_INVALID_ARG, "copy_src and copy_dst are required");
+  unsigned long long* flagged = nullptr;
+  rc = cache_ready(cache, true, &flagged);
+  return rc ? rc : launched(launch_cache_compact(*cache, copy_src, copy_dst, n_moves, row_status, flagged, (cudaStream_t)cuda_stream), cache->B ? 2 : 1, "compaction kernel launch");
+}
+
+SAKI_API int saki_cache_copy_pages(void* const* pools, const int64_t* page_stride, const int64_t* page_bytes, int32_t n_pools,
+                                   const int32_t* src, const int32_t* dst, int64_t n, int32_t n_pages, void* cuda_stream) {
+  g_err[0] = 0;
+  if (n_pools < 0 || n < 0 || n_pages < 1) return fail(SAKI_ERR_INVALID_ARG, "negative number of pools or pairs, or no pages");
+  if (n_pools == 0 || n == 0) return SAKI_OK;
+  if (!pools || !page_stride || !page_bytes || !src || !dst) return fail(SAKI_ERR_INVALID_ARG, "NULL argument");
+  for (int k = 0; k < n_pools; ++k)
+    if (!pools[k] || page_bytes[k] < 1 || page_stride[k] < page_bytes[k]) return fail(SAKI_ERR_INVALID_ARG, "pool %d: NULL pointer, or a page stride smaller than a page", k);
+  unsigned long long* flagged = nullptr;
+  const int rc = device_ready(&flagged);
+  if (rc) return rc;
+  int launches = 0;
+  const cudaError_t e = launch_copy_pages(pools, page_stride, page_bytes, n_pools, src, dst, n, n_pages, &launches, (cudaStream_t)cuda_stream);
+  return launched(e, launches, "page copy kernel launch");
+}
+
+SAKI_API int saki_cache_write(const saki_cache* cache, const saki_cache_kv* kv, void* cuda_stream) {
+  int rc = cache_check(cache);
+  if (rc) return rc;
+  if (!kv) return fail(SAKI_ERR_INVALID_ARG, "NULL argument struct");
+  if (kv->dtype != SAKI_F32 && kv->dtype != SAKI_BF16) return fail(SAKI_ERR_INVALID_ARG, "unknown dtype %d", kv->dtype);
+  if (kv->Q < 0 || kv->H < 1 || kv->D < 1 || (int64_t)kv->H * kv->D > (1 << 24)) return fail(SAKI_ERR_INVALID_ARG, "Q must be >= 0, H and D >= 1 and H * D at most 2^24 (got %d, %d, %d)", kv->Q, kv->H, kv->D);
+  if (cache->B * kv->Q >= (1LL << 31)) return fail(SAKI_ERR_INVALID_ARG, "B * Q must be below 2^31");
+  if (cache->B == 0 || kv->Q == 0) return SAKI_OK;
+  if (!kv->k || !kv->v || !kv->k_pages || !kv->v_pages) return fail(SAKI_ERR_INVALID_ARG, "NULL k, v, k_pages or v_pages pointer");
+  unsigned long long* flagged = nullptr;
+  rc = cache_ready(cache, false, &flagged);
+  return rc ? rc : launched(launch_cache_write(*cache, *kv, (cudaStream_t)cuda_stream), 1, "cache write kernel launch");
+}
+
 SAKI_API int saki_check(void* cuda_stream, uint64_t* n_flagged) {
   g_err[0] = 0;
   unsigned long long* flagged = nullptr;
@@ -635,7 +741,7 @@ SAKI_API int saki_check(void* cuda_stream, uint64_t* n_flagged) {
   e = cudaMemcpy(flagged, &zero, sizeof(zero), cudaMemcpyHostToDevice);
   if (e != cudaSuccess) return cuda_fail(e, "cudaMemcpy");
   if (n_flagged) *n_flagged = h;
-  if (h) return fail(SAKI_ERR_ROW_STATUS, "%llu row(s) flagged (non-finite logits, bad proposal id or timeout)", h);
+  if (h) return fail(SAKI_ERR_ROW_STATUS, "%llu row(s) flagged (non-finite logits, bad id, timeout, or a paged cache's pages or lengths)", h);
   return SAKI_OK;
 }
 

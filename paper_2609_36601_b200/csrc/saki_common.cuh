@@ -255,6 +255,18 @@ cudaError_t launch_vshard_combine(const saki_vshard_in& in, int stage, const dou
 int64_t lmhead_scratch_bytes(int64_t N, int32_t V);
 cudaError_t launch_lmhead(const saki_lmhead_in& in, void* logits, int64_t ld_l, float* row_max, float* lse, void* scratch,
                           cudaStream_t st, const char** why);
+int64_t cache_scratch_bytes(int64_t B, int32_t max_pages, int32_t n_pages);
+cudaError_t launch_cache_reserve(const saki_cache& c, const int32_t* n_new, int32_t n_all, int32_t* src, int32_t* dst, uint32_t* status,
+                                 unsigned long long* flagged, cudaStream_t st);
+cudaError_t launch_cache_truncate(const saki_cache& c, const int32_t* keep, int32_t add, int32_t of, uint32_t* status,
+                                  unsigned long long* flagged, cudaStream_t st);
+cudaError_t launch_cache_fork(const saki_cache& c, const int32_t* parent, int64_t group, uint32_t* status, unsigned long long* flagged,
+                              cudaStream_t st);
+cudaError_t launch_cache_compact(const saki_cache& c, int32_t* src, int32_t* dst, int32_t* n_moves, uint32_t* status,
+                                 unsigned long long* flagged, cudaStream_t st);
+cudaError_t launch_copy_pages(void* const* pools, const int64_t* stride, const int64_t* bytes, int32_t n_pools, const int32_t* src,
+                              const int32_t* dst, int64_t n, int32_t n_pages, int* n_launches, cudaStream_t st);
+cudaError_t launch_cache_write(const saki_cache& c, const saki_cache_kv& w, cudaStream_t st);
 int vshard_combine_host(const saki_vshard_in& in, int stage, const double* gathered, double* state, const saki_out& out,
                         bool allow_fast);
 

@@ -10,7 +10,9 @@
 #include <ATen/ops/empty_native.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <algorithm>
 #include <string>
+#include <utility>
 #include <vector>
 #include "../../include/saki.h"
 
@@ -25,6 +27,13 @@ struct Lib {
   decltype(&saki_spec_verify) spec_verify;
   decltype(&saki_sample_proposal) sample_proposal;
   decltype(&saki_vshard_stage) vshard_stage;
+  decltype(&saki_cache_scratch_bytes) cache_scratch_bytes;
+  decltype(&saki_cache_reserve) cache_reserve;
+  decltype(&saki_cache_truncate) cache_truncate;
+  decltype(&saki_cache_fork) cache_fork;
+  decltype(&saki_cache_compact) cache_compact;
+  decltype(&saki_cache_copy_pages) cache_copy_pages;
+  decltype(&saki_cache_write) cache_write;
   decltype(&saki_last_error) last_error;
 };
 Lib lib = {};
@@ -426,6 +435,209 @@ PyObject* py_vshard_local(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- the pages of a key-value cache ----
+
+// The tensors' device and the caller's stream are the current ones while it lives: outputs and scratch come from the pool of the
+// stream that uses them.
+struct OnStream {
+  c10::cuda::OptionalCUDAGuard device;
+  c10::cuda::OptionalCUDAStreamGuard stream;
+  void* handle;
+  OnStream(at::Device dev, PyObject* given) {
+    if (!dev.is_cuda()) raise_value("tensors must be on a GPU");
+    device.set_device(dev);
+    if (given != Py_None) stream.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)word(given), dev.index()));
+    handle = (void*)c10::cuda::getCurrentCUDAStream(dev.index()).stream();
+  }
+};
+const char* type_name(at::ScalarType t) { return t == at::kInt ? "int32" : t == at::kByte ? "uint8" : t == at::kFloat ? "float32" : "other"; }
+// a contiguous tensor of n elements, any shape
+const at::Tensor& packed(PyObject* o, at::ScalarType type, int64_t n, at::Device dev, const char* name) {
+  const at::Tensor& v = tensor(o);
+  if (v.scalar_type() != type || v.numel() != n || v.device() != dev || !v.is_contiguous())
+    raise_value(std::string(name) + " must be a contiguous " + type_name(type) + " tensor of " + std::to_string(n) + " elements on the same device");
+  return v;
+}
+int64_t step_of(const at::Tensor& t, int64_t d) { return t.size(d) > 1 ? t.stride(d) : 0; }      // (of a dimension of one: never used)
+
+struct Cache {
+  saki_cache c = {};
+  at::Device dev = at::kCPU;
+  at::Tensor scratch;
+};
+constexpr int CACHE_ARGS = 5;      // meta, B, max_pages, n_pages, page_size
+Cache cache_of(PyObject* const* a) {
+  Cache k;
+  const at::Tensor& m = tensor(a[0]);
+  saki_cache& c = k.c;
+  c.B = integer(a[1]);
+  const int64_t max_pages = integer(a[2]), n_pages = integer(a[3]), page = integer(a[4]);
+  if (c.B < 0 || max_pages < 1 || n_pages < 1 || page < 1 || max_pages > INT32_MAX || n_pages > INT32_MAX || page > INT32_MAX || c.B > INT32_MAX)
+    raise_value("a cache has B >= 0 sequences, and at least one page per sequence, page and position");
+  c.max_pages = (int32_t)max_pages; c.n_pages = (int32_t)n_pages; c.page_size = (int32_t)page; c.ld_table = max_pages;
+  if (m.scalar_type() != at::kInt || !m.is_contiguous() || m.numel() != c.B * max_pages + c.B + n_pages)
+    raise_value("a cache's tables must be a contiguous int32 tensor of B * max_pages + B + n_pages elements");
+  k.dev = m.device();
+  c.page_table = (int32_t*)m.data_ptr();
+  c.length = c.page_table + c.B * max_pages;
+  c.ref_count = c.length + c.B;
+  return k;
+}
+void with_scratch(Cache& k, PyObject* o) {
+  k.c.scratch_bytes = lib.cache_scratch_bytes(k.c.B, k.c.max_pages, k.c.n_pages);
+  if (o == Py_None) k.scratch = empty({k.c.scratch_bytes}, at::kByte, k.dev);
+  else {
+    k.scratch = tensor(o);
+    if (k.scratch.device() != k.dev || !k.scratch.is_contiguous() || (int64_t)(k.scratch.numel() * k.scratch.element_size()) < k.c.scratch_bytes)
+      raise_value("scratch must be a contiguous tensor of " + std::to_string(k.c.scratch_bytes) + " bytes on the cache's device");
+  }
+  k.c.scratch = k.scratch.data_ptr();
+}
+
+// cache_reserve(cache..., scratch, n_new, stream) -> (copy_src, copy_dst, row_status)
+PyObject* py_cache_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, CACHE_ARGS + 3);
+    Cache k = cache_of(a);
+    const OnStream on(k.dev, a[7]);
+    with_scratch(k, a[5]);
+    const int32_t* each = nullptr;
+    int64_t all = 0;
+    if (THPVariable_Check(a[6])) each = (const int32_t*)packed(a[6], at::kInt, k.c.B, k.dev, "n_new").data_ptr();
+    else if ((all = integer(a[6])) > INT32_MAX || all < INT32_MIN) raise_value("n_new out of range");
+    const at::Tensor src = empty({k.c.B}, at::kInt, k.dev), dst = empty({k.c.B}, at::kInt, k.dev), st = empty({k.c.B}, at::kInt, k.dev);
+    check_rc(unlocked([&] { return lib.cache_reserve(&k.c, each, (int32_t)all, (int32_t*)src.data_ptr(), (int32_t*)dst.data_ptr(), (uint32_t*)st.data_ptr(), on.handle); }));
+    Owned x(THPVariable_Wrap(src)), y(THPVariable_Wrap(dst)), z(THPVariable_Wrap(st));
+    return PyTuple_Pack(3, x.p, y.p, z.p);
+  });
+}
+
+// cache_truncate(cache..., keep, keep_add, of, stream) -> row_status
+PyObject* py_cache_truncate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, CACHE_ARGS + 4);
+    Cache k = cache_of(a);
+    const OnStream on(k.dev, a[8]);
+    const int32_t* const keep = (const int32_t*)packed(a[5], at::kInt, k.c.B, k.dev, "keep").data_ptr();
+    const int64_t add = integer(a[6]), of = integer(a[7]);
+    if (add > INT32_MAX || add < INT32_MIN || of > INT32_MAX || of < INT32_MIN) raise_value("keep_add or of out of range");
+    const at::Tensor st = empty({k.c.B}, at::kInt, k.dev);
+    check_rc(unlocked([&] { return lib.cache_truncate(&k.c, keep, (int32_t)add, (int32_t)of, (uint32_t*)st.data_ptr(), on.handle); }));
+    return THPVariable_Wrap(st);
+  });
+}
+
+// cache_fork(cache..., scratch, parent, group, stream) -> row_status
+PyObject* py_cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, CACHE_ARGS + 4);
+    Cache k = cache_of(a);
+    const OnStream on(k.dev, a[8]);
+    with_scratch(k, a[5]);
+    const int32_t* const parent = (const int32_t*)packed(a[6], at::kInt, k.c.B, k.dev, "parent").data_ptr();
+    const int64_t group = integer(a[7]);
+    const at::Tensor st = empty({k.c.B}, at::kInt, k.dev);
+    check_rc(unlocked([&] { return lib.cache_fork(&k.c, parent, group, (uint32_t*)st.data_ptr(), on.handle); }));
+    return THPVariable_Wrap(st);
+  });
+}
+
+// cache_compact(cache..., scratch, stream) -> (copy_src, copy_dst, n_moves, row_status)
+PyObject* py_cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, CACHE_ARGS + 2);
+    Cache k = cache_of(a);
+    const OnStream on(k.dev, a[6]);
+    with_scratch(k, a[5]);
+    const int64_t half = k.c.n_pages / 2;
+    const at::Tensor src = empty({half}, at::kInt, k.dev), dst = empty({half}, at::kInt, k.dev), moves = empty({}, at::kInt, k.dev), st = empty({k.c.B}, at::kInt, k.dev);
+    check_rc(unlocked([&] { return lib.cache_compact(&k.c, (int32_t*)src.data_ptr(), (int32_t*)dst.data_ptr(), (int32_t*)moves.data_ptr(), (uint32_t*)st.data_ptr(), on.handle); }));
+    Owned x(THPVariable_Wrap(src)), y(THPVariable_Wrap(dst)), z(THPVariable_Wrap(moves)), w(THPVariable_Wrap(st));
+    return PyTuple_Pack(4, x.p, y.p, z.p, w.p);
+  });
+}
+
+// bytes of a page, if a page of the pool is one run of bytes
+int64_t page_bytes(const at::Tensor& t) {
+  std::vector<std::pair<int64_t, int64_t>> dims;
+  for (int64_t d = 1; d < t.dim(); ++d)
+    if (t.size(d) != 1) dims.emplace_back(t.stride(d), t.size(d));
+  std::sort(dims.begin(), dims.end());
+  int64_t run = 1;
+  for (const auto& d : dims) {
+    if (d.first != run) raise_value("a page of a pool must be one run of memory");
+    run *= d.second;
+  }
+  return run * (int64_t)t.element_size();
+}
+// copy_pages(pools, copy_src, copy_dst, stream)
+PyObject* py_copy_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, 4);
+    Owned seq(PySequence_Fast(a[0], "pools must be a sequence of tensors"));
+    const int m = (int)PySequence_Fast_GET_SIZE(seq.p);
+    if (m == 0) Py_RETURN_NONE;
+    const at::Tensor &src = tensor(a[1]);
+    const at::Device dev = src.device();
+    const OnStream on(dev, a[3]);
+    packed(a[1], at::kInt, src.numel(), dev, "copy_src");
+    const at::Tensor& dst = packed(a[2], at::kInt, src.numel(), dev, "copy_dst");
+    std::vector<void*> pool((size_t)m);
+    std::vector<int64_t> step((size_t)m), bytes((size_t)m);
+    int64_t pages = 0;
+    for (int i = 0; i < m; ++i) {
+      const at::Tensor& t = tensor(PySequence_Fast_GET_ITEM(seq.p, i));
+      if (t.device() != dev || t.dim() < 2 || t.numel() == 0) raise_value("a pool must be a tensor [n_pages, ...] on the lists' device");
+      if (i == 0) pages = t.size(0);
+      if (t.size(0) != pages || pages > INT32_MAX) raise_value("the pools of a call have the same number of pages");
+      pool[(size_t)i] = t.data_ptr();
+      bytes[(size_t)i] = page_bytes(t);
+      step[(size_t)i] = pages > 1 ? t.stride(0) * (int64_t)t.element_size() : bytes[(size_t)i];
+    }
+    check_rc(unlocked([&] {
+      return lib.cache_copy_pages(pool.data(), step.data(), bytes.data(), m, (const int32_t*)src.data_ptr(), (const int32_t*)dst.data_ptr(), src.numel(), (int32_t)pages, on.handle);
+    }));
+    Py_RETURN_NONE;
+  });
+}
+
+int kv_dtype(const at::Tensor& t) {
+  if (t.scalar_type() == at::kFloat) return SAKI_F32;
+  if (t.scalar_type() == at::kBFloat16) return SAKI_BF16;
+  raise_value(std::string("unsupported dtype ") + c10::toString(t.scalar_type()));
+}
+void check_pool(const at::Tensor& t, const at::Tensor& like, at::Device dev, int64_t n_pages, int64_t page, int64_t H, int64_t D, const char* name) {
+  if (t.dim() != 4 || t.device() != dev || t.scalar_type() != like.scalar_type() || t.size(1) != page || t.size(2) != H || t.size(3) != D ||
+      (n_pages >= 0 && t.size(0) != n_pages) || (D > 1 && t.stride(3) != 1))
+    raise_value(std::string(name) + " must be a tensor [n_pages, page_size, H, D] of the other tensors' type and device, with unit stride along D");
+}
+// cache_write(cache..., k, v, k_pages, v_pages, row_status, n_new, stream)
+PyObject* py_cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, CACHE_ARGS + 7);
+    Cache c = cache_of(a);
+    const OnStream on(c.dev, a[11]);
+    const at::Tensor &k = tensor(a[5]), &v = tensor(a[6]), &kp = tensor(a[7]), &vp = tensor(a[8]);
+    if (k.dim() != 4 || !v.sizes().equals(k.sizes()) || v.scalar_type() != k.scalar_type() || k.size(0) != c.c.B || k.device() != c.dev || v.device() != c.dev ||
+        (k.size(3) > 1 && (k.stride(3) != 1 || v.stride(3) != 1)))
+      raise_value("k and v must be [B, Q, H, D] of one type on the cache's device, with unit stride along D");
+    const int64_t H = k.size(2), D = k.size(3);
+    check_pool(kp, k, c.dev, c.c.n_pages, c.c.page_size, H, D, "k_pages");
+    check_pool(vp, k, c.dev, c.c.n_pages, c.c.page_size, H, D, "v_pages");
+    if (k.size(1) > INT32_MAX || H > INT32_MAX || D > INT32_MAX) raise_value("sizes out of range");
+    saki_cache_kv w = {};
+    w.k = k.data_ptr(); w.k_seq = step_of(k, 0); w.k_pos = step_of(k, 1); w.k_head = step_of(k, 2);
+    w.v = v.data_ptr(); w.v_seq = step_of(v, 0); w.v_pos = step_of(v, 1); w.v_head = step_of(v, 2);
+    w.k_pages = kp.data_ptr(); w.kp_page = step_of(kp, 0); w.kp_pos = step_of(kp, 1); w.kp_head = step_of(kp, 2);
+    w.v_pages = vp.data_ptr(); w.vp_page = step_of(vp, 0); w.vp_pos = step_of(vp, 1); w.vp_head = step_of(vp, 2);
+    w.Q = (int32_t)k.size(1); w.H = (int32_t)H; w.D = (int32_t)D; w.dtype = kv_dtype(k);
+    if (a[9] != Py_None) w.row_status = (const uint32_t*)packed(a[9], at::kInt, c.c.B, c.dev, "row_status").data_ptr();
+    if (a[10] != Py_None) w.n_new = (const int32_t*)packed(a[10], at::kInt, c.c.B, c.dev, "n_new").data_ptr();
+    check_rc(unlocked([&] { return lib.cache_write(&c.c, &w, on.handle); }));
+    Py_RETURN_NONE;
+  });
+}
+
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))py_bind, METH_FASTCALL, nullptr},
     {"alloc_outputs", (PyCFunction)(void (*)(void))py_alloc_outputs, METH_FASTCALL, nullptr},
@@ -434,6 +646,12 @@ PyMethodDef methods[] = {
     {"select", (PyCFunction)(void (*)(void))py_select, METH_FASTCALL, nullptr},
     {"spec", (PyCFunction)(void (*)(void))py_spec, METH_FASTCALL, nullptr},
     {"propose", (PyCFunction)(void (*)(void))py_propose, METH_FASTCALL, nullptr},
+    {"cache_reserve", (PyCFunction)(void (*)(void))py_cache_reserve, METH_FASTCALL, nullptr},
+    {"cache_truncate", (PyCFunction)(void (*)(void))py_cache_truncate, METH_FASTCALL, nullptr},
+    {"cache_fork", (PyCFunction)(void (*)(void))py_cache_fork, METH_FASTCALL, nullptr},
+    {"cache_compact", (PyCFunction)(void (*)(void))py_cache_compact, METH_FASTCALL, nullptr},
+    {"copy_pages", (PyCFunction)(void (*)(void))py_copy_pages, METH_FASTCALL, nullptr},
+    {"cache_write", (PyCFunction)(void (*)(void))py_cache_write, METH_FASTCALL, nullptr},
     {"vshard_local", (PyCFunction)(void (*)(void))py_vshard_local, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_saki_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
