@@ -434,6 +434,32 @@ typedef struct {
 } saki_cache_kv;
 SAKI_API int saki_cache_write(const saki_cache* cache, const saki_cache_kv* kv, void* cuda_stream);
 
+/* Beam selection over vocabulary rows: of the continuations (w, v) of the W beams of every group, with keys
+ *     score[b,w] + logits[b,w,v] / temperature - log sum_u exp(logits[b,w,u] / temperature)
+ * the n with the largest keys, largest first; ties go to the lower w * V + v, and within a beam the order is that of the logits.  Keys are
+ * formed in float64 (from a log-sum-exp of float32 exponentials, some 1e-8 off).  A finished beam (finished[b,w] != 0) has one
+ * continuation, `pad`, with the key score[b,w]; its logits are not read.  -inf logits and beams of score -inf have no continuations; where
+ * fewer than n are left, parent and token are -1 and the score -inf.  A beam with a NaN or +inf logit, or a NaN or +inf score, is flagged
+ * NONFINITE and has none either.  `parent` is the beam within its group: what saki_cache_fork takes with group = W (where n = W).
+ * scratch: saki_beam_scratch_bytes(B, W, V, n) bytes, 256-byte aligned, owned by one call at a time. */
+typedef struct {
+  const void* logits; int64_t ld_seq, ld_beam;              /* [B, W, V], strides in elements, unit stride along V */
+  const float* score;                                       /* [B, W] */
+  const uint8_t* finished;                                  /* [B, W] or NULL */
+  int64_t B;                                                /* >= 0; B * W at most 2^20, blocks of the call below 2^31 */
+  int32_t W, V, n;                                          /* W 1..64, V 2..2^22, n 1..64 */
+  int32_t dtype, pad;                                       /* pad in [0, V) */
+  float temperature;                                        /* finite, >= 1e-30 */
+} saki_beam_in;
+typedef struct {
+  int32_t* parent;        /* [B, n] */
+  int32_t* token;         /* [B, n] */
+  float* score;           /* [B, n] the keys */
+  uint32_t* row_status;   /* [B, W] or NULL */
+} saki_beam_out;
+SAKI_API int64_t saki_beam_scratch_bytes(int64_t B, int32_t W, int32_t V, int32_t n);
+SAKI_API int saki_beam_select(const saki_beam_in* in, const saki_beam_out* out, void* scratch, int64_t scratch_bytes, void* cuda_stream);
+
 /* Synchronises the stream, then reports and clears the number of rows flagged
  * NONFINITE, BAD_ID, TIMEOUT, BAD_PAGE, BAD_LENGTH or NO_PAGES by calls on this device since the last check.
  * Returns SAKI_ERR_ROW_STATUS if that number is non-zero.  n_flagged may be NULL. */

@@ -190,7 +190,7 @@ def beam_select(logits, score, n, temperature=1.0, finished=None, pad=0):
             m = z.max()
             if m == -np.inf:
                 continue
-            keys[w] = score[b, w] + (z - (m + np.log(np.exp(z - m).sum())))
+            keys[w] = score[b, w] + ((z - m) - np.log(np.exp(z - m).sum()))
         flat = keys.reshape(-1)
         order = np.argsort(-flat, kind="stable")[:n]
         for i, at in enumerate(order):

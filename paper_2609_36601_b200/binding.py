@@ -18,7 +18,7 @@ _lib = None
 _fast = None          # the module _saki_torch, bound to the library
 _BOUND = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc", "saki_route_bwd_from_meta", "saki_select_tm",
           "saki_spec_verify", "saki_sample_proposal", "saki_vshard_stage", "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate",
-          "saki_cache_fork", "saki_cache_compact", "saki_cache_copy_pages", "saki_cache_write", "saki_last_error")
+          "saki_cache_fork", "saki_cache_compact", "saki_cache_copy_pages", "saki_cache_write", "saki_beam_scratch_bytes", "saki_beam_select", "saki_last_error")
 
 SAKI_F32, SAKI_BF16 = 0, 1
 ROW_SATURATED, ROW_EPS_ZERO, ROW_MASKED, ROW_NONFINITE, ROW_BAD_ID, ROW_TIMEOUT, ROW_NOT_COMPUTED = 1, 2, 4, 8, 16, 32, 64
@@ -30,7 +30,7 @@ EXPORTS = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc",
            "saki_vshard_partial", "saki_vshard_stage", "saki_vshard_combine", "saki_vshard_combine_host",
            "saki_lmhead_scratch_bytes", "saki_lmhead_lse",
            "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate", "saki_cache_fork", "saki_cache_compact",
-           "saki_cache_copy_pages", "saki_cache_write",
+           "saki_cache_copy_pages", "saki_cache_write", "saki_beam_scratch_bytes", "saki_beam_select",
            "saki_sample_proposal", "saki_check", "saki_set_kernel", "saki_last_kernel", "saki_last_layout", "saki_last_rowsm_layout", "saki_redo_count",
            "saki_set_spec_early_out", "saki_spec_positions_routed", "saki_solve_evaluations", "saki_set_wait_limit", "saki_set_phase_clock", "saki_phase_cycles",
            "saki_launch_count",
@@ -122,6 +122,16 @@ class SakiCacheKv(C.Structure):
                 ("n_new", C.c_void_p), ("row_status", C.c_void_p)]
 
 
+class SakiBeamIn(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("ld_seq", C.c_int64), ("ld_beam", C.c_int64), ("score", C.c_void_p), ("finished", C.c_void_p),
+                ("B", C.c_int64), ("W", C.c_int32), ("V", C.c_int32), ("n", C.c_int32), ("dtype", C.c_int32), ("pad", C.c_int32),
+                ("temperature", C.c_float)]
+
+
+class SakiBeamOut(C.Structure):
+    _fields_ = [("parent", C.c_void_p), ("token", C.c_void_p), ("score", C.c_void_p), ("row_status", C.c_void_p)]
+
+
 def load_library(path: str | None = None):
     """Loads libsaki.so (built in-tree by `python -m paper_2609_36601_b200.build`)."""
     global _lib, _fast
@@ -180,6 +190,10 @@ def load_library(path: str | None = None):
     lib.saki_cache_copy_pages.argtypes = [C.POINTER(C.c_void_p), C.POINTER(C.c_int64), C.POINTER(C.c_int64), C.c_int32, C.c_void_p,
                                           C.c_void_p, C.c_int64, C.c_int32, C.c_void_p]
     lib.saki_cache_copy_pages.restype = C.c_int
+    lib.saki_beam_scratch_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32]
+    lib.saki_beam_scratch_bytes.restype = C.c_int64
+    lib.saki_beam_select.argtypes = [C.POINTER(SakiBeamIn), C.POINTER(SakiBeamOut), C.c_void_p, C.c_int64, C.c_void_p]
+    lib.saki_beam_select.restype = C.c_int
     lib.saki_set_wait_limit.argtypes = [C.c_int64]
     lib.saki_set_wait_limit.restype = C.c_int64
     lib.saki_set_phase_clock.argtypes = [C.c_int]
@@ -421,6 +435,14 @@ def spec_verify(s, t, draft, eps, temperature=1.0, seed=0, seq_offset=0, stream=
 def sample_proposal(s, temperature=1.0, seed=0, row_offset=0, stream=None):
     """saki_sample_proposal: x_i ~ softmax(s_i / temperature) by Philox-keyed Gumbel-max."""
     return (_fast or _tensors()).propose(s, temperature, seed, row_offset, _handle(stream))
+
+
+def beam_select(logits, score, n, temperature=1.0, finished=None, pad=0, stream=None):
+    """saki_beam_select: the n best continuations of every group of beams.  logits [B, W, V], score float32 [B, W] (sums of
+    log-probabilities so far), finished uint8 [B, W] or None: such a beam goes on with the token `pad` and its own score.  Returns
+    a dict of parent, token (int32 [B, n]), score (float32 [B, n]) and row_status (int32 [B, W])."""
+    parent, token, best, status = (_fast or _tensors()).beams(logits, score, n, temperature, finished, pad, _handle(stream))
+    return {"parent": parent, "token": token, "score": best, "row_status": status}
 
 
 class PageCache:

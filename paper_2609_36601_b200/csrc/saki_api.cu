@@ -727,6 +727,38 @@ SAKI_API int saki_cache_write(const saki_cache* cache, const saki_cache_kv* kv, 
   return rc ? rc : launched(launch_cache_write(*cache, *kv, (cudaStream_t)cuda_stream), 1, "cache write kernel launch");
 }
 
+// ---- beam selection ----
+static int beam_check(int64_t B, int32_t W, int32_t V, int32_t n) {
+  g_err[0] = 0;
+  if (W < 1 || W > 64 || n < 1 || n > 64) return fail(SAKI_ERR_INVALID_ARG, "W and n must be in [1,64] (got %d, %d)", W, n);
+  if (B < 0 || B > (1 << 20) || B * W > (1 << 20)) return fail(SAKI_ERR_INVALID_ARG, "B must be >= 0 and B * W at most 2^20");
+  if (V < 2 || V > (1 << 22)) return fail(SAKI_ERR_INVALID_ARG, "V must be in [2, 2^22] (got %d)", V);
+  return SAKI_OK;
+}
+
+SAKI_API int64_t saki_beam_scratch_bytes(int64_t B, int32_t W, int32_t V, int32_t n) { return beam_check(B, W, V, n) ? 0 : beam_scratch_bytes(B, W, V, n); }
+
+SAKI_API int saki_beam_select(const saki_beam_in* in, const saki_beam_out* out, void* scratch, int64_t scratch_bytes, void* cuda_stream) {
+  g_err[0] = 0;
+  if (!in || !out) return fail(SAKI_ERR_INVALID_ARG, "NULL argument struct");
+  int rc = beam_check(in->B, in->W, in->V, in->n);
+  if (rc) return rc;
+  if (in->dtype != SAKI_F32 && in->dtype != SAKI_BF16) return fail(SAKI_ERR_INVALID_ARG, "unknown dtype %d", in->dtype);
+  if (!(in->temperature >= 1e-30f) || std::isinf(in->temperature)) return fail(SAKI_ERR_INVALID_ARG, "temperature must be finite and >= 1e-30");
+  if (in->pad < 0 || in->pad >= in->V) return fail(SAKI_ERR_INVALID_ARG, "pad must be in [0,V) (got %d)", in->pad);
+  if (in->ld_seq < 0 || (in->W > 1 && in->ld_beam < in->V)) return fail(SAKI_ERR_INVALID_ARG, "beam stride smaller than V, or a negative stride");
+  if (in->B == 0) return SAKI_OK;
+  if (!in->logits || !in->score || !out->parent || !out->token || !out->score || !scratch)
+    return fail(SAKI_ERR_INVALID_ARG, "NULL logits, score, parent, token or scratch pointer");
+  if (scratch_bytes < beam_scratch_bytes(in->B, in->W, in->V, in->n))
+    return fail(SAKI_ERR_INVALID_ARG, "scratch too small: %lld bytes needed", (long long)beam_scratch_bytes(in->B, in->W, in->V, in->n));
+  if (!aligned(scratch, 256)) return fail(SAKI_ERR_UNSUPPORTED, "scratch must be 256-byte aligned");
+  unsigned long long* flagged = nullptr;
+  rc = device_ready(&flagged);
+  if (rc) return rc;
+  return launched(launch_beams(*in, *out, scratch, flagged, (cudaStream_t)cuda_stream), 2, "beam selection kernel launch");
+}
+
 SAKI_API int saki_check(void* cuda_stream, uint64_t* n_flagged) {
   g_err[0] = 0;
   unsigned long long* flagged = nullptr;

@@ -1,0 +1,357 @@
+// Beam selection over vocabulary rows: the n best continuations of a group of W beams by the sum of the beam's score and the
+// log-probability of the token.
+//
+// Within a beam the order of the keys is that of the logits, so a row is read once: a block holds a slice of it in registers, sums
+// its exponentials, and picks the slice's n best logits.  For those, a bar: of the maxima of the 64 groups of four threads the n-th
+// largest is at most the slice's n-th largest logit, and little below it as a rule.  What reaches the bar (about n elements) goes to a list in
+// shared memory, is ranked by counting, and leaves as n sorted pairs.  Slices that would overflow the list (hundreds of equal logits) are picked one
+// by one instead.  A second, small kernel joins the slices of a beam (log-sum-exp in float64) and the beams of a group (float64 keys).
+#include "saki_device.cuh"
+#include <algorithm>
+
+namespace saki {
+
+namespace {
+
+constexpr int BT = 256, BWARPS = BT / 32, GROUPS = 64, LIST = 512;
+
+struct BeamParams {
+  saki_beam_in in;
+  saki_beam_out out;
+  int slices, slice;        // per row, and elements of one
+  float c_hi, c_lo;         // log2(e) / temperature
+  uint64_t* cand;           // [B * W][slices][n] pairs of a slice, best first; 0: none
+  double2* part;            // [B * W][slices] (maximum, sum of 2^(c (x - maximum))) of a slice
+  unsigned long long* flagged;
+};
+
+// a pair (logit, token) as one word: larger logits first, then lower tokens; never 0 for a logit above -inf
+__device__ __forceinline__ uint64_t pair_word(float x, uint32_t v) {
+  const uint32_t u = __float_as_uint(x + 0.f);      // (-0 counts as 0)
+  const uint32_t o = u & 0x80000000u ? ~u : u | 0x80000000u;
+  return ((uint64_t)o << 32) | (0xffffffffu - v);
+}
+__device__ __forceinline__ float pair_logit(uint64_t w) {
+  const uint32_t o = (uint32_t)(w >> 32);
+  return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+__device__ __forceinline__ uint32_t pair_token(uint64_t w) { return 0xffffffffu - (uint32_t)w; }
+
+template <typename T> struct Vec;
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int E = 8;
+  uint32_t r[4];
+  __device__ __forceinline__ float2 pair(int i) const { return unpack_bf16x2(r[i]); }
+  __device__ __forceinline__ void set(int i, float x, float y) { r[i] = pack_bf16x2(x, y); }
+};
+template <> struct Vec<float> {
+  static constexpr int E = 4;
+  uint32_t r[4];
+  __device__ __forceinline__ float2 pair(int i) const { return make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])); }
+  __device__ __forceinline__ void set(int i, float x, float y) { r[2 * i] = __float_as_uint(x); r[2 * i + 1] = __float_as_uint(y); }
+};
+
+// what was unpacked from x before is not kept for what comes: 64 elements as floats are more than the registers hold
+template <typename T, int NV> __device__ __forceinline__ void keep_packed(Vec<T> (&x)[NV]) {
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+r"(x[k].r[i]));
+}
+
+struct BeamShared {
+  float group_max[GROUPS];
+  float warp_max[BWARPS];
+  double warp_sum[BWARPS];
+  uint64_t warp_best[BWARPS];
+  float bar;
+  unsigned count;
+  uint64_t list[LIST];
+};
+
+// NV: 16-byte vectors that a thread holds
+template <typename T, int NV> __global__ void __launch_bounds__(BT, 3) beam_rows_kernel(const BeamParams p) {
+  constexpr int E = Vec<T>::E;
+  __shared__ BeamShared sh;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = p.in.V, n = p.in.n;
+  const int64_t row = blockIdx.x / p.slices;
+  const int slice = (int)(blockIdx.x - row * p.slices);
+  wait_for_predecessor();
+  launch_dependents();
+  uint64_t* const cand = p.cand + (row * p.slices + slice) * n;
+  double2* const part = p.part + row * p.slices + slice;
+  if ((p.in.finished && p.in.finished[row]) || !(fabsf(p.in.score[row]) < CUDART_INF_F)) return;      // (the joining kernel does not look at its slices)
+  const int64_t b = row / p.in.W;
+  const T* const s = (const T*)p.in.logits + b * p.in.ld_seq + (row - b * p.in.W) * p.in.ld_beam;
+  const bool vec = ((uintptr_t)s & 15) == 0;
+  const int v0 = slice * p.slice;
+  if (tid == 0) sh.count = 0;
+  Vec<T> x[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = v0 + (k * BT + tid) * E;
+    if (vec && v + E <= V) {
+      const uint4 a = __ldg((const uint4*)(s + v));
+      x[k].r[0] = a.x; x[k].r[1] = a.y; x[k].r[2] = a.z; x[k].r[3] = a.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i)
+        x[k].set(i, v + 2 * i < V ? ld_as_float(s, v + 2 * i) : -CUDART_INF_F, v + 2 * i + 1 < V ? ld_as_float(s, v + 2 * i + 1) : -CUDART_INF_F);
+    }
+  }
+  float mine = -CUDART_INF_F;
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) { const float2 a = x[k].pair(i); mine = fmaxf(mine, fmaxf(a.x, a.y)); }
+  keep_packed(x);
+  float m = mine;
+  m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+  if ((lane & 3) == 0) sh.group_max[tid >> 2] = m;
+#pragma unroll
+  for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (lane == 0) sh.warp_max[warp] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < BWARPS; ++w) m = fmaxf(m, sh.warp_max[w]);
+  if (m == -CUDART_INF_F) {        // nothing but -inf (or NaN)
+    bool nan = false;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) { const float2 a = x[k].pair(i); nan = nan || a.x != a.x || a.y != a.y; }
+    nan = __syncthreads_or(nan);
+    if (tid == 0) *part = make_double2(m, nan ? CUDART_NAN : 0.);
+    for (int i = tid; i < n; i += BT) cand[i] = 0;
+    return;
+  }
+  if (warp == 0) {                 // the bar, while the other warps sum
+    const float g0 = sh.group_max[lane], g1 = sh.group_max[lane + 32];
+    int r0 = 0, r1 = 0;
+    for (int i = 0; i < GROUPS; ++i) {
+      const float g = sh.group_max[i];
+      r0 += g > g0 || (g == g0 && i < lane);
+      r1 += g > g1 || (g == g1 && i < lane + 32);
+    }
+    if (r0 == n - 1) sh.bar = g0;
+    if (r1 == n - 1) sh.bar = g1;
+  }
+  // x - m is exact where it matters, and the constant has two terms: an error of the argument that is the same for all elements would not average out
+  float2 sum = make_float2(0.f, 0.f);
+  const float2 hi = splat(p.c_hi), lo = splat(p.c_lo), nm = splat(-m);
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {
+      const float2 d = fadd2(x[k].pair(i), nm);
+      // -inf: 2^-inf = 0 needs an argument without the second term (-inf * lo may be NaN)
+      const float2 a = ffma2(d, hi, fmul2(make_float2(fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f)), lo));
+      sum = fadd2(sum, ex2f2(a));
+    }
+  double total = warp_sum((double)sum.x + (double)sum.y);
+  if (lane == 0) sh.warp_sum[warp] = total;
+  __syncthreads();
+  const float bar = sh.bar;
+  if (tid == 0) {
+    total = 0;
+    for (int w = 0; w < BWARPS; ++w) total += sh.warp_sum[w];
+    *part = make_double2(m, total);
+  }
+  keep_packed(x);
+  if (mine >= bar && mine > -CUDART_INF_F) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float2 a = x[k].pair(i >> 1);
+        const float e = i & 1 ? a.y : a.x;
+        if (e >= bar && e > -CUDART_INF_F) {
+          const unsigned at = atomicAdd(&sh.count, 1u);
+          if (at < LIST) sh.list[at] = pair_word(e, (uint32_t)(v0 + (k * BT + tid) * E + i));
+        }
+      }
+  }
+  __syncthreads();
+  const int count = (int)sh.count;
+  if (count <= LIST) {
+    for (int i = tid; i < count; i += BT) {
+      const uint64_t w = sh.list[i];
+      int r = 0;
+      for (int j = 0; j < count; ++j) r += sh.list[j] > w;
+      if (r < n) cand[r] = w;
+    }
+    for (int i = count + tid; i < n; i += BT) cand[i] = 0;
+  } else {                          // one by one: the largest word below the last
+    uint64_t last = ~0ull;
+#pragma unroll 1
+    for (int r = 0; r < n; ++r) {
+      uint64_t best = 0;
+      keep_packed(x);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float2 a = x[k].pair(i >> 1);
+          const float e = i & 1 ? a.y : a.x;
+          const uint64_t w = e > -CUDART_INF_F ? pair_word(e, (uint32_t)(v0 + (k * BT + tid) * E + i)) : 0;
+          if (w < last && w > best) best = w;
+        }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) best = max(best, (uint64_t)__shfl_xor_sync(0xffffffffu, best, o));
+      if (lane == 0) sh.warp_best[warp] = best;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < BWARPS; ++w) best = max(best, sh.warp_best[w]);
+      __syncthreads();
+      if (tid == 0) cand[r] = best;
+      last = best;
+    }
+  }
+}
+
+struct Best { double key; int64_t at; };      // at: w * V + v
+__device__ __forceinline__ bool before(const Best& a, const Best& b) { return a.key > b.key || (a.key == b.key && a.at < b.at); }
+__device__ __forceinline__ Best warp_first(Best a) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const Best u = {__shfl_xor_sync(0xffffffffu, a.key, o), __shfl_xor_sync(0xffffffffu, a.at, o)};
+    if (before(u, a)) a = u;
+  }
+  return a;
+}
+
+// a block per group: a thread holds the heads of some of the sorted lists, one per beam and slice
+__global__ void __launch_bounds__(BT) beam_join_kernel(const BeamParams p) {
+  __shared__ double top[64], rest[64];     // the log-sum-exp of a beam is top / tau + rest
+  __shared__ int how[64];           // 0: nothing to choose, 1: slices, 2: finished
+  __shared__ Best first[BWARPS];
+  extern __shared__ unsigned char taken[];     // of every list
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = p.in.W, n = p.in.n, lists = W * p.slices;
+  const int64_t b = blockIdx.x;
+  const double tau = (double)p.in.temperature;
+  wait_for_predecessor();
+  launch_dependents();
+  for (int i = tid; i < lists; i += BT) taken[i] = 0;
+  for (int w = warp; w < W; w += BWARPS) {
+    const int64_t row = b * W + w;
+    const float score = p.in.score[row];
+    const bool done = p.in.finished && p.in.finished[row];
+    bool bad = !(score < CUDART_INF_F);
+    int h = 0;
+    if (!bad && score > -CUDART_INF_F) {
+      h = 2;
+      if (!done) {
+        float m = -CUDART_INF_F;
+        bool nan = false;
+        for (int s = lane; s < p.slices; s += 32) { const double2 a = p.part[row * p.slices + s]; m = fmaxf(m, (float)a.x); nan = nan || a.y != a.y; }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        bad = __any_sync(0xffffffffu, nan) || m == CUDART_INF_F;
+        h = bad || m == -CUDART_INF_F ? 0 : 1;
+        if (h) {
+          double sum = 0;
+          for (int s = lane; s < p.slices; s += 32) {
+            const double2 a = p.part[row * p.slices + s];
+            if (a.x > -CUDART_INF) sum += a.y * exp((a.x - (double)m) / tau);
+          }
+          sum = warp_sum(sum);
+          if (lane == 0) { top[w] = m; rest[w] = log(sum); }
+        }
+      }
+    }
+    if (lane == 0) {
+      how[w] = h;
+      if (p.out.row_status) p.out.row_status[row] = bad ? SAKI_ROW_NONFINITE : 0u;
+      if (bad) atomicAdd(p.flagged, 1ull);
+    }
+  }
+  __syncthreads();
+  auto head = [&](int l) -> Best {
+    const int w = l / p.slices, s = l - w * p.slices, k = taken[l];
+    const double score = (double)p.in.score[b * W + w];
+    if (how[w] == 2) return s == 0 && k == 0 ? Best{score, (int64_t)w * p.in.V + p.in.pad} : Best{-CUDART_INF, INT64_MAX};
+    if (how[w] == 0 || k >= n) return {-CUDART_INF, INT64_MAX};
+    const uint64_t c = p.cand[((b * W + w) * p.slices + s) * n + k];
+    if (c == 0) return {-CUDART_INF, INT64_MAX};
+    return {score + (((double)pair_logit(c) - top[w]) / tau - rest[w]), (int64_t)w * p.in.V + pair_token(c)};
+  };
+  Best mine = {-CUDART_INF, INT64_MAX};
+  int from = -1;
+  auto look = [&] {
+    mine = {-CUDART_INF, INT64_MAX};
+    from = -1;
+    for (int l = tid; l < lists; l += BT) {
+      const Best h = head(l);
+      if (before(h, mine)) { mine = h; from = l; }
+    }
+  };
+  look();
+  for (int r = 0; r < n; ++r) {
+    Best a = warp_first(mine);
+    if (lane == 0) first[warp] = a;
+    __syncthreads();
+    a = first[0];
+#pragma unroll
+    for (int w = 1; w < BWARPS; ++w)
+      if (before(first[w], a)) a = first[w];
+    __syncthreads();
+    const bool none = a.at == INT64_MAX;
+    if (tid == 0) {
+      const int w = none ? -1 : (int)(a.at / p.in.V);
+      p.out.parent[b * n + r] = w;
+      p.out.token[b * n + r] = none ? -1 : (int)(a.at - (int64_t)w * p.in.V);
+      p.out.score[b * n + r] = (float)a.key;
+    }
+    if (!none && mine.at == a.at) { ++taken[from]; look(); }
+  }
+}
+
+struct Layout { int nv, slice, slices; };
+constexpr int MAX_SMS = 256;
+// Slices as long as a thread's registers hold (eight vectors); shorter ones for few rows, so that there are two blocks for every
+// SM.  (V has at most 2^22 entries, so the lists of a group fit into the joining kernel's shared memory.)
+Layout layout(int64_t rows, int V, int dtype, int sms) {
+  const int e = dtype == SAKI_BF16 ? 8 : 4;
+  for (int nv = 8;; nv /= 2) {
+    const int slice = BT * nv * e, slices = (V + slice - 1) / slice;
+    if (nv == 1 || rows * slices >= 2 * std::min(sms, MAX_SMS)) return {nv, slice, slices};
+  }
+}
+int sm_count() {
+  int dev = 0, sms = 148;
+  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  return sms;
+}
+int64_t round256(int64_t x) { return (x + 255) & ~(int64_t)255; }
+
+}  // namespace
+
+// enough for either type and any number of SMs: slices of eight vectors, or, shorter, fewer than four for every SM
+int64_t beam_scratch_bytes(int64_t B, int32_t W, int32_t V, int32_t n) {
+  const int64_t rows = B * W, longest = BT * 8 * 4, most = std::max<int64_t>(rows * ((V + longest - 1) / longest), 4 * MAX_SMS);
+  return round256(most * n * 8) + round256(most * 16);
+}
+
+cudaError_t launch_beams(const saki_beam_in& in, const saki_beam_out& out, void* scratch, unsigned long long* flagged, cudaStream_t st) {
+  const int64_t rows = in.B * in.W;
+  const Layout l = layout(rows, in.V, in.dtype, sm_count());
+  BeamParams p = {};
+  p.in = in; p.out = out; p.slices = l.slices; p.slice = l.slice; p.flagged = flagged;
+  const double c = 1.4426950408889634 / (double)in.temperature;
+  p.c_hi = (float)c; p.c_lo = (float)(c - (double)p.c_hi);
+  p.cand = (uint64_t*)scratch;
+  p.part = (double2*)((char*)scratch + round256(rows * l.slices * in.n * 8));
+  const dim3 grid((unsigned)(rows * l.slices));
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, BT, 0, st, true, p); };
+  cudaError_t e;
+  if (in.dtype == SAKI_BF16) {
+    using T = __nv_bfloat16;
+    e = l.nv == 8 ? go(beam_rows_kernel<T, 8>) : l.nv == 4 ? go(beam_rows_kernel<T, 4>) : l.nv == 2 ? go(beam_rows_kernel<T, 2>) : go(beam_rows_kernel<T, 1>);
+  } else
+    e = l.nv == 8 ? go(beam_rows_kernel<float, 8>) : l.nv == 4 ? go(beam_rows_kernel<float, 4>) : l.nv == 2 ? go(beam_rows_kernel<float, 2>) : go(beam_rows_kernel<float, 1>);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(beam_join_kernel, dim3((unsigned)in.B), BT, (size_t)in.W * l.slices, st, true, p);
+}
+
+}  // namespace saki

@@ -34,6 +34,8 @@ struct Lib {
   decltype(&saki_cache_compact) cache_compact;
   decltype(&saki_cache_copy_pages) cache_copy_pages;
   decltype(&saki_cache_write) cache_write;
+  decltype(&saki_beam_scratch_bytes) beam_scratch_bytes;
+  decltype(&saki_beam_select) beam_select;
   decltype(&saki_last_error) last_error;
 };
 Lib lib = {};
@@ -638,6 +640,32 @@ PyObject* py_cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// beams(logits, score, n, temperature, finished, pad, stream) -> (parent, token, score, row_status)
+PyObject* py_beams(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, 7);
+    const at::Tensor& z = tensor(a[0]);
+    if (z.dim() != 3 || (z.size(2) > 1 && z.stride(2) != 1)) raise_value("logits must be [B, W, V] with unit stride along V");
+    const at::Device dev = z.device();
+    const int64_t B = z.size(0), W = z.size(1), V = z.size(2), m = integer(a[2]), pad = integer(a[5]);
+    if (W > INT32_MAX || V > INT32_MAX || m < 1 || m > 64 || pad < 0 || pad >= V) raise_value("n must be in [1,64] and pad in [0,V)");
+    saki_beam_in in = {};
+    in.dtype = dtype_code(z);
+    const OnStream on(dev, a[6]);
+    in.logits = z.data_ptr(); in.ld_seq = step_of(z, 0); in.ld_beam = W > 1 ? z.stride(1) : V;
+    in.score = (const float*)packed(a[1], at::kFloat, B * W, dev, "score").data_ptr();
+    if (a[4] != Py_None) in.finished = (const uint8_t*)packed(a[4], at::kByte, B * W, dev, "finished").data_ptr();
+    in.B = B; in.W = (int32_t)W; in.V = (int32_t)V; in.n = (int32_t)m; in.pad = (int32_t)pad; in.temperature = (float)number(a[3]);
+    const at::Tensor parent = empty({B, m}, at::kInt, dev), token = empty({B, m}, at::kInt, dev), score = empty({B, m}, at::kFloat, dev), st = empty({B, W}, at::kInt, dev);
+    const int64_t bytes = lib.beam_scratch_bytes(B, in.W, in.V, in.n);
+    const at::Tensor scratch = empty({bytes}, at::kByte, dev);
+    saki_beam_out out = {(int32_t*)parent.data_ptr(), (int32_t*)token.data_ptr(), (float*)score.data_ptr(), (uint32_t*)st.data_ptr()};
+    check_rc(unlocked([&] { return lib.beam_select(&in, &out, scratch.data_ptr(), bytes, on.handle); }));
+    Owned x(THPVariable_Wrap(parent)), y(THPVariable_Wrap(token)), w(THPVariable_Wrap(score)), v(THPVariable_Wrap(st));
+    return PyTuple_Pack(4, x.p, y.p, w.p, v.p);
+  });
+}
+
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))py_bind, METH_FASTCALL, nullptr},
     {"alloc_outputs", (PyCFunction)(void (*)(void))py_alloc_outputs, METH_FASTCALL, nullptr},
@@ -652,6 +680,7 @@ PyMethodDef methods[] = {
     {"cache_compact", (PyCFunction)(void (*)(void))py_cache_compact, METH_FASTCALL, nullptr},
     {"copy_pages", (PyCFunction)(void (*)(void))py_copy_pages, METH_FASTCALL, nullptr},
     {"cache_write", (PyCFunction)(void (*)(void))py_cache_write, METH_FASTCALL, nullptr},
+    {"beams", (PyCFunction)(void (*)(void))py_beams, METH_FASTCALL, nullptr},
     {"vshard_local", (PyCFunction)(void (*)(void))py_vshard_local, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_saki_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
