@@ -434,6 +434,39 @@ typedef struct {
 } saki_cache_kv;
 SAKI_API int saki_cache_write(const saki_cache* cache, const saki_cache_kv* kv, void* cuda_stream);
 
+/* Attention of new tokens, one or a drafted block, over such a cache (the evaluation of drafted positions by student and teacher,
+ * Appendix K).  Query j of sequence b stands at position p = length[b] - n + j, n = n_query[b] or Q, and sees the positions
+ * x <= p, with window > 0 of them only x > p - window and x < sinks.  Per head h (key head h / (Hq / H)):
+ *     s_x = scale <q, k_x>,  lse = log sum_x exp(s_x),  out = sum_x exp(s_x - lse) v_x
+ * A query that sees nothing (p < 0, j >= n), or no score above -inf: out 0, lse -inf.  Keys and values of positions that a query does not
+ * see have no influence, whatever they hold; non-finite ones that it sees make its output non-finite.  bf16: products on the tensor cores,
+ * sums, maxima and exponentials in float32, the weights in two bf16 terms (16 bits); f32: float32 throughout.  A sequence with a length outside
+ * [0, max_pages * page_size], or n outside [0, Q], is flagged BAD_LENGTH, one with an id outside the pool among the pages that its
+ * queries see BAD_PAGE: out 0, lse -inf.
+ * Requirements: Q 1..32, Hq a multiple of H, Hq / H <= 64, D <= 256 and a multiple of 8 (f32: 4); 16-byte aligned pools, and strides
+ * of the pools that are multiples of 16 bytes (SAKI_ERR_UNSUPPORTED otherwise).  scratch: saki_paged_attention_scratch_bytes(in) bytes,
+ * 256-byte aligned, owned by one call at a time. */
+typedef struct {
+  const void* q; int64_t q_seq, q_pos, q_head;              /* [B, Q, Hq, D], strides in elements, unit stride along D */
+  const void* k_pages; int64_t kp_page, kp_pos, kp_head;    /* [n_pages, page_size, H, D] */
+  const void* v_pages; int64_t vp_page, vp_pos, vp_head;
+  const int32_t* page_table; int64_t ld_table;              /* [B, max_pages] */
+  const int32_t* length;                                    /* [B], the new tokens included */
+  const int32_t* n_query;                                   /* [B] or NULL */
+  int64_t B;                                                /* >= 0, at most 2^20 */
+  int32_t Q, Hq, H, D, page_size, max_pages, n_pages;
+  int32_t dtype;                                            /* of q, the pools and out */
+  int32_t window, sinks;                                    /* window 0: all positions */
+  float scale;
+} saki_attn_in;
+typedef struct {
+  void* out; int64_t o_seq, o_pos, o_head;                  /* [B, Q, Hq, D] */
+  float* lse;                                               /* [B, Q, Hq] or NULL */
+  uint32_t* row_status;                                     /* [B] or NULL */
+} saki_attn_out;
+SAKI_API int64_t saki_paged_attention_scratch_bytes(const saki_attn_in* in);
+SAKI_API int saki_paged_attention(const saki_attn_in* in, const saki_attn_out* out, void* scratch, int64_t scratch_bytes, void* cuda_stream);
+
 /* Beam selection over vocabulary rows: of the continuations (w, v) of the W beams of every group, with keys
  *     score[b,w] + logits[b,w,v] / temperature - log sum_u exp(logits[b,w,u] / temperature)
  * the n with the largest keys, largest first; ties go to the lower w * V + v, and within a beam the order is that of the logits.  Keys are

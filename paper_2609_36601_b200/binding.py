@@ -18,7 +18,8 @@ _lib = None
 _fast = None          # the module _saki_torch, bound to the library
 _BOUND = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc", "saki_route_bwd_from_meta", "saki_select_tm",
           "saki_spec_verify", "saki_sample_proposal", "saki_vshard_stage", "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate",
-          "saki_cache_fork", "saki_cache_compact", "saki_cache_copy_pages", "saki_cache_write", "saki_beam_scratch_bytes", "saki_beam_select", "saki_last_error")
+          "saki_cache_fork", "saki_cache_compact", "saki_cache_copy_pages", "saki_cache_write", "saki_paged_attention_scratch_bytes", "saki_paged_attention",
+          "saki_beam_scratch_bytes", "saki_beam_select", "saki_last_error")
 
 SAKI_F32, SAKI_BF16 = 0, 1
 ROW_SATURATED, ROW_EPS_ZERO, ROW_MASKED, ROW_NONFINITE, ROW_BAD_ID, ROW_TIMEOUT, ROW_NOT_COMPUTED = 1, 2, 4, 8, 16, 32, 64
@@ -30,7 +31,7 @@ EXPORTS = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc",
            "saki_vshard_partial", "saki_vshard_stage", "saki_vshard_combine", "saki_vshard_combine_host",
            "saki_lmhead_scratch_bytes", "saki_lmhead_lse",
            "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate", "saki_cache_fork", "saki_cache_compact",
-           "saki_cache_copy_pages", "saki_cache_write", "saki_beam_scratch_bytes", "saki_beam_select",
+           "saki_cache_copy_pages", "saki_cache_write", "saki_paged_attention_scratch_bytes", "saki_paged_attention", "saki_beam_scratch_bytes", "saki_beam_select",
            "saki_sample_proposal", "saki_check", "saki_set_kernel", "saki_last_kernel", "saki_last_layout", "saki_last_rowsm_layout", "saki_redo_count",
            "saki_set_spec_early_out", "saki_spec_positions_routed", "saki_solve_evaluations", "saki_set_wait_limit", "saki_set_phase_clock", "saki_phase_cycles",
            "saki_launch_count",
@@ -122,6 +123,21 @@ class SakiCacheKv(C.Structure):
                 ("n_new", C.c_void_p), ("row_status", C.c_void_p)]
 
 
+class SakiAttnIn(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_seq", C.c_int64), ("q_pos", C.c_int64), ("q_head", C.c_int64),
+                ("k_pages", C.c_void_p), ("kp_page", C.c_int64), ("kp_pos", C.c_int64), ("kp_head", C.c_int64),
+                ("v_pages", C.c_void_p), ("vp_page", C.c_int64), ("vp_pos", C.c_int64), ("vp_head", C.c_int64),
+                ("page_table", C.c_void_p), ("ld_table", C.c_int64), ("length", C.c_void_p), ("n_query", C.c_void_p), ("B", C.c_int64),
+                ("Q", C.c_int32), ("Hq", C.c_int32), ("H", C.c_int32), ("D", C.c_int32), ("page_size", C.c_int32),
+                ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("dtype", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class SakiAttnOut(C.Structure):
+    _fields_ = [("out", C.c_void_p), ("o_seq", C.c_int64), ("o_pos", C.c_int64), ("o_head", C.c_int64), ("lse", C.c_void_p),
+                ("row_status", C.c_void_p)]
+
+
 class SakiBeamIn(C.Structure):
     _fields_ = [("logits", C.c_void_p), ("ld_seq", C.c_int64), ("ld_beam", C.c_int64), ("score", C.c_void_p), ("finished", C.c_void_p),
                 ("B", C.c_int64), ("W", C.c_int32), ("V", C.c_int32), ("n", C.c_int32), ("dtype", C.c_int32), ("pad", C.c_int32),
@@ -190,6 +206,10 @@ def load_library(path: str | None = None):
     lib.saki_cache_copy_pages.argtypes = [C.POINTER(C.c_void_p), C.POINTER(C.c_int64), C.POINTER(C.c_int64), C.c_int32, C.c_void_p,
                                           C.c_void_p, C.c_int64, C.c_int32, C.c_void_p]
     lib.saki_cache_copy_pages.restype = C.c_int
+    lib.saki_paged_attention_scratch_bytes.argtypes = [C.POINTER(SakiAttnIn)]
+    lib.saki_paged_attention_scratch_bytes.restype = C.c_int64
+    lib.saki_paged_attention.argtypes = [C.POINTER(SakiAttnIn), C.POINTER(SakiAttnOut), C.c_void_p, C.c_int64, C.c_void_p]
+    lib.saki_paged_attention.restype = C.c_int
     lib.saki_beam_scratch_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32]
     lib.saki_beam_scratch_bytes.restype = C.c_int64
     lib.saki_beam_select.argtypes = [C.POINTER(SakiBeamIn), C.POINTER(SakiBeamOut), C.c_void_p, C.c_int64, C.c_void_p]
@@ -518,6 +538,14 @@ def cache_compact(cache, stream=None):
 def copy_pages(pools, copy_src, copy_dst, stream=None):
     """saki_cache_copy_pages: page copy_src[i] to page copy_dst[i] (int32; -1: none) in every pool of the sequence `pools`."""
     (_fast or _tensors()).copy_pages(pools, copy_src, copy_dst, _handle(stream))
+
+
+def paged_attention(q, k_pages, v_pages, page_table, length, scale=None, window=0, sinks=0, n_query=None, out=None, stream=None):
+    """saki_paged_attention: attention of the last Q (n_query[b], int32) positions of every sequence over a paged cache.  q [B, Q, Hq, D],
+    pools [n_pages, page_size, H, D] of its type, page_table int32 [B, max_pages], length int32 [B] (a PageCache's), scale 1 / sqrt(D)
+    where None; window > 0: only the last `window` positions and the first `sinks` are seen.  Returns (out like q, lse float32
+    [B, Q, Hq], row_status int32 [B])."""
+    return (_fast or _tensors()).attention(q, k_pages, v_pages, page_table, length, scale, window, sinks, n_query, out, _handle(stream))
 
 
 def check(stream=None) -> int:

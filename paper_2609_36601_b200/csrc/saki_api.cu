@@ -727,6 +727,47 @@ SAKI_API int saki_cache_write(const saki_cache* cache, const saki_cache_kv* kv, 
   return rc ? rc : launched(launch_cache_write(*cache, *kv, (cudaStream_t)cuda_stream), 1, "cache write kernel launch");
 }
 
+// ---- attention over a paged cache ----
+static int attention_check(const saki_attn_in* in) {
+  g_err[0] = 0;
+  if (!in) return fail(SAKI_ERR_INVALID_ARG, "NULL argument struct");
+  if (in->dtype != SAKI_F32 && in->dtype != SAKI_BF16) return fail(SAKI_ERR_INVALID_ARG, "unknown dtype %d", in->dtype);
+  if (in->B < 0 || in->B > (1 << 20)) return fail(SAKI_ERR_INVALID_ARG, "B must be in [0, 2^20] (got %lld)", (long long)in->B);
+  if (in->Q < 1 || in->Q > 32) return fail(SAKI_ERR_INVALID_ARG, "Q must be in [1,32] (got %d)", in->Q);
+  if (in->H < 1 || in->H > 65536 || in->Hq < 1 || in->Hq % in->H || in->Hq / in->H > 64)
+    return fail(SAKI_ERR_INVALID_ARG, "query heads must be a multiple, at most 64 times, of the key heads (got %d, %d)", in->Hq, in->H);
+  const int step = in->dtype == SAKI_BF16 ? 8 : 4;
+  if (in->D < step || in->D > 256 || in->D % step) return fail(SAKI_ERR_INVALID_ARG, "D must be a multiple of %d in [%d,256] (got %d)", step, step, in->D);
+  if (in->max_pages < 1 || in->page_size < 1 || (int64_t)in->max_pages * in->page_size >= (1LL << 31) || in->n_pages < 1)
+    return fail(SAKI_ERR_INVALID_ARG, "max_pages, page_size and n_pages must be >= 1, max_pages * page_size below 2^31");
+  if (in->ld_table < in->max_pages) return fail(SAKI_ERR_INVALID_ARG, "page table stride smaller than max_pages");
+  if (in->window < 0 || in->sinks < 0) return fail(SAKI_ERR_INVALID_ARG, "window and sinks must be >= 0");
+  if (!std::isfinite(in->scale)) return fail(SAKI_ERR_INVALID_ARG, "scale must be finite");
+  return SAKI_OK;
+}
+
+SAKI_API int64_t saki_paged_attention_scratch_bytes(const saki_attn_in* in) { return attention_check(in) ? 0 : attention_scratch_bytes(*in); }
+
+SAKI_API int saki_paged_attention(const saki_attn_in* in, const saki_attn_out* out, void* scratch, int64_t scratch_bytes, void* cuda_stream) {
+  int rc = attention_check(in);
+  if (rc) return rc;
+  if (!out) return fail(SAKI_ERR_INVALID_ARG, "NULL argument struct");
+  if (in->B == 0) return SAKI_OK;
+  if (!in->q || !in->k_pages || !in->v_pages || !in->page_table || !in->length || !out->out || !scratch)
+    return fail(SAKI_ERR_INVALID_ARG, "NULL q, k_pages, v_pages, page_table, length, out or scratch pointer");
+  if (scratch_bytes < attention_scratch_bytes(*in)) return fail(SAKI_ERR_INVALID_ARG, "scratch too small: %lld bytes needed", (long long)attention_scratch_bytes(*in));
+  const int64_t size = in->dtype == SAKI_BF16 ? 2 : 4;
+  bool ok = aligned(in->k_pages, 16) && aligned(in->v_pages, 16) && aligned(scratch, 256);
+  for (int64_t s : {in->kp_page, in->kp_pos, in->kp_head, in->vp_page, in->vp_pos, in->vp_head}) ok = ok && s * size % 16 == 0;
+  if (!ok) return fail(SAKI_ERR_UNSUPPORTED, "the pools and their strides must be multiples of 16 bytes, scratch 256-byte aligned");
+  unsigned long long* flagged = nullptr;
+  rc = device_ready(&flagged);
+  if (rc) return rc;
+  int launches = 0;
+  const cudaError_t e = launch_attention(*in, *out, scratch, flagged, &launches, (cudaStream_t)cuda_stream);
+  return launched(e, launches, "attention kernel launch");
+}
+
 // ---- beam selection ----
 static int beam_check(int64_t B, int32_t W, int32_t V, int32_t n) {
   g_err[0] = 0;

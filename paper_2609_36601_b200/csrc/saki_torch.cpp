@@ -11,6 +11,7 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <algorithm>
+#include <cmath>
 #include <string>
 #include <utility>
 #include <vector>
@@ -34,6 +35,8 @@ struct Lib {
   decltype(&saki_cache_compact) cache_compact;
   decltype(&saki_cache_copy_pages) cache_copy_pages;
   decltype(&saki_cache_write) cache_write;
+  decltype(&saki_paged_attention_scratch_bytes) paged_attention_scratch_bytes;
+  decltype(&saki_paged_attention) paged_attention;
   decltype(&saki_beam_scratch_bytes) beam_scratch_bytes;
   decltype(&saki_beam_select) beam_select;
   decltype(&saki_last_error) last_error;
@@ -640,6 +643,49 @@ PyObject* py_cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// attention(q, k_pages, v_pages, page_table, length, scale, window, sinks, n_query, out, stream) -> (out, lse, row_status)
+PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, 11);
+    const at::Tensor &q = tensor(a[0]), &kp = tensor(a[1]), &vp = tensor(a[2]), &table = tensor(a[3]);
+    if (q.dim() != 4 || kp.dim() != 4 || (q.size(3) > 1 && q.stride(3) != 1)) raise_value("q must be [B, Q, Hq, D] with unit stride along D, the pools [n_pages, page_size, H, D]");
+    const at::Device dev = q.device();
+    const int64_t B = q.size(0), Q = q.size(1), Hq = q.size(2), D = q.size(3), pages = kp.size(0), page = kp.size(1), H = kp.size(2);
+    check_pool(kp, q, dev, -1, page, H, D, "k_pages");
+    check_pool(vp, q, dev, pages, page, H, D, "v_pages");
+    if (table.dim() != 2 || table.size(0) != B || table.scalar_type() != at::kInt || table.device() != dev || (table.size(1) > 1 && table.stride(1) != 1))
+      raise_value("page_table must be an int32 tensor [B, max_pages] on the same device, with unit stride along the pages");
+    for (int64_t s : {Q, Hq, D, pages, page, H, table.size(1)})
+      if (s > INT32_MAX) raise_value("sizes out of range");
+    saki_attn_in in = {};
+    in.dtype = kv_dtype(q);
+    const OnStream on(dev, a[10]);
+    in.q = q.data_ptr(); in.q_seq = step_of(q, 0); in.q_pos = step_of(q, 1); in.q_head = step_of(q, 2);
+    in.k_pages = kp.data_ptr(); in.kp_page = step_of(kp, 0); in.kp_pos = step_of(kp, 1); in.kp_head = step_of(kp, 2);
+    in.v_pages = vp.data_ptr(); in.vp_page = step_of(vp, 0); in.vp_pos = step_of(vp, 1); in.vp_head = step_of(vp, 2);
+    in.page_table = (const int32_t*)table.data_ptr(); in.ld_table = B > 1 ? table.stride(0) : table.size(1);
+    in.length = (const int32_t*)packed(a[4], at::kInt, B, dev, "length").data_ptr();
+    if (a[8] != Py_None) in.n_query = (const int32_t*)packed(a[8], at::kInt, B, dev, "n_query").data_ptr();
+    in.B = B; in.Q = (int32_t)Q; in.Hq = (int32_t)Hq; in.H = (int32_t)H; in.D = (int32_t)D;
+    in.page_size = (int32_t)page; in.max_pages = (int32_t)table.size(1); in.n_pages = (int32_t)pages;
+    const int64_t window = integer(a[6]), sinks = integer(a[7]);
+    if (window < 0 || sinks < 0) raise_value("window and sinks must be >= 0");
+    in.window = (int32_t)std::min<int64_t>(window, INT32_MAX); in.sinks = (int32_t)std::min<int64_t>(sinks, INT32_MAX);
+    in.scale = a[5] == Py_None ? (float)(1.0 / std::sqrt((double)std::max<int64_t>(D, 1))) : (float)number(a[5]);
+    const at::Tensor out = a[9] == Py_None ? empty({B, Q, Hq, D}, q.scalar_type(), dev) : tensor(a[9]);
+    if (!out.sizes().equals(q.sizes()) || out.scalar_type() != q.scalar_type() || out.device() != dev || (D > 1 && out.stride(3) != 1))
+      raise_value("out must be like q, with unit stride along D");
+    const at::Tensor lse = empty({B, Q, Hq}, at::kFloat, dev), st = empty({B}, at::kInt, dev);
+    saki_attn_out o = {out.data_ptr(), step_of(out, 0), step_of(out, 1), step_of(out, 2), (float*)lse.data_ptr(), (uint32_t*)st.data_ptr()};
+    const int64_t bytes = lib.paged_attention_scratch_bytes(&in);
+    if (bytes == 0) raise_saki(SAKI_ERR_INVALID_ARG, lib.last_error());
+    const at::Tensor scratch = empty({bytes}, at::kByte, dev);
+    check_rc(unlocked([&] { return lib.paged_attention(&in, &o, scratch.data_ptr(), bytes, on.handle); }));
+    Owned x(THPVariable_Wrap(out)), y(THPVariable_Wrap(lse)), z(THPVariable_Wrap(st));
+    return PyTuple_Pack(3, x.p, y.p, z.p);
+  });
+}
+
 // beams(logits, score, n, temperature, finished, pad, stream) -> (parent, token, score, row_status)
 PyObject* py_beams(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -680,6 +726,7 @@ PyMethodDef methods[] = {
     {"cache_compact", (PyCFunction)(void (*)(void))py_cache_compact, METH_FASTCALL, nullptr},
     {"copy_pages", (PyCFunction)(void (*)(void))py_copy_pages, METH_FASTCALL, nullptr},
     {"cache_write", (PyCFunction)(void (*)(void))py_cache_write, METH_FASTCALL, nullptr},
+    {"attention", (PyCFunction)(void (*)(void))py_attention, METH_FASTCALL, nullptr},
     {"beams", (PyCFunction)(void (*)(void))py_beams, METH_FASTCALL, nullptr},
     {"vshard_local", (PyCFunction)(void (*)(void))py_vshard_local, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
