@@ -738,8 +738,8 @@ static int attention_check(const saki_attn_in* in) {
     return fail(SAKI_ERR_INVALID_ARG, "query heads must be a multiple, at most 64 times, of the key heads (got %d, %d)", in->Hq, in->H);
   const int step = in->dtype == SAKI_BF16 ? 8 : 4;
   if (in->D < step || in->D > 256 || in->D % step) return fail(SAKI_ERR_INVALID_ARG, "D must be a multiple of %d in [%d,256] (got %d)", step, step, in->D);
-  if (in->max_pages < 1 || in->page_size < 1 || (int64_t)in->max_pages * in->page_size >= (1LL << 31) || in->n_pages < 1)
-    return fail(SAKI_ERR_INVALID_ARG, "max_pages, page_size and n_pages must be >= 1, max_pages * page_size below 2^31");
+  if (in->max_pages < 1 || in->page_size < 1 || (int64_t)in->max_pages * in->page_size >= (1LL << 31) - 256 || in->n_pages < 1)
+    return fail(SAKI_ERR_INVALID_ARG, "max_pages, page_size and n_pages must be >= 1, max_pages * page_size below 2^31 - 256");
   if (in->ld_table < in->max_pages) return fail(SAKI_ERR_INVALID_ARG, "page table stride smaller than max_pages");
   if (in->window < 0 || in->sinks < 0) return fail(SAKI_ERR_INVALID_ARG, "window and sinks must be >= 0");
   if (!std::isfinite(in->scale)) return fail(SAKI_ERR_INVALID_ARG, "scale must be finite");
@@ -764,7 +764,7 @@ SAKI_API int saki_paged_attention(const saki_attn_in* in, const saki_attn_out* o
   rc = device_ready(&flagged);
   if (rc) return rc;
   int launches = 0;
-  const cudaError_t e = launch_attention(*in, *out, scratch, flagged, &launches, (cudaStream_t)cuda_stream);
+  const cudaError_t e = launch_attention(*in, *out, scratch, flagged, std::min<long long>(g_wait_limit.load(), 1LL << 61), &launches, (cudaStream_t)cuda_stream);
   return launched(e, launches, "attention kernel launch");
 }
 

@@ -268,8 +268,8 @@ cudaError_t launch_copy_pages(void* const* pools, const int64_t* stride, const i
                               const int32_t* dst, int64_t n, int32_t n_pages, int* n_launches, cudaStream_t st);
 cudaError_t launch_cache_write(const saki_cache& c, const saki_cache_kv& w, cudaStream_t st);
 int64_t attention_scratch_bytes(const saki_attn_in& in);
-cudaError_t launch_attention(const saki_attn_in& in, const saki_attn_out& out, void* scratch, unsigned long long* flagged, int* n_launches,
-                             cudaStream_t st);
+cudaError_t launch_attention(const saki_attn_in& in, const saki_attn_out& out, void* scratch, unsigned long long* flagged, long long wait_limit,
+                             int* n_launches, cudaStream_t st);
 int64_t beam_scratch_bytes(int64_t B, int32_t W, int32_t V, int32_t n);
 cudaError_t launch_beams(const saki_beam_in& in, const saki_beam_out& out, void* scratch, unsigned long long* flagged, cudaStream_t st);
 int vshard_combine_host(const saki_vshard_in& in, int stage, const double* gathered, double* state, const saki_out& out,
