@@ -14,40 +14,22 @@
 // padding by a factor of four and more.  bf16: m16n8k16; the weights go into the second product as two bf16 terms, so that they carry 16 bits: one
 // term would add an error as large as the rounding of the output (2^-9 each).  f32: m16n8k8 on tf32 terms, x = hi + lo with 11 bits each and
 // hi.hi + hi.lo + lo.hi: what is dropped is 2^-22 of a product and less.
-#include "saki_device.cuh"
-#include <cuda.h>
+#include "saki_attention.cuh"
 #include <algorithm>
 #include <cmath>
 #include <mutex>
 
 namespace saki {
 
-namespace {
+using namespace attn;
 
-struct AttnParams {
-  saki_attn_in in;
-  saki_attn_out out;
-  int G, R, RB;             // query heads per key head; rows of a key head (Q * G); blocks of rows
-  int q_vec;                // q can be read in 16-byte pieces
-  int box;                  // positions of a TMA box
-  int page_shift;           // page_size is 1 << page_shift; -1: no power of two
-  uint32_t q_sign;          // a negative scale turns the queries' signs
-  float c;                  // |scale| * log2(e), above 0
-  int4* desc;               // [workers] the segment that starts in a piece and goes on: (b, head and row block, pieces behind, status)
-  float* part;              // [workers][2] partial results: of the segment that goes on from the piece before, of the one that goes on behind
-  unsigned long long* flagged;
-  long long wait_limit;
-};
+namespace {
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool real) {      // zeros where not real
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_arrive(uint64_t* bar) {      // once the thread's copies so far are there
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
-}
-__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int x, int head, int slot, int page, uint64_t* bar) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-               ::"r"(dst), "l"(map), "r"(x), "r"(head), "r"(slot), "r"(page), "r"(smem_addr(bar)) : "memory");
 }
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
@@ -70,127 +52,6 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], 
 __device__ __forceinline__ void two_terms(uint32_t x, uint32_t& hi, uint32_t& lo) {
   hi = x & 0xffffe000u;
   lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) + 0x1000u;
-}
-
-// What the queries of a sequence see, in tiles of T positions: the tiles of the first `sk` positions, then those from tile m0 on.  (Positions are
-// below 2^31.)
-struct Span {
-  int n, p0, nq, lo, sk, ns, m0, nt;
-  uint32_t status;
-};
-template <int T> __device__ __forceinline__ Span span_of(const AttnParams& p, int64_t b) {
-  Span s;
-  s.n = p.in.length[b];
-  s.nq = p.in.n_query ? p.in.n_query[b] : p.in.Q;
-  s.status = 0;
-  if (s.n < 0 || (int64_t)s.n > (int64_t)p.in.max_pages * p.in.page_size || s.nq < 0 || s.nq > p.in.Q) { s.status = SAKI_ROW_BAD_LENGTH; s.n = 0; s.nq = 0; }
-  s.p0 = s.n - s.nq;
-  s.lo = p.in.window > 0 ? (int)max((int64_t)0, (int64_t)s.p0 - p.in.window + 1) : 0;
-  if (s.nq == 0) s.lo = s.n;
-  s.sk = s.nq == 0 ? 0 : min(p.in.sinks, s.lo);
-  s.ns = (int)(((unsigned)s.sk + T - 1) / T);
-  s.m0 = max(s.lo / T, s.ns);
-  s.nt = max(1, s.ns + max(0, (int)(((unsigned)s.n + T - 1) / T) - s.m0));
-  return s;
-}
-template <int T> __device__ __forceinline__ int tile_start(const Span& s, int t) { return (t < s.ns ? t : s.m0 + t - s.ns) * T; }
-
-// A place on the line of tiles: sequence, key head and row block, tile.
-template <int T> struct Cursor {
-  int b, hr, t;
-  Span s;
-  __device__ __forceinline__ void at(const AttnParams& p, int64_t b_, int64_t offset) {
-    b = (int)b_;
-    s = span_of<T>(p, b);
-    hr = (int)(offset / s.nt);
-    t = (int)(offset - (int64_t)hr * s.nt);
-  }
-  __device__ __forceinline__ void next(const AttnParams& p) {
-    if (++t < s.nt) return;
-    t = 0;
-    if (++hr < p.in.H * p.RB) return;
-    hr = 0;
-    if (++b < p.in.B) s = span_of<T>(p, b);
-  }
-};
-
-template <int THREADS> struct LineShared {
-  long long sum[THREADS / 32];
-  long long b[THREADS / 32], before[THREADS / 32];      // by worker of the block: the sequence of its first tile, tiles in front of it
-};
-// The pieces of a block's workers [u0, u0 + chunk) of the line: worker w of block i is number w * blocks + i (few tiles: one worker on each SM).  Every
-// block adds up all sequences' tiles, a few per thread.
-template <int T, int THREADS, int WORKERS> __device__ __forceinline__ void pieces(const AttnParams& p, LineShared<THREADS>& sh, long long& chunk, long long& total) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int64_t per = (p.in.B + THREADS - 1) / THREADS, b0 = min((int64_t)tid * per, p.in.B), b1 = min(b0 + per, p.in.B);
-  const int each = p.in.H * p.RB;
-  long long mine = 0;
-  for (int64_t b = b0; b < b1; ++b) mine += (long long)span_of<T>(p, b).nt * each;
-  long long upto = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += v;
-  }
-  if (lane == 31) sh.sum[warp] = upto;
-  __syncthreads();
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) {
-    if (w < warp) upto += sh.sum[w];
-    total += sh.sum[w];
-  }
-  chunk = max(1ll, (total + gridDim.x * WORKERS - 1) / (gridDim.x * WORKERS));
-#pragma unroll 1
-  for (int w = 0; w < WORKERS; ++w) {
-    const long long u0 = ((long long)w * gridDim.x + blockIdx.x) * chunk;
-    if (upto - mine <= u0 && u0 < upto) {
-      long long at = upto - mine;
-      int64_t b = b0;
-      for (;; ++b) {
-        const long long n = (long long)span_of<T>(p, b).nt * each;
-        if (u0 < at + n) break;
-        at += n;
-      }
-      sh.b[w] = b; sh.before[w] = at;
-    }
-  }
-  __syncthreads();
-}
-
-__device__ __forceinline__ int64_t out_at(const AttnParams& p, int64_t b, int h, int r) {
-  const int j = r / p.G;
-  return b * p.out.o_seq + j * p.out.o_pos + (int64_t)(h * p.G + r - j * p.G) * p.out.o_head;
-}
-__device__ __forceinline__ void put_lse(const AttnParams& p, int64_t b, int h, int r, float m, float l) {
-  if (!p.out.lse) return;
-  const int j = r / p.G;
-  p.out.lse[(b * p.in.Q + j) * p.in.Hq + h * p.G + r - j * p.G] = l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -CUDART_INF_F;
-}
-__device__ __forceinline__ void put_status(const AttnParams& p, int64_t b, uint32_t st) {
-  if (p.out.row_status) p.out.row_status[b] = st;
-  if (st) atomicAdd(p.flagged, 1ull);
-}
-
-// Segments (sequence, key head, row block) that several workers had a part of: ROWS rows of DP values, then ROWS pairs (m, l); l = -1: a bad
-// page, -2: a wait ran out.
-template <int ROWS, int DP> constexpr int PART = ROWS * (DP + 2);
-__device__ __forceinline__ uint32_t status_of(float l) { return l == -1.f ? SAKI_ROW_BAD_PAGE : l == -2.f ? SAKI_ROW_TIMEOUT : 0u; }
-
-// what a row sees: positions up to `to`, from `from` on or below `first`
-struct Sight {
-  int to, from, first;
-  __device__ __forceinline__ bool operator()(int x) const { return x <= to && (x >= from || x < first); }
-};
-__device__ __forceinline__ Sight sight_of(const AttnParams& p, const Span& s, int r) {      // r: row within the key head
-  const int j = r / p.G;
-  if (r >= p.R || j >= s.nq) return {-1, 0, 0};
-  const int at = s.p0 + j;
-  return {at, p.in.window > 0 ? (int)max((int64_t)0, (int64_t)at - p.in.window + 1) : 0, p.in.window > 0 ? p.in.sinks : 0};
-}
-// all rows see all of a tile's positions
-template <int T> __device__ __forceinline__ bool whole(const AttnParams& p, const Span& s, int x0) {
-  return s.nq == p.in.Q && x0 + (T - 1) <= s.p0 && (p.in.window <= 0 || x0 > s.n - 1 - p.in.window || x0 + T <= s.sk);
 }
 
 // NW: warps of a worker, 16 rows each
@@ -711,15 +572,22 @@ bool pool_map(CUtensorMap* map, const void* pool, int64_t page, int64_t pos, int
 
 }  // namespace
 
-int64_t attention_scratch_bytes(const saki_attn_in& in) { return MAX_WORKERS * 16 + MAX_WORKERS * 2 * part_floats(pick(in)) * 4; }
+// bf16 heads of up to 128 on pages of whole eights go to the kernel on tcgen05
+static bool on_umma(const saki_attn_in& in) { return in.dtype == SAKI_BF16 && in.D <= 128 && in.page_size % 8 == 0; }
+
+int64_t attention_scratch_bytes(const saki_attn_in& in) {
+  const Kernel k = pick(in);
+  int64_t most = MAX_WORKERS * 2 * part_floats(k);
+  if (on_umma(in)) most = std::max<int64_t>(most, MAX_WORKERS / 8 * 2 * (int64_t)umma_rows(in) * (k.dp + 2));
+  return MAX_WORKERS * 16 + most * 4;
+}
 
 cudaError_t launch_attention(const saki_attn_in& in, const saki_attn_out& out, void* scratch, unsigned long long* flagged, long long wait_limit,
                              int* n_launches, cudaStream_t st) {
-  const Kernel k = pick(in);
   AttnParams p = {};
   p.in = in; p.out = out; p.flagged = flagged;
   p.wait_limit = wait_limit > 0 ? wait_limit : WAIT_LIMIT_CYCLES;
-  p.G = in.Hq / in.H; p.R = in.Q * p.G; p.RB = (p.R + k.rows - 1) / k.rows;
+  p.G = in.Hq / in.H; p.R = in.Q * p.G;
   p.c = std::max(std::fabs(in.scale) * 1.4426950408889634f, 1e-37f);      // (scale 0: what is not seen has the score -inf, also times c)
   p.q_sign = in.scale < 0.f ? in.dtype == SAKI_BF16 ? 0x80008000u : 0x80000000u : 0u;
   p.page_shift = -1;
@@ -729,33 +597,45 @@ cudaError_t launch_attention(const saki_attn_in& in, const saki_attn_out& out, v
   p.q_vec = ((uintptr_t)in.q | (uintptr_t)(in.q_seq * size) | (uintptr_t)(in.q_pos * size) | (uintptr_t)(in.q_head * size)) % 16 == 0;
   p.desc = (int4*)scratch;
   p.part = (float*)((char*)scratch + MAX_WORKERS * 16);
-  // Boxes: as many positions of a page as a tile takes (8, 16 or 32).  A page that is no multiple of eight, or strides that the map does not take
+  Kernel k = pick(in);
+  bool umma = on_umma(in);
+  // Boxes: as many positions of a page as a tile takes.  A page that is no multiple of eight, or strides that the map does not take
   // (2^40 bytes), go through the plain loads.
   p.box = 1;
-  while (p.box < k.t && in.page_size % (2 * p.box) == 0) p.box *= 2;
+  while (p.box < (umma ? UMMA_T : k.t) && in.page_size % (2 * p.box) == 0) p.box *= 2;
   CUtensorMap k_map = {}, v_map = {};
   const bool tma = p.box >= 8 && pool_map(&k_map, in.k_pages, in.kp_page, in.kp_pos, in.kp_head, in, p.box) &&
                    pool_map(&v_map, in.v_pages, in.vp_page, in.vp_pos, in.vp_head, in, p.box);
-  const void* const fn = tma ? k.tma : k.plain;
-  int dev = 0, sms = 148, per = 1;
+  umma = umma && tma;
+  int dev = 0, sms = 148, per = 1, workers = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
-  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, fn, k.threads, k.smem);
   if (e != cudaSuccess) return e;
+  if (umma) { k.rows = umma_rows(in); k.t = UMMA_T; }
+  p.RB = (p.R + k.rows - 1) / k.rows;
   const int64_t most = in.B * in.H * p.RB * (((int64_t)in.max_pages * in.page_size + k.t - 1) / k.t);      // tiles, if every table were full
-  const int blocks = (int)std::min<int64_t>(most, std::min(sms * std::max(per, 1), MAX_WORKERS / k.workers));
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3((unsigned)k.threads); cfg.dynamicSmemBytes = (size_t)k.smem; cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at; cfg.numAttrs = 1;
-  void* args[] = {&p, &k_map, &v_map};
-  e = cudaLaunchKernelExC(&cfg, fn, args);
+  if (umma) {
+    workers = (int)std::min<int64_t>(most, std::min(sms, MAX_WORKERS / 8));
+    e = launch_umma(p, k_map, v_map, workers, st);
+  } else {
+    const void* const fn = tma ? k.tma : k.plain;
+    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, fn, k.threads, k.smem);
+    if (e != cudaSuccess) return e;
+    const int blocks = (int)std::min<int64_t>(most, std::min(sms * std::max(per, 1), MAX_WORKERS / k.workers));
+    workers = blocks * k.workers;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3((unsigned)k.threads); cfg.dynamicSmemBytes = (size_t)k.smem; cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at; cfg.numAttrs = 1;
+    void* args[] = {&p, &k_map, &v_map};
+    e = cudaLaunchKernelExC(&cfg, fn, args);
+  }
   if (e != cudaSuccess) return e;
   ++*n_launches;
-  e = in.dtype == SAKI_BF16 ? join<__nv_bfloat16>(p, k, blocks * k.workers, st) : join<float>(p, k, blocks * k.workers, st);
+  e = in.dtype == SAKI_BF16 ? join<__nv_bfloat16>(p, k, workers, st) : join<float>(p, k, workers, st);
   if (e == cudaSuccess) ++*n_launches;
   return e;
 }

@@ -1,0 +1,552 @@
+// The attention of saki_attention.cu on the fifth-generation tensor cores, for bf16 with D up to 128 and pages of whole eights.
+//
+// A tile is 128 positions of one key head, and the products are turned round: positions and head columns are the 128 rows of tcgen05.mma, the queries
+// (16, 32 or 64 rows of a key head) its columns.  So nothing is padded but the queries, and a tile costs a handful of instructions:
+//   scores^T [128 positions x N]  = K [128 x D] . Q^T [D x N]              K as stored (K-major), 128-byte swizzle as TMA lays it down
+//   out^T    [128 columns x 2 N] += V^T [D x 128] . P^T [128 x 2 N]        V as stored (M-major); P in two bf16 terms (16 bits), side by side: V is read once
+// One block on each SM, its piece of the line, and
+//   warp 0     looks pages up and loads keys and values by TMA into a ring of slots (one tile's keys or values each), the queries of a new segment by plain loads
+//   warp 1     one thread issues the products: scores of tile i + 1 ahead of the sums of tile i
+//   warp 2     holds tensor memory
+//   warps 4-7  a thread per position: reads its N scores, takes 2^(c s - m), adds them up, and leaves the weights in shared memory for the next
+//              product.  m is a row's maximum as of some tile: it is brought up to date (and sums and outputs with it) only when a weight passes 2^8,
+//              so that a common tile needs no maximum over its positions and no pass over the output.  At a segment's end a thread per
+//              column of the output divides and writes, after the next tile's weights are on their way.
+// What bounds it: HBM (two tiles of 64 KB in flight on an SM); a tile's exponentials take a third of its time on the bus at N = 32.
+// Every wait is bounded: a wait that runs out ends all roles' waits, the segments that are left are flagged, and the block leaves.
+#include "saki_attention.cuh"
+
+namespace saki {
+
+namespace attn {
+
+namespace {
+
+constexpr int UT = 128, UTHREADS = 256;      // positions of a tile
+
+template <int DP, int N> struct UShape {
+  static constexpr int SLABS = DP / 64, SLOT = UT * DP * 2;                // keys or values of a tile
+  static constexpr int P_BYTES = 2 * N * UT * 2, P_BUFS = N <= 32 ? 2 : 1; // two terms
+  static constexpr int Q_BYTES = N * DP * 2;
+  static constexpr int FIXED = P_BUFS * P_BYTES + 2 * Q_BYTES + 7168 + 1024;      // and the rest, alignment
+  static constexpr int FIT = (227 * 1024 - FIXED) / SLOT, SLOTS = FIT < 12 ? FIT : 12;
+  static constexpr int SMEM = SLOTS * SLOT + FIXED;
+  static constexpr int COLS = 6 * N <= 128 ? 128 : 6 * N <= 256 ? 256 : 512;             // scores and outputs (two terms), two buffers each
+  static_assert(SLOTS >= 4, "two tiles");
+};
+
+struct URest {            // of shared memory
+  uint64_t full[12], empty[12], q_full[2], q_empty[2], s_full[2], p_ready[2], pv_done[2], drain;
+  LineShared<UTHREADS> line;
+  alignas(16) float m[64];      // (read four at a time)
+  float m_before[64], factor[64], top[4][64], sum[2][4][64];      // (sums: by segment and warp)
+  int64_t row_at[2][64];  // by segment: where a row's output starts, -1: there is none
+  int to[64], from[64], lse_at[2][64];
+  int bad[8];             // by tile: a page outside the pool
+  int keep[2];            // by P buffer: the tile's sums go on top of what is there although it is its segment's first
+  int abort;
+  uint32_t tmem;
+};
+static_assert(sizeof(URest) <= 7168, "what is left of shared memory");
+
+__device__ __forceinline__ bool u_wait(uint64_t* bar, uint32_t parity, URest& r, long long limit) {
+  if (limit >= WAIT_LIMIT_CYCLES && mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  for (;;) {
+    if (*(volatile int*)&r.abort) return false;
+    if (clock64() - t0 > limit) { *(volatile int*)&r.abort = 1; return false; }
+    if (limit >= WAIT_LIMIT_CYCLES ? mbar_try_wait(bar, parity) : mbar_test_wait(bar, parity)) return true;
+  }
+}
+__device__ __forceinline__ void u_arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
+__device__ __forceinline__ void u_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void u_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void u_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// shared-memory matrix descriptor, 128-byte swizzle.  K-major: `stride` from eight rows to the next.  M-major: `stride` from eight k to the next, `lead` from
+// 64 rows to the next
+__device__ __forceinline__ uint64_t u_desc(uint32_t at, uint32_t lead, uint32_t stride) {
+  return (uint64_t)((at & 0x3FFFF) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// instruction descriptor: float32 sums, bf16 operands, M = 128; A M-major if `a_m`
+template <int N> __host__ __device__ constexpr uint32_t u_idesc(bool a_m) { return (1u << 4) | (1u << 7) | (1u << 10) | (a_m ? 1u << 15 : 0u) | ((uint32_t)(N >> 3) << 17) | (8u << 24); }
+__device__ __forceinline__ void u_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void u_ld16(uint32_t at, float* x) {
+  uint32_t r[16];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                 "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(at) : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void u_st16(uint32_t at, const float* x) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+               ::"r"(at), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]),
+                 "f"(x[8]), "f"(x[9]), "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]) : "memory");
+}
+__device__ __forceinline__ void u_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// the 128 threads of warps 4 to 7
+__device__ __forceinline__ void u_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool u_any(bool yes) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(yes ? 1u : 0u) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ float u_warp_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+// 16-byte piece j of row r, slabs of `rows` rows of 128 bytes
+__device__ __forceinline__ uint32_t u_piece(int rows, int r, int j) { return (uint32_t)((j >> 3) * (rows * 128) + r * 128 + (((j & 7) ^ (r & 7)) << 4)); }
+
+// sums over the warp of N values per lane, left in `to` (the next u_sync or u_any makes them seen): half of the values change hands at a time
+template <int N> __device__ __forceinline__ void column_sums(float (&l)[N], float* to, int lane) {
+  float x[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) x[n] = l[n];
+  int n0 = 0;
+#pragma unroll
+  for (int o = 16, m = N; o > 0; o >>= 1) {
+    const bool up = lane & o;
+    if (m > 1) {
+      m /= 2;
+#pragma unroll
+      for (int k = 0; k < N / 2; ++k)
+        if (k < m) {
+          const float give = up ? x[k] : x[m + k], mine = up ? x[m + k] : x[k];
+          x[k] = mine + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+      n0 += up ? m : 0;
+    } else x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+  }
+  constexpr int LEFT = N > 32 ? N / 32 : 1;
+#pragma unroll
+  for (int k = 0; k < LEFT; ++k) to[n0 + k] = x[k];      // (N = 16: two lanes write the same)
+}
+
+constexpr float NOTHING = -1e30f;       // the maximum of a row that has seen nothing so far
+
+template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+  using S = UShape<DP, N>;
+  using E = __nv_bfloat16;
+  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS;
+  extern __shared__ char u_raw[];
+  char* const smem = (char*)(((uintptr_t)u_raw + 1023) & ~(uintptr_t)1023);
+  char* const p_s = smem + SLOTS * S::SLOT;
+  char* const q_s = p_s + PB * S::P_BYTES;
+  URest& r = *(URest*)(q_s + 2 * S::Q_BYTES);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+  if (tid == 0) {
+    for (int i = 0; i < SLOTS; ++i) { mbar_init(r.full + i, 1); mbar_init(r.empty + i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(r.q_full + i, 1); mbar_init(r.q_empty + i, 1); mbar_init(r.s_full + i, 1); mbar_init(r.p_ready + i, 128); mbar_init(r.pv_done + i, 1); }
+    mbar_init(&r.drain, 1);
+    r.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&r.tmem)), "n"(S::COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  u_before();
+  wait_for_predecessor();
+  launch_dependents();
+  long long chunk, total;
+  pieces<UT, UTHREADS, 1>(p, r.line, chunk, total);        // (ends with a barrier)
+  u_after();
+  const uint32_t tmem = *(volatile uint32_t*)&r.tmem;
+  const int number = (int)blockIdx.x;
+  const long long u0 = number * chunk, limit = p.wait_limit;
+  const int n_tiles = u0 < total ? (int)min(chunk, total - u0) : 0;
+
+  if (n_tiles == 0) {
+    if (tid == 0) p.desc[number] = make_int4(0, 0, 0, 0);
+  } else if (warp == 0) {
+    // ---- loads: tile i's keys are load 2 i, its values load 2 i + 1; load j goes to slot j % SLOTS
+    Cursor<UT> look;
+    look.at(p, r.line.b[0], u0 - r.line.before[0]);
+    const int boxes = UT / p.box, box_x = lane % boxes * p.box, slab = lane / boxes;
+    const bool loads = slab < S::SLABS && slab * 64 < p.in.D;
+    const uint32_t box_at = (uint32_t)(slab * (UT * 128) + box_x * 128);
+    int found = -1, slot_x = 0, head = 0, seg = 0;
+    // the page of the lane's box in the tile at the cursor, -1: nothing of it is seen, -2: outside the pool
+    auto look_up = [&] {
+      const int x = tile_start<UT>(look.s, look.t) + box_x;
+      found = -1;
+      if (loads && x < look.s.n && (x + p.box > look.s.lo || x < look.s.sk)) {
+        const int page = p.page_shift >= 0 ? x >> p.page_shift : (int)((unsigned)x / (unsigned)p.in.page_size);
+        found = p.in.page_table[look.b * p.in.ld_table + page];
+        slot_x = x - page * p.in.page_size;
+        if ((unsigned)found >= (unsigned)p.in.n_pages) found = -2;
+      }
+      head = p.RB == 1 ? look.hr : look.hr / p.RB;
+    };
+    look_up();
+    int j = 0, slot = 0, done = 0;            // loads so far that have left
+    uint32_t turn = 0;
+    bool ok = true;
+    for (int i = 0; i < n_tiles && ok; ++i) {
+      if (i == 0 || look.t == 0) {            // a segment's queries
+        const int qb = seg & 1;
+        ok = u_wait(r.q_empty + qb, ((seg >> 1) & 1) ^ 1u, r, limit);
+        if (!ok) break;
+        const int row0 = (look.hr - head * p.RB) * N;
+        for (int e = lane; e < N * PIECES; e += 32) {
+          const int rr = e / PIECES, jj = e % PIECES, row = row0 + rr, t = row / p.G;
+          uint4 x = make_uint4(0, 0, 0, 0);
+          if (row < p.R && jj * 8 < p.in.D) {
+            const E* const q = (const E*)p.in.q + look.b * p.in.q_seq + t * p.in.q_pos + (int64_t)(head * p.G + row - t * p.G) * p.in.q_head + jj * 8;
+            if (p.q_vec) x = *(const uint4*)q;
+            else {
+              const uint16_t* const w = (const uint16_t*)q;
+              x = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
+            }
+            x.x ^= p.q_sign; x.y ^= p.q_sign; x.z ^= p.q_sign; x.w ^= p.q_sign;
+          }
+          *(uint4*)(q_s + qb * S::Q_BYTES + u_piece(N, rr, jj)) = x;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) u_arrive(r.q_full + qb);
+        ++seg;
+      }
+      const bool mine = found >= 0, bad = __any_sync(0xffffffffu, found == -2);
+      const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, mine)) * p.box * 128);
+      const int page = found, x = slot_x, h = head;
+      if (lane == 0) { *(volatile int*)(r.bad + (i & 7)) = bad; __threadfence_block(); }
+      look.next(p);
+      if (i + 1 < n_tiles) look_up();         // (in flight while the slots are waited for)
+#pragma unroll 1
+      for (int kv = 0; kv < 2; ++kv) {
+        ok = ok && u_wait(r.empty + slot, turn ^ 1u, r, limit);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (lane == 0) mbar_expect_tx(r.full + slot, bytes);
+        __syncwarp();
+        if (mine) tma_box(smem_addr(smem + slot * S::SLOT) + box_at, kv ? &v_map : &k_map, slab * 64, h, x, page, r.full + slot);
+        ++j;
+        if (++slot == SLOTS) { slot = 0; turn ^= 1u; }
+      }
+    }
+    if (!ok)                                  // copies that are still on their way land before the block leaves
+      for (done = max(0, j - SLOTS); done < j; ++done) mbar_wait_bounded(r.full + done % SLOTS, (uint32_t)(done / SLOTS) & 1u);
+  } else if (warp == 1) {
+    if (lane == 0) {
+      // ---- products
+      Cursor<UT> qk;
+      qk.at(p, r.line.b[0], u0 - r.line.before[0]);
+      int seg = 0, acc = -1;                  // segments whose queries have been used; output buffer of the sums' segment
+      bool qk_first = true;
+      uint32_t first = 0;                     // bit i % 2: tile i is its segment's first
+      const uint32_t id_s = u_idesc<N>(false), id_o = u_idesc<2 * N>(true);
+      auto scores = [&](int i) -> bool {
+        const int load = 2 * i, slot = load % SLOTS, qb = seg & 1;
+        if (qk_first && !u_wait(r.q_full + qb, (seg >> 1) & 1, r, limit)) return false;
+        if (!u_wait(r.full + slot, (load / SLOTS) & 1, r, limit)) return false;
+        u_after();
+        const uint32_t k = smem_addr(smem + slot * S::SLOT), q = smem_addr(q_s + qb * S::Q_BYTES);
+        first = (first & ~(1u << (i & 1))) | (uint32_t)qk_first << (i & 1);
+#pragma unroll
+        for (int e = 0; e < DP / 16; ++e)
+          if (e * 16 < p.in.D)
+            u_mma(tmem + (i & 1) * N, u_desc(k + (e >> 2) * (UT * 128) + (e & 3) * 32, 16, 1024), u_desc(q + (e >> 2) * (N * 128) + (e & 3) * 32, 16, 1024), id_s, e > 0);
+        u_commit(r.empty + slot);
+        u_commit(r.s_full + (i & 1));
+        qk_first = qk.t + 1 == qk.s.nt;
+        if (qk_first) { u_commit(r.q_empty + qb); ++seg; }
+        qk.next(p);
+        return true;
+      };
+      bool ok = scores(0);
+      for (int i = 0; i < n_tiles && ok; ++i) {
+        if (i + 1 < n_tiles && !scores(i + 1)) { ok = false; break; }
+        const int load = 2 * i + 1, slot = load % SLOTS, pb = i % PB;
+        if (!u_wait(r.p_ready + (i & 1), (i >> 1) & 1, r, limit) || !u_wait(r.full + slot, (load / SLOTS) & 1, r, limit)) { ok = false; break; }
+        u_after();
+        const bool new_seg = first >> (i & 1) & 1u;
+        if (new_seg) ++acc;
+        const bool on_top = !new_seg || *(volatile int*)(r.keep + (i & 1));
+        const uint32_t v = smem_addr(smem + slot * S::SLOT), pa = smem_addr(p_s + pb * S::P_BYTES), o = tmem + 2 * N + (acc & 1) * 2 * N;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)           // steps of 16 positions
+          u_mma(o, u_desc(v + e * 2048, DP == 128 ? UT * 128 : 0, 1024), u_desc(pa + (e >> 2) * (N * 256) + (e & 3) * 32, 16, 1024), id_o, e > 0 || on_top);
+        u_commit(r.empty + slot);
+        u_commit(r.pv_done + (i & 1));
+      }
+      if (!ok) {                              // nothing of it is under way when tensor memory goes
+        u_commit(&r.drain);
+        mbar_wait_bounded(&r.drain, 0);
+      }
+    }
+  } else if (warp >= 4) {
+    // ---- weights: thread t is position t of the tile, and column t of the output
+    const int t = tid - 128, q4 = warp - 4;
+    const uint32_t lanes = (uint32_t)(q4 * 32) << 16;
+    Cursor<UT> now;
+    now.at(p, r.line.b[0], u0 - r.line.before[0]);
+    bool dead = false;
+    float l[N];
+    float bad = 0.f;
+    int seg = -1;
+    struct Done { int b, hr, seg; uint32_t st; bool head, tail, there; float bad; } last = {};      // a segment whose results are not written yet
+    last.there = false;
+    // segment `d`, whose last tile is tile i, with the maxima m
+    auto finish = [&](const Done& d, int i, const float* m) {
+      if (!dead && !u_wait(r.pv_done + (i & 1), (i >> 1) & 1, r, limit)) dead = true;
+      u_after();
+      const float b = u_any(dead) ? -2.f : d.bad;
+      const uint32_t st = d.st | status_of(b);
+      float* const part = p.part + (number * 2 + (d.head ? 0 : 1)) * (int64_t)PART<N, DP>;
+      const int sb = d.seg & 1;
+      auto sum_of = [&](int n) { return (r.sum[sb][0][n] + r.sum[sb][1][n]) + (r.sum[sb][2][n] + r.sum[sb][3][n]); };
+      const bool partial = d.head || d.tail;
+#pragma unroll
+      for (int n0 = 0; n0 < N; n0 += 16) {
+        float o[16], lo[16];
+        u_ld16(tmem + lanes + 2 * N + sb * 2 * N + n0, o);
+        u_ld16(tmem + lanes + 2 * N + sb * 2 * N + N + n0, lo);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const int n = n0 + k;
+          const int64_t at = r.row_at[sb][n];
+          if (at < 0) break;
+          if (partial) {
+            if (t < DP) part[n * DP + t] = o[k] + lo[k];
+          } else if (t < p.in.D) {
+            const float sum = sum_of(n);
+            ((E*)p.out.out)[at + t] = __float2bfloat16_rn(st || sum == 0.f ? 0.f : __fdividef(o[k] + lo[k], sum));
+          }
+        }
+      }
+      if (t < N && r.row_at[sb][t] >= 0) {
+        const float sum = sum_of(t);
+        if (partial) *(float2*)(part + N * DP + t * 2) = make_float2(m[t], b < 0.f ? b : sum);
+        else if (p.out.lse) p.out.lse[(int64_t)d.b * p.in.Q * p.in.Hq + r.lse_at[sb][t]] = lse_of(m[t], st ? 0.f : sum);
+      }
+      if (!partial && d.hr == 0 && t == 0) put_status(p, d.b, st);
+      u_before();
+    };
+#pragma unroll 1
+    for (int i = 0; i < n_tiles; ++i) {
+      const bool first = i == 0 || now.t == 0;
+      const int x0 = tile_start<UT>(now.s, now.t), x = x0 + t;
+      if (first) {
+        ++seg;
+        bad = 0.f;
+        const int h = p.RB == 1 ? now.hr : now.hr / p.RB;
+        if (i > 0) u_sync();       // (the segments before have been read out)
+        if (t < N) {
+          const int row = (now.hr - h * p.RB) * N + t, j = row / p.G;
+          const Sight s = sight_of(p, now.s, row);
+          r.to[t] = s.to; r.from[t] = s.from;
+          r.row_at[seg & 1][t] = row < p.R ? out_at(p, now.b, h, row) : -1;
+          r.lse_at[seg & 1][t] = j * p.in.Hq + h * p.G + row - j * p.G;
+          r.m_before[t] = r.m[t];
+          r.m[t] = NOTHING;
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) l[n] = 0.f;
+        u_sync();
+      }
+      if (!dead && !u_wait(r.s_full + (i & 1), (i >> 1) & 1, r, limit)) dead = true;
+      u_after();
+      float w[N];
+      if (*(volatile int*)(r.bad + (i & 7))) bad = -1.f;
+      const bool edge = !whole<UT>(p, now.s, x0), hidden = !(x < now.s.n && (x >= now.s.lo || x < now.s.sk));
+      const int sinks = p.in.window > 0 ? p.in.sinks : 0;
+      auto scores = [&] {
+#pragma unroll
+        for (int n = 0; n < N; n += 16) u_ld16(tmem + lanes + (i & 1) * N + n, w + n);
+        if (edge) {
+#pragma unroll
+          for (int n = 0; n < N; ++n)
+            if (hidden || !(x <= r.to[n] && (x >= r.from[n] || x < sinks))) w[n] = -CUDART_INF_F;
+        }
+      };
+      float big = 0.f;
+      auto weights = [&] {
+#pragma unroll
+        for (int n = 0; n < N; n += 4) {
+          const float4 m = *(const float4*)(r.m + n);
+          w[n] = ex2f(fmaf(w[n], p.c, -m.x)); w[n + 1] = ex2f(fmaf(w[n + 1], p.c, -m.y));
+          w[n + 2] = ex2f(fmaf(w[n + 2], p.c, -m.z)); w[n + 3] = ex2f(fmaf(w[n + 3], p.c, -m.w));
+          big = fmaxf(fmaxf(big, fmaxf(w[n], w[n + 1])), fmaxf(w[n + 2], w[n + 3]));
+        }
+      };
+      scores();
+      bool fresh = first;          // no sums or outputs of this segment yet
+      if (first && !edge) {
+        // any maximum will do that none of the positions passes by 2^8: that of a quarter of them, each warp for a quarter of the rows
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) {
+          const float top = u_warp_max(q4 == 0 ? w[k] : q4 == 1 ? w[N / 4 + k] : q4 == 2 ? w[N / 2 + k] : w[3 * N / 4 + k]);
+          if (lane == k % 32) r.m[q4 * (N / 4) + k] = fmaxf(NOTHING, top * p.c);
+        }
+        u_sync();
+      }
+      bool renew = first && edge;
+      if (!renew) {
+        weights();
+        renew = u_any(big > 256.f);
+        if (renew) scores();
+      }
+      if (renew) {                 // the rows' maxima
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const float top = u_warp_max(w[n]);
+          if (lane == (n & 31)) r.top[q4][n] = top;
+        }
+        u_sync();
+        if (t < N) {
+          const float top = fmaxf(fmaxf(r.top[0][t], r.top[1][t]), fmaxf(r.top[2][t], r.top[3][t])), before = r.m[t], m = fmaxf(before, top * p.c);
+          r.m[t] = m;
+          r.factor[t] = ex2f(before - m);
+        }
+        u_sync();
+        if (!fresh) {              // ... and what is there already
+          if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
+          u_after();
+#pragma unroll
+          for (int n0 = 0; n0 < 2 * N; n0 += 16) {
+            const uint32_t at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + n0;
+            float y[16];
+            u_ld16(at, y);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] *= r.factor[(n0 + e) % N];
+            u_st16(at, y);
+          }
+          u_st_wait();
+#pragma unroll
+          for (int n = 0; n < N; ++n) l[n] *= r.factor[n];
+        }
+        weights();
+      }
+#pragma unroll
+      for (int n = 0; n < N; ++n) l[n] += w[n];
+      char* const v_s = smem + (2 * i + 1) % SLOTS * S::SLOT;
+      bool keep = false;
+      if (edge) {
+        if (!dead && !u_wait(r.full + (2 * i + 1) % SLOTS, ((2 * i + 1) / SLOTS) & 1, r, limit)) dead = true;
+        if (hidden)                // values of positions that nothing sees: whatever lies there
+          for (int j = 0; j < PIECES; ++j) *(uint4*)(v_s + u_piece(UT, t, j)) = make_uint4(0, 0, 0, 0);
+        if (p.in.Q > 1) {          // some rows do not see all of the tile: a value that is not finite must not reach those as 0 * inf
+          auto odd = [](uint32_t y) { return (y & 0x7f800000u) == 0x7f800000u || (y & 0x7f80u) == 0x7f80u; };
+          bool strange = false;
+          if (!hidden)
+            for (int j = 0; j < PIECES; ++j) {
+              const uint4 y = *(const uint4*)(v_s + u_piece(UT, t, j));
+              strange = strange || odd(y.x) || odd(y.y) || odd(y.z) || odd(y.w);
+            }
+          if (u_any(strange)) {    // it goes to the rows that see it by itself, and 0 takes its place
+            if (!first) {
+              if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
+              u_after();
+            }
+            keep = first;
+#pragma unroll 1
+            for (int n0 = 0; n0 < N; n0 += 16) {
+              const uint32_t o_at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + n0;
+              float y[16];
+              if (first) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) y[e] = 0.f;
+                u_st16(o_at + N, y);
+              } else u_ld16(o_at, y);
+              if (t < DP)
+#pragma unroll 1
+                for (int pos = 0; pos < UT; ++pos) {
+                  const float z = __bfloat162float(*(const E*)(v_s + u_piece(UT, pos, t >> 3) + (t & 7) * 2));
+                  if (!(fabsf(z) < CUDART_INF_F))
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                      const int xx = x0 + pos;
+                      if (xx <= r.to[n0 + e] && (xx >= r.from[n0 + e] || xx < sinks)) y[e] += z;
+                    }
+                }
+              u_st16(o_at, y);
+            }
+            u_st_wait();
+            u_sync();
+            for (int j = 0; j < PIECES; ++j) {
+              uint4* const at = (uint4*)(v_s + u_piece(UT, t, j));
+              auto clean = [](uint32_t y) { return ((y & 0x7f800000u) == 0x7f800000u ? 0u : y & 0xffff0000u) | ((y & 0x7f80u) == 0x7f80u ? 0u : y & 0xffffu); };
+              const uint4 y = *at;
+              *at = make_uint4(clean(y.x), clean(y.y), clean(y.z), clean(y.w));
+            }
+          }
+        }
+      }
+      if (t == 0) *(volatile int*)(r.keep + (i & 1)) = keep;
+      if (i >= PB && !dead && !u_wait(r.pv_done + ((i - PB) & 1), ((i - PB) >> 1) & 1, r, limit)) dead = true;      // the buffer's last product
+      {
+        char* const at = p_s + (i % PB) * S::P_BYTES + (t >> 6) * (N * 256) + (t & 7) * 2;
+        const uint32_t piece = (uint32_t)((t >> 3) & 7) << 4;
+#pragma unroll
+        for (int n = 0; n < N; n += 2) {
+          const uint32_t a = __float_as_uint(w[n]), b = __float_as_uint(w[n + 1]);
+          const float2 rest = fadd2(make_float2(w[n], w[n + 1]), make_float2(-__uint_as_float(a & 0xffff0000u), -__uint_as_float(b & 0xffff0000u)));
+          const uint32_t lo = pack_bf16x2(rest.x, rest.y);
+          char* const c0 = at + n * 128 + (piece ^ (uint32_t)((n & 7) << 4));
+          char* const c1 = at + (n + 1) * 128 + (piece ^ (uint32_t)(((n + 1) & 7) << 4));
+          *(uint16_t*)c0 = (uint16_t)(a >> 16);
+          *(uint16_t*)c1 = (uint16_t)(b >> 16);
+          *(uint16_t*)(c0 + N * 128) = (uint16_t)lo;
+          *(uint16_t*)(c1 + N * 128) = (uint16_t)(lo >> 16);
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      u_before();
+      u_arrive(r.p_ready + (i & 1));
+      if (last.there) { finish(last, i - 1, r.m_before); last.there = false; }
+      if (now.t + 1 == now.s.nt || i + 1 == n_tiles) {        // the segment ends, or the piece does
+        column_sums<N>(l, r.sum[seg & 1][q4], lane);
+        last = {now.b, now.hr, seg, now.s.status, i < now.t, now.t + 1 < now.s.nt, true, bad};
+        if (i + 1 == n_tiles) {
+          finish(last, i, r.m);
+          if (t == 0) {            // a segment that starts here and goes on: how many pieces behind have a share of it
+            const long long end = u0 + i - now.t + now.s.nt;
+            p.desc[number] = last.tail && !last.head ? make_int4(now.b, now.hr, (int)((end - 1) / chunk) - number, (int)now.s.status) : make_int4(0, 0, 0, 0);
+          }
+        }
+      }
+      now.next(p);
+    }
+  }
+  u_before();
+  __syncthreads();
+  if (warp == 2) {
+    u_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::COLS) : "memory");
+  }
+}
+
+template <int DP, int N> cudaError_t launch(const AttnParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int blocks, cudaStream_t st) {
+  using S = UShape<DP, N>;
+  auto* const fn = attn_umma_kernel<DP, N>;
+  const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+  return e != cudaSuccess ? e : launch_pdl(fn, dim3((unsigned)blocks), UTHREADS, S::SMEM, st, true, p, k_map, v_map);
+}
+
+}  // namespace
+
+int umma_rows(const saki_attn_in& in) {
+  const int R = in.Q * (in.Hq / in.H);
+  return R <= 16 ? 16 : R <= 32 ? 32 : 64;
+}
+
+cudaError_t launch_umma(const AttnParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int blocks, cudaStream_t st) {
+  const int n = umma_rows(p.in);
+  if (p.in.D <= 64) return n == 16 ? launch<64, 16>(p, k_map, v_map, blocks, st) : n == 32 ? launch<64, 32>(p, k_map, v_map, blocks, st) : launch<64, 64>(p, k_map, v_map, blocks, st);
+  return n == 16 ? launch<128, 16>(p, k_map, v_map, blocks, st) : n == 32 ? launch<128, 32>(p, k_map, v_map, blocks, st) : launch<128, 64>(p, k_map, v_map, blocks, st);
+}
+
+}  // namespace attn
+
+}  // namespace saki
