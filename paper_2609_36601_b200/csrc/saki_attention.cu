@@ -570,6 +570,26 @@ bool pool_map(CUtensorMap* map, const void* pool, int64_t page, int64_t pos, int
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// ... as `mode` sees it (bf16, D = 128)
+bool eights_map(CUtensorMap* map, const void* pool, int64_t page, int64_t pos, int64_t head, const saki_attn_in& in, int box, int mode) {
+  const EncodeFn fn = encode();
+  const cuuint64_t eights = (cuuint64_t)in.page_size / 8, pages = (cuuint64_t)in.n_pages, H = (cuuint64_t)in.H;
+  auto step = [](int64_t s, cuuint64_t n) { return (cuuint64_t)(n > 1 ? s * 2 : 256); };      // (of a dimension of one: never used)
+  const cuuint64_t c4 = mode == MAP_HEADS ? pages : mode == MAP_PAGES ? pages * H : H;
+  const cuuint64_t dims[5] = {64, 8, mode == MAP_HEADS ? 2 * H : 2, mode == MAP_RUN ? eights * pages : eights, c4};
+  const cuuint64_t strides[4] = {step(pos, 8), 128, step(8 * pos, dims[3]), step(mode == MAP_HEADS ? page : head, c4)};
+  const cuuint32_t boxes[5] = {64, 8, 2, (cuuint32_t)(box / 8), 1}, one[5] = {1, 1, 1, 1, 1};
+  if (!fn || dims[3] >= (1ull << 31) || c4 >= (1ull << 31)) return false;
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(pool), dims, strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// whether what `mode` takes for granted holds for a pool
+bool mode_fits(int mode, int64_t page, int64_t pos, int64_t head, const saki_attn_in& in) {
+  if (mode == MAP_HEADS) return in.H == 1 || head == 128;
+  if (mode == MAP_PAGES) return in.H > 1 && (in.n_pages == 1 || page == in.H * head);
+  return in.n_pages == 1 || page == in.page_size * pos;
+}
+
 }  // namespace
 
 // bf16 heads of up to 128 on pages of whole eights go to the kernel on tcgen05
@@ -607,6 +627,13 @@ cudaError_t launch_attention(const saki_attn_in& in, const saki_attn_out& out, v
   const bool tma = p.box >= 8 && pool_map(&k_map, in.k_pages, in.kp_page, in.kp_pos, in.kp_head, in, p.box) &&
                    pool_map(&v_map, in.v_pages, in.vp_page, in.vp_pos, in.vp_head, in, p.box);
   umma = umma && tma;
+  for (int mode = MAP_HEADS; umma && in.D == 128 && mode <= MAP_RUN && p.map_mode == MAP_BOXES; ++mode) {
+    CUtensorMap k5 = {}, v5 = {};
+    if (mode_fits(mode, in.kp_page, in.kp_pos, in.kp_head, in) && mode_fits(mode, in.vp_page, in.vp_pos, in.vp_head, in) &&
+        eights_map(&k5, in.k_pages, in.kp_page, in.kp_pos, in.kp_head, in, p.box, mode) && eights_map(&v5, in.v_pages, in.vp_page, in.vp_pos, in.vp_head, in, p.box, mode)) {
+      k_map = k5; v_map = v5; p.map_mode = mode;
+    }
+  }
   int dev = 0, sms = 148, per = 1, workers = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);

@@ -10,12 +10,19 @@ namespace saki {
 
 namespace attn {
 
+// Tensor maps of a pool.  MAP_BOXES: (column, head, position, page), boxes of 128 bytes by `box` positions.  The others, for D = 128: (column of a half, position
+// of eight, half, eights of positions, the rest), boxes of all 256 bytes of their positions, where five dimensions say where these lie: heads are
+// side by side (halves and heads are one dimension), pages hold one head after the other (pages and heads are one), or positions run on from page to page (eights
+// and pages are one).
+enum { MAP_BOXES = 0, MAP_HEADS, MAP_PAGES, MAP_RUN };
+
 struct AttnParams {
   saki_attn_in in;
   saki_attn_out out;
   int G, R, RB;             // query heads per key head; rows of a key head (Q * G); blocks of rows
   int q_vec;                // q can be read in 16-byte pieces
   int box;                  // positions of a TMA box
+  int map_mode;             // how the tensor maps see a pool: MAP_*
   int page_shift;           // page_size is 1 << page_shift; -1: no power of two
   uint32_t q_sign;          // a negative scale turns the queries' signs
   float c;                  // |scale| * log2(e), above 0
@@ -28,6 +35,10 @@ struct AttnParams {
 __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int x, int head, int slot, int page, uint64_t* bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                ::"r"(dst), "l"(map), "r"(x), "r"(head), "r"(slot), "r"(page), "r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void tma_eights(uint32_t dst, const CUtensorMap* map, int c2, int c3, int c4, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %3, %4, %5}], [%6];"
+               ::"r"(dst), "l"(map), "r"(0), "r"(c2), "r"(c3), "r"(c4), "r"(smem_addr(bar)) : "memory");
 }
 // What the queries of a sequence see, in tiles of T positions: the tiles of the first `sk` positions, then those from tile m0 on.  (Positions are
 // below 2^31.)

@@ -5,11 +5,12 @@
 //   scores^T [128 positions x N]  = K [128 x D] . Q^T [D x N]              K as stored (K-major), 128-byte swizzle as TMA lays it down
 //   out^T    [128 columns x 2 N] += V^T [D x 128] . P^T [128 x 2 N]        V as stored (M-major); P in two bf16 terms (16 bits), side by side: V is read once
 // One block on each SM, its piece of the line, and
-//   warp 0     looks pages up and loads keys and values by TMA into a ring of slots (one tile's keys or values each), the queries of a new segment by plain loads
+//   warp 0     looks pages up and loads keys and values by TMA into a ring of slots (one tile's keys or values each)
 //   warp 1     one thread issues the products: scores of tile i + 1 ahead of the sums of tile i
 //   warp 2     holds tensor memory
-//   warps 4-7  a thread per position: reads its N scores, takes 2^(c s - m), adds them up, and leaves the weights in shared memory for the next
-//              product.  m is a row's maximum as of some tile: it is brought up to date (and sums and outputs with it) only when a weight passes 2^8,
+//   warp 3     loads the queries of the segments, two ahead
+//   from 4 on  groups of four warps, 16 queries each (one group took 2.2 us for a tile of 32 queries, against 1.5 us on the bus), a thread per position:
+//              reads its scores, takes 2^(c s - m), adds them up, and leaves the weights in shared memory for the next product.  m is a row's maximum as of some tile: it is brought up to date (and sums and outputs with it) only when a weight passes 2^8,
 //              so that a common tile needs no maximum over its positions and no pass over the output.  At a segment's end a thread per
 //              column of the output divides and writes, after the next tile's weights are on their way.
 // What bounds it: HBM (two tiles of 64 KB in flight on an SM); a tile's exponentials take a third of its time on the bus at N = 32.
@@ -22,9 +23,10 @@ namespace attn {
 
 namespace {
 
-constexpr int UT = 128, UTHREADS = 256;      // positions of a tile
+constexpr int UT = 128, CW = 16;             // positions of a tile; queries of a group of warps
 
 template <int DP, int N> struct UShape {
+  static constexpr int GROUPS = N / CW, THREADS = 128 + 128 * GROUPS;
   static constexpr int SLABS = DP / 64, SLOT = UT * DP * 2;                // keys or values of a tile
   static constexpr int P_BYTES = 2 * N * UT * 2, P_BUFS = N <= 32 ? 2 : 1; // two terms
   static constexpr int Q_BYTES = N * DP * 2;
@@ -35,11 +37,11 @@ template <int DP, int N> struct UShape {
   static_assert(SLOTS >= 4, "two tiles");
 };
 
-struct URest {            // of shared memory
+template <int THREADS> struct URest {      // of shared memory
   uint64_t full[12], empty[12], q_full[2], q_empty[2], s_full[2], p_ready[2], pv_done[2], drain;
-  LineShared<UTHREADS> line;
+  LineShared<THREADS> line;
   alignas(16) float m[64];      // (read four at a time)
-  float m_before[64], factor[64], top[4][64], sum[2][4][64];      // (sums: by segment and warp)
+  float m_before[64], factor[64], top[4][64], sum[2][4][64], inverse[64];      // (sums: by segment and warp)
   int64_t row_at[2][64];  // by segment: where a row's output starts, -1: there is none
   int to[64], from[64], lse_at[2][64];
   int bad[8];             // by tile: a page outside the pool
@@ -47,9 +49,9 @@ struct URest {            // of shared memory
   int abort;
   uint32_t tmem;
 };
-static_assert(sizeof(URest) <= 7168, "what is left of shared memory");
+static_assert(sizeof(URest<640>) <= 7168, "what is left of shared memory");
 
-__device__ __forceinline__ bool u_wait(uint64_t* bar, uint32_t parity, URest& r, long long limit) {
+template <typename R> __device__ __forceinline__ bool u_wait(uint64_t* bar, uint32_t parity, R& r, long long limit) {
   if (limit >= WAIT_LIMIT_CYCLES && mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   for (;;) {
@@ -90,11 +92,11 @@ __device__ __forceinline__ void u_st16(uint32_t at, const float* x) {
                  "f"(x[8]), "f"(x[9]), "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]) : "memory");
 }
 __device__ __forceinline__ void u_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// the 128 threads of warps 4 to 7
-__device__ __forceinline__ void u_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ bool u_any(bool yes) {
+// the 128 threads of group g of warps
+__device__ __forceinline__ void u_sync(int g) { asm volatile("bar.sync %0, 128;" ::"r"(g + 1) : "memory"); }
+__device__ __forceinline__ bool u_any(int g, bool yes) {
   uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(yes ? 1u : 0u) : "memory");
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(yes ? 1u : 0u), "r"(g + 1) : "memory");
   return r != 0;
 }
 __device__ __forceinline__ float u_warp_max(float x) {
@@ -132,20 +134,24 @@ template <int N> __device__ __forceinline__ void column_sums(float (&l)[N], floa
 
 constexpr float NOTHING = -1e30f;       // the maximum of a row that has seen nothing so far
 
-template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+// GROUPED (D = 128): a box brings both slabs of its positions, [8 positions][2 slabs][8 rows of 128 bytes]; else [slab][128 rows of 128 bytes].  (Boxes of a page
+// of 16 positions are 2 KB then, and 32 of them a tile take longer than the bus: 64 sequences of 4096 at 72 % of the copy rate, 88 % with pages of 64.)
+template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<DP, N>::THREADS, 1) attn_umma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using S = UShape<DP, N>;
   using E = __nv_bfloat16;
-  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS;
+  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS, THREADS = S::THREADS, GROUPS = S::GROUPS;
+  constexpr uint32_t SLAB = GROUPED ? 1024 : UT * 128, EIGHT = GROUPED ? S::SLABS * 1024 : 1024;      // bytes from a slab to the next, from eight positions to the next
+  auto piece_of = [](int t, int j) { return (uint32_t)((t >> 3) * EIGHT + (j >> 3) * SLAB + (t & 7) * 128 + (((j & 7) ^ (t & 7)) << 4)); };
   extern __shared__ char u_raw[];
   char* const smem = (char*)(((uintptr_t)u_raw + 1023) & ~(uintptr_t)1023);
   char* const p_s = smem + SLOTS * S::SLOT;
   char* const q_s = p_s + PB * S::P_BYTES;
-  URest& r = *(URest*)(q_s + 2 * S::Q_BYTES);
+  URest<THREADS>& r = *(URest<THREADS>*)(q_s + 2 * S::Q_BYTES);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
     for (int i = 0; i < SLOTS; ++i) { mbar_init(r.full + i, 1); mbar_init(r.empty + i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(r.q_full + i, 1); mbar_init(r.q_empty + i, 1); mbar_init(r.s_full + i, 1); mbar_init(r.p_ready + i, 128); mbar_init(r.pv_done + i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(r.q_full + i, 1); mbar_init(r.q_empty + i, 1); mbar_init(r.s_full + i, 1); mbar_init(r.p_ready + i, 128 * GROUPS); mbar_init(r.pv_done + i, 1); }
     mbar_init(&r.drain, 1);
     r.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -159,7 +165,7 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
   wait_for_predecessor();
   launch_dependents();
   long long chunk, total;
-  pieces<UT, UTHREADS, 1>(p, r.line, chunk, total);        // (ends with a barrier)
+  pieces<UT, THREADS, 1>(p, r.line, chunk, total);        // (ends with a barrier)
   u_after();
   const uint32_t tmem = *(volatile uint32_t*)&r.tmem;
   const int number = (int)blockIdx.x;
@@ -173,9 +179,9 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
     Cursor<UT> look;
     look.at(p, r.line.b[0], u0 - r.line.before[0]);
     const int boxes = UT / p.box, box_x = lane % boxes * p.box, slab = lane / boxes;
-    const bool loads = slab < S::SLABS && slab * 64 < p.in.D;
-    const uint32_t box_at = (uint32_t)(slab * (UT * 128) + box_x * 128);
-    int found = -1, slot_x = 0, head = 0, seg = 0;
+    const bool loads = GROUPED ? slab == 0 : slab < S::SLABS && slab * 64 < p.in.D;
+    const uint32_t box_at = (uint32_t)(slab * SLAB + box_x / 8 * EIGHT), box_bytes = (uint32_t)p.box * (GROUPED ? 256 : 128);
+    int found = -1, slot_x = 0, head = 0;
     // the page of the lane's box in the tile at the cursor, -1: nothing of it is seen, -2: outside the pool
     auto look_up = [&] {
       const int x = tile_start<UT>(look.s, look.t) + box_x;
@@ -193,32 +199,8 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
     uint32_t turn = 0;
     bool ok = true;
     for (int i = 0; i < n_tiles && ok; ++i) {
-      if (i == 0 || look.t == 0) {            // a segment's queries
-        const int qb = seg & 1;
-        ok = u_wait(r.q_empty + qb, ((seg >> 1) & 1) ^ 1u, r, limit);
-        if (!ok) break;
-        const int row0 = (look.hr - head * p.RB) * N;
-        for (int e = lane; e < N * PIECES; e += 32) {
-          const int rr = e / PIECES, jj = e % PIECES, row = row0 + rr, t = row / p.G;
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (row < p.R && jj * 8 < p.in.D) {
-            const E* const q = (const E*)p.in.q + look.b * p.in.q_seq + t * p.in.q_pos + (int64_t)(head * p.G + row - t * p.G) * p.in.q_head + jj * 8;
-            if (p.q_vec) x = *(const uint4*)q;
-            else {
-              const uint16_t* const w = (const uint16_t*)q;
-              x = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
-            }
-            x.x ^= p.q_sign; x.y ^= p.q_sign; x.z ^= p.q_sign; x.w ^= p.q_sign;
-          }
-          *(uint4*)(q_s + qb * S::Q_BYTES + u_piece(N, rr, jj)) = x;
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) u_arrive(r.q_full + qb);
-        ++seg;
-      }
       const bool mine = found >= 0, bad = __any_sync(0xffffffffu, found == -2);
-      const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, mine)) * p.box * 128);
+      const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * box_bytes;
       const int page = found, x = slot_x, h = head;
       if (lane == 0) { *(volatile int*)(r.bad + (i & 7)) = bad; __threadfence_block(); }
       look.next(p);
@@ -230,7 +212,15 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
         if (!ok) break;
         if (lane == 0) mbar_expect_tx(r.full + slot, bytes);
         __syncwarp();
-        if (mine) tma_box(smem_addr(smem + slot * S::SLOT) + box_at, kv ? &v_map : &k_map, slab * 64, h, x, page, r.full + slot);
+        if (mine) {
+          const uint32_t to = smem_addr(smem + slot * S::SLOT) + box_at;
+          const CUtensorMap* const map = kv ? &v_map : &k_map;
+          if constexpr (GROUPED) {
+            const int eights = p.in.page_size / 8;
+            tma_eights(to, map, p.map_mode == MAP_HEADS ? 2 * h : 0, x / 8 + (p.map_mode == MAP_RUN ? page * eights : 0),
+                       p.map_mode == MAP_HEADS ? page : p.map_mode == MAP_PAGES ? page * p.in.H + h : h, r.full + slot);
+          } else tma_box(to, map, slab * 64, h, x, page, r.full + slot);
+        }
         ++j;
         if (++slot == SLOTS) { slot = 0; turn ^= 1u; }
       }
@@ -256,7 +246,7 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
 #pragma unroll
         for (int e = 0; e < DP / 16; ++e)
           if (e * 16 < p.in.D)
-            u_mma(tmem + (i & 1) * N, u_desc(k + (e >> 2) * (UT * 128) + (e & 3) * 32, 16, 1024), u_desc(q + (e >> 2) * (N * 128) + (e & 3) * 32, 16, 1024), id_s, e > 0);
+            u_mma(tmem + (i & 1) * N, u_desc(k + (e >> 2) * SLAB + (e & 3) * 32, 16, EIGHT), u_desc(q + (e >> 2) * (N * 128) + (e & 3) * 32, 16, 1024), id_s, e > 0);
         u_commit(r.empty + slot);
         u_commit(r.s_full + (i & 1));
         qk_first = qk.t + 1 == qk.s.nt;
@@ -276,7 +266,7 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
         const uint32_t v = smem_addr(smem + slot * S::SLOT), pa = smem_addr(p_s + pb * S::P_BYTES), o = tmem + 2 * N + (acc & 1) * 2 * N;
 #pragma unroll
         for (int e = 0; e < 8; ++e)           // steps of 16 positions
-          u_mma(o, u_desc(v + e * 2048, DP == 128 ? UT * 128 : 0, 1024), u_desc(pa + (e >> 2) * (N * 256) + (e & 3) * 32, 16, 1024), id_o, e > 0 || on_top);
+          u_mma(o, u_desc(v + e * 2 * EIGHT, DP == 128 ? SLAB : 0, EIGHT), u_desc(pa + (e >> 2) * (N * 256) + (e & 3) * 32, 16, 1024), id_o, e > 0 || on_top);
         u_commit(r.empty + slot);
         u_commit(r.pv_done + (i & 1));
       }
@@ -285,14 +275,54 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
         mbar_wait_bounded(&r.drain, 0);
       }
     }
+  } else if (warp == 3) {
+    // ---- queries of the piece's segments
+    Cursor<UT> at;
+    at.at(p, r.line.b[0], u0 - r.line.before[0]);
+    constexpr int EACH = N * PIECES / 32, BATCH = EACH < 16 ? EACH : 16;
+    long long left = n_tiles;
+    for (int seg = 0; left > 0; ++seg) {
+      const int qb = seg & 1;
+      if (!__all_sync(0xffffffffu, u_wait(r.q_empty + qb, ((seg >> 1) & 1) ^ 1u, r, limit))) break;
+      const int h = p.RB == 1 ? at.hr : at.hr / p.RB, row0 = (at.hr - h * p.RB) * N;
+#pragma unroll 1
+      for (int e0 = 0; e0 < EACH; e0 += BATCH) {
+        uint4 x[BATCH];                       // all on their way before the first is put down
+#pragma unroll
+        for (int e = 0; e < BATCH; ++e) {
+          const int c = (e0 + e) * 32 + lane, jj = c % PIECES, row = row0 + c / PIECES, t = row / p.G;
+          x[e] = make_uint4(0, 0, 0, 0);
+          if (row < p.R && jj * 8 < p.in.D) {
+            const E* const q = (const E*)p.in.q + at.b * p.in.q_seq + t * p.in.q_pos + (int64_t)(h * p.G + row - t * p.G) * p.in.q_head + jj * 8;
+            if (p.q_vec) x[e] = *(const uint4*)q;
+            else {
+              const uint16_t* const w = (const uint16_t*)q;
+              x[e] = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
+            }
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < BATCH; ++e) {
+          const int c = (e0 + e) * 32 + lane;
+          const uint32_t g = p.q_sign;
+          *(uint4*)(q_s + qb * S::Q_BYTES + u_piece(N, c / PIECES, c % PIECES)) = make_uint4(x[e].x ^ g, x[e].y ^ g, x[e].z ^ g, x[e].w ^ g);
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) u_arrive(r.q_full + qb);
+      left -= at.s.nt - at.t;
+      at.t = at.s.nt - 1;
+      at.next(p);
+    }
   } else if (warp >= 4) {
-    // ---- weights: thread t is position t of the tile, and column t of the output
-    const int t = tid - 128, q4 = warp - 4;
+    // ---- weights: thread t of group g is position t of the tile, and column t of the output, for queries c0 to c0 + CW
+    const int t = (tid - 128) & 127, q4 = warp & 3, g = (warp - 4) >> 2, c0 = g * CW;
     const uint32_t lanes = (uint32_t)(q4 * 32) << 16;
     Cursor<UT> now;
     now.at(p, r.line.b[0], u0 - r.line.before[0]);
     bool dead = false;
-    float l[N];
+    float l[CW];
     float bad = 0.f;
     int seg = -1;
     struct Done { int b, hr, seg; uint32_t st; bool head, tail, there; float bad; } last = {};      // a segment whose results are not written yet
@@ -301,36 +331,32 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
     auto finish = [&](const Done& d, int i, const float* m) {
       if (!dead && !u_wait(r.pv_done + (i & 1), (i >> 1) & 1, r, limit)) dead = true;
       u_after();
-      const float b = u_any(dead) ? -2.f : d.bad;
+      const float b = u_any(g, dead) ? -2.f : d.bad;      // (and the sums are there)
       const uint32_t st = d.st | status_of(b);
       float* const part = p.part + (number * 2 + (d.head ? 0 : 1)) * (int64_t)PART<N, DP>;
       const int sb = d.seg & 1;
-      auto sum_of = [&](int n) { return (r.sum[sb][0][n] + r.sum[sb][1][n]) + (r.sum[sb][2][n] + r.sum[sb][3][n]); };
       const bool partial = d.head || d.tail;
+      if (t < CW && r.row_at[sb][c0 + t] >= 0) {
+        const int n = c0 + t;
+        const float sum = (r.sum[sb][0][n] + r.sum[sb][1][n]) + (r.sum[sb][2][n] + r.sum[sb][3][n]);
+        r.inverse[n] = partial ? 1.f : st || sum == 0.f ? 0.f : 1.f / sum;
+        if (partial) *(float2*)(part + N * DP + n * 2) = make_float2(m[n], b < 0.f ? b : sum);
+        else if (p.out.lse) p.out.lse[(int64_t)d.b * p.in.Q * p.in.Hq + r.lse_at[sb][n]] = lse_of(m[n], st ? 0.f : sum);
+      }
+      float o[CW], lo[CW];
+      u_ld16(tmem + lanes + 2 * N + sb * 2 * N + c0, o);
+      u_ld16(tmem + lanes + 2 * N + sb * 2 * N + N + c0, lo);
+      u_sync(g);
 #pragma unroll
-      for (int n0 = 0; n0 < N; n0 += 16) {
-        float o[16], lo[16];
-        u_ld16(tmem + lanes + 2 * N + sb * 2 * N + n0, o);
-        u_ld16(tmem + lanes + 2 * N + sb * 2 * N + N + n0, lo);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const int n = n0 + k;
-          const int64_t at = r.row_at[sb][n];
-          if (at < 0) break;
-          if (partial) {
-            if (t < DP) part[n * DP + t] = o[k] + lo[k];
-          } else if (t < p.in.D) {
-            const float sum = sum_of(n);
-            ((E*)p.out.out)[at + t] = __float2bfloat16_rn(st || sum == 0.f ? 0.f : __fdividef(o[k] + lo[k], sum));
-          }
+      for (int k = 0; k < CW; ++k) {
+        const int64_t at = r.row_at[sb][c0 + k];
+        const float inv = r.inverse[c0 + k];
+        if (at >= 0) {
+          if (partial) { if (t < DP) part[(c0 + k) * DP + t] = o[k] + lo[k]; }
+          else if (t < p.in.D) ((E*)p.out.out)[at + t] = __float2bfloat16_rn(inv == 0.f ? 0.f : (o[k] + lo[k]) * inv);
         }
       }
-      if (t < N && r.row_at[sb][t] >= 0) {
-        const float sum = sum_of(t);
-        if (partial) *(float2*)(part + N * DP + t * 2) = make_float2(m[t], b < 0.f ? b : sum);
-        else if (p.out.lse) p.out.lse[(int64_t)d.b * p.in.Q * p.in.Hq + r.lse_at[sb][t]] = lse_of(m[t], st ? 0.f : sum);
-      }
-      if (!partial && d.hr == 0 && t == 0) put_status(p, d.b, st);
+      if (!partial && d.hr == 0 && t == 0 && g == 0) put_status(p, d.b, st);
       u_before();
     };
 #pragma unroll 1
@@ -340,165 +366,162 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
       if (first) {
         ++seg;
         bad = 0.f;
-        const int h = p.RB == 1 ? now.hr : now.hr / p.RB;
-        if (i > 0) u_sync();       // (the segments before have been read out)
-        if (t < N) {
-          const int row = (now.hr - h * p.RB) * N + t, j = row / p.G;
+        if (i > 0) u_sync(g);      // (the segments before have been read out)
+        if (t < CW) {
+          const int n = c0 + t, h = p.RB == 1 ? now.hr : now.hr / p.RB, row = (now.hr - h * p.RB) * N + n, j = row / p.G;
           const Sight s = sight_of(p, now.s, row);
-          r.to[t] = s.to; r.from[t] = s.from;
-          r.row_at[seg & 1][t] = row < p.R ? out_at(p, now.b, h, row) : -1;
-          r.lse_at[seg & 1][t] = j * p.in.Hq + h * p.G + row - j * p.G;
-          r.m_before[t] = r.m[t];
-          r.m[t] = NOTHING;
+          r.to[n] = s.to; r.from[n] = s.from;
+          r.row_at[seg & 1][n] = row < p.R ? out_at(p, now.b, h, row) : -1;
+          r.lse_at[seg & 1][n] = j * p.in.Hq + h * p.G + row - j * p.G;
+          r.m_before[n] = r.m[n];
+          r.m[n] = NOTHING;
         }
 #pragma unroll
-        for (int n = 0; n < N; ++n) l[n] = 0.f;
-        u_sync();
+        for (int n = 0; n < CW; ++n) l[n] = 0.f;
+        u_sync(g);
       }
       if (!dead && !u_wait(r.s_full + (i & 1), (i >> 1) & 1, r, limit)) dead = true;
       u_after();
-      float w[N];
+      float w[CW];
       if (*(volatile int*)(r.bad + (i & 7))) bad = -1.f;
       const bool edge = !whole<UT>(p, now.s, x0), hidden = !(x < now.s.n && (x >= now.s.lo || x < now.s.sk));
       const int sinks = p.in.window > 0 ? p.in.sinks : 0;
       auto scores = [&] {
-#pragma unroll
-        for (int n = 0; n < N; n += 16) u_ld16(tmem + lanes + (i & 1) * N + n, w + n);
+        u_ld16(tmem + lanes + (i & 1) * N + c0, w);
         if (edge) {
 #pragma unroll
-          for (int n = 0; n < N; ++n)
-            if (hidden || !(x <= r.to[n] && (x >= r.from[n] || x < sinks))) w[n] = -CUDART_INF_F;
+          for (int n = 0; n < CW; ++n)
+            if (hidden || !(x <= r.to[c0 + n] && (x >= r.from[c0 + n] || x < sinks))) w[n] = -CUDART_INF_F;
         }
       };
       float big = 0.f;
       auto weights = [&] {
 #pragma unroll
-        for (int n = 0; n < N; n += 4) {
-          const float4 m = *(const float4*)(r.m + n);
+        for (int n = 0; n < CW; n += 4) {
+          const float4 m = *(const float4*)(r.m + c0 + n);
           w[n] = ex2f(fmaf(w[n], p.c, -m.x)); w[n + 1] = ex2f(fmaf(w[n + 1], p.c, -m.y));
           w[n + 2] = ex2f(fmaf(w[n + 2], p.c, -m.z)); w[n + 3] = ex2f(fmaf(w[n + 3], p.c, -m.w));
           big = fmaxf(fmaxf(big, fmaxf(w[n], w[n + 1])), fmaxf(w[n + 2], w[n + 3]));
         }
       };
       scores();
-      bool fresh = first;          // no sums or outputs of this segment yet
       if (first && !edge) {
         // any maximum will do that none of the positions passes by 2^8: that of a quarter of them, each warp for a quarter of the rows
 #pragma unroll
-        for (int k = 0; k < N / 4; ++k) {
-          const float top = u_warp_max(q4 == 0 ? w[k] : q4 == 1 ? w[N / 4 + k] : q4 == 2 ? w[N / 2 + k] : w[3 * N / 4 + k]);
-          if (lane == k % 32) r.m[q4 * (N / 4) + k] = fmaxf(NOTHING, top * p.c);
+        for (int k = 0; k < CW / 4; ++k) {
+          const float top = u_warp_max(q4 == 0 ? w[k] : q4 == 1 ? w[CW / 4 + k] : q4 == 2 ? w[CW / 2 + k] : w[3 * CW / 4 + k]);
+          if (lane == k) r.m[c0 + q4 * (CW / 4) + k] = fmaxf(NOTHING, top * p.c);
         }
-        u_sync();
+        u_sync(g);
       }
       bool renew = first && edge;
       if (!renew) {
         weights();
-        renew = u_any(big > 256.f);
+        renew = u_any(g, big > 256.f);
         if (renew) scores();
       }
       if (renew) {                 // the rows' maxima
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
+        for (int n = 0; n < CW; ++n) {
           const float top = u_warp_max(w[n]);
-          if (lane == (n & 31)) r.top[q4][n] = top;
+          if (lane == n) r.top[q4][c0 + n] = top;
         }
-        u_sync();
-        if (t < N) {
-          const float top = fmaxf(fmaxf(r.top[0][t], r.top[1][t]), fmaxf(r.top[2][t], r.top[3][t])), before = r.m[t], m = fmaxf(before, top * p.c);
-          r.m[t] = m;
-          r.factor[t] = ex2f(before - m);
+        u_sync(g);
+        if (t < CW) {
+          const int n = c0 + t;
+          const float top = fmaxf(fmaxf(r.top[0][n], r.top[1][n]), fmaxf(r.top[2][n], r.top[3][n])), before = r.m[n], m = fmaxf(before, top * p.c);
+          r.m[n] = m;
+          r.factor[n] = ex2f(before - m);
         }
-        u_sync();
-        if (!fresh) {              // ... and what is there already
+        u_sync(g);
+        if (!first) {              // ... and what is there already
           if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
           u_after();
 #pragma unroll
-          for (int n0 = 0; n0 < 2 * N; n0 += 16) {
-            const uint32_t at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + n0;
-            float y[16];
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + k * N + c0;
+            float y[CW];
             u_ld16(at, y);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] *= r.factor[(n0 + e) % N];
+            for (int e = 0; e < CW; ++e) y[e] *= r.factor[c0 + e];
             u_st16(at, y);
           }
           u_st_wait();
 #pragma unroll
-          for (int n = 0; n < N; ++n) l[n] *= r.factor[n];
+          for (int n = 0; n < CW; ++n) l[n] *= r.factor[c0 + n];
         }
         weights();
       }
 #pragma unroll
-      for (int n = 0; n < N; ++n) l[n] += w[n];
+      for (int n = 0; n < CW; ++n) l[n] += w[n];
       char* const v_s = smem + (2 * i + 1) % SLOTS * S::SLOT;
       bool keep = false;
       if (edge) {
         if (!dead && !u_wait(r.full + (2 * i + 1) % SLOTS, ((2 * i + 1) / SLOTS) & 1, r, limit)) dead = true;
-        if (hidden)                // values of positions that nothing sees: whatever lies there
-          for (int j = 0; j < PIECES; ++j) *(uint4*)(v_s + u_piece(UT, t, j)) = make_uint4(0, 0, 0, 0);
+        if (hidden && g == 0)      // values of positions that nothing sees: whatever lies there
+          for (int j = 0; j < PIECES; ++j) *(uint4*)(v_s + piece_of(t, j)) = make_uint4(0, 0, 0, 0);
         if (p.in.Q > 1) {          // some rows do not see all of the tile: a value that is not finite must not reach those as 0 * inf
           auto odd = [](uint32_t y) { return (y & 0x7f800000u) == 0x7f800000u || (y & 0x7f80u) == 0x7f80u; };
           bool strange = false;
           if (!hidden)
+#pragma unroll
             for (int j = 0; j < PIECES; ++j) {
-              const uint4 y = *(const uint4*)(v_s + u_piece(UT, t, j));
+              const uint4 y = *(const uint4*)(v_s + piece_of(t, j));
               strange = strange || odd(y.x) || odd(y.y) || odd(y.z) || odd(y.w);
             }
-          if (u_any(strange)) {    // it goes to the rows that see it by itself, and 0 takes its place
+          if (u_any(g, strange)) { // it goes to the rows that see it by itself, and 0 takes its place
             if (!first) {
               if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
               u_after();
             }
             keep = first;
-#pragma unroll 1
-            for (int n0 = 0; n0 < N; n0 += 16) {
-              const uint32_t o_at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + n0;
-              float y[16];
-              if (first) {
+            const uint32_t o_at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + c0;
+            float y[CW];
+            if (first) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) y[e] = 0.f;
-                u_st16(o_at + N, y);
-              } else u_ld16(o_at, y);
-              if (t < DP)
+              for (int e = 0; e < CW; ++e) y[e] = 0.f;
+              u_st16(o_at + N, y);
+            } else u_ld16(o_at, y);
+            if (t < DP)
 #pragma unroll 1
-                for (int pos = 0; pos < UT; ++pos) {
-                  const float z = __bfloat162float(*(const E*)(v_s + u_piece(UT, pos, t >> 3) + (t & 7) * 2));
-                  if (!(fabsf(z) < CUDART_INF_F))
+              for (int pos = 0; pos < UT; ++pos) {
+                const int xx = x0 + pos;
+                if (!(xx < now.s.n && (xx >= now.s.lo || xx < now.s.sk))) continue;
+                const float z = __bfloat162float(*(const E*)(v_s + piece_of(pos, t >> 3) + (t & 7) * 2));
+                if (!(fabsf(z) < CUDART_INF_F))
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                      const int xx = x0 + pos;
-                      if (xx <= r.to[n0 + e] && (xx >= r.from[n0 + e] || xx < sinks)) y[e] += z;
-                    }
-                }
-              u_st16(o_at, y);
-            }
+                  for (int e = 0; e < CW; ++e)
+                    if (xx <= r.to[c0 + e] && (xx >= r.from[c0 + e] || xx < sinks)) y[e] += z;
+              }
+            u_st16(o_at, y);
             u_st_wait();
-            u_sync();
-            for (int j = 0; j < PIECES; ++j) {
-              uint4* const at = (uint4*)(v_s + u_piece(UT, t, j));
-              auto clean = [](uint32_t y) { return ((y & 0x7f800000u) == 0x7f800000u ? 0u : y & 0xffff0000u) | ((y & 0x7f80u) == 0x7f80u ? 0u : y & 0xffffu); };
-              const uint4 y = *at;
-              *at = make_uint4(clean(y.x), clean(y.y), clean(y.z), clean(y.w));
-            }
+            asm volatile("bar.sync 7, %0;" ::"n"(128 * GROUPS) : "memory");      // (all groups have found it)
+            if (g == 0 && !hidden)
+              for (int j = 0; j < PIECES; ++j) {
+                uint4* const at = (uint4*)(v_s + piece_of(t, j));
+                auto clean = [](uint32_t y) { return ((y & 0x7f800000u) == 0x7f800000u ? 0u : y & 0xffff0000u) | ((y & 0x7f80u) == 0x7f80u ? 0u : y & 0xffffu); };
+                const uint4 y = *at;
+                *at = make_uint4(clean(y.x), clean(y.y), clean(y.z), clean(y.w));
+              }
           }
         }
       }
-      if (t == 0) *(volatile int*)(r.keep + (i & 1)) = keep;
+      if (t == 0 && g == 0) *(volatile int*)(r.keep + (i & 1)) = keep;
       if (i >= PB && !dead && !u_wait(r.pv_done + ((i - PB) & 1), ((i - PB) >> 1) & 1, r, limit)) dead = true;      // the buffer's last product
       {
-        char* const at = p_s + (i % PB) * S::P_BYTES + (t >> 6) * (N * 256) + (t & 7) * 2;
+        char* const at = p_s + (i % PB) * S::P_BYTES + (t >> 6) * (N * 256) + (t & 7) * 2 + c0 * 128;
         const uint32_t piece = (uint32_t)((t >> 3) & 7) << 4;
 #pragma unroll
-        for (int n = 0; n < N; n += 2) {
+        for (int n = 0; n < CW; n += 2) {
           const uint32_t a = __float_as_uint(w[n]), b = __float_as_uint(w[n + 1]);
           const float2 rest = fadd2(make_float2(w[n], w[n + 1]), make_float2(-__uint_as_float(a & 0xffff0000u), -__uint_as_float(b & 0xffff0000u)));
           const uint32_t lo = pack_bf16x2(rest.x, rest.y);
-          char* const c0 = at + n * 128 + (piece ^ (uint32_t)((n & 7) << 4));
-          char* const c1 = at + (n + 1) * 128 + (piece ^ (uint32_t)(((n + 1) & 7) << 4));
-          *(uint16_t*)c0 = (uint16_t)(a >> 16);
-          *(uint16_t*)c1 = (uint16_t)(b >> 16);
-          *(uint16_t*)(c0 + N * 128) = (uint16_t)lo;
-          *(uint16_t*)(c1 + N * 128) = (uint16_t)(lo >> 16);
+          char* const p0 = at + n * 128 + (piece ^ (uint32_t)((n & 7) << 4));
+          char* const p1 = at + (n + 1) * 128 + (piece ^ (uint32_t)(((n + 1) & 7) << 4));
+          *(uint16_t*)p0 = (uint16_t)(a >> 16);
+          *(uint16_t*)p1 = (uint16_t)(b >> 16);
+          *(uint16_t*)(p0 + N * 128) = (uint16_t)lo;
+          *(uint16_t*)(p1 + N * 128) = (uint16_t)(lo >> 16);
         }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -506,11 +529,11 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
       u_arrive(r.p_ready + (i & 1));
       if (last.there) { finish(last, i - 1, r.m_before); last.there = false; }
       if (now.t + 1 == now.s.nt || i + 1 == n_tiles) {        // the segment ends, or the piece does
-        column_sums<N>(l, r.sum[seg & 1][q4], lane);
+        column_sums<CW>(l, r.sum[seg & 1][q4] + c0, lane);
         last = {now.b, now.hr, seg, now.s.status, i < now.t, now.t + 1 < now.s.nt, true, bad};
         if (i + 1 == n_tiles) {
           finish(last, i, r.m);
-          if (t == 0) {            // a segment that starts here and goes on: how many pieces behind have a share of it
+          if (t == 0 && g == 0) {  // a segment that starts here and goes on: how many pieces behind have a share of it
             const long long end = u0 + i - now.t + now.s.nt;
             p.desc[number] = last.tail && !last.head ? make_int4(now.b, now.hr, (int)((end - 1) / chunk) - number, (int)now.s.status) : make_int4(0, 0, 0, 0);
           }
@@ -527,11 +550,15 @@ template <int DP, int N> __global__ void __launch_bounds__(UTHREADS, 1) attn_umm
   }
 }
 
-template <int DP, int N> cudaError_t launch(const AttnParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int blocks, cudaStream_t st) {
+template <int DP, int N, bool GROUPED> cudaError_t launch(const AttnParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int blocks, cudaStream_t st) {
   using S = UShape<DP, N>;
-  auto* const fn = attn_umma_kernel<DP, N>;
+  auto* const fn = attn_umma_kernel<DP, N, GROUPED>;
   const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-  return e != cudaSuccess ? e : launch_pdl(fn, dim3((unsigned)blocks), UTHREADS, S::SMEM, st, true, p, k_map, v_map);
+  return e != cudaSuccess ? e : launch_pdl(fn, dim3((unsigned)blocks), S::THREADS, S::SMEM, st, true, p, k_map, v_map);
+}
+template <int DP, bool GROUPED> cudaError_t launch(const AttnParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int blocks, cudaStream_t st) {
+  const int n = umma_rows(p.in);
+  return n == 16 ? launch<DP, 16, GROUPED>(p, k_map, v_map, blocks, st) : n == 32 ? launch<DP, 32, GROUPED>(p, k_map, v_map, blocks, st) : launch<DP, 64, GROUPED>(p, k_map, v_map, blocks, st);
 }
 
 }  // namespace
@@ -542,9 +569,7 @@ int umma_rows(const saki_attn_in& in) {
 }
 
 cudaError_t launch_umma(const AttnParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int blocks, cudaStream_t st) {
-  const int n = umma_rows(p.in);
-  if (p.in.D <= 64) return n == 16 ? launch<64, 16>(p, k_map, v_map, blocks, st) : n == 32 ? launch<64, 32>(p, k_map, v_map, blocks, st) : launch<64, 64>(p, k_map, v_map, blocks, st);
-  return n == 16 ? launch<128, 16>(p, k_map, v_map, blocks, st) : n == 32 ? launch<128, 32>(p, k_map, v_map, blocks, st) : launch<128, 64>(p, k_map, v_map, blocks, st);
+  return p.in.D <= 64 ? launch<64, false>(p, k_map, v_map, blocks, st) : p.map_mode ? launch<128, true>(p, k_map, v_map, blocks, st) : launch<128, false>(p, k_map, v_map, blocks, st);
 }
 
 }  // namespace attn
