@@ -5,15 +5,17 @@
 //   scores^T [128 positions x N]  = K [128 x D] . Q^T [D x N]              K as stored (K-major), 128-byte swizzle as TMA lays it down
 //   out^T    [128 columns x 2 N] += V^T [D x 128] . P^T [128 x 2 N]        V as stored (M-major); P in two bf16 terms (16 bits), side by side: V is read once
 // One block on each SM, its piece of the line, and
-//   warp 0     looks pages up and loads keys and values by TMA into a ring of slots (one tile's keys or values each)
-//   warp 1     one thread issues the products: scores of tile i + 1 ahead of the sums of tile i
-//   warp 2     holds tensor memory
-//   warp 3     loads the queries of the segments, two ahead
-//   from 4 on  groups of four warps, 16 queries each (one group took 2.2 us for a tile of 32 queries, against 1.5 us on the bus), a thread per position:
-//              reads its scores, takes 2^(c s - m), adds them up, and leaves the weights in shared memory for the next product.  m is a row's maximum as of some tile: it is brought up to date (and sums and outputs with it) only when a weight passes 2^8,
-//              so that a common tile needs no maximum over its positions and no pass over the output.  At a segment's end a thread per
-//              column of the output divides and writes, after the next tile's weights are on their way.
-// What bounds it: HBM (two tiles of 64 KB in flight on an SM); a tile's exponentials take a third of its time on the bus at N = 32.
+//   warp 0      looks pages up and loads keys and values by TMA into a ring of slots (one tile's keys or values each)
+//   warp 1      one thread issues the products: scores of tile i + 1 ahead of the sums of tile i
+//   warp 2      holds tensor memory
+//   warp 3      loads the queries of the segments, two ahead
+//   warps 4-11  two groups, a thread per position: it reads its scores, takes 2^(c s - m), adds them up, and leaves the weights in shared memory for the next
+//               product.  Up to 32 queries the groups take turns, a tile each, with sums, maxima and outputs of their own (a tile takes one group about as long
+//               as it takes on the bus; most of that is latency); 64 queries they share.  m is a row's maximum as of some tile: it is brought up
+//               to date (and sums and outputs with it) only when a weight passes 2^8, so that a common tile needs no maximum over its positions and no pass over
+//               the output.
+//   warps 12-15 a thread per column of the output: at a segment's end they join the groups' outputs, divide and write, while the groups go on
+// What bounds it: HBM (two to three tiles of 64 KB in flight on an SM).
 // Every wait is bounded: a wait that runs out ends all roles' waits, the segments that are left are flagged, and the block leaves.
 #include "saki_attention.cuh"
 
@@ -23,33 +25,39 @@ namespace attn {
 
 namespace {
 
-constexpr int UT = 128, CW = 16;             // positions of a tile; queries of a group of warps
+constexpr int UT = 128, THREADS = 512;       // positions of a tile
 
 template <int DP, int N> struct UShape {
-  static constexpr int GROUPS = N / CW, THREADS = 128 + 128 * GROUPS;
+  static constexpr int TEAMS = 1, CW = N * TEAMS / 2;        // groups that take turns; queries of a group
   static constexpr int SLABS = DP / 64, SLOT = UT * DP * 2;                // keys or values of a tile
   static constexpr int P_BYTES = 2 * N * UT * 2, P_BUFS = N <= 32 ? 2 : 1; // two terms
   static constexpr int Q_BYTES = N * DP * 2;
-  static constexpr int FIXED = P_BUFS * P_BYTES + 2 * Q_BYTES + 7168 + 1024;      // and the rest, alignment
+  static constexpr int FIXED = P_BUFS * P_BYTES + 2 * Q_BYTES + 6656 + 1024;      // and the rest, alignment
   static constexpr int FIT = (227 * 1024 - FIXED) / SLOT, SLOTS = FIT < 12 ? FIT : 12;
   static constexpr int SMEM = SLOTS * SLOT + FIXED;
-  static constexpr int COLS = 6 * N <= 128 ? 128 : 6 * N <= 256 ? 256 : 512;             // scores and outputs (two terms), two buffers each
+  static constexpr int COLS = (2 + 4 * TEAMS) * N <= 128 ? 128 : (2 + 4 * TEAMS) * N <= 256 ? 256 : 512;                    // two buffers of scores; by segment and team, outputs in two terms
   static_assert(SLOTS >= 4, "two tiles");
 };
 
-template <int THREADS> struct URest {      // of shared memory
+struct URest {            // of shared memory
   uint64_t full[12], empty[12], q_full[2], q_empty[2], s_full[2], p_ready[2], pv_done[2], drain;
+  uint64_t seg_sums[2], seg_pv[2], seg_free[2];      // by segment: the groups' sums are there; so are the outputs; both have been read
   LineShared<THREADS> line;
-  alignas(16) float m[64];      // (read four at a time)
-  float m_before[64], factor[64], top[4][64], sum[2][4][64], inverse[64];      // (sums: by segment and warp)
-  int64_t row_at[2][64];  // by segment: where a row's output starts, -1: there is none
-  int to[64], from[64], lse_at[2][64];
+  // by team and query (two teams: 32 queries each)
+  alignas(16) float m[64];                   // (read four at a time)
+  float factor[64], top[4][64];
+  int to[64], from[64];
+  // by segment, team and query, for the warps that write
+  float end_m[2][64], end_sum[2][4][64];
+  int end_has[2][2], end_bad[2][2];
+  float scale[64];
+  int64_t row_at[64];     // where a row's output starts, -1: there is none
   int bad[8];             // by tile: a page outside the pool
-  int keep[2];            // by P buffer: the tile's sums go on top of what is there although it is its segment's first
+  int keep[2];            // by tile: its sums go on top of what is there although it is its team's first of the segment
   int abort;
   uint32_t tmem;
 };
-static_assert(sizeof(URest<640>) <= 7168, "what is left of shared memory");
+static_assert(sizeof(URest) <= 6656, "what is left of shared memory");
 
 template <typename R> __device__ __forceinline__ bool u_wait(uint64_t* bar, uint32_t parity, R& r, long long limit) {
   if (limit >= WAIT_LIMIT_CYCLES && mbar_try_wait(bar, parity)) return true;
@@ -77,19 +85,28 @@ __device__ __forceinline__ void u_mma(uint32_t d, uint64_t a, uint64_t b, uint32
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void u_ld16(uint32_t at, float* x) {
-  uint32_t r[16];
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                 "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(at) : "memory");
+// 8 or 16 columns of the thread's lane
+template <int C> __device__ __forceinline__ void u_ld(uint32_t at, float* x) {
+  uint32_t r[C];
+  if constexpr (C == 16)
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(at) : "memory");
+  else
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(at) : "memory");
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r[i]);
+  for (int i = 0; i < C; ++i) x[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void u_st16(uint32_t at, const float* x) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-               ::"r"(at), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]),
-                 "f"(x[8]), "f"(x[9]), "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]) : "memory");
+template <int C> __device__ __forceinline__ void u_st(uint32_t at, const float* x) {
+  if constexpr (C == 16)
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(at), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]),
+                   "f"(x[8]), "f"(x[9]), "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]) : "memory");
+  else
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(at), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
 }
 __device__ __forceinline__ void u_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // the 128 threads of group g of warps
@@ -136,22 +153,22 @@ constexpr float NOTHING = -1e30f;       // the maximum of a row that has seen no
 
 // GROUPED (D = 128): a box brings both slabs of its positions, [8 positions][2 slabs][8 rows of 128 bytes]; else [slab][128 rows of 128 bytes].  (Boxes of a page
 // of 16 positions are 2 KB then, and 32 of them a tile take longer than the bus: 64 sequences of 4096 at 72 % of the copy rate, 88 % with pages of 64.)
-template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<DP, N>::THREADS, 1) attn_umma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS, 1) attn_umma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using S = UShape<DP, N>;
   using E = __nv_bfloat16;
-  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS, THREADS = S::THREADS, GROUPS = S::GROUPS;
+  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS, TEAMS = S::TEAMS, CW = S::CW, LD = CW < 16 ? CW : 16;
   constexpr uint32_t SLAB = GROUPED ? 1024 : UT * 128, EIGHT = GROUPED ? S::SLABS * 1024 : 1024;      // bytes from a slab to the next, from eight positions to the next
   auto piece_of = [](int t, int j) { return (uint32_t)((t >> 3) * EIGHT + (j >> 3) * SLAB + (t & 7) * 128 + (((j & 7) ^ (t & 7)) << 4)); };
   extern __shared__ char u_raw[];
   char* const smem = (char*)(((uintptr_t)u_raw + 1023) & ~(uintptr_t)1023);
   char* const p_s = smem + SLOTS * S::SLOT;
   char* const q_s = p_s + PB * S::P_BYTES;
-  URest<THREADS>& r = *(URest<THREADS>*)(q_s + 2 * S::Q_BYTES);
+  URest& r = *(URest*)(q_s + 2 * S::Q_BYTES);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
     for (int i = 0; i < SLOTS; ++i) { mbar_init(r.full + i, 1); mbar_init(r.empty + i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(r.q_full + i, 1); mbar_init(r.q_empty + i, 1); mbar_init(r.s_full + i, 1); mbar_init(r.p_ready + i, 128 * GROUPS); mbar_init(r.pv_done + i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(r.q_full + i, 1); mbar_init(r.q_empty + i, 1); mbar_init(r.s_full + i, 1); mbar_init(r.p_ready + i, TEAMS == 2 ? 128 : 256); mbar_init(r.pv_done + i, 1); mbar_init(r.seg_sums + i, 256); mbar_init(r.seg_pv + i, 1); mbar_init(r.seg_free + i, 128); }
     mbar_init(&r.drain, 1);
     r.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -232,7 +249,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       // ---- products
       Cursor<UT> qk;
       qk.at(p, r.line.b[0], u0 - r.line.before[0]);
-      int seg = 0, acc = -1;                  // segments whose queries have been used; output buffer of the sums' segment
+      int seg = 0, out = -1, in_seg = 0;      // segments whose queries have been used; the sums' segment, and its tiles so far
       bool qk_first = true;
       uint32_t first = 0;                     // bit i % 2: tile i is its segment's first
       const uint32_t id_s = u_idesc<N>(false), id_o = u_idesc<2 * N>(true);
@@ -260,15 +277,20 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         const int load = 2 * i + 1, slot = load % SLOTS, pb = i % PB;
         if (!u_wait(r.p_ready + (i & 1), (i >> 1) & 1, r, limit) || !u_wait(r.full + slot, (load / SLOTS) & 1, r, limit)) { ok = false; break; }
         u_after();
-        const bool new_seg = first >> (i & 1) & 1u;
-        if (new_seg) ++acc;
-        const bool on_top = !new_seg || *(volatile int*)(r.keep + (i & 1));
-        const uint32_t v = smem_addr(smem + slot * S::SLOT), pa = smem_addr(p_s + pb * S::P_BYTES), o = tmem + 2 * N + (acc & 1) * 2 * N;
+        if (first >> (i & 1) & 1u) {
+          ++out; in_seg = 0;
+          if (!u_wait(r.seg_free + (out & 1), ((out >> 1) & 1) ^ 1u, r, limit)) { ok = false; break; }
+          u_after();
+        }
+        const bool on_top = in_seg >= TEAMS || *(volatile int*)(r.keep + (i & 1));
+        ++in_seg;
+        const uint32_t v = smem_addr(smem + slot * S::SLOT), pa = smem_addr(p_s + pb * S::P_BYTES), o = tmem + 2 * N + ((out & 1) * TEAMS + (TEAMS == 2 ? i & 1 : 0)) * 2 * N;
 #pragma unroll
         for (int e = 0; e < 8; ++e)           // steps of 16 positions
           u_mma(o, u_desc(v + e * 2 * EIGHT, DP == 128 ? SLAB : 0, EIGHT), u_desc(pa + (e >> 2) * (N * 256) + (e & 3) * 32, 16, 1024), id_o, e > 0 || on_top);
         u_commit(r.empty + slot);
         u_commit(r.pv_done + (i & 1));
+        if (i + 1 == n_tiles || (first >> ((i + 1) & 1) & 1u)) u_commit(r.seg_pv + (out & 1));
       }
       if (!ok) {                              // nothing of it is under way when tensor memory goes
         u_commit(&r.drain);
@@ -315,231 +337,281 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       at.t = at.s.nt - 1;
       at.next(p);
     }
-  } else if (warp >= 4) {
-    // ---- weights: thread t of group g is position t of the tile, and column t of the output, for queries c0 to c0 + CW
-    const int t = (tid - 128) & 127, q4 = warp & 3, g = (warp - 4) >> 2, c0 = g * CW;
+  } else if (warp >= 4 && warp < 12) {
+    // ---- weights: thread t of group g is position t of the tile, for queries c0 to c0 + CW
+    const int t = (tid - 128) & 127, q4 = warp & 3, g = (warp - 4) >> 2, team = TEAMS == 2 ? g : 0, c0 = TEAMS == 2 ? 0 : g * CW;
     const uint32_t lanes = (uint32_t)(q4 * 32) << 16;
+    const int mine = team * 32 + c0;          // where the group's queries are in what is kept by query
+    float* const m_s = r.m + mine;
+    float* const factor_s = r.factor + mine;
+    int* const to_s = r.to + mine;
+    int* const from_s = r.from + mine;
+    auto by_four = [&](const float* x, auto&& f) {
+#pragma unroll
+      for (int n = 0; n < CW; n += 4) { const float4 y = *(const float4*)(x + n); f(n, y.x); f(n + 1, y.y); f(n + 2, y.z); f(n + 3, y.w); }
+    };
     Cursor<UT> now;
     now.at(p, r.line.b[0], u0 - r.line.before[0]);
-    bool dead = false;
-    float l[CW];
-    float bad = 0.f;
-    int seg = -1;
-    struct Done { int b, hr, seg; uint32_t st; bool head, tail, there; float bad; } last = {};      // a segment whose results are not written yet
-    last.there = false;
-    // segment `d`, whose last tile is tile i, with the maxima m
-    auto finish = [&](const Done& d, int i, const float* m) {
-      if (!dead && !u_wait(r.pv_done + (i & 1), (i >> 1) & 1, r, limit)) dead = true;
-      u_after();
-      const float b = u_any(g, dead) ? -2.f : d.bad;      // (and the sums are there)
-      const uint32_t st = d.st | status_of(b);
-      float* const part = p.part + (number * 2 + (d.head ? 0 : 1)) * (int64_t)PART<N, DP>;
-      const int sb = d.seg & 1;
-      const bool partial = d.head || d.tail;
-      if (t < CW && r.row_at[sb][c0 + t] >= 0) {
-        const int n = c0 + t;
-        const float sum = (r.sum[sb][0][n] + r.sum[sb][1][n]) + (r.sum[sb][2][n] + r.sum[sb][3][n]);
-        r.inverse[n] = partial ? 1.f : st || sum == 0.f ? 0.f : 1.f / sum;
-        if (partial) *(float2*)(part + N * DP + n * 2) = make_float2(m[n], b < 0.f ? b : sum);
-        else if (p.out.lse) p.out.lse[(int64_t)d.b * p.in.Q * p.in.Hq + r.lse_at[sb][n]] = lse_of(m[n], st ? 0.f : sum);
-      }
-      float o[CW], lo[CW];
-      u_ld16(tmem + lanes + 2 * N + sb * 2 * N + c0, o);
-      u_ld16(tmem + lanes + 2 * N + sb * 2 * N + N + c0, lo);
-      u_sync(g);
-#pragma unroll
-      for (int k = 0; k < CW; ++k) {
-        const int64_t at = r.row_at[sb][c0 + k];
-        const float inv = r.inverse[c0 + k];
-        if (at >= 0) {
-          if (partial) { if (t < DP) part[(c0 + k) * DP + t] = o[k] + lo[k]; }
-          else if (t < p.in.D) ((E*)p.out.out)[at + t] = __float2bfloat16_rn(inv == 0.f ? 0.f : (o[k] + lo[k]) * inv);
-        }
-      }
-      if (!partial && d.hr == 0 && t == 0 && g == 0) put_status(p, d.b, st);
-      u_before();
-    };
+    bool dead = false, fresh = true;          // no tile of the segment so far
+    float l[CW], bad = 0.f;
+    int seg = 0;
 #pragma unroll 1
     for (int i = 0; i < n_tiles; ++i) {
-      const bool first = i == 0 || now.t == 0;
-      const int x0 = tile_start<UT>(now.s, now.t), x = x0 + t;
-      if (first) {
-        ++seg;
-        bad = 0.f;
-        if (i > 0) u_sync(g);      // (the segments before have been read out)
-        if (t < CW) {
-          const int n = c0 + t, h = p.RB == 1 ? now.hr : now.hr / p.RB, row = (now.hr - h * p.RB) * N + n, j = row / p.G;
-          const Sight s = sight_of(p, now.s, row);
-          r.to[n] = s.to; r.from[n] = s.from;
-          r.row_at[seg & 1][n] = row < p.R ? out_at(p, now.b, h, row) : -1;
-          r.lse_at[seg & 1][n] = j * p.in.Hq + h * p.G + row - j * p.G;
-          r.m_before[n] = r.m[n];
-          r.m[n] = NOTHING;
-        }
-#pragma unroll
-        for (int n = 0; n < CW; ++n) l[n] = 0.f;
-        u_sync(g);
-      }
-      if (!dead && !u_wait(r.s_full + (i & 1), (i >> 1) & 1, r, limit)) dead = true;
-      u_after();
-      float w[CW];
-      if (*(volatile int*)(r.bad + (i & 7))) bad = -1.f;
-      const bool edge = !whole<UT>(p, now.s, x0), hidden = !(x < now.s.n && (x >= now.s.lo || x < now.s.sk));
-      const int sinks = p.in.window > 0 ? p.in.sinks : 0;
-      auto scores = [&] {
-        u_ld16(tmem + lanes + (i & 1) * N + c0, w);
-        if (edge) {
-#pragma unroll
-          for (int n = 0; n < CW; ++n)
-            if (hidden || !(x <= r.to[c0 + n] && (x >= r.from[c0 + n] || x < sinks))) w[n] = -CUDART_INF_F;
-        }
-      };
-      float big = 0.f;
-      auto weights = [&] {
-#pragma unroll
-        for (int n = 0; n < CW; n += 4) {
-          const float4 m = *(const float4*)(r.m + c0 + n);
-          w[n] = ex2f(fmaf(w[n], p.c, -m.x)); w[n + 1] = ex2f(fmaf(w[n + 1], p.c, -m.y));
-          w[n + 2] = ex2f(fmaf(w[n + 2], p.c, -m.z)); w[n + 3] = ex2f(fmaf(w[n + 3], p.c, -m.w));
-          big = fmaxf(fmaxf(big, fmaxf(w[n], w[n + 1])), fmaxf(w[n + 2], w[n + 3]));
-        }
-      };
-      scores();
-      if (first && !edge) {
-        // any maximum will do that none of the positions passes by 2^8: that of a quarter of them, each warp for a quarter of the rows
-#pragma unroll
-        for (int k = 0; k < CW / 4; ++k) {
-          const float top = u_warp_max(q4 == 0 ? w[k] : q4 == 1 ? w[CW / 4 + k] : q4 == 2 ? w[CW / 2 + k] : w[3 * CW / 4 + k]);
-          if (lane == k) r.m[c0 + q4 * (CW / 4) + k] = fmaxf(NOTHING, top * p.c);
-        }
-        u_sync(g);
-      }
-      bool renew = first && edge;
-      if (!renew) {
-        weights();
-        renew = u_any(g, big > 256.f);
-        if (renew) scores();
-      }
-      if (renew) {                 // the rows' maxima
-#pragma unroll
-        for (int n = 0; n < CW; ++n) {
-          const float top = u_warp_max(w[n]);
-          if (lane == n) r.top[q4][c0 + n] = top;
-        }
-        u_sync(g);
-        if (t < CW) {
-          const int n = c0 + t;
-          const float top = fmaxf(fmaxf(r.top[0][n], r.top[1][n]), fmaxf(r.top[2][n], r.top[3][n])), before = r.m[n], m = fmaxf(before, top * p.c);
-          r.m[n] = m;
-          r.factor[n] = ex2f(before - m);
-        }
-        u_sync(g);
-        if (!first) {              // ... and what is there already
-          if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
-          u_after();
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const uint32_t at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + k * N + c0;
-            float y[CW];
-            u_ld16(at, y);
-#pragma unroll
-            for (int e = 0; e < CW; ++e) y[e] *= r.factor[c0 + e];
-            u_st16(at, y);
+      if (TEAMS == 1 || (i & 1) == g) {
+        const int x0 = tile_start<UT>(now.s, now.t), x = x0 + t;
+        if (fresh) {
+          u_sync(g);               // (the segment before is done with what is written here)
+          if (t < CW) {
+            const int h = p.RB == 1 ? now.hr : now.hr / p.RB;
+            const Sight s = sight_of(p, now.s, (now.hr - h * p.RB) * N + c0 + t);
+            to_s[t] = s.to; from_s[t] = s.from;
+            m_s[t] = NOTHING;
           }
-          u_st_wait();
 #pragma unroll
-          for (int n = 0; n < CW; ++n) l[n] *= r.factor[c0 + n];
+          for (int n = 0; n < CW; ++n) l[n] = 0.f;
+          bad = 0.f;
+          u_sync(g);
         }
-        weights();
-      }
+        if (!dead && !u_wait(r.s_full + (i & 1), (i >> 1) & 1, r, limit)) dead = true;
+        u_after();
+        float w[CW];
+        if (*(volatile int*)(r.bad + (i & 7))) bad = -1.f;
+        const bool edge = !whole<UT>(p, now.s, x0), hidden = !(x < now.s.n && (x >= now.s.lo || x < now.s.sk));
+        const int sinks = p.in.window > 0 ? p.in.sinks : 0;
+        auto scores = [&] {
 #pragma unroll
-      for (int n = 0; n < CW; ++n) l[n] += w[n];
-      char* const v_s = smem + (2 * i + 1) % SLOTS * S::SLOT;
-      bool keep = false;
-      if (edge) {
-        if (!dead && !u_wait(r.full + (2 * i + 1) % SLOTS, ((2 * i + 1) / SLOTS) & 1, r, limit)) dead = true;
-        if (hidden && g == 0)      // values of positions that nothing sees: whatever lies there
-          for (int j = 0; j < PIECES; ++j) *(uint4*)(v_s + piece_of(t, j)) = make_uint4(0, 0, 0, 0);
-        if (p.in.Q > 1) {          // some rows do not see all of the tile: a value that is not finite must not reach those as 0 * inf
-          auto odd = [](uint32_t y) { return (y & 0x7f800000u) == 0x7f800000u || (y & 0x7f80u) == 0x7f80u; };
-          bool strange = false;
-          if (!hidden)
+          for (int n = 0; n < CW; n += LD) u_ld<LD>(tmem + lanes + (i & 1) * N + c0 + n, w + n);
+          if (edge) {
 #pragma unroll
-            for (int j = 0; j < PIECES; ++j) {
-              const uint4 y = *(const uint4*)(v_s + piece_of(t, j));
-              strange = strange || odd(y.x) || odd(y.y) || odd(y.z) || odd(y.w);
-            }
-          if (u_any(g, strange)) { // it goes to the rows that see it by itself, and 0 takes its place
-            if (!first) {
-              if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
-              u_after();
-            }
-            keep = first;
-            const uint32_t o_at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + c0;
-            float y[CW];
-            if (first) {
+            for (int n = 0; n < CW; ++n)
+              if (hidden || !(x <= to_s[n] && (x >= from_s[n] || x < sinks))) w[n] = -CUDART_INF_F;
+          }
+        };
+        float big = 0.f;
+        auto weights = [&] {
+          by_four(m_s, [&](int n, float m) { w[n] = ex2f(fmaf(w[n], p.c, -m)); big = fmaxf(big, w[n]); });
+        };
+        scores();
+        if (fresh && !edge) {
+          // any maximum will do that none of the positions passes by 2^8: that of a quarter of them, each warp for a quarter of the rows
 #pragma unroll
-              for (int e = 0; e < CW; ++e) y[e] = 0.f;
-              u_st16(o_at + N, y);
-            } else u_ld16(o_at, y);
-            if (t < DP)
-#pragma unroll 1
-              for (int pos = 0; pos < UT; ++pos) {
-                const int xx = x0 + pos;
-                if (!(xx < now.s.n && (xx >= now.s.lo || xx < now.s.sk))) continue;
-                const float z = __bfloat162float(*(const E*)(v_s + piece_of(pos, t >> 3) + (t & 7) * 2));
-                if (!(fabsf(z) < CUDART_INF_F))
+          for (int k = 0; k < CW / 4; ++k) {
+            const float top = u_warp_max(q4 == 0 ? w[k] : q4 == 1 ? w[CW / 4 + k] : q4 == 2 ? w[CW / 2 + k] : w[3 * CW / 4 + k]);
+            if (lane == k) m_s[q4 * (CW / 4) + k] = fmaxf(NOTHING, top * p.c);
+          }
+          u_sync(g);
+        }
+        bool renew = fresh && edge;
+        if (!renew) {
+          weights();
+          renew = u_any(g, big > 256.f);
+          if (renew) scores();
+        }
+        if (renew) {               // the rows' maxima
 #pragma unroll
-                  for (int e = 0; e < CW; ++e)
-                    if (xx <= r.to[c0 + e] && (xx >= r.from[c0 + e] || xx < sinks)) y[e] += z;
+          for (int n = 0; n < CW; ++n) {
+            const float top = u_warp_max(w[n]);
+            if (lane == (n & 31)) r.top[q4][mine + n] = top;
+          }
+          u_sync(g);
+          if (t < CW) {
+            const int n = mine + t;
+            const float most = fmaxf(fmaxf(r.top[0][n], r.top[1][n]), fmaxf(r.top[2][n], r.top[3][n])), before = m_s[t], m = fmaxf(before, most * p.c);
+            m_s[t] = m;
+            factor_s[t] = ex2f(before - m);
+          }
+          u_sync(g);
+          if (!fresh) {            // ... and what is there already
+            if (!dead && !u_wait(r.pv_done + ((i - TEAMS) & 1), ((i - TEAMS) >> 1) & 1, r, limit)) dead = true;
+            u_after();
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int n0 = 0; n0 < CW; n0 += LD) {
+                const uint32_t at = tmem + lanes + 2 * N + ((seg & 1) * TEAMS + team) * 2 * N + k * N + c0 + n0;
+                float y[LD];
+                u_ld<LD>(at, y);
+#pragma unroll
+                for (int e = 0; e < LD; ++e) y[e] *= factor_s[n0 + e];
+                u_st<LD>(at, y);
               }
-            u_st16(o_at, y);
             u_st_wait();
-            asm volatile("bar.sync 7, %0;" ::"n"(128 * GROUPS) : "memory");      // (all groups have found it)
-            if (g == 0 && !hidden)
-              for (int j = 0; j < PIECES; ++j) {
-                uint4* const at = (uint4*)(v_s + piece_of(t, j));
-                auto clean = [](uint32_t y) { return ((y & 0x7f800000u) == 0x7f800000u ? 0u : y & 0xffff0000u) | ((y & 0x7f80u) == 0x7f80u ? 0u : y & 0xffffu); };
-                const uint4 y = *at;
-                *at = make_uint4(clean(y.x), clean(y.y), clean(y.z), clean(y.w));
-              }
+            by_four(factor_s, [&](int n, float f) { l[n] *= f; });
           }
+          weights();
         }
-      }
-      if (t == 0 && g == 0) *(volatile int*)(r.keep + (i & 1)) = keep;
-      if (i >= PB && !dead && !u_wait(r.pv_done + ((i - PB) & 1), ((i - PB) >> 1) & 1, r, limit)) dead = true;      // the buffer's last product
-      {
-        char* const at = p_s + (i % PB) * S::P_BYTES + (t >> 6) * (N * 256) + (t & 7) * 2 + c0 * 128;
-        const uint32_t piece = (uint32_t)((t >> 3) & 7) << 4;
 #pragma unroll
-        for (int n = 0; n < CW; n += 2) {
-          const uint32_t a = __float_as_uint(w[n]), b = __float_as_uint(w[n + 1]);
-          const float2 rest = fadd2(make_float2(w[n], w[n + 1]), make_float2(-__uint_as_float(a & 0xffff0000u), -__uint_as_float(b & 0xffff0000u)));
-          const uint32_t lo = pack_bf16x2(rest.x, rest.y);
-          char* const p0 = at + n * 128 + (piece ^ (uint32_t)((n & 7) << 4));
-          char* const p1 = at + (n + 1) * 128 + (piece ^ (uint32_t)(((n + 1) & 7) << 4));
-          *(uint16_t*)p0 = (uint16_t)(a >> 16);
-          *(uint16_t*)p1 = (uint16_t)(b >> 16);
-          *(uint16_t*)(p0 + N * 128) = (uint16_t)lo;
-          *(uint16_t*)(p1 + N * 128) = (uint16_t)(lo >> 16);
-        }
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      u_before();
-      u_arrive(r.p_ready + (i & 1));
-      if (last.there) { finish(last, i - 1, r.m_before); last.there = false; }
-      if (now.t + 1 == now.s.nt || i + 1 == n_tiles) {        // the segment ends, or the piece does
-        column_sums<CW>(l, r.sum[seg & 1][q4] + c0, lane);
-        last = {now.b, now.hr, seg, now.s.status, i < now.t, now.t + 1 < now.s.nt, true, bad};
-        if (i + 1 == n_tiles) {
-          finish(last, i, r.m);
-          if (t == 0 && g == 0) {  // a segment that starts here and goes on: how many pieces behind have a share of it
-            const long long end = u0 + i - now.t + now.s.nt;
-            p.desc[number] = last.tail && !last.head ? make_int4(now.b, now.hr, (int)((end - 1) / chunk) - number, (int)now.s.status) : make_int4(0, 0, 0, 0);
+        for (int n = 0; n < CW; ++n) l[n] += w[n];
+        char* const v_s = smem + (2 * i + 1) % SLOTS * S::SLOT;
+        bool keep = false;
+        if (edge) {
+          if (!dead && !u_wait(r.full + (2 * i + 1) % SLOTS, ((2 * i + 1) / SLOTS) & 1, r, limit)) dead = true;
+          if (hidden && (TEAMS == 2 || g == 0))      // values of positions that nothing sees: whatever lies there
+            for (int j = 0; j < PIECES; ++j) *(uint4*)(v_s + piece_of(t, j)) = make_uint4(0, 0, 0, 0);
+          if (p.in.Q > 1) {        // some rows do not see all of the tile: a value that is not finite must not reach those as 0 * inf
+            auto odd = [](uint32_t y) { return (y & 0x7f800000u) == 0x7f800000u || (y & 0x7f80u) == 0x7f80u; };
+            bool strange = false;
+            if (!hidden)
+#pragma unroll 4
+              for (int j = 0; j < PIECES; ++j) {
+                const uint4 y = *(const uint4*)(v_s + piece_of(t, j));
+                strange = strange || odd(y.x) || odd(y.y) || odd(y.z) || odd(y.w);
+              }
+            if (u_any(g, strange)) { // it goes to the rows that see it by itself, and 0 takes its place
+              if (!fresh) {
+                if (!dead && !u_wait(r.pv_done + ((i - TEAMS) & 1), ((i - TEAMS) >> 1) & 1, r, limit)) dead = true;
+              } else if (!dead && !u_wait(r.seg_free + (seg & 1), ((seg >> 1) & 1) ^ 1u, r, limit)) dead = true;
+              u_after();
+              keep = fresh;
+#pragma unroll 1
+              for (int n0 = 0; n0 < CW; n0 += LD) {
+                const uint32_t o_at = tmem + lanes + 2 * N + ((seg & 1) * TEAMS + team) * 2 * N + c0 + n0;
+                float y[LD];
+                if (fresh) {
+#pragma unroll
+                  for (int e = 0; e < LD; ++e) y[e] = 0.f;
+                  u_st<LD>(o_at + N, y);
+                } else u_ld<LD>(o_at, y);
+                if (t < DP)
+#pragma unroll 1
+                  for (int pos = 0; pos < UT; ++pos) {
+                    const int xx = x0 + pos;
+                    if (!(xx < now.s.n && (xx >= now.s.lo || xx < now.s.sk))) continue;
+                    const float z = __bfloat162float(*(const E*)(v_s + piece_of(pos, t >> 3) + (t & 7) * 2));
+                    if (!(fabsf(z) < CUDART_INF_F))
+#pragma unroll
+                      for (int e = 0; e < LD; ++e)
+                        if (xx <= to_s[n0 + e] && (xx >= from_s[n0 + e] || xx < sinks)) y[e] += z;
+                  }
+                u_st<LD>(o_at, y);
+              }
+              u_st_wait();
+              if constexpr (TEAMS == 2) u_sync(g);
+              else asm volatile("bar.sync 7, 256;" ::: "memory");      // (both groups have found it)
+              if (!hidden && (TEAMS == 2 || g == 0))
+                for (int j = 0; j < PIECES; ++j) {
+                  uint4* const at = (uint4*)(v_s + piece_of(t, j));
+                  auto clean = [](uint32_t y) { return ((y & 0x7f800000u) == 0x7f800000u ? 0u : y & 0xffff0000u) | ((y & 0x7f80u) == 0x7f80u ? 0u : y & 0xffffu); };
+                  const uint4 y = *at;
+                  *at = make_uint4(clean(y.x), clean(y.y), clean(y.z), clean(y.w));
+                }
+            }
           }
         }
+        if (t == 0 && (TEAMS == 2 || g == 0)) *(volatile int*)(r.keep + (i & 1)) = keep;
+        if (i >= PB && !dead && !u_wait(r.pv_done + ((i - PB) & 1), ((i - PB) >> 1) & 1, r, limit)) dead = true;      // the buffer's last product
+        {
+          char* const at = p_s + (i % PB) * S::P_BYTES + (t >> 6) * (N * 256) + (t & 7) * 2 + c0 * 128;
+          const uint32_t piece = (uint32_t)((t >> 3) & 7) << 4;
+#pragma unroll
+          for (int n = 0; n < CW; n += 2) {
+            const uint32_t a = __float_as_uint(w[n]), b = __float_as_uint(w[n + 1]);
+            const float2 rest = fadd2(make_float2(w[n], w[n + 1]), make_float2(-__uint_as_float(a & 0xffff0000u), -__uint_as_float(b & 0xffff0000u)));
+            const uint32_t lo = pack_bf16x2(rest.x, rest.y);
+            char* const p0 = at + n * 128 + (piece ^ (uint32_t)((n & 7) << 4));
+            char* const p1 = at + (n + 1) * 128 + (piece ^ (uint32_t)(((n + 1) & 7) << 4));
+            *(uint16_t*)p0 = (uint16_t)(a >> 16);
+            *(uint16_t*)p1 = (uint16_t)(b >> 16);
+            *(uint16_t*)(p0 + N * 128) = (uint16_t)lo;
+            *(uint16_t*)(p1 + N * 128) = (uint16_t)(lo >> 16);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        u_before();
+        u_arrive(r.p_ready + (i & 1));
+        fresh = false;
+      }
+      if (now.t + 1 == now.s.nt || i + 1 == n_tiles) {        // the segment ends, or the piece does: to the warps that write
+        const int sb = seg & 1;
+        if (!dead && !u_wait(r.seg_free + sb, ((seg >> 1) & 1) ^ 1u, r, limit)) dead = true;
+        if (!fresh) {
+          column_sums<CW>(l, r.end_sum[sb][q4] + mine, lane);
+          if (t < CW) r.end_m[sb][mine + t] = m_s[t];
+        }
+        if (t == 0 && (TEAMS == 2 || g == 0)) { r.end_has[sb][team] = !fresh; r.end_bad[sb][team] = !fresh && bad < 0.f; }
+        u_arrive(r.seg_sums + sb);
+        fresh = true;
+        ++seg;
       }
       now.next(p);
+    }
+  } else if (warp >= 12) {
+    // ---- results: thread t is column t of the output
+    const int t = tid & 127, q4 = warp & 3;
+    const uint32_t lanes = (uint32_t)(q4 * 32) << 16;
+    Cursor<UT> at;
+    at.at(p, r.line.b[0], u0 - r.line.before[0]);
+    bool dead = false;
+    int left = n_tiles;
+#pragma unroll 1
+    for (int seg = 0; left > 0; ++seg) {
+      const int sb = seg & 1, rest = at.s.nt - at.t;
+      const bool head = at.t > 0, tail = left < rest;        // the segment goes on from the piece before, or behind
+      const int h = p.RB == 1 ? at.hr : at.hr / p.RB;
+      const int n = t, row = (at.hr - h * p.RB) * N + t, j = row / p.G;
+      if (t < N) r.row_at[t] = row < p.R ? out_at(p, at.b, h, row) : -1;
+      if (!dead && !u_wait(r.seg_sums + sb, (seg >> 1) & 1, r, limit)) dead = true;
+      if (!dead && !u_wait(r.seg_pv + sb, (seg >> 1) & 1, r, limit)) dead = true;
+      u_after();
+      const float b = u_any(2, dead) ? -2.f : r.end_bad[sb][0] || (TEAMS == 2 && r.end_bad[sb][1]) ? -1.f : 0.f;
+      const uint32_t st = at.s.status | status_of(b);
+      const bool has0 = r.end_has[sb][0], has1 = TEAMS == 2 && r.end_has[sb][1], partial = head || tail;
+      float* const part = p.part + (number * 2 + (head ? 0 : 1)) * (int64_t)PART<N, DP>;
+      if (t < N) {
+        float m = NOTHING, sum = 0.f, f[2] = {0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < TEAMS; ++k)
+          if (k ? has1 : has0) m = fmaxf(m, r.end_m[sb][k * 32 + n]);
+#pragma unroll
+        for (int k = 0; k < TEAMS; ++k)
+          if (k ? has1 : has0) {
+            f[k] = ex2f(r.end_m[sb][k * 32 + n] - m);
+            sum += f[k] * ((r.end_sum[sb][0][k * 32 + n] + r.end_sum[sb][1][k * 32 + n]) + (r.end_sum[sb][2][k * 32 + n] + r.end_sum[sb][3][k * 32 + n]));
+          }
+        const float inv = partial ? 1.f : st || sum == 0.f ? 0.f : 1.f / sum;
+        r.scale[n] = inv == 0.f ? 0.f : f[0] * inv;      // (of a flagged segment nothing is used, whatever it is)
+        if constexpr (TEAMS == 2) r.scale[32 + n] = inv == 0.f ? 0.f : f[1] * inv;
+        if (row < p.R) {
+          if (partial) *(float2*)(part + N * DP + n * 2) = make_float2(m, b < 0.f ? b : sum);
+          else if (p.out.lse) p.out.lse[((int64_t)at.b * p.in.Q + j) * p.in.Hq + h * p.G + row - j * p.G] = lse_of(m, st ? 0.f : sum);
+        }
+      }
+      u_sync(2);
+#pragma unroll 1
+      for (int n0 = 0; n0 < N; n0 += 16) {
+        float o[16], y[16];
+        const uint32_t o_at = tmem + lanes + 2 * N + sb * TEAMS * 2 * N + n0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < TEAMS; ++k)
+          if (k ? has1 : has0)
+#pragma unroll
+            for (int term = 0; term < 2; ++term) {
+              u_ld<16>(o_at + k * 2 * N + term * N, y);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) { const float f = r.scale[k * 32 + n0 + e]; o[e] += f == 0.f ? 0.f : y[e] * f; }
+            }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int64_t to = r.row_at[n0 + e];
+          if (to >= 0) {
+            if (partial) { if (t < DP) part[(n0 + e) * DP + t] = o[e]; }
+            else if (t < p.in.D) ((E*)p.out.out)[to + t] = __float2bfloat16_rn(o[e]);
+          }
+        }
+      }
+      u_before();
+      u_arrive(r.seg_free + sb);
+      if (t == 0) {
+        if (!partial && at.hr == 0) put_status(p, at.b, st);
+        if (left <= rest)          // a segment that starts here and goes on: how many pieces behind have a share of it
+          p.desc[number] = tail && !head ? make_int4(at.b, at.hr, (int)((u0 + n_tiles - left - at.t + at.s.nt - 1) / chunk) - number, (int)at.s.status) : make_int4(0, 0, 0, 0);
+      }
+      left -= rest;
+      at.t = at.s.nt - 1;
+      at.next(p);
+      u_sync(2);                   // (row_at and scale are written again)
     }
   }
   u_before();
@@ -554,7 +626,7 @@ template <int DP, int N, bool GROUPED> cudaError_t launch(const AttnParams& p, c
   using S = UShape<DP, N>;
   auto* const fn = attn_umma_kernel<DP, N, GROUPED>;
   const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-  return e != cudaSuccess ? e : launch_pdl(fn, dim3((unsigned)blocks), S::THREADS, S::SMEM, st, true, p, k_map, v_map);
+  return e != cudaSuccess ? e : launch_pdl(fn, dim3((unsigned)blocks), THREADS, S::SMEM, st, true, p, k_map, v_map);
 }
 template <int DP, bool GROUPED> cudaError_t launch(const AttnParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int blocks, cudaStream_t st) {
   const int n = umma_rows(p.in);
