@@ -593,7 +593,7 @@ bool mode_fits(int mode, int64_t page, int64_t pos, int64_t head, const saki_att
 }  // namespace
 
 // bf16 heads of up to 128 on pages of whole eights go to the kernel on tcgen05
-static bool on_umma(const saki_attn_in& in) { return in.dtype == SAKI_BF16 && in.D <= 128 && in.page_size % 8 == 0; }
+static bool on_umma(const saki_attn_in& in) { return in.dtype == SAKI_BF16 && in.D > 16 && in.D <= 128 && in.page_size % 8 == 0; }
 
 int64_t attention_scratch_bytes(const saki_attn_in& in) {
   const Kernel k = pick(in);

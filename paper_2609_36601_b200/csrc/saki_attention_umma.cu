@@ -9,15 +9,16 @@
 //   warp 1      one thread issues the products: scores of tile i + 1 ahead of the sums of tile i
 //   warp 2      holds tensor memory
 //   warp 3      loads the queries of the segments, two ahead
-//   warps 4-11  two groups, a thread per position: it reads its scores, takes 2^(c s - m), adds them up, and leaves the weights in shared memory for the next
-//               product.  Up to 32 queries the groups take turns, a tile each, with sums, maxima and outputs of their own (a tile takes one group about as long
-//               as it takes on the bus; most of that is latency); 64 queries they share.  m is a row's maximum as of some tile: it is brought up
-//               to date (and sums and outputs with it) only when a weight passes 2^8, so that a common tile needs no maximum over its positions and no pass over
-//               the output.
-//   warps 12-15 a thread per column of the output: at a segment's end they join the groups' outputs, divide and write, while the groups go on
+//   from 4 on   groups of four warps that share a tile's queries (8 each, 16 of 64), a thread per position: it reads its scores, takes 2^(c s - m), adds them up, and
+//               leaves the weights in shared memory for the next product.  m is a row's maximum as of some tile: it is brought up to date (and
+//               sums and outputs with it) only when a weight passes 2^8, so that a common tile needs no maximum over its positions and no pass over
+//               the output.  (A group is a warp on each scheduler, which issues an instruction in four to six cycles: so few queries, and groups that
+//               share a tile.  Groups that took turns, a tile each, were slower: a tile's keys and values wait twice as long for their turn in the ring.)
+//   the last 4  a thread per column of the output: at a segment's end they divide and write, while the groups go on
 // What bounds it: HBM (two to three tiles of 64 KB in flight on an SM).
 // Every wait is bounded: a wait that runs out ends all roles' waits, the segments that are left are flagged, and the block leaves.
 #include "saki_attention.cuh"
+#include <climits>
 
 namespace saki {
 
@@ -25,39 +26,44 @@ namespace attn {
 
 namespace {
 
-constexpr int UT = 128, THREADS = 512;       // positions of a tile
+constexpr int UT = 128;                      // positions of a tile
 
 template <int DP, int N> struct UShape {
-  static constexpr int TEAMS = 1, CW = N * TEAMS / 2;        // groups that take turns; queries of a group
+  static constexpr int GROUPS = N == 16 ? 2 : 4, CW = N / GROUPS, THREADS = 256 + 128 * GROUPS;      // groups of warps, queries of a group
   static constexpr int SLABS = DP / 64, SLOT = UT * DP * 2;                // keys or values of a tile
   static constexpr int P_BYTES = 2 * N * UT * 2, P_BUFS = N <= 32 ? 2 : 1; // two terms
   static constexpr int Q_BYTES = N * DP * 2;
   static constexpr int FIXED = P_BUFS * P_BYTES + 2 * Q_BYTES + 6656 + 1024;      // and the rest, alignment
   static constexpr int FIT = (227 * 1024 - FIXED) / SLOT, SLOTS = FIT < 12 ? FIT : 12;
   static constexpr int SMEM = SLOTS * SLOT + FIXED;
-  static constexpr int COLS = (2 + 4 * TEAMS) * N <= 128 ? 128 : (2 + 4 * TEAMS) * N <= 256 ? 256 : 512;                    // two buffers of scores; by segment and team, outputs in two terms
+  // A product that goes on top of the one before it waits for it, some 170 cycles: sums are kept in as many chains as tensor memory has room for
+  static constexpr int CHAINS = 1;
+  static constexpr int COLS = 6 * CHAINS * N <= 256 ? 256 : 512;                         // two buffers of scores; by segment, outputs in two terms
   static_assert(SLOTS >= 4, "two tiles");
 };
 
-struct URest {            // of shared memory
+template <int THREADS> struct URest {      // of shared memory
   uint64_t full[12], empty[12], q_full[2], q_empty[2], s_full[2], p_ready[2], pv_done[2], drain;
   uint64_t seg_sums[2], seg_pv[2], seg_free[2];      // by segment: the groups' sums are there; so are the outputs; both have been read
   LineShared<THREADS> line;
-  // by team and query (two teams: 32 queries each)
+  // by query
   alignas(16) float m[64];                   // (read four at a time)
-  float factor[64], top[4][64];
+  float factor[64], top[4][64], inverse[64];
   int to[64], from[64];
-  // by segment, team and query, for the warps that write
+  int64_t row_at[64];                        // where a row's output starts, -1: there is none
+  // by segment, for the warps that write
   float end_m[2][64], end_sum[2][4][64];
-  int end_has[2][2], end_bad[2][2];
-  float scale[64];
-  int64_t row_at[64];     // where a row's output starts, -1: there is none
+  int end_bad[2];
   int bad[8];             // by tile: a page outside the pool
-  int keep[2];            // by tile: its sums go on top of what is there although it is its team's first of the segment
+  int keep[2];            // by tile: its sums go on top of what is there although it is the segment's first
   int abort;
   uint32_t tmem;
 };
-static_assert(sizeof(URest) <= 6656, "what is left of shared memory");
+static_assert(sizeof(URest<768>) <= 6656, "what is left of shared memory");
+
+// The loads of n tiles, in the order of the products: K0 K1 V0 K2 V1 ... V(n-1).  (Values with their keys would hold a slot for a tile's time longer.)
+__device__ __forceinline__ int load_of_keys(int i) { return i == 0 ? 0 : 2 * i - 1; }
+__device__ __forceinline__ int load_of_values(int i, int n) { return i + 1 < n ? 2 * i + 2 : 2 * n - 1; }
 
 template <typename R> __device__ __forceinline__ bool u_wait(uint64_t* bar, uint32_t parity, R& r, long long limit) {
   if (limit >= WAIT_LIMIT_CYCLES && mbar_try_wait(bar, parity)) return true;
@@ -74,16 +80,22 @@ __device__ __forceinline__ void u_commit(uint64_t* bar) {
 }
 __device__ __forceinline__ void u_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void u_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// shared-memory matrix descriptor, 128-byte swizzle.  K-major: `stride` from eight rows to the next.  M-major: `stride` from eight k to the next, `lead` from
-// 64 rows to the next
-__device__ __forceinline__ uint64_t u_desc(uint32_t at, uint32_t lead, uint32_t stride) {
-  return (uint64_t)((at & 0x3FFFF) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+// Shared-memory matrix descriptor, 128-byte swizzle, in two words.  Lower: address and, for an M-major operand, `lead`, the bytes from 64 rows to the next, in units
+// of 16 bytes; upper: `stride`, the bytes from eight rows (K-major) or eight k (M-major) to the next.  (The issuing thread takes its time for every
+// word that it has to compute and move: what is constant goes into the instruction.)
+__device__ __forceinline__ uint32_t u_lower(uint32_t at, uint32_t lead = 16) { return (at >> 4) | (lead >> 4) << 16; }
+__host__ __device__ constexpr uint32_t u_upper(uint32_t stride) { return (stride >> 4) | 1u << 14 | 2u << 29; }
 // instruction descriptor: float32 sums, bf16 operands, M = 128; A M-major if `a_m`
-template <int N> __host__ __device__ constexpr uint32_t u_idesc(bool a_m) { return (1u << 4) | (1u << 7) | (1u << 10) | (a_m ? 1u << 15 : 0u) | ((uint32_t)(N >> 3) << 17) | (8u << 24); }
-__device__ __forceinline__ void u_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+__host__ __device__ constexpr uint32_t u_idesc(int n, bool a_m) { return (1u << 4) | (1u << 7) | (1u << 10) | (a_m ? 1u << 15 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
+template <uint32_t A, uint32_t B, uint32_t IDESC> __device__ __forceinline__ void u_mma(uint32_t d, uint32_t a, uint32_t b) {      // on top of what is there
+  asm volatile("{\n\t.reg .b64 da, db;\n\t.reg .pred p;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %4};\n\tsetp.eq.u32 p, 0, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n\t}"
+               ::"r"(d), "r"(a), "r"(b), "n"(A), "n"(B), "n"(IDESC) : "memory");
+}
+template <uint32_t A, uint32_t B, uint32_t IDESC> __device__ __forceinline__ void u_mma(uint32_t d, uint32_t a, uint32_t b, bool on_top) {
+  asm volatile("{\n\t.reg .b64 da, db;\n\t.reg .pred p;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %4};\n\tsetp.ne.u32 p, %6, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n\t}"
+               ::"r"(d), "r"(a), "r"(b), "n"(A), "n"(B), "n"(IDESC), "r"((uint32_t)on_top) : "memory");
 }
 // 8 or 16 columns of the thread's lane
 template <int C> __device__ __forceinline__ void u_ld(uint32_t at, float* x) {
@@ -153,22 +165,22 @@ constexpr float NOTHING = -1e30f;       // the maximum of a row that has seen no
 
 // GROUPED (D = 128): a box brings both slabs of its positions, [8 positions][2 slabs][8 rows of 128 bytes]; else [slab][128 rows of 128 bytes].  (Boxes of a page
 // of 16 positions are 2 KB then, and 32 of them a tile take longer than the bus: 64 sequences of 4096 at 72 % of the copy rate, 88 % with pages of 64.)
-template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS, 1) attn_umma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<DP, N>::THREADS, 1) attn_umma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using S = UShape<DP, N>;
   using E = __nv_bfloat16;
-  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS, TEAMS = S::TEAMS, CW = S::CW, LD = CW < 16 ? CW : 16;
+  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS, GROUPS = S::GROUPS, THREADS = S::THREADS, CW = S::CW, LD = CW < 16 ? CW : 16, CH = S::CHAINS, O_AT = 2 * CH * N, O_COLS = 2 * CH * N;      // (where outputs start in tensor memory, columns of a segment's)
   constexpr uint32_t SLAB = GROUPED ? 1024 : UT * 128, EIGHT = GROUPED ? S::SLABS * 1024 : 1024;      // bytes from a slab to the next, from eight positions to the next
   auto piece_of = [](int t, int j) { return (uint32_t)((t >> 3) * EIGHT + (j >> 3) * SLAB + (t & 7) * 128 + (((j & 7) ^ (t & 7)) << 4)); };
   extern __shared__ char u_raw[];
   char* const smem = (char*)(((uintptr_t)u_raw + 1023) & ~(uintptr_t)1023);
   char* const p_s = smem + SLOTS * S::SLOT;
   char* const q_s = p_s + PB * S::P_BYTES;
-  URest& r = *(URest*)(q_s + 2 * S::Q_BYTES);
+  URest<THREADS>& r = *(URest<THREADS>*)(q_s + 2 * S::Q_BYTES);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
     for (int i = 0; i < SLOTS; ++i) { mbar_init(r.full + i, 1); mbar_init(r.empty + i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(r.q_full + i, 1); mbar_init(r.q_empty + i, 1); mbar_init(r.s_full + i, 1); mbar_init(r.p_ready + i, TEAMS == 2 ? 128 : 256); mbar_init(r.pv_done + i, 1); mbar_init(r.seg_sums + i, 256); mbar_init(r.seg_pv + i, 1); mbar_init(r.seg_free + i, 128); }
+    for (int i = 0; i < 2; ++i) { mbar_init(r.q_full + i, 1); mbar_init(r.q_empty + i, 1); mbar_init(r.s_full + i, 1); mbar_init(r.p_ready + i, 128 * GROUPS); mbar_init(r.pv_done + i, 1); mbar_init(r.seg_sums + i, 128 * GROUPS); mbar_init(r.seg_pv + i, 1); mbar_init(r.seg_free + i, 128); }
     mbar_init(&r.drain, 1);
     r.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -192,105 +204,123 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
   if (n_tiles == 0) {
     if (tid == 0) p.desc[number] = make_int4(0, 0, 0, 0);
   } else if (warp == 0) {
-    // ---- loads: tile i's keys are load 2 i, its values load 2 i + 1; load j goes to slot j % SLOTS
+    // ---- loads, in the order in which the products take them up; load j goes to slot j % SLOTS
     Cursor<UT> look;
     look.at(p, r.line.b[0], u0 - r.line.before[0]);
     const int boxes = UT / p.box, box_x = lane % boxes * p.box, slab = lane / boxes;
     const bool loads = GROUPED ? slab == 0 : slab < S::SLABS && slab * 64 < p.in.D;
     const uint32_t box_at = (uint32_t)(slab * SLAB + box_x / 8 * EIGHT), box_bytes = (uint32_t)p.box * (GROUPED ? 256 : 128);
-    int found = -1, slot_x = 0, head = 0;
-    // the page of the lane's box in the tile at the cursor, -1: nothing of it is seen, -2: outside the pool
-    auto look_up = [&] {
+    struct Box { int page, x, head; };        // page -1: nothing of the lane's box is seen, -2: it is outside the pool
+    auto look_up = [&]() -> Box {             // of the tile at the cursor
       const int x = tile_start<UT>(look.s, look.t) + box_x;
-      found = -1;
+      Box f = {-1, 0, p.RB == 1 ? look.hr : look.hr / p.RB};
       if (loads && x < look.s.n && (x + p.box > look.s.lo || x < look.s.sk)) {
         const int page = p.page_shift >= 0 ? x >> p.page_shift : (int)((unsigned)x / (unsigned)p.in.page_size);
-        found = p.in.page_table[look.b * p.in.ld_table + page];
-        slot_x = x - page * p.in.page_size;
-        if ((unsigned)found >= (unsigned)p.in.n_pages) found = -2;
+        f.page = p.in.page_table[look.b * p.in.ld_table + page];
+        f.x = x - page * p.in.page_size;
+        if ((unsigned)f.page >= (unsigned)p.in.n_pages) f.page = -2;
       }
-      head = p.RB == 1 ? look.hr : look.hr / p.RB;
+      return f;
     };
-    look_up();
-    int j = 0, slot = 0, done = 0;            // loads so far that have left
+    int j = 0, slot = 0;                      // loads so far
     uint32_t turn = 0;
     bool ok = true;
-    for (int i = 0; i < n_tiles && ok; ++i) {
-      const bool mine = found >= 0, bad = __any_sync(0xffffffffu, found == -2);
+    auto load = [&](const Box& f, bool values) {
+      const bool mine = f.page >= 0;
       const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * box_bytes;
-      const int page = found, x = slot_x, h = head;
+      ok = __all_sync(0xffffffffu, ok && u_wait(r.empty + slot, turn ^ 1u, r, limit));
+      if (!ok) return;
+      if (lane == 0) mbar_expect_tx(r.full + slot, bytes);
+      __syncwarp();
+      if (mine) {
+        const uint32_t to = smem_addr(smem + slot * S::SLOT) + box_at;
+        const CUtensorMap* const map = values ? &v_map : &k_map;
+        if constexpr (GROUPED) {
+          const int eights = p.in.page_size / 8;
+          tma_eights(to, map, p.map_mode == MAP_HEADS ? 2 * f.head : 0, f.x / 8 + (p.map_mode == MAP_RUN ? f.page * eights : 0),
+                     p.map_mode == MAP_HEADS ? f.page : p.map_mode == MAP_PAGES ? f.page * p.in.H + f.head : f.head, r.full + slot);
+        } else tma_box(to, map, slab * 64, f.head, f.x, f.page, r.full + slot);
+      }
+      ++j;
+      if (++slot == SLOTS) { slot = 0; turn ^= 1u; }
+    };
+    Box before = {}, now = look_up();
+    for (int i = 0; i < n_tiles && ok; ++i) {
+      const bool bad = __any_sync(0xffffffffu, now.page == -2);
       if (lane == 0) { *(volatile int*)(r.bad + (i & 7)) = bad; __threadfence_block(); }
       look.next(p);
-      if (i + 1 < n_tiles) look_up();         // (in flight while the slots are waited for)
-#pragma unroll 1
-      for (int kv = 0; kv < 2; ++kv) {
-        ok = ok && u_wait(r.empty + slot, turn ^ 1u, r, limit);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (lane == 0) mbar_expect_tx(r.full + slot, bytes);
-        __syncwarp();
-        if (mine) {
-          const uint32_t to = smem_addr(smem + slot * S::SLOT) + box_at;
-          const CUtensorMap* const map = kv ? &v_map : &k_map;
-          if constexpr (GROUPED) {
-            const int eights = p.in.page_size / 8;
-            tma_eights(to, map, p.map_mode == MAP_HEADS ? 2 * h : 0, x / 8 + (p.map_mode == MAP_RUN ? page * eights : 0),
-                       p.map_mode == MAP_HEADS ? page : p.map_mode == MAP_PAGES ? page * p.in.H + h : h, r.full + slot);
-          } else tma_box(to, map, slab * 64, h, x, page, r.full + slot);
-        }
-        ++j;
-        if (++slot == SLOTS) { slot = 0; turn ^= 1u; }
-      }
+      Box next = {};
+      if (i + 1 < n_tiles) next = look_up();  // (in flight while slots are waited for)
+      load(now, false);
+      if (i > 0 && ok) load(before, true);
+      before = now; now = next;
     }
+    if (ok) load(before, true);
     if (!ok)                                  // copies that are still on their way land before the block leaves
-      for (done = max(0, j - SLOTS); done < j; ++done) mbar_wait_bounded(r.full + done % SLOTS, (uint32_t)(done / SLOTS) & 1u);
+      for (int done = max(0, j - SLOTS); done < j; ++done) mbar_wait_bounded(r.full + done % SLOTS, (uint32_t)(done / SLOTS) & 1u);
   } else if (warp == 1) {
     if (lane == 0) {
-      // ---- products
+      // ---- products: scores of tiles 0 and 1; then, once tile i's weights are there, its outputs, and in between them the scores of tile i + 2
       Cursor<UT> qk;
       qk.at(p, r.line.b[0], u0 - r.line.before[0]);
-      int seg = 0, out = -1, in_seg = 0;      // segments whose queries have been used; the sums' segment, and its tiles so far
+      int seg = 0, out = -1;                  // segments whose queries have been used; the outputs' segment
       bool qk_first = true;
-      uint32_t first = 0;                     // bit i % 2: tile i is its segment's first
-      const uint32_t id_s = u_idesc<N>(false), id_o = u_idesc<2 * N>(true);
-      auto scores = [&](int i) -> bool {
-        const int load = 2 * i, slot = load % SLOTS, qb = seg & 1;
-        if (qk_first && !u_wait(r.q_full + qb, (seg >> 1) & 1, r, limit)) return false;
-        if (!u_wait(r.full + slot, (load / SLOTS) & 1, r, limit)) return false;
+      uint32_t first = 0;                     // bit i % 4: tile i is its segment's first
+      bool ok = true;
+      constexpr uint32_t ID_S = u_idesc(N, false), ID_O = u_idesc(2 * N, true), UP_KV = u_upper(EIGHT), UP_PQ = u_upper(1024);
+      const int steps = (p.in.D + 15) / 16;
+      uint32_t k_at = 0, q_at = 0, s_to = 0;
+      // the operands of tile i's scores are there (wait: waits for them)
+      auto scores_ready = [&](int i, bool wait) -> bool {
+        const int load = load_of_keys(i), slot = load % SLOTS, qb = seg & 1;
+        if (wait) {
+          if ((qk_first && !u_wait(r.q_full + qb, (seg >> 1) & 1, r, limit)) || !u_wait(r.full + slot, (load / SLOTS) & 1, r, limit)) { ok = false; return false; }
+        } else if ((qk_first && !mbar_test_wait(r.q_full + qb, (seg >> 1) & 1)) || !mbar_test_wait(r.full + slot, (load / SLOTS) & 1)) return false;
         u_after();
-        const uint32_t k = smem_addr(smem + slot * S::SLOT), q = smem_addr(q_s + qb * S::Q_BYTES);
-        first = (first & ~(1u << (i & 1))) | (uint32_t)qk_first << (i & 1);
-#pragma unroll
-        for (int e = 0; e < DP / 16; ++e)
-          if (e * 16 < p.in.D)
-            u_mma(tmem + (i & 1) * N, u_desc(k + (e >> 2) * SLAB + (e & 3) * 32, 16, EIGHT), u_desc(q + (e >> 2) * (N * 128) + (e & 3) * 32, 16, 1024), id_s, e > 0);
-        u_commit(r.empty + slot);
-        u_commit(r.s_full + (i & 1));
-        qk_first = qk.t + 1 == qk.s.nt;
-        if (qk_first) { u_commit(r.q_empty + qb); ++seg; }
-        qk.next(p);
+        k_at = u_lower(smem_addr(smem + slot * S::SLOT)); q_at = u_lower(smem_addr(q_s + qb * S::Q_BYTES)); s_to = tmem + (i & 1) * CH * N;
+        first = (first & ~(1u << (i & 3))) | (uint32_t)qk_first << (i & 3);
         return true;
       };
-      bool ok = scores(0);
-      for (int i = 0; i < n_tiles && ok; ++i) {
-        if (i + 1 < n_tiles && !scores(i + 1)) { ok = false; break; }
-        const int load = 2 * i + 1, slot = load % SLOTS, pb = i % PB;
-        if (!u_wait(r.p_ready + (i & 1), (i >> 1) & 1, r, limit) || !u_wait(r.full + slot, (load / SLOTS) & 1, r, limit)) { ok = false; break; }
-        u_after();
-        if (first >> (i & 1) & 1u) {
-          ++out; in_seg = 0;
-          if (!u_wait(r.seg_free + (out & 1), ((out >> 1) & 1) ^ 1u, r, limit)) { ok = false; break; }
-          u_after();
-        }
-        const bool on_top = in_seg >= TEAMS || *(volatile int*)(r.keep + (i & 1));
-        ++in_seg;
-        const uint32_t v = smem_addr(smem + slot * S::SLOT), pa = smem_addr(p_s + pb * S::P_BYTES), o = tmem + 2 * N + ((out & 1) * TEAMS + (TEAMS == 2 ? i & 1 : 0)) * 2 * N;
+      auto scores_step = [&](int e) {
+        const uint32_t k = k_at + ((e >> 2) * SLAB + (e & 3) * 32) / 16, q = q_at + ((e >> 2) * (N * 128) + (e & 3) * 32) / 16;
+        if (e == 0) u_mma<UP_KV, UP_PQ, ID_S>(s_to, k, q, false);
+        else if (e < steps) u_mma<UP_KV, UP_PQ, ID_S>(s_to, k, q);
+      };
+      auto scores_done = [&](int i) {
+        u_commit(r.empty + load_of_keys(i) % SLOTS);
+        u_commit(r.s_full + (i & 1));
+        qk_first = qk.t + 1 == qk.s.nt;
+        if (qk_first) { u_commit(r.q_empty + (seg & 1)); ++seg; }
+        qk.next(p);
+      };
+      auto scores = [&](int i) {
+        if (!scores_ready(i, true)) return;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)           // steps of 16 positions
-          u_mma(o, u_desc(v + e * 2 * EIGHT, DP == 128 ? SLAB : 0, EIGHT), u_desc(pa + (e >> 2) * (N * 256) + (e & 3) * 32, 16, 1024), id_o, e > 0 || on_top);
+        for (int e = 0; e < DP / 16; ++e) scores_step(e);
+        scores_done(i);
+      };
+      scores(0);
+      if (ok && n_tiles > 1) scores(1);
+      for (int i = 0; i < n_tiles && ok; ++i) {
+        const int load = load_of_values(i, n_tiles), slot = load % SLOTS;
+        if (!u_wait(r.p_ready + (i & 1), (i >> 1) & 1, r, limit) || !u_wait(r.full + slot, (load / SLOTS) & 1, r, limit)) { ok = false; break; }
+        const bool new_seg = first >> (i & 3) & 1u;
+        if (new_seg && !u_wait(r.seg_free + (++out & 1), ((out >> 1) & 1) ^ 1u, r, limit)) { ok = false; break; }
+        u_after();
+        const bool on_top = !new_seg || *(volatile int*)(r.keep + (i & 1)), more = i + 2 < n_tiles, along = more && scores_ready(i + 2, false);
+        const uint32_t v = u_lower(smem_addr(smem + slot * S::SLOT), DP == 128 ? SLAB : 0), w = u_lower(smem_addr(p_s + i % PB * S::P_BYTES)), o = tmem + O_AT + (out & 1) * O_COLS;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {         // steps of 16 positions
+          const uint32_t a = v + e * 2 * EIGHT / 16, b = w + ((e >> 2) * (N * 256) + (e & 3) * 32) / 16;
+          if (e == 0) u_mma<UP_KV, UP_PQ, ID_O>(o, a, b, on_top);
+          else u_mma<UP_KV, UP_PQ, ID_O>(o, a, b);
+          if (along) scores_step(e);
+        }
         u_commit(r.empty + slot);
         u_commit(r.pv_done + (i & 1));
-        if (i + 1 == n_tiles || (first >> ((i + 1) & 1) & 1u)) u_commit(r.seg_pv + (out & 1));
+        if (i + 1 == n_tiles || (first >> ((i + 1) & 3) & 1u)) u_commit(r.seg_pv + (out & 1));
+        if (along) scores_done(i + 2);
+        else if (more) scores(i + 2);
       }
       if (!ok) {                              // nothing of it is under way when tensor memory goes
         u_commit(&r.drain);
@@ -337,15 +367,14 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
       at.t = at.s.nt - 1;
       at.next(p);
     }
-  } else if (warp >= 4 && warp < 12) {
+  } else if (warp >= 4 && warp < 4 + 4 * GROUPS) {
     // ---- weights: thread t of group g is position t of the tile, for queries c0 to c0 + CW
-    const int t = (tid - 128) & 127, q4 = warp & 3, g = (warp - 4) >> 2, team = TEAMS == 2 ? g : 0, c0 = TEAMS == 2 ? 0 : g * CW;
+    const int t = (tid - 128) & 127, q4 = warp & 3, g = (warp - 4) >> 2, c0 = g * CW;
     const uint32_t lanes = (uint32_t)(q4 * 32) << 16;
-    const int mine = team * 32 + c0;          // where the group's queries are in what is kept by query
-    float* const m_s = r.m + mine;
-    float* const factor_s = r.factor + mine;
-    int* const to_s = r.to + mine;
-    int* const from_s = r.from + mine;
+    float* const m_s = r.m + c0;
+    float* const factor_s = r.factor + c0;
+    int* const to_s = r.to + c0;
+    int* const from_s = r.from + c0;
     auto by_four = [&](const float* x, auto&& f) {
 #pragma unroll
       for (int n = 0; n < CW; n += 4) { const float4 y = *(const float4*)(x + n); f(n, y.x); f(n + 1, y.y); f(n + 2, y.z); f(n + 3, y.w); }
@@ -354,17 +383,20 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
     now.at(p, r.line.b[0], u0 - r.line.before[0]);
     bool dead = false, fresh = true;          // no tile of the segment so far
     float l[CW], bad = 0.f;
-    int seg = 0;
+    int seg = 0, my_query = 0;
 #pragma unroll 1
     for (int i = 0; i < n_tiles; ++i) {
-      if (TEAMS == 1 || (i & 1) == g) {
+      {
         const int x0 = tile_start<UT>(now.s, now.t), x = x0 + t;
         if (fresh) {
           u_sync(g);               // (the segment before is done with what is written here)
           if (t < CW) {
-            const int h = p.RB == 1 ? now.hr : now.hr / p.RB;
-            const Sight s = sight_of(p, now.s, (now.hr - h * p.RB) * N + c0 + t);
-            to_s[t] = s.to; from_s[t] = s.from;
+            if (p.RB > 1 || seg == 0) {       // (a division)
+              const int row = now.hr % p.RB * N + c0 + t;
+              my_query = row < p.R ? row / p.G : INT_MAX;
+            }
+            const int at = my_query < now.s.nq ? now.s.p0 + my_query : -1;
+            to_s[t] = at; from_s[t] = p.in.window > 0 ? (int)max((int64_t)0, (int64_t)at - p.in.window + 1) : 0;
             m_s[t] = NOTHING;
           }
 #pragma unroll
@@ -378,13 +410,24 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
         if (*(volatile int*)(r.bad + (i & 7))) bad = -1.f;
         const bool edge = !whole<UT>(p, now.s, x0), hidden = !(x < now.s.n && (x >= now.s.lo || x < now.s.sk));
         const int sinks = p.in.window > 0 ? p.in.sinks : 0;
+        // in front of some rows, behind others
+        const bool partly = edge && !hidden && !(now.s.nq == p.in.Q && x <= now.s.p0 && (p.in.window <= 0 || x > now.s.n - 1 - p.in.window || x < sinks));
         auto scores = [&] {
 #pragma unroll
-          for (int n = 0; n < CW; n += LD) u_ld<LD>(tmem + lanes + (i & 1) * N + c0 + n, w + n);
-          if (edge) {
+          for (int n = 0; n < CW; n += LD) u_ld<LD>(tmem + lanes + (i & 1) * CH * N + c0 + n, w + n);
+          if constexpr (CH == 2) {
+            float y[CW];
+            u_ld<CW>(tmem + lanes + ((i & 1) * CH + 1) * N + c0, y);
+#pragma unroll
+            for (int n = 0; n < CW; ++n) w[n] += y[n];
+          }
+          if (hidden) {
+#pragma unroll
+            for (int n = 0; n < CW; ++n) w[n] = -CUDART_INF_F;
+          } else if (partly) {
 #pragma unroll
             for (int n = 0; n < CW; ++n)
-              if (hidden || !(x <= to_s[n] && (x >= from_s[n] || x < sinks))) w[n] = -CUDART_INF_F;
+              if (!(x <= to_s[n] && (x >= from_s[n] || x < sinks))) w[n] = -CUDART_INF_F;
           }
         };
         float big = 0.f;
@@ -411,24 +454,24 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
 #pragma unroll
           for (int n = 0; n < CW; ++n) {
             const float top = u_warp_max(w[n]);
-            if (lane == (n & 31)) r.top[q4][mine + n] = top;
+            if (lane == (n & 31)) r.top[q4][c0 + n] = top;
           }
           u_sync(g);
           if (t < CW) {
-            const int n = mine + t;
+            const int n = c0 + t;
             const float most = fmaxf(fmaxf(r.top[0][n], r.top[1][n]), fmaxf(r.top[2][n], r.top[3][n])), before = m_s[t], m = fmaxf(before, most * p.c);
             m_s[t] = m;
             factor_s[t] = ex2f(before - m);
           }
           u_sync(g);
           if (!fresh) {            // ... and what is there already
-            if (!dead && !u_wait(r.pv_done + ((i - TEAMS) & 1), ((i - TEAMS) >> 1) & 1, r, limit)) dead = true;
+            if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
             u_after();
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < 2 * CH; ++k)
 #pragma unroll
               for (int n0 = 0; n0 < CW; n0 += LD) {
-                const uint32_t at = tmem + lanes + 2 * N + ((seg & 1) * TEAMS + team) * 2 * N + k * N + c0 + n0;
+                const uint32_t at = tmem + lanes + O_AT + (seg & 1) * O_COLS + k * N + c0 + n0;
                 float y[LD];
                 u_ld<LD>(at, y);
 #pragma unroll
@@ -442,41 +485,44 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
         }
 #pragma unroll
         for (int n = 0; n < CW; ++n) l[n] += w[n];
-        char* const v_s = smem + (2 * i + 1) % SLOTS * S::SLOT;
+        const int v_load = load_of_values(i, n_tiles);
+        char* const v_s = smem + v_load % SLOTS * S::SLOT;
         bool keep = false;
         if (edge) {
-          if (!dead && !u_wait(r.full + (2 * i + 1) % SLOTS, ((2 * i + 1) / SLOTS) & 1, r, limit)) dead = true;
-          if (hidden && (TEAMS == 2 || g == 0))      // values of positions that nothing sees: whatever lies there
+          if (!dead && !u_wait(r.full + v_load % SLOTS, (v_load / SLOTS) & 1, r, limit)) dead = true;
+          if (hidden && g == 0)    // values of positions that nothing sees: whatever lies there
             for (int j = 0; j < PIECES; ++j) *(uint4*)(v_s + piece_of(t, j)) = make_uint4(0, 0, 0, 0);
           if (p.in.Q > 1) {        // some rows do not see all of the tile: a value that is not finite must not reach those as 0 * inf
-            auto odd = [](uint32_t y) { return (y & 0x7f800000u) == 0x7f800000u || (y & 0x7f80u) == 0x7f80u; };
-            bool strange = false;
-            if (!hidden)
-#pragma unroll 4
+            uint32_t top = 0;      // of the exponents (as halves: what is not finite is the largest)
+            if (partly)
+#pragma unroll
               for (int j = 0; j < PIECES; ++j) {
                 const uint4 y = *(const uint4*)(v_s + piece_of(t, j));
-                strange = strange || odd(y.x) || odd(y.y) || odd(y.z) || odd(y.w);
+                top = __vmaxu2(__vmaxu2(__vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu), __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu)), top);
               }
+            const bool strange = (top & 0xffffu) >= 0x7f80u || top >= 0x7f800000u;
             if (u_any(g, strange)) { // it goes to the rows that see it by itself, and 0 takes its place
               if (!fresh) {
-                if (!dead && !u_wait(r.pv_done + ((i - TEAMS) & 1), ((i - TEAMS) >> 1) & 1, r, limit)) dead = true;
+                if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
               } else if (!dead && !u_wait(r.seg_free + (seg & 1), ((seg >> 1) & 1) ^ 1u, r, limit)) dead = true;
               u_after();
               keep = fresh;
 #pragma unroll 1
               for (int n0 = 0; n0 < CW; n0 += LD) {
-                const uint32_t o_at = tmem + lanes + 2 * N + ((seg & 1) * TEAMS + team) * 2 * N + c0 + n0;
+                const uint32_t o_at = tmem + lanes + O_AT + (seg & 1) * O_COLS + c0 + n0;
                 float y[LD];
                 if (fresh) {
 #pragma unroll
                   for (int e = 0; e < LD; ++e) y[e] = 0.f;
-                  u_st<LD>(o_at + N, y);
+#pragma unroll
+                  for (int k = 1; k < 2 * CH; ++k) u_st<LD>(o_at + k * N, y);
                 } else u_ld<LD>(o_at, y);
                 if (t < DP)
 #pragma unroll 1
-                  for (int pos = 0; pos < UT; ++pos) {
+                  for (int pos = 0; pos < UT; ++pos) {      // (positions that all rows see are left to the product)
                     const int xx = x0 + pos;
                     if (!(xx < now.s.n && (xx >= now.s.lo || xx < now.s.sk))) continue;
+                    if (now.s.nq == p.in.Q && xx <= now.s.p0 && (p.in.window <= 0 || xx > now.s.n - 1 - p.in.window || xx < sinks)) continue;
                     const float z = __bfloat162float(*(const E*)(v_s + piece_of(pos, t >> 3) + (t & 7) * 2));
                     if (!(fabsf(z) < CUDART_INF_F))
 #pragma unroll
@@ -486,9 +532,8 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
                 u_st<LD>(o_at, y);
               }
               u_st_wait();
-              if constexpr (TEAMS == 2) u_sync(g);
-              else asm volatile("bar.sync 7, 256;" ::: "memory");      // (both groups have found it)
-              if (!hidden && (TEAMS == 2 || g == 0))
+              asm volatile("bar.sync 7, %0;" ::"n"(128 * GROUPS) : "memory");      // (all groups have found it)
+              if (partly && g == 0)
                 for (int j = 0; j < PIECES; ++j) {
                   uint4* const at = (uint4*)(v_s + piece_of(t, j));
                   auto clean = [](uint32_t y) { return ((y & 0x7f800000u) == 0x7f800000u ? 0u : y & 0xffff0000u) | ((y & 0x7f80u) == 0x7f80u ? 0u : y & 0xffffu); };
@@ -498,7 +543,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
             }
           }
         }
-        if (t == 0 && (TEAMS == 2 || g == 0)) *(volatile int*)(r.keep + (i & 1)) = keep;
+        if (t == 0 && g == 0) *(volatile int*)(r.keep + (i & 1)) = keep;
         if (i >= PB && !dead && !u_wait(r.pv_done + ((i - PB) & 1), ((i - PB) >> 1) & 1, r, limit)) dead = true;      // the buffer's last product
         {
           char* const at = p_s + (i % PB) * S::P_BYTES + (t >> 6) * (N * 256) + (t & 7) * 2 + c0 * 128;
@@ -524,18 +569,16 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
       if (now.t + 1 == now.s.nt || i + 1 == n_tiles) {        // the segment ends, or the piece does: to the warps that write
         const int sb = seg & 1;
         if (!dead && !u_wait(r.seg_free + sb, ((seg >> 1) & 1) ^ 1u, r, limit)) dead = true;
-        if (!fresh) {
-          column_sums<CW>(l, r.end_sum[sb][q4] + mine, lane);
-          if (t < CW) r.end_m[sb][mine + t] = m_s[t];
-        }
-        if (t == 0 && (TEAMS == 2 || g == 0)) { r.end_has[sb][team] = !fresh; r.end_bad[sb][team] = !fresh && bad < 0.f; }
+        column_sums<CW>(l, r.end_sum[sb][q4] + c0, lane);
+        if (t < CW) r.end_m[sb][c0 + t] = m_s[t];
+        if (t == 0 && g == 0) r.end_bad[sb] = bad < 0.f;
         u_arrive(r.seg_sums + sb);
         fresh = true;
         ++seg;
       }
       now.next(p);
     }
-  } else if (warp >= 12) {
+  } else if (warp >= 4 + 4 * GROUPS) {
     // ---- results: thread t is column t of the output
     const int t = tid & 127, q4 = warp & 3;
     const uint32_t lanes = (uint32_t)(q4 * 32) << 16;
@@ -553,51 +596,37 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
       if (!dead && !u_wait(r.seg_sums + sb, (seg >> 1) & 1, r, limit)) dead = true;
       if (!dead && !u_wait(r.seg_pv + sb, (seg >> 1) & 1, r, limit)) dead = true;
       u_after();
-      const float b = u_any(2, dead) ? -2.f : r.end_bad[sb][0] || (TEAMS == 2 && r.end_bad[sb][1]) ? -1.f : 0.f;
+      const float b = u_any(GROUPS, dead) ? -2.f : r.end_bad[sb] ? -1.f : 0.f;
       const uint32_t st = at.s.status | status_of(b);
-      const bool has0 = r.end_has[sb][0], has1 = TEAMS == 2 && r.end_has[sb][1], partial = head || tail;
+      const bool partial = head || tail;
       float* const part = p.part + (number * 2 + (head ? 0 : 1)) * (int64_t)PART<N, DP>;
       if (t < N) {
-        float m = NOTHING, sum = 0.f, f[2] = {0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < TEAMS; ++k)
-          if (k ? has1 : has0) m = fmaxf(m, r.end_m[sb][k * 32 + n]);
-#pragma unroll
-        for (int k = 0; k < TEAMS; ++k)
-          if (k ? has1 : has0) {
-            f[k] = ex2f(r.end_m[sb][k * 32 + n] - m);
-            sum += f[k] * ((r.end_sum[sb][0][k * 32 + n] + r.end_sum[sb][1][k * 32 + n]) + (r.end_sum[sb][2][k * 32 + n] + r.end_sum[sb][3][k * 32 + n]));
-          }
-        const float inv = partial ? 1.f : st || sum == 0.f ? 0.f : 1.f / sum;
-        r.scale[n] = inv == 0.f ? 0.f : f[0] * inv;      // (of a flagged segment nothing is used, whatever it is)
-        if constexpr (TEAMS == 2) r.scale[32 + n] = inv == 0.f ? 0.f : f[1] * inv;
+        const float m = r.end_m[sb][n], sum = (r.end_sum[sb][0][n] + r.end_sum[sb][1][n]) + (r.end_sum[sb][2][n] + r.end_sum[sb][3][n]);
+        r.inverse[n] = partial ? 1.f : st || sum == 0.f ? 0.f : 1.f / sum;      // (of a flagged segment nothing is used, whatever it is)
         if (row < p.R) {
           if (partial) *(float2*)(part + N * DP + n * 2) = make_float2(m, b < 0.f ? b : sum);
           else if (p.out.lse) p.out.lse[((int64_t)at.b * p.in.Q + j) * p.in.Hq + h * p.G + row - j * p.G] = lse_of(m, st ? 0.f : sum);
         }
       }
-      u_sync(2);
+      u_sync(GROUPS);
 #pragma unroll 1
       for (int n0 = 0; n0 < N; n0 += 16) {
         float o[16], y[16];
-        const uint32_t o_at = tmem + lanes + 2 * N + sb * TEAMS * 2 * N + n0;
+        const uint32_t o_at = tmem + lanes + O_AT + sb * O_COLS + n0;
+        u_ld<16>(o_at, o);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[e] = 0.f;
+        for (int k = 1; k < 2 * CH; ++k) {
+          u_ld<16>(o_at + k * N, y);
 #pragma unroll
-        for (int k = 0; k < TEAMS; ++k)
-          if (k ? has1 : has0)
-#pragma unroll
-            for (int term = 0; term < 2; ++term) {
-              u_ld<16>(o_at + k * 2 * N + term * N, y);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) { const float f = r.scale[k * 32 + n0 + e]; o[e] += f == 0.f ? 0.f : y[e] * f; }
-            }
+          for (int e = 0; e < 16; ++e) o[e] += y[e];
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int64_t to = r.row_at[n0 + e];
           if (to >= 0) {
+            const float f = r.inverse[n0 + e];
             if (partial) { if (t < DP) part[(n0 + e) * DP + t] = o[e]; }
-            else if (t < p.in.D) ((E*)p.out.out)[to + t] = __float2bfloat16_rn(o[e]);
+            else if (t < p.in.D) ((E*)p.out.out)[to + t] = __float2bfloat16_rn(f == 0.f ? 0.f : o[e] * f);
           }
         }
       }
@@ -611,7 +640,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(THREADS
       left -= rest;
       at.t = at.s.nt - 1;
       at.next(p);
-      u_sync(2);                   // (row_at and scale are written again)
+      u_sync(GROUPS);              // (row_at and inverse are written again)
     }
   }
   u_before();
@@ -626,7 +655,7 @@ template <int DP, int N, bool GROUPED> cudaError_t launch(const AttnParams& p, c
   using S = UShape<DP, N>;
   auto* const fn = attn_umma_kernel<DP, N, GROUPED>;
   const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-  return e != cudaSuccess ? e : launch_pdl(fn, dim3((unsigned)blocks), THREADS, S::SMEM, st, true, p, k_map, v_map);
+  return e != cudaSuccess ? e : launch_pdl(fn, dim3((unsigned)blocks), S::THREADS, S::SMEM, st, true, p, k_map, v_map);
 }
 template <int DP, bool GROUPED> cudaError_t launch(const AttnParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int blocks, cudaStream_t st) {
   const int n = umma_rows(p.in);
