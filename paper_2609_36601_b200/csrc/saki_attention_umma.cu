@@ -6,8 +6,8 @@
 //   out^T    [128 columns x 2 N] += V^T [D x 128] . P^T [128 x 2 N]        V as stored (M-major); P in two bf16 terms (16 bits), side by side: V is read once
 // One block on each SM, its piece of the line, and
 //   warp 0      looks pages up and loads keys and values by TMA into a ring of slots (one tile's keys or values each)
-//   warp 1      one thread issues the products: scores of tile i + 1 ahead of the sums of tile i
-//   warp 2      holds tensor memory
+//   warps 1, 2  a thread of one issues the products for the scores, up to two tiles ahead, a thread of the other those for the outputs (one thread for both was what a tile
+//               waited for: 16 products take 1200 cycles of shared memory's time, waits and commits around them as long again); warp 2 holds tensor memory
 //   warp 3      loads the queries of the segments, two ahead
 //   from 4 on   groups of four warps that share a tile's queries (8 each, 16 of 64), a thread per position: it reads its scores, takes 2^(c s - m), adds them up, and
 //               leaves the weights in shared memory for the next product.  m is a row's maximum as of some tile: it is brought up to date (and
@@ -36,14 +36,12 @@ template <int DP, int N> struct UShape {
   static constexpr int FIXED = P_BUFS * P_BYTES + 2 * Q_BYTES + 6656 + 1024;      // and the rest, alignment
   static constexpr int FIT = (227 * 1024 - FIXED) / SLOT, SLOTS = FIT < 12 ? FIT : 12;
   static constexpr int SMEM = SLOTS * SLOT + FIXED;
-  // A product that goes on top of the one before it waits for it, some 170 cycles: sums are kept in as many chains as tensor memory has room for
-  static constexpr int CHAINS = 1;
-  static constexpr int COLS = 6 * CHAINS * N <= 256 ? 256 : 512;                         // two buffers of scores; by segment, outputs in two terms
+  static constexpr int COLS = 6 * N <= 128 ? 128 : 6 * N <= 256 ? 256 : 512;             // two buffers of scores; by segment, outputs in two terms
   static_assert(SLOTS >= 4, "two tiles");
 };
 
 template <int THREADS> struct URest {      // of shared memory
-  uint64_t full[12], empty[12], q_full[2], q_empty[2], s_full[2], p_ready[2], pv_done[2], drain;
+  uint64_t full[12], empty[12], q_full[2], q_empty[2], s_full[2], p_ready[2], pv_done[2], drain[2];
   uint64_t seg_sums[2], seg_pv[2], seg_free[2];      // by segment: the groups' sums are there; so are the outputs; both have been read
   LineShared<THREADS> line;
   // by query
@@ -168,7 +166,7 @@ constexpr float NOTHING = -1e30f;       // the maximum of a row that has seen no
 template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<DP, N>::THREADS, 1) attn_umma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using S = UShape<DP, N>;
   using E = __nv_bfloat16;
-  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS, GROUPS = S::GROUPS, THREADS = S::THREADS, CW = S::CW, LD = CW < 16 ? CW : 16, CH = S::CHAINS, O_AT = 2 * CH * N, O_COLS = 2 * CH * N;      // (where outputs start in tensor memory, columns of a segment's)
+  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS, GROUPS = S::GROUPS, THREADS = S::THREADS, CW = S::CW, LD = CW < 16 ? CW : 16;
   constexpr uint32_t SLAB = GROUPED ? 1024 : UT * 128, EIGHT = GROUPED ? S::SLABS * 1024 : 1024;      // bytes from a slab to the next, from eight positions to the next
   auto piece_of = [](int t, int j) { return (uint32_t)((t >> 3) * EIGHT + (j >> 3) * SLAB + (t & 7) * 128 + (((j & 7) ^ (t & 7)) << 4)); };
   extern __shared__ char u_raw[];
@@ -181,7 +179,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
   if (tid == 0) {
     for (int i = 0; i < SLOTS; ++i) { mbar_init(r.full + i, 1); mbar_init(r.empty + i, 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(r.q_full + i, 1); mbar_init(r.q_empty + i, 1); mbar_init(r.s_full + i, 1); mbar_init(r.p_ready + i, 128 * GROUPS); mbar_init(r.pv_done + i, 1); mbar_init(r.seg_sums + i, 128 * GROUPS); mbar_init(r.seg_pv + i, 1); mbar_init(r.seg_free + i, 128); }
-    mbar_init(&r.drain, 1);
+    mbar_init(r.drain, 1); mbar_init(r.drain + 1, 1);
     r.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -260,71 +258,62 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       for (int done = max(0, j - SLOTS); done < j; ++done) mbar_wait_bounded(r.full + done % SLOTS, (uint32_t)(done / SLOTS) & 1u);
   } else if (warp == 1) {
     if (lane == 0) {
-      // ---- products: scores of tiles 0 and 1; then, once tile i's weights are there, its outputs, and in between them the scores of tile i + 2
-      Cursor<UT> qk;
-      qk.at(p, r.line.b[0], u0 - r.line.before[0]);
-      int seg = 0, out = -1;                  // segments whose queries have been used; the outputs' segment
-      bool qk_first = true;
-      uint32_t first = 0;                     // bit i % 4: tile i is its segment's first
-      bool ok = true;
-      constexpr uint32_t ID_S = u_idesc(N, false), ID_O = u_idesc(2 * N, true), UP_KV = u_upper(EIGHT), UP_PQ = u_upper(1024);
+      // ---- scores: those of tile i once its keys are there and the weights of tile i - 2 have left their buffer
+      constexpr uint32_t ID = u_idesc(N, false), UP_K = u_upper(EIGHT), UP_Q = u_upper(1024);
+      Cursor<UT> at;
+      at.at(p, r.line.b[0], u0 - r.line.before[0]);
       const int steps = (p.in.D + 15) / 16;
-      uint32_t k_at = 0, q_at = 0, s_to = 0;
-      // the operands of tile i's scores are there (wait: waits for them)
-      auto scores_ready = [&](int i, bool wait) -> bool {
+      int seg = 0;                            // segments whose queries have been used
+      bool first = true;
+      for (int i = 0; i < n_tiles; ++i) {
         const int load = load_of_keys(i), slot = load % SLOTS, qb = seg & 1;
-        if (wait) {
-          if ((qk_first && !u_wait(r.q_full + qb, (seg >> 1) & 1, r, limit)) || !u_wait(r.full + slot, (load / SLOTS) & 1, r, limit)) { ok = false; return false; }
-        } else if ((qk_first && !mbar_test_wait(r.q_full + qb, (seg >> 1) & 1)) || !mbar_test_wait(r.full + slot, (load / SLOTS) & 1)) return false;
+        if ((i >= 2 && !u_wait(r.p_ready + (i & 1), ((i - 2) >> 1) & 1, r, limit)) || (first && !u_wait(r.q_full + qb, (seg >> 1) & 1, r, limit)) ||
+            !u_wait(r.full + slot, (load / SLOTS) & 1, r, limit)) break;
         u_after();
-        k_at = u_lower(smem_addr(smem + slot * S::SLOT)); q_at = u_lower(smem_addr(q_s + qb * S::Q_BYTES)); s_to = tmem + (i & 1) * CH * N;
-        first = (first & ~(1u << (i & 3))) | (uint32_t)qk_first << (i & 3);
-        return true;
-      };
-      auto scores_step = [&](int e) {
-        const uint32_t k = k_at + ((e >> 2) * SLAB + (e & 3) * 32) / 16, q = q_at + ((e >> 2) * (N * 128) + (e & 3) * 32) / 16;
-        if (e == 0) u_mma<UP_KV, UP_PQ, ID_S>(s_to, k, q, false);
-        else if (e < steps) u_mma<UP_KV, UP_PQ, ID_S>(s_to, k, q);
-      };
-      auto scores_done = [&](int i) {
-        u_commit(r.empty + load_of_keys(i) % SLOTS);
+        const uint32_t k = u_lower(smem_addr(smem + slot * S::SLOT)), q = u_lower(smem_addr(q_s + qb * S::Q_BYTES)), s_to = tmem + (i & 1) * N;
+        u_mma<UP_K, UP_Q, ID>(s_to, k, q, false);
+#pragma unroll
+        for (int e = 1; e < DP / 16; ++e)
+          if (e < steps) u_mma<UP_K, UP_Q, ID>(s_to, k + ((e >> 2) * SLAB + (e & 3) * 32) / 16, q + ((e >> 2) * (N * 128) + (e & 3) * 32) / 16);
         u_commit(r.s_full + (i & 1));
-        qk_first = qk.t + 1 == qk.s.nt;
-        if (qk_first) { u_commit(r.q_empty + (seg & 1)); ++seg; }
-        qk.next(p);
-      };
-      auto scores = [&](int i) {
-        if (!scores_ready(i, true)) return;
-#pragma unroll
-        for (int e = 0; e < DP / 16; ++e) scores_step(e);
-        scores_done(i);
-      };
-      scores(0);
-      if (ok && n_tiles > 1) scores(1);
-      for (int i = 0; i < n_tiles && ok; ++i) {
-        const int load = load_of_values(i, n_tiles), slot = load % SLOTS;
-        if (!u_wait(r.p_ready + (i & 1), (i >> 1) & 1, r, limit) || !u_wait(r.full + slot, (load / SLOTS) & 1, r, limit)) { ok = false; break; }
-        const bool new_seg = first >> (i & 3) & 1u;
-        if (new_seg && !u_wait(r.seg_free + (++out & 1), ((out >> 1) & 1) ^ 1u, r, limit)) { ok = false; break; }
-        u_after();
-        const bool on_top = !new_seg || *(volatile int*)(r.keep + (i & 1)), more = i + 2 < n_tiles, along = more && scores_ready(i + 2, false);
-        const uint32_t v = u_lower(smem_addr(smem + slot * S::SLOT), DP == 128 ? SLAB : 0), w = u_lower(smem_addr(p_s + i % PB * S::P_BYTES)), o = tmem + O_AT + (out & 1) * O_COLS;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {         // steps of 16 positions
-          const uint32_t a = v + e * 2 * EIGHT / 16, b = w + ((e >> 2) * (N * 256) + (e & 3) * 32) / 16;
-          if (e == 0) u_mma<UP_KV, UP_PQ, ID_O>(o, a, b, on_top);
-          else u_mma<UP_KV, UP_PQ, ID_O>(o, a, b);
-          if (along) scores_step(e);
-        }
         u_commit(r.empty + slot);
-        u_commit(r.pv_done + (i & 1));
-        if (i + 1 == n_tiles || (first >> ((i + 1) & 3) & 1u)) u_commit(r.seg_pv + (out & 1));
-        if (along) scores_done(i + 2);
-        else if (more) scores(i + 2);
+        first = at.t + 1 == at.s.nt;
+        if (first) { u_commit(r.q_empty + qb); ++seg; }
+        at.next(p);
       }
-      if (!ok) {                              // nothing of it is under way when tensor memory goes
-        u_commit(&r.drain);
-        mbar_wait_bounded(&r.drain, 0);
+      if (*(volatile int*)&r.abort) {         // nothing of it is under way when tensor memory goes
+        u_commit(r.drain);
+        mbar_wait_bounded(r.drain, 0);
+      }
+    }
+  } else if (warp == 2) {
+    if (lane == 0) {
+      // ---- outputs: tile i's once its weights are there
+      constexpr uint32_t ID = u_idesc(2 * N, true), UP_V = u_upper(EIGHT), UP_P = u_upper(1024);
+      Cursor<UT> at;
+      at.at(p, r.line.b[0], u0 - r.line.before[0]);
+      int seg = 0;
+      bool first = true;
+      for (int i = 0; i < n_tiles; ++i) {
+        const int load = load_of_values(i, n_tiles), slot = load % SLOTS;
+        if ((first && !u_wait(r.seg_free + (seg & 1), ((seg >> 1) & 1) ^ 1u, r, limit)) || !u_wait(r.full + slot, (load / SLOTS) & 1, r, limit) ||
+            !u_wait(r.p_ready + (i & 1), (i >> 1) & 1, r, limit)) break;
+        u_after();
+        const bool on_top = !first || *(volatile int*)(r.keep + (i & 1));
+        const uint32_t v = u_lower(smem_addr(smem + slot * S::SLOT), DP == 128 ? SLAB : 0), w = u_lower(smem_addr(p_s + i % PB * S::P_BYTES)), o = tmem + 2 * N + (seg & 1) * 2 * N;
+        u_mma<UP_V, UP_P, ID>(o, v, w, on_top);
+#pragma unroll
+        for (int e = 1; e < 8; ++e)           // steps of 16 positions
+          u_mma<UP_V, UP_P, ID>(o, v + e * 2 * EIGHT / 16, w + ((e >> 2) * (N * 256) + (e & 3) * 32) / 16);
+        u_commit(r.pv_done + (i & 1));
+        u_commit(r.empty + slot);
+        first = at.t + 1 == at.s.nt;
+        if (first || i + 1 == n_tiles) { u_commit(r.seg_pv + (seg & 1)); ++seg; }
+        at.next(p);
+      }
+      if (*(volatile int*)&r.abort) {
+        u_commit(r.drain + 1);
+        mbar_wait_bounded(r.drain + 1, 0);
       }
     }
   } else if (warp == 3) {
@@ -414,13 +403,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         const bool partly = edge && !hidden && !(now.s.nq == p.in.Q && x <= now.s.p0 && (p.in.window <= 0 || x > now.s.n - 1 - p.in.window || x < sinks));
         auto scores = [&] {
 #pragma unroll
-          for (int n = 0; n < CW; n += LD) u_ld<LD>(tmem + lanes + (i & 1) * CH * N + c0 + n, w + n);
-          if constexpr (CH == 2) {
-            float y[CW];
-            u_ld<CW>(tmem + lanes + ((i & 1) * CH + 1) * N + c0, y);
-#pragma unroll
-            for (int n = 0; n < CW; ++n) w[n] += y[n];
-          }
+          for (int n = 0; n < CW; n += LD) u_ld<LD>(tmem + lanes + (i & 1) * N + c0 + n, w + n);
           if (hidden) {
 #pragma unroll
             for (int n = 0; n < CW; ++n) w[n] = -CUDART_INF_F;
@@ -468,10 +451,10 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
             if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
             u_after();
 #pragma unroll
-            for (int k = 0; k < 2 * CH; ++k)
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
               for (int n0 = 0; n0 < CW; n0 += LD) {
-                const uint32_t at = tmem + lanes + O_AT + (seg & 1) * O_COLS + k * N + c0 + n0;
+                const uint32_t at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + k * N + c0 + n0;
                 float y[LD];
                 u_ld<LD>(at, y);
 #pragma unroll
@@ -509,13 +492,13 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
               keep = fresh;
 #pragma unroll 1
               for (int n0 = 0; n0 < CW; n0 += LD) {
-                const uint32_t o_at = tmem + lanes + O_AT + (seg & 1) * O_COLS + c0 + n0;
+                const uint32_t o_at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + c0 + n0;
                 float y[LD];
                 if (fresh) {
 #pragma unroll
                   for (int e = 0; e < LD; ++e) y[e] = 0.f;
 #pragma unroll
-                  for (int k = 1; k < 2 * CH; ++k) u_st<LD>(o_at + k * N, y);
+                  for (int k = 1; k < 2; ++k) u_st<LD>(o_at + k * N, y);
                 } else u_ld<LD>(o_at, y);
                 if (t < DP)
 #pragma unroll 1
@@ -612,10 +595,10 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
 #pragma unroll 1
       for (int n0 = 0; n0 < N; n0 += 16) {
         float o[16], y[16];
-        const uint32_t o_at = tmem + lanes + O_AT + sb * O_COLS + n0;
+        const uint32_t o_at = tmem + lanes + 2 * N + sb * 2 * N + n0;
         u_ld<16>(o_at, o);
 #pragma unroll
-        for (int k = 1; k < 2 * CH; ++k) {
+        for (int k = 1; k < 2; ++k) {
           u_ld<16>(o_at + k * N, y);
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[e] += y[e];
