@@ -93,6 +93,7 @@ template <int T, int THREADS, int WORKERS> __device__ __forceinline__ void piece
   const int64_t per = (p.in.B + THREADS - 1) / THREADS, b0 = min((int64_t)tid * per, p.in.B), b1 = min(b0 + per, p.in.B);
   const int each = p.in.H * p.RB;
   long long mine = 0;
+#pragma unroll 1
   for (int64_t b = b0; b < b1; ++b) mine += (long long)span_of<T>(p, b).nt * each;
   long long upto = mine;
 #pragma unroll
@@ -115,6 +116,7 @@ template <int T, int THREADS, int WORKERS> __device__ __forceinline__ void piece
     if (upto - mine <= u0 && u0 < upto) {
       long long at = upto - mine;
       int64_t b = b0;
+#pragma unroll 1
       for (;; ++b) {
         const long long n = (long long)span_of<T>(p, b).nt * each;
         if (u0 < at + n) break;

@@ -33,7 +33,7 @@ template <int DP, int N> struct UShape {
   static constexpr int SLABS = DP / 64, SLOT = UT * DP * 2;                // keys or values of a tile
   static constexpr int P_BYTES = 2 * N * UT * 2, P_BUFS = N <= 32 ? 2 : 1; // two terms
   static constexpr int Q_BYTES = N * DP * 2;
-  static constexpr int FIXED = P_BUFS * P_BYTES + 2 * Q_BYTES + 6656 + 1024;      // and the rest, alignment
+  static constexpr int FIXED = P_BUFS * P_BYTES + 2 * Q_BYTES + 7168 + 1024;      // and the rest, alignment
   static constexpr int FIT = (227 * 1024 - FIXED) / SLOT, SLOTS = FIT < 12 ? FIT : 12;
   static constexpr int SMEM = SLOTS * SLOT + FIXED;
   static constexpr int COLS = 6 * N <= 128 ? 128 : 6 * N <= 256 ? 256 : 512;             // two buffers of scores; by segment, outputs in two terms
@@ -48,7 +48,7 @@ template <int THREADS> struct URest {      // of shared memory
   alignas(16) float m[64];                   // (read four at a time)
   float factor[64], top[4][64], inverse[64];
   int to[64], from[64];
-  int64_t row_at[64];                        // where a row's output starts, -1: there is none
+  int64_t row_at[64], q_at[64];              // where a row's output starts, where its queries are in a sequence and key head; -1: there is none
   // by segment, for the warps that write
   float end_m[2][64], end_sum[2][4][64];
   int end_bad[2];
@@ -57,20 +57,26 @@ template <int THREADS> struct URest {      // of shared memory
   int abort;
   uint32_t tmem;
 };
-static_assert(sizeof(URest<768>) <= 6656, "what is left of shared memory");
+static_assert(sizeof(URest<768>) <= 7168, "what is left of shared memory");
 
 // The loads of n tiles, in the order of the products: K0 K1 V0 K2 V1 ... V(n-1).  (Values with their keys would hold a slot for a tile's time longer.)
 __device__ __forceinline__ int load_of_keys(int i) { return i == 0 ? 0 : 2 * i - 1; }
 __device__ __forceinline__ int load_of_values(int i, int n) { return i + 1 < n ? 2 * i + 2 : 2 * n - 1; }
 
-template <typename R> __device__ __forceinline__ bool u_wait(uint64_t* bar, uint32_t parity, R& r, long long limit) {
-  if (limit >= WAIT_LIMIT_CYCLES && mbar_try_wait(bar, parity)) return true;
+// Code that is rarely run, or run from many places, is kept out of line: with all of it in place a kernel had 107 to 139 KB, and its warps, each in a part of its
+// own, waited for instructions more than for anything else.
+static __device__ __noinline__ bool u_wait_long(uint64_t* bar, uint32_t parity, int* abort, long long limit) {
+  const bool common = limit >= WAIT_LIMIT_CYCLES;
+  if (common && mbar_try_wait(bar, parity)) return true;       // (which itself waits for a while)
   const long long t0 = clock64();
   for (;;) {
-    if (*(volatile int*)&r.abort) return false;
-    if (clock64() - t0 > limit) { *(volatile int*)&r.abort = 1; return false; }
-    if (limit >= WAIT_LIMIT_CYCLES ? mbar_try_wait(bar, parity) : mbar_test_wait(bar, parity)) return true;
+    if (*(volatile int*)abort) return false;
+    if (clock64() - t0 > limit) { *(volatile int*)abort = 1; return false; }
+    if (common ? mbar_try_wait(bar, parity) : mbar_test_wait(bar, parity)) return true;
   }
+}
+template <typename R> __device__ __forceinline__ bool u_wait(uint64_t* bar, uint32_t parity, R& r, long long limit) {
+  return (limit >= WAIT_LIMIT_CYCLES && mbar_try_wait(bar, parity)) || u_wait_long(bar, parity, &r.abort, limit);
 }
 __device__ __forceinline__ void u_arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
 __device__ __forceinline__ void u_commit(uint64_t* bar) {
@@ -159,6 +165,16 @@ template <int N> __device__ __forceinline__ void column_sums(float (&l)[N], floa
   for (int k = 0; k < LEFT; ++k) to[n0 + k] = x[k];      // (N = 16: two lanes write the same)
 }
 
+static __device__ __noinline__ uint4 u_eight(const uint16_t* w) {      // not aligned
+  return make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
+}
+static __device__ __noinline__ void u_at(const AttnParams& p, Cursor<UT>& c, long long b, long long offset) { c.at(p, b, offset); }
+static __device__ __noinline__ void u_next_row(const AttnParams& p, Cursor<UT>& c) { c.next(p); }
+__device__ __forceinline__ void u_next(const AttnParams& p, Cursor<UT>& c) {
+  if (c.t + 1 < c.s.nt) ++c.t;
+  else u_next_row(p, c);
+}
+
 constexpr float NOTHING = -1e30f;       // the maximum of a row that has seen nothing so far
 
 // GROUPED (D = 128): a box brings both slabs of its positions, [8 positions][2 slabs][8 rows of 128 bytes]; else [slab][128 rows of 128 bytes].  (Boxes of a page
@@ -166,7 +182,7 @@ constexpr float NOTHING = -1e30f;       // the maximum of a row that has seen no
 template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<DP, N>::THREADS, 1) attn_umma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using S = UShape<DP, N>;
   using E = __nv_bfloat16;
-  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS, GROUPS = S::GROUPS, THREADS = S::THREADS, CW = S::CW, LD = CW < 16 ? CW : 16;
+  constexpr int SLOTS = S::SLOTS, PIECES = DP / 8, PB = S::P_BUFS, GROUPS = S::GROUPS, THREADS = S::THREADS, CW = S::CW;
   constexpr uint32_t SLAB = GROUPED ? 1024 : UT * 128, EIGHT = GROUPED ? S::SLABS * 1024 : 1024;      // bytes from a slab to the next, from eight positions to the next
   auto piece_of = [](int t, int j) { return (uint32_t)((t >> 3) * EIGHT + (j >> 3) * SLAB + (t & 7) * 128 + (((j & 7) ^ (t & 7)) << 4)); };
   extern __shared__ char u_raw[];
@@ -204,56 +220,61 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
   } else if (warp == 0) {
     // ---- loads, in the order in which the products take them up; load j goes to slot j % SLOTS
     Cursor<UT> look;
-    look.at(p, r.line.b[0], u0 - r.line.before[0]);
+    u_at(p, look, r.line.b[0], u0 - r.line.before[0]);
     const int boxes = UT / p.box, box_x = lane % boxes * p.box, slab = lane / boxes;
     const bool loads = GROUPED ? slab == 0 : slab < S::SLABS && slab * 64 < p.in.D;
     const uint32_t box_at = (uint32_t)(slab * SLAB + box_x / 8 * EIGHT), box_bytes = (uint32_t)p.box * (GROUPED ? 256 : 128);
-    struct Box { int page, x, head; };        // page -1: nothing of the lane's box is seen, -2: it is outside the pool
+    struct Box { int page, x, head; };        // page as it is in the table (what is made of it here would wait for it), x -1: nothing of the lane's box is seen
     auto look_up = [&]() -> Box {             // of the tile at the cursor
       const int x = tile_start<UT>(look.s, look.t) + box_x;
-      Box f = {-1, 0, p.RB == 1 ? look.hr : look.hr / p.RB};
+      Box f = {0, -1, p.RB == 1 ? look.hr : look.hr / p.RB};
       if (loads && x < look.s.n && (x + p.box > look.s.lo || x < look.s.sk)) {
         const int page = p.page_shift >= 0 ? x >> p.page_shift : (int)((unsigned)x / (unsigned)p.in.page_size);
         f.page = p.in.page_table[look.b * p.in.ld_table + page];
         f.x = x - page * p.in.page_size;
-        if ((unsigned)f.page >= (unsigned)p.in.n_pages) f.page = -2;
       }
       return f;
     };
-    int j = 0, slot = 0;                      // loads so far
+    struct Load { int c1, c2, c3; uint32_t bytes; };           // coordinates of the lane's box (c1 -1: there is none), bytes of the tile
+    const int eights = p.in.page_size / 8, mode = p.map_mode;
+    const uint32_t ring = smem_addr(smem) + box_at;
+    int slot = 0, j = 0;                      // loads so far
     uint32_t turn = 0;
     bool ok = true;
-    auto load = [&](const Box& f, bool values) {
-      const bool mine = f.page >= 0;
-      const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * box_bytes;
-      ok = __all_sync(0xffffffffu, ok && u_wait(r.empty + slot, turn ^ 1u, r, limit));
+    auto load = [&](const CUtensorMap* map, const Load& f) {
+      ok = __all_sync(0xffffffffu, u_wait(r.empty + slot, turn ^ 1u, r, limit));
       if (!ok) return;
-      if (lane == 0) mbar_expect_tx(r.full + slot, bytes);
+      if (lane == 0) mbar_expect_tx(r.full + slot, f.bytes);
       __syncwarp();
-      if (mine) {
-        const uint32_t to = smem_addr(smem + slot * S::SLOT) + box_at;
-        const CUtensorMap* const map = values ? &v_map : &k_map;
-        if constexpr (GROUPED) {
-          const int eights = p.in.page_size / 8;
-          tma_eights(to, map, p.map_mode == MAP_HEADS ? 2 * f.head : 0, f.x / 8 + (p.map_mode == MAP_RUN ? f.page * eights : 0),
-                     p.map_mode == MAP_HEADS ? f.page : p.map_mode == MAP_PAGES ? f.page * p.in.H + f.head : f.head, r.full + slot);
-        } else tma_box(to, map, slab * 64, f.head, f.x, f.page, r.full + slot);
+      if (f.c1 >= 0) {
+        if constexpr (GROUPED) tma_eights(ring + slot * S::SLOT, map, f.c1, f.c2, f.c3, r.full + slot);
+        else tma_box(ring + slot * S::SLOT, map, slab * 64, f.c1, f.c2, f.c3, r.full + slot);
       }
       ++j;
       if (++slot == SLOTS) { slot = 0; turn ^= 1u; }
     };
-    Box before = {}, now = look_up();
-    for (int i = 0; i < n_tiles && ok; ++i) {
-      const bool bad = __any_sync(0xffffffffu, now.page == -2);
-      if (lane == 0) { *(volatile int*)(r.bad + (i & 7)) = bad; __threadfence_block(); }
-      look.next(p);
-      Box next = {};
-      if (i + 1 < n_tiles) next = look_up();  // (in flight while slots are waited for)
-      load(now, false);
-      if (i > 0 && ok) load(before, true);
-      before = now; now = next;
+    Box ahead = look_up();                    // the boxes of the next tile, looked up a tile ahead
+    Load tile = {}, before = {};              // of the tile whose keys are next or were last, of the one before
+#pragma unroll 1
+    for (int i = 0; i <= n_tiles && ok; ++i) {      // K0 | K1 V0 | K2 V1 | ... | V(n-1)
+      before = tile;
+      if (i < n_tiles) {
+        const Box f = ahead;
+        const bool there = f.x >= 0, in = (unsigned)f.page < (unsigned)p.in.n_pages;
+        tile.bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, there && in)) * box_bytes;
+        const bool bad = __any_sync(0xffffffffu, there && !in);
+        if (lane == 0) { *(volatile int*)(r.bad + (i & 7)) = bad; __threadfence_block(); }
+        if constexpr (GROUPED) {
+          tile.c1 = mode == MAP_HEADS ? 2 * f.head : 0;
+          tile.c2 = (f.x >> 3) + (mode == MAP_RUN ? f.page * eights : 0);
+          tile.c3 = mode == MAP_HEADS ? f.page : mode == MAP_PAGES ? f.page * p.in.H + f.head : f.head;
+        } else { tile.c1 = f.head; tile.c2 = f.x; tile.c3 = f.page; }
+        if (!there || !in) tile.c1 = -1;
+        if (i + 1 < n_tiles) { u_next(p, look); ahead = look_up(); }
+        load(&k_map, tile);
+      }
+      if (i > 0 && ok) load(&v_map, before);
     }
-    if (ok) load(before, true);
     if (!ok)                                  // copies that are still on their way land before the block leaves
       for (int done = max(0, j - SLOTS); done < j; ++done) mbar_wait_bounded(r.full + done % SLOTS, (uint32_t)(done / SLOTS) & 1u);
   } else if (warp == 1) {
@@ -261,7 +282,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       // ---- scores: those of tile i once its keys are there and the weights of tile i - 2 have left their buffer
       constexpr uint32_t ID = u_idesc(N, false), UP_K = u_upper(EIGHT), UP_Q = u_upper(1024);
       Cursor<UT> at;
-      at.at(p, r.line.b[0], u0 - r.line.before[0]);
+      u_at(p, at, r.line.b[0], u0 - r.line.before[0]);
       const int steps = (p.in.D + 15) / 16;
       int seg = 0;                            // segments whose queries have been used
       bool first = true;
@@ -279,7 +300,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         u_commit(r.empty + slot);
         first = at.t + 1 == at.s.nt;
         if (first) { u_commit(r.q_empty + qb); ++seg; }
-        at.next(p);
+        u_next(p, at);
       }
       if (*(volatile int*)&r.abort) {         // nothing of it is under way when tensor memory goes
         u_commit(r.drain);
@@ -291,7 +312,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       // ---- outputs: tile i's once its weights are there
       constexpr uint32_t ID = u_idesc(2 * N, true), UP_V = u_upper(EIGHT), UP_P = u_upper(1024);
       Cursor<UT> at;
-      at.at(p, r.line.b[0], u0 - r.line.before[0]);
+      u_at(p, at, r.line.b[0], u0 - r.line.before[0]);
       int seg = 0;
       bool first = true;
       for (int i = 0; i < n_tiles; ++i) {
@@ -309,7 +330,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         u_commit(r.empty + slot);
         first = at.t + 1 == at.s.nt;
         if (first || i + 1 == n_tiles) { u_commit(r.seg_pv + (seg & 1)); ++seg; }
-        at.next(p);
+        u_next(p, at);
       }
       if (*(volatile int*)&r.abort) {
         u_commit(r.drain + 1);
@@ -319,34 +340,49 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
   } else if (warp == 3) {
     // ---- queries of the piece's segments
     Cursor<UT> at;
-    at.at(p, r.line.b[0], u0 - r.line.before[0]);
-    constexpr int EACH = N * PIECES / 32, BATCH = EACH < 16 ? EACH : 16;
+    u_at(p, at, r.line.b[0], u0 - r.line.before[0]);
+    constexpr int EACH = N * PIECES / 32, BATCH = EACH < 8 ? EACH : 8;
     long long left = n_tiles;
+#pragma unroll 1
     for (int seg = 0; left > 0; ++seg) {
       const int qb = seg & 1;
       if (!__all_sync(0xffffffffu, u_wait(r.q_empty + qb, ((seg >> 1) & 1) ^ 1u, r, limit))) break;
-      const int h = p.RB == 1 ? at.hr : at.hr / p.RB, row0 = (at.hr - h * p.RB) * N;
-#pragma unroll 1
-      for (int e0 = 0; e0 < EACH; e0 += BATCH) {
-        uint4 x[BATCH];                       // all on their way before the first is put down
-#pragma unroll
-        for (int e = 0; e < BATCH; ++e) {
-          const int c = (e0 + e) * 32 + lane, jj = c % PIECES, row = row0 + c / PIECES, t = row / p.G;
-          x[e] = make_uint4(0, 0, 0, 0);
-          if (row < p.R && jj * 8 < p.in.D) {
-            const E* const q = (const E*)p.in.q + at.b * p.in.q_seq + t * p.in.q_pos + (int64_t)(h * p.G + row - t * p.G) * p.in.q_head + jj * 8;
-            if (p.q_vec) x[e] = *(const uint4*)q;
-            else {
-              const uint16_t* const w = (const uint16_t*)q;
-              x[e] = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
-            }
-          }
+      const int h = p.RB == 1 ? at.hr : at.hr / p.RB;
+      if (seg == 0 || p.RB > 1) {             // where the rows' queries are within a sequence and key head
+        __syncwarp();
+        for (int n = lane; n < N; n += 32) {
+          const int row = at.hr % p.RB * N + n, t = row / p.G;
+          r.q_at[n] = row < p.R ? t * p.in.q_pos + (int64_t)(row - t * p.G) * p.in.q_head : -1;
         }
+        __syncwarp();
+      }
+      const E* const from = (const E*)p.in.q + at.b * p.in.q_seq + (int64_t)(h * p.G) * p.in.q_head;
+      const int jj = lane % PIECES;
+      const uint32_t g = p.q_sign;
+      auto put = [&](int e, uint4 x) {
+        *(uint4*)(q_s + qb * S::Q_BYTES + u_piece(N, e * (32 / PIECES) + lane / PIECES, jj)) = make_uint4(x.x ^ g, x.y ^ g, x.z ^ g, x.w ^ g);
+      };
+      auto at_of = [&](int e) -> int64_t {
+        const int64_t q_at = r.q_at[e * (32 / PIECES) + lane / PIECES];
+        return jj * 8 < p.in.D ? q_at : -1;
+      };
+      if (p.q_vec) {
+#pragma unroll 1
+        for (int e0 = 0; e0 < EACH; e0 += BATCH) {
+          uint4 x[BATCH];                     // all on their way before the first is put down
 #pragma unroll
-        for (int e = 0; e < BATCH; ++e) {
-          const int c = (e0 + e) * 32 + lane;
-          const uint32_t g = p.q_sign;
-          *(uint4*)(q_s + qb * S::Q_BYTES + u_piece(N, c / PIECES, c % PIECES)) = make_uint4(x[e].x ^ g, x[e].y ^ g, x[e].z ^ g, x[e].w ^ g);
+          for (int e = 0; e < BATCH; ++e) {
+            const int64_t q_at = at_of(e0 + e);
+            x[e] = q_at >= 0 ? *(const uint4*)(from + q_at + jj * 8) : make_uint4(0, 0, 0, 0);
+          }
+#pragma unroll
+          for (int e = 0; e < BATCH; ++e) put(e0 + e, x[e]);
+        }
+      } else {
+#pragma unroll 1
+        for (int e = 0; e < EACH; ++e) {
+          const int64_t q_at = at_of(e);
+          put(e, q_at >= 0 ? u_eight((const uint16_t*)(from + q_at + jj * 8)) : make_uint4(0, 0, 0, 0));
         }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -354,7 +390,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       if (lane == 0) u_arrive(r.q_full + qb);
       left -= at.s.nt - at.t;
       at.t = at.s.nt - 1;
-      at.next(p);
+      u_next(p, at);
     }
   } else if (warp >= 4 && warp < 4 + 4 * GROUPS) {
     // ---- weights: thread t of group g is position t of the tile, for queries c0 to c0 + CW
@@ -369,7 +405,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       for (int n = 0; n < CW; n += 4) { const float4 y = *(const float4*)(x + n); f(n, y.x); f(n + 1, y.y); f(n + 2, y.z); f(n + 3, y.w); }
     };
     Cursor<UT> now;
-    now.at(p, r.line.b[0], u0 - r.line.before[0]);
+    u_at(p, now, r.line.b[0], u0 - r.line.before[0]);
     bool dead = false, fresh = true;          // no tile of the segment so far
     float l[CW], bad = 0.f;
     int seg = 0, my_query = 0;
@@ -403,7 +439,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         const bool partly = edge && !hidden && !(now.s.nq == p.in.Q && x <= now.s.p0 && (p.in.window <= 0 || x > now.s.n - 1 - p.in.window || x < sinks));
         auto scores = [&] {
 #pragma unroll
-          for (int n = 0; n < CW; n += LD) u_ld<LD>(tmem + lanes + (i & 1) * N + c0 + n, w + n);
+          for (int n = 0; n < CW; n += CW) u_ld<CW>(tmem + lanes + (i & 1) * N + c0 + n, w + n);
           if (hidden) {
 #pragma unroll
             for (int n = 0; n < CW; ++n) w[n] = -CUDART_INF_F;
@@ -417,54 +453,51 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         auto weights = [&] {
           by_four(m_s, [&](int n, float m) { w[n] = ex2f(fmaf(w[n], p.c, -m)); big = fmaxf(big, w[n]); });
         };
-        scores();
-        if (fresh && !edge) {
-          // any maximum will do that none of the positions passes by 2^8: that of a quarter of them, each warp for a quarter of the rows
+        bool exact = fresh && edge;
+#pragma unroll 1
+        for (;;) {
+          scores();
+          if (exact) {             // the rows' maxima
 #pragma unroll
-          for (int k = 0; k < CW / 4; ++k) {
-            const float top = u_warp_max(q4 == 0 ? w[k] : q4 == 1 ? w[CW / 4 + k] : q4 == 2 ? w[CW / 2 + k] : w[3 * CW / 4 + k]);
-            if (lane == k) m_s[q4 * (CW / 4) + k] = fmaxf(NOTHING, top * p.c);
-          }
-          u_sync(g);
-        }
-        bool renew = fresh && edge;
-        if (!renew) {
-          weights();
-          renew = u_any(g, big > 256.f);
-          if (renew) scores();
-        }
-        if (renew) {               // the rows' maxima
+            for (int n = 0; n < CW; ++n) {
+              const float top = u_warp_max(w[n]);
+              if (lane == n) r.top[q4][c0 + n] = top;
+            }
+            u_sync(g);
+            if (t < CW) {
+              const int n = c0 + t;
+              const float most = fmaxf(fmaxf(r.top[0][n], r.top[1][n]), fmaxf(r.top[2][n], r.top[3][n])), before = m_s[t], m = fmaxf(before, most * p.c);
+              m_s[t] = m;
+              factor_s[t] = ex2f(before - m);
+            }
+            u_sync(g);
+            if (!fresh) {          // ... and what is there already
+              if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
+              u_after();
+#pragma unroll 1
+              for (int k = 0; k < 2; ++k) {
+                const uint32_t at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + k * N + c0;
+                float y[CW];
+                u_ld<CW>(at, y);
 #pragma unroll
-          for (int n = 0; n < CW; ++n) {
-            const float top = u_warp_max(w[n]);
-            if (lane == (n & 31)) r.top[q4][c0 + n] = top;
-          }
-          u_sync(g);
-          if (t < CW) {
-            const int n = c0 + t;
-            const float most = fmaxf(fmaxf(r.top[0][n], r.top[1][n]), fmaxf(r.top[2][n], r.top[3][n])), before = m_s[t], m = fmaxf(before, most * p.c);
-            m_s[t] = m;
-            factor_s[t] = ex2f(before - m);
-          }
-          u_sync(g);
-          if (!fresh) {            // ... and what is there already
-            if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
-            u_after();
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-              for (int n0 = 0; n0 < CW; n0 += LD) {
-                const uint32_t at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + k * N + c0 + n0;
-                float y[LD];
-                u_ld<LD>(at, y);
-#pragma unroll
-                for (int e = 0; e < LD; ++e) y[e] *= factor_s[n0 + e];
-                u_st<LD>(at, y);
+                for (int e = 0; e < CW; ++e) y[e] *= factor_s[e];
+                u_st<CW>(at, y);
               }
-            u_st_wait();
-            by_four(factor_s, [&](int n, float f) { l[n] *= f; });
+              u_st_wait();
+              by_four(factor_s, [&](int n, float f) { l[n] *= f; });
+            }
+          } else if (fresh) {
+            // any maximum will do that none of the positions passes by 2^8: that of a quarter of them, each warp for a quarter of the rows
+#pragma unroll
+            for (int k = 0; k < CW / 4; ++k) {
+              const float top = u_warp_max(q4 == 0 ? w[k] : q4 == 1 ? w[CW / 4 + k] : q4 == 2 ? w[CW / 2 + k] : w[3 * CW / 4 + k]);
+              if (lane == k) m_s[q4 * (CW / 4) + k] = fmaxf(NOTHING, top * p.c);
+            }
+            u_sync(g);
           }
           weights();
+          if (exact || !u_any(g, big > 256.f)) break;
+          exact = true;
         }
 #pragma unroll
         for (int n = 0; n < CW; ++n) l[n] += w[n];
@@ -474,11 +507,12 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         if (edge) {
           if (!dead && !u_wait(r.full + v_load % SLOTS, (v_load / SLOTS) & 1, r, limit)) dead = true;
           if (hidden && g == 0)    // values of positions that nothing sees: whatever lies there
+#pragma unroll 1
             for (int j = 0; j < PIECES; ++j) *(uint4*)(v_s + piece_of(t, j)) = make_uint4(0, 0, 0, 0);
           if (p.in.Q > 1) {        // some rows do not see all of the tile: a value that is not finite must not reach those as 0 * inf
             uint32_t top = 0;      // of the exponents (as halves: what is not finite is the largest)
             if (partly)
-#pragma unroll
+#pragma unroll 4
               for (int j = 0; j < PIECES; ++j) {
                 const uint4 y = *(const uint4*)(v_s + piece_of(t, j));
                 top = __vmaxu2(__vmaxu2(__vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu), __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu)), top);
@@ -491,15 +525,15 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
               u_after();
               keep = fresh;
 #pragma unroll 1
-              for (int n0 = 0; n0 < CW; n0 += LD) {
+              for (int n0 = 0; n0 < CW; n0 += CW) {
                 const uint32_t o_at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + c0 + n0;
-                float y[LD];
+                float y[CW];
                 if (fresh) {
 #pragma unroll
-                  for (int e = 0; e < LD; ++e) y[e] = 0.f;
+                  for (int e = 0; e < CW; ++e) y[e] = 0.f;
 #pragma unroll
-                  for (int k = 1; k < 2; ++k) u_st<LD>(o_at + k * N, y);
-                } else u_ld<LD>(o_at, y);
+                  for (int k = 1; k < 2; ++k) u_st<CW>(o_at + k * N, y);
+                } else u_ld<CW>(o_at, y);
                 if (t < DP)
 #pragma unroll 1
                   for (int pos = 0; pos < UT; ++pos) {      // (positions that all rows see are left to the product)
@@ -509,14 +543,15 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
                     const float z = __bfloat162float(*(const E*)(v_s + piece_of(pos, t >> 3) + (t & 7) * 2));
                     if (!(fabsf(z) < CUDART_INF_F))
 #pragma unroll
-                      for (int e = 0; e < LD; ++e)
+                      for (int e = 0; e < CW; ++e)
                         if (xx <= to_s[n0 + e] && (xx >= from_s[n0 + e] || xx < sinks)) y[e] += z;
                   }
-                u_st<LD>(o_at, y);
+                u_st<CW>(o_at, y);
               }
               u_st_wait();
               asm volatile("bar.sync 7, %0;" ::"n"(128 * GROUPS) : "memory");      // (all groups have found it)
               if (partly && g == 0)
+#pragma unroll 1
                 for (int j = 0; j < PIECES; ++j) {
                   uint4* const at = (uint4*)(v_s + piece_of(t, j));
                   auto clean = [](uint32_t y) { return ((y & 0x7f800000u) == 0x7f800000u ? 0u : y & 0xffff0000u) | ((y & 0x7f80u) == 0x7f80u ? 0u : y & 0xffffu); };
@@ -559,23 +594,29 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         fresh = true;
         ++seg;
       }
-      now.next(p);
+      u_next(p, now);
     }
   } else if (warp >= 4 + 4 * GROUPS) {
     // ---- results: thread t is column t of the output
     const int t = tid & 127, q4 = warp & 3;
     const uint32_t lanes = (uint32_t)(q4 * 32) << 16;
     Cursor<UT> at;
-    at.at(p, r.line.b[0], u0 - r.line.before[0]);
+    u_at(p, at, r.line.b[0], u0 - r.line.before[0]);
     bool dead = false;
-    int left = n_tiles;
+    int left = n_tiles, row = 0, j = 0;
 #pragma unroll 1
     for (int seg = 0; left > 0; ++seg) {
       const int sb = seg & 1, rest = at.s.nt - at.t;
       const bool head = at.t > 0, tail = left < rest;        // the segment goes on from the piece before, or behind
       const int h = p.RB == 1 ? at.hr : at.hr / p.RB;
-      const int n = t, row = (at.hr - h * p.RB) * N + t, j = row / p.G;
-      if (t < N) r.row_at[t] = row < p.R ? out_at(p, at.b, h, row) : -1;
+      const int n = t;
+      if (t < N) {
+        if (seg == 0 || p.RB > 1) {           // (a division)
+          row = at.hr % p.RB * N + t;
+          j = row / p.G;
+        }
+        r.row_at[t] = row < p.R ? at.b * p.out.o_seq + j * p.out.o_pos + (int64_t)(h * p.G + row - j * p.G) * p.out.o_head : -1;
+      }
       if (!dead && !u_wait(r.seg_sums + sb, (seg >> 1) & 1, r, limit)) dead = true;
       if (!dead && !u_wait(r.seg_pv + sb, (seg >> 1) & 1, r, limit)) dead = true;
       u_after();
@@ -592,24 +633,21 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         }
       }
       u_sync(GROUPS);
+      const int D = partial ? DP : p.in.D;
 #pragma unroll 1
-      for (int n0 = 0; n0 < N; n0 += 16) {
-        float o[16], y[16];
+      for (int n0 = 0; n0 < N; n0 += 8) {
+        if (r.row_at[n0] < 0) break;          // (rows that there are come first)
+        float o[8], y[8];
         const uint32_t o_at = tmem + lanes + 2 * N + sb * 2 * N + n0;
-        u_ld<16>(o_at, o);
+        u_ld<8>(o_at, o);
+        u_ld<8>(o_at + N, y);
 #pragma unroll
-        for (int k = 1; k < 2; ++k) {
-          u_ld<16>(o_at + k * N, y);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] += y[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
+        for (int e = 0; e < 8; ++e) {
           const int64_t to = r.row_at[n0 + e];
-          if (to >= 0) {
-            const float f = r.inverse[n0 + e];
-            if (partial) { if (t < DP) part[(n0 + e) * DP + t] = o[e]; }
-            else if (t < p.in.D) ((E*)p.out.out)[to + t] = __float2bfloat16_rn(f == 0.f ? 0.f : o[e] * f);
+          const float f = r.inverse[n0 + e], x = f == 0.f ? 0.f : (o[e] + y[e]) * f;
+          if (to >= 0 && t < D) {
+            if (partial) part[(n0 + e) * DP + t] = x;
+            else ((E*)p.out.out)[to + t] = __float2bfloat16_rn(x);
           }
         }
       }
@@ -622,7 +660,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       }
       left -= rest;
       at.t = at.s.nt - 1;
-      at.next(p);
+      u_next(p, at);
       u_sync(GROUPS);              // (row_at and inverse are written again)
     }
   }
