@@ -168,11 +168,19 @@ template <int N> __device__ __forceinline__ void column_sums(float (&l)[N], floa
 static __device__ __noinline__ uint4 u_eight(const uint16_t* w) {      // not aligned
   return make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
 }
-static __device__ __noinline__ void u_at(const AttnParams& p, Cursor<UT>& c, long long b, long long offset) { c.at(p, b, offset); }
+// (a copy goes in and out: the cursor itself stays in registers)
+static __device__ __noinline__ void u_at_far(const AttnParams& p, Cursor<UT>& c, long long b, long long offset) { c.at(p, b, offset); }
 static __device__ __noinline__ void u_next_row(const AttnParams& p, Cursor<UT>& c) { c.next(p); }
+__device__ __forceinline__ void u_at(const AttnParams& p, Cursor<UT>& c, long long b, long long offset) {
+  Cursor<UT> to;
+  u_at_far(p, to, b, offset);
+  c = to;
+}
 __device__ __forceinline__ void u_next(const AttnParams& p, Cursor<UT>& c) {
-  if (c.t + 1 < c.s.nt) ++c.t;
-  else u_next_row(p, c);
+  if (c.t + 1 < c.s.nt) { ++c.t; return; }
+  Cursor<UT> to = c;
+  u_next_row(p, to);
+  c = to;
 }
 
 constexpr float NOTHING = -1e30f;       // the maximum of a row that has seen nothing so far
