@@ -165,6 +165,7 @@ template <int N> __device__ __forceinline__ void column_sums(float (&l)[N], floa
   for (int k = 0; k < LEFT; ++k) to[n0 + k] = x[k];      // (N = 16: two lanes write the same)
 }
 
+__device__ __forceinline__ __nv_bfloat162 bf16x2_of(uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); }
 static __device__ __noinline__ uint4 u_eight(const uint16_t* w) {      // not aligned
   return make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
 }
@@ -518,14 +519,17 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
 #pragma unroll 1
             for (int j = 0; j < PIECES; ++j) *(uint4*)(v_s + piece_of(t, j)) = make_uint4(0, 0, 0, 0);
           if (p.in.Q > 1) {        // some rows do not see all of the tile: a value that is not finite must not reach those as 0 * inf
-            uint32_t top = 0;      // of the exponents (as halves: what is not finite is the largest)
+            const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+            __nv_bfloat162 z[4] = {zero, zero, zero, zero};      // 0 x, added up: NaN once there is such a value
             if (partly)
 #pragma unroll 4
               for (int j = 0; j < PIECES; ++j) {
                 const uint4 y = *(const uint4*)(v_s + piece_of(t, j));
-                top = __vmaxu2(__vmaxu2(__vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu), __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu)), top);
+                z[0] = __hfma2(bf16x2_of(y.x), zero, z[0]); z[1] = __hfma2(bf16x2_of(y.y), zero, z[1]);
+                z[2] = __hfma2(bf16x2_of(y.z), zero, z[2]); z[3] = __hfma2(bf16x2_of(y.w), zero, z[3]);
               }
-            const bool strange = (top & 0xffffu) >= 0x7f80u || top >= 0x7f800000u;
+            const float2 z2 = __bfloat1622float2(__hadd2(__hadd2(z[0], z[1]), __hadd2(z[2], z[3])));
+            const bool strange = !(z2.x + z2.y == 0.f);
             if (u_any(g, strange)) { // it goes to the rows that see it by itself, and 0 takes its place
               if (!fresh) {
                 if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
