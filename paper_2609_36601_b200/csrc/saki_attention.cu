@@ -522,7 +522,9 @@ constexpr int MAX_WORKERS = 8 * 148;  // of a call
 struct Kernel { const void *tma, *plain; int rows, dp, t, smem, workers, threads; };
 template <typename E, int DP, int NW> Kernel kernel() {
   using S = Shape<E, DP, NW>;
-  return {(const void*)attn_kernel<E, DP, NW, true>, (const void*)attn_kernel<E, DP, NW, false>, S::ROWS, DP, S::T, S::SMEM, S::WORKERS, S::THREADS};
+  const void* tma = nullptr;       // (bf16 heads of 65 to 128 with more rows, boxes and all, are for tcgen05)
+  if constexpr (sizeof(E) == 4 || DP != 128 || NW == 1) tma = (const void*)attn_kernel<E, DP, NW, true>;
+  return {tma, (const void*)attn_kernel<E, DP, NW, false>, S::ROWS, DP, S::T, S::SMEM, S::WORKERS, S::THREADS};
 }
 template <typename E, int DP> Kernel pick(int R) {
   if constexpr (DP == 256 && sizeof(E) == 4) return R <= 16 ? kernel<E, DP, 1>() : R <= 32 ? kernel<E, DP, 2>() : kernel<E, DP, 4>();
@@ -592,8 +594,14 @@ bool mode_fits(int mode, int64_t page, int64_t pos, int64_t head, const saki_att
 
 }  // namespace
 
-// bf16 heads of up to 128 on pages of whole eights go to the kernel on tcgen05
-static bool on_umma(const saki_attn_in& in) { return in.dtype == SAKI_BF16 && in.D > 16 && in.D <= 128 && in.page_size % 8 == 0; }
+// bf16 heads of up to 128 on pages of whole eights go to the kernel on tcgen05, but for single tokens of few rows where its tiles of 128 positions cost more than they
+// bring: heads of up to 64 (96 sequences of 8000 positions, 5 rows: 309 us here, 384 there; of 1024: 64 and 78; but two tokens of 8 rows, 4000 positions: 261 and 237),
+// and where nothing sees more than 256 positions (512 sequences of 128 positions, heads of 128: 85 and 101 us; of 256: 140 and 155; of 512: 254 and 233).
+static bool on_umma(const saki_attn_in& in) {
+  if (in.dtype != SAKI_BF16 || in.D <= 16 || in.D > 128 || in.page_size % 8 != 0) return false;
+  const int64_t table = (int64_t)in.max_pages * in.page_size, seen = in.window > 0 ? std::min<int64_t>(table, (int64_t)in.window + in.sinks) : table;
+  return in.Q > 1 || in.Hq / in.H > 16 || (in.D > 64 && seen > 256);
+}
 
 int64_t attention_scratch_bytes(const saki_attn_in& in) {
   const Kernel k = pick(in);
