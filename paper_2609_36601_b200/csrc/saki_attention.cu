@@ -58,12 +58,13 @@ __device__ __forceinline__ void two_terms(uint32_t x, uint32_t& hi, uint32_t& lo
 template <typename E, int DP, int NW_> struct Shape {
   static constexpr bool F32 = sizeof(E) == 4;
   static constexpr int NW = NW_, WARPS = DP == 256 && NW <= 4 ? 4 : 8, THREADS = 32 * WARPS, WORKERS = WARPS / NW, ROWS = 16 * NW;
-  static constexpr int T = F32 ? (DP == 64 ? 16 : 8) : (DP == 64 ? 32 : 16);         // positions of a tile
+  static constexpr int T = F32 ? (DP <= 96 ? 16 : 8) : (DP == 64 ? 32 : 16);         // positions of a tile (f32, heads of 80, 8 and 16: 294 and 217 us at 24 sequences of 15000)
   static constexpr int COLS = 128 / (int)sizeof(E), SLABS = DP / COLS;               // columns of a 128-byte slab [T][128 bytes]
   static constexpr int HALF = T * DP * (int)sizeof(E), STAGE = 2 * HALF;             // keys, then values
-  static constexpr int Q_BYTES = ROWS * DP * (int)sizeof(E);                         // of a worker
+  static constexpr bool Q_REGS = F32 && DP <= 128;                                   // queries in registers: the room is for the ring
+  static constexpr int Q_BYTES = Q_REGS ? 0 : ROWS * DP * (int)sizeof(E);            // of a worker
   static constexpr int FIT = (226 * 1024 - WORKERS * Q_BYTES - 1024 - 8 * THREADS) / (WORKERS * (STAGE + 8));
-  static constexpr int STAGES = FIT < 3 * NW ? FIT : 3 * NW;
+  static constexpr int MOST = NW == 8 ? 24 : 4 * NW, STAGES = FIT < MOST ? FIT : MOST;
   static constexpr int SMEM = WORKERS * (STAGES * (STAGE + 8) + Q_BYTES + 4) + (int)sizeof(LineShared<THREADS>) + 1024;
   static_assert(STAGES >= 2 && STAGES < 32 && SMEM <= 227 * 1024, "a block's shared memory");
 };
@@ -174,6 +175,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
 #pragma unroll 1
   for (int i = 0; i < ST - 1; ++i) { load(); look_up(); }
 
+  uint32_t q_r[S::Q_REGS ? DP / 8 : 1][4];      // the lane's share of the queries, as the products take them
   float o[ND][4], m[2], l[2];
   Sight sight[2];
   float bad = 0.f;                 // -1: a page outside the pool, -2: a wait ran out (from then on nothing is loaded or waited for)
@@ -189,20 +191,35 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
   for (int i = 0; i < n_tiles; ++i) {
     const int h = p.RB == 1 ? now.hr : now.hr / p.RB, row0 = (now.hr - h * p.RB) * S::ROWS;
     if (fresh) {                   // a new segment: its queries
-      for (int e = part_of * 32 + lane; e < S::ROWS * PIECES; e += 32 * NW) {
-        const int rr = e / PIECES, jj = e % PIECES, r = row0 + rr, j = r / p.G;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (r < p.R && jj * PE < p.in.D) {
-          const E* const q = (const E*)p.in.q + now.b * p.in.q_seq + j * p.in.q_pos + (int64_t)(h * p.G + r - j * p.G) * p.in.q_head + jj * PE;
-          if (p.q_vec) x = *(const uint4*)q;
-          else if constexpr (F32) { const uint32_t* const w = (const uint32_t*)q; x = make_uint4(w[0], w[1], w[2], w[3]); }
-          else {
-            const uint16_t* const w = (const uint16_t*)q;
-            x = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
-          }
-          x.x ^= p.q_sign; x.y ^= p.q_sign; x.z ^= p.q_sign; x.w ^= p.q_sign;
+      if constexpr (S::Q_REGS) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = row0 + part_of * 16 + (lane >> 2) + 8 * i, j = r / p.G;
+          const E* const q = (const E*)p.in.q + now.b * p.in.q_seq + j * p.in.q_pos + (int64_t)(h * p.G + r - j * p.G) * p.in.q_head;
+#pragma unroll
+          for (int k = 0; k < DP / 8; ++k)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const int col = k * 8 + (lane & 3) + 4 * c;
+              q_r[k][2 * c + i] = r < p.R && col < p.in.D ? __float_as_uint((float)q[col]) ^ p.q_sign : 0u;
+            }
         }
-        *(uint4*)(q_s + piece_at<S::ROWS>(rr, jj)) = x;
+      } else {
+        for (int e = part_of * 32 + lane; e < S::ROWS * PIECES; e += 32 * NW) {
+          const int rr = e / PIECES, jj = e % PIECES, r = row0 + rr, j = r / p.G;
+          uint4 x = make_uint4(0, 0, 0, 0);
+          if (r < p.R && jj * PE < p.in.D) {
+            const E* const q = (const E*)p.in.q + now.b * p.in.q_seq + j * p.in.q_pos + (int64_t)(h * p.G + r - j * p.G) * p.in.q_head + jj * PE;
+            if (p.q_vec) x = *(const uint4*)q;
+            else if constexpr (F32) { const uint32_t* const w = (const uint32_t*)q; x = make_uint4(w[0], w[1], w[2], w[3]); }
+            else {
+              const uint16_t* const w = (const uint16_t*)q;
+              x = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
+            }
+            x.x ^= p.q_sign; x.y ^= p.q_sign; x.z ^= p.q_sign; x.w ^= p.q_sign;
+          }
+          *(uint4*)(q_s + piece_at<S::ROWS>(rr, jj)) = x;
+        }
       }
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f;
@@ -270,9 +287,9 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
       for (int k = 0; k < DP / 8; ++k) {
         if (k * 8 >= p.in.D) break;
         uint32_t q[4], qh[4], ql[4];
-        ldm4(q, pair_at<S::ROWS>(q_l, k));
+        if constexpr (!S::Q_REGS) ldm4(q, pair_at<S::ROWS>(q_l, k));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) two_terms(q[e], qh[e], ql[e]);
+        for (int e = 0; e < 4; ++e) two_terms(S::Q_REGS ? q_r[S::Q_REGS ? k : 0][e] : q[e], qh[e], ql[e]);
 #pragma unroll
         for (int e = 0; e < NT; ++e) {
           uint32_t kf[2], kh[2], kl[2];
@@ -459,9 +476,10 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
     for (int i = max(0, loaded - ST); i < loaded; ++i) mbar_wait_bounded(full + i % ST, (uint32_t)(i / ST) & 1u);
 }
 
-// Joins the segments that several workers had a part of: block i the one that starts in piece i of the line.  A row at a time, the partials
-// spread over the warps (in the order of the line within a warp, then warp by warp: the same sum every time).
-template <typename E, int ROWS, int DP> __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnParams p) {
+// Joins the segments that several workers had a part of: block i the one that starts in piece i of the line.  `share` (1, 2, 4, 8) warps take a row's partials in
+// turns, in the order of the line, and put theirs together warp by warp: the same sum every time.  (Eight warps for each row whatever the number of partials: 17 us where
+// 1184 pieces had 5 rows, nine blocks of ten with nothing to do.)
+template <typename E, int ROWS, int DP> __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnParams p, int share) {
   constexpr int PER = DP / 32;
   __shared__ float o_s[8][DP];
   __shared__ float2 ml_s[8];
@@ -471,47 +489,50 @@ template <typename E, int ROWS, int DP> __global__ void __launch_bounds__(256) a
   const int4 d = p.desc[blockIdx.x];
   if (d.z == 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = d.y / p.RB, row0 = (d.y - h * p.RB) * ROWS;
-  for (int rr = blockIdx.y; rr < ROWS && row0 + rr < p.R; rr += gridDim.y) {
+  const int w0 = warp & ~(share - 1), mine = warp - w0, at_once = 8 / share;
+  const int rows = min(ROWS, p.R - row0);
+  for (int r0 = blockIdx.y * at_once; r0 < rows; r0 += gridDim.y * at_once) {
+    const int rr = r0 + warp / share;
+    const bool there = rr < rows;
     float m = -CUDART_INF_F, l = 0.f, o[PER];
     uint32_t bad = 0;
 #pragma unroll
     for (int k = 0; k < PER; ++k) o[k] = 0.f;
-    for (int i = warp; i <= d.z; i += 8) {
-      const float* const part = p.part + ((blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * (int64_t)PART<ROWS, DP>;
-      const float2 ml = *(const float2*)(part + ROWS * DP + rr * 2);
-      bad |= status_of(ml.y);
-      const float top = fmaxf(m, ml.x), sh = top == -CUDART_INF_F ? 0.f : top, a = ex2f(m - sh), c = ex2f(ml.x - sh);
+    if (there) {
+#pragma unroll 2
+      for (int i = mine; i <= d.z; i += share) {
+        const float* const part = p.part + ((blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * (int64_t)PART<ROWS, DP>;
+        const float2 ml = *(const float2*)(part + ROWS * DP + rr * 2);
+        bad |= status_of(ml.y);
+        const float top = fmaxf(m, ml.x), sh = top == -CUDART_INF_F ? 0.f : top, a = ex2f(m - sh), c = ex2f(ml.x - sh);
 #pragma unroll
-      for (int k = 0; k < PER; ++k) o[k] = o[k] * a + part[rr * DP + k * 32 + lane] * c;
-      l = l * a + ml.y * c;
-      m = top;
+        for (int k = 0; k < PER; ++k) o[k] = o[k] * a + part[rr * DP + k * 32 + lane] * c;
+        l = l * a + ml.y * c;
+        m = top;
+      }
     }
 #pragma unroll
     for (int k = 0; k < PER; ++k) o_s[warp][k * 32 + lane] = o[k];
-    if (lane == 0) ml_s[warp] = make_float2(m, l);
-    if (lane == 0) bad_s[warp] = bad;
+    if (lane == 0) { ml_s[warp] = make_float2(m, l); bad_s[warp] = bad; }
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 8; ++w) bad |= bad_s[w];
-    float top = -CUDART_INF_F;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, ml_s[w].x);
-    const float sh = top == -CUDART_INF_F ? 0.f : top;
-    float sum = 0.f, a[8];
-#pragma unroll
-    for (int w = 0; w < 8; ++w) { a[w] = ex2f(ml_s[w].x - sh); sum += ml_s[w].y * a[w]; }
-    const uint32_t st = (uint32_t)d.w | bad;
-    const bool none = st || sum == 0.f;
-    E* const out = (E*)p.out.out + out_at(p, d.x, h, row0 + rr);
-    for (int k = threadIdx.x; k < p.in.D; k += 256) {
-      float x = 0.f;
-#pragma unroll
-      for (int w = 0; w < 8; ++w) x += o_s[w][k] * a[w];
-      st_from_float(out, k, none ? 0.f : x / sum);
-    }
-    if (threadIdx.x == 0) {
-      put_lse(p, d.x, h, row0 + rr, top, none ? 0.f : sum);
-      if (rr == 0 && d.y == 0) put_status(p, d.x, st);
+    if (there) {
+      float top = -CUDART_INF_F;
+      for (int w = w0; w < w0 + share; ++w) { bad |= bad_s[w]; top = fmaxf(top, ml_s[w].x); }
+      const float sh = top == -CUDART_INF_F ? 0.f : top;
+      float sum = 0.f;
+      for (int w = w0; w < w0 + share; ++w) sum += ml_s[w].y * ex2f(ml_s[w].x - sh);
+      const uint32_t st = (uint32_t)d.w | bad;
+      const bool none = st || sum == 0.f;
+      E* const out = (E*)p.out.out + out_at(p, d.x, h, row0 + rr);
+      for (int k = mine * 32 + lane; k < p.in.D; k += 32 * share) {
+        float x = 0.f;
+        for (int w = w0; w < w0 + share; ++w) x += o_s[w][k] * ex2f(ml_s[w].x - sh);
+        st_from_float(out, k, none ? 0.f : x / sum);
+      }
+      if (mine == 0 && lane == 0) {
+        put_lse(p, d.x, h, row0 + rr, top, none ? 0.f : sum);
+        if (rr == 0 && d.y == 0) put_status(p, d.x, st);
+      }
     }
     __syncthreads();
   }
@@ -532,19 +553,26 @@ template <typename E, int DP> Kernel pick(int R) {
 }
 template <typename E> Kernel pick(const saki_attn_in& in) {
   const int R = in.Q * (in.Hq / in.H);
+  if constexpr (sizeof(E) == 4)
+    if (in.D > 64 && in.D <= 96) return pick<E, 96>(R);      // (a ring of four tiles, not three)
   return in.D <= 64 ? pick<E, 64>(R) : in.D <= 128 ? pick<E, 128>(R) : pick<E, 256>(R);
 }
 Kernel pick(const saki_attn_in& in) { return in.dtype == SAKI_BF16 ? pick<__nv_bfloat16>(in) : pick<float>(in); }
 int64_t part_floats(const Kernel& k) { return (int64_t)k.rows * (k.dp + 2); }
 
 template <typename E, int DP> cudaError_t join(const AttnParams& p, int rows, int workers, cudaStream_t st) {
-  const dim3 grid((unsigned)workers, (unsigned)std::min(p.R, std::min(rows, 16)));
-  if (rows == 16) return launch_pdl(attn_join_kernel<E, 16, DP>, grid, 256, 0, st, true, p);
-  if (rows == 32) return launch_pdl(attn_join_kernel<E, 32, DP>, grid, 256, 0, st, true, p);
-  if (rows == 64) return launch_pdl(attn_join_kernel<E, 64, DP>, grid, 256, 0, st, true, p);
-  return launch_pdl(attn_join_kernel<E, 128, DP>, grid, 256, 0, st, true, p);
+  // a warp for some four partials: as many as a segment of average length has
+  const int64_t partials = workers / std::max<int64_t>(1, p.in.B * p.in.H * p.RB) + 1;
+  const int share = partials <= 4 ? 1 : partials <= 8 ? 2 : partials <= 16 ? 4 : 8, at_once = 8 / share;
+  const dim3 grid((unsigned)workers, (unsigned)std::min((std::min(p.R, rows) + at_once - 1) / at_once, 16));
+  if (rows == 16) return launch_pdl(attn_join_kernel<E, 16, DP>, grid, 256, 0, st, true, p, share);
+  if (rows == 32) return launch_pdl(attn_join_kernel<E, 32, DP>, grid, 256, 0, st, true, p, share);
+  if (rows == 64) return launch_pdl(attn_join_kernel<E, 64, DP>, grid, 256, 0, st, true, p, share);
+  return launch_pdl(attn_join_kernel<E, 128, DP>, grid, 256, 0, st, true, p, share);
 }
 template <typename E> cudaError_t join(const AttnParams& p, const Kernel& k, int workers, cudaStream_t st) {
+  if constexpr (sizeof(E) == 4)
+    if (k.dp == 96) return join<E, 96>(p, k.rows, workers, st);
   return k.dp == 64 ? join<E, 64>(p, k.rows, workers, st) : k.dp == 128 ? join<E, 128>(p, k.rows, workers, st) : join<E, 256>(p, k.rows, workers, st);
 }
 
