@@ -20,6 +20,7 @@ struct BeamParams {
   saki_beam_out out;
   int slices, slice;        // per row, and elements of one
   float c_hi, c_lo;         // log2(e) / temperature
+  double inv_tau;
   uint64_t* cand;           // [B * W][slices][n] pairs of a slice, best first; 0: none
   double2* part;            // [B * W][slices] (maximum, sum of 2^(c (x - maximum))) of a slice
   unsigned long long* flagged;
@@ -43,12 +44,18 @@ template <> struct Vec<__nv_bfloat16> {
   uint32_t r[4];
   __device__ __forceinline__ float2 pair(int i) const { return unpack_bf16x2(r[i]); }
   __device__ __forceinline__ void set(int i, float x, float y) { r[i] = pack_bf16x2(x, y); }
+  __device__ __forceinline__ float top() const {      // (of a pair with a NaN the other)
+    auto h = [](uint32_t a) { return *reinterpret_cast<const __nv_bfloat162*>(&a); };
+    const float2 a = __bfloat1622float2(__hmax2(__hmax2(h(r[0]), h(r[1])), __hmax2(h(r[2]), h(r[3]))));
+    return fmaxf(a.x, a.y);
+  }
 };
 template <> struct Vec<float> {
   static constexpr int E = 4;
   uint32_t r[4];
   __device__ __forceinline__ float2 pair(int i) const { return make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])); }
   __device__ __forceinline__ void set(int i, float x, float y) { r[2 * i] = __float_as_uint(x); r[2 * i + 1] = __float_as_uint(y); }
+  __device__ __forceinline__ float top() const { return fmaxf(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])), fmaxf(__uint_as_float(r[2]), __uint_as_float(r[3]))); }
 };
 
 // what was unpacked from x before is not kept for what comes: 64 elements as floats are more than the registers hold
@@ -60,7 +67,7 @@ template <typename T, int NV> __device__ __forceinline__ void keep_packed(Vec<T>
 }
 
 struct BeamShared {
-  float group_max[GROUPS];
+  alignas(16) float group_max[GROUPS];
   float warp_max[BWARPS];
   double warp_sum[BWARPS];
   uint64_t warp_best[BWARPS];
@@ -99,12 +106,9 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 3) beam_rows
         x[k].set(i, v + 2 * i < V ? ld_as_float(s, v + 2 * i) : -CUDART_INF_F, v + 2 * i + 1 < V ? ld_as_float(s, v + 2 * i + 1) : -CUDART_INF_F);
     }
   }
-  float mine = -CUDART_INF_F;
+  float top[NV], mine = -CUDART_INF_F;
 #pragma unroll
-  for (int k = 0; k < NV; ++k)
-#pragma unroll
-    for (int i = 0; i < E / 2; ++i) { const float2 a = x[k].pair(i); mine = fmaxf(mine, fmaxf(a.x, a.y)); }
-  keep_packed(x);
+  for (int k = 0; k < NV; ++k) { top[k] = x[k].top(); mine = fmaxf(mine, top[k]); }
   float m = mine;
   m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
   m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
@@ -126,16 +130,18 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 3) beam_rows
     for (int i = tid; i < n; i += BT) cand[i] = 0;
     return;
   }
-  if (warp == 0) {                 // the bar, while the other warps sum
-    const float g0 = sh.group_max[lane], g1 = sh.group_max[lane + 32];
-    int r0 = 0, r1 = 0;
-    for (int i = 0; i < GROUPS; ++i) {
-      const float g = sh.group_max[i];
-      r0 += g > g0 || (g == g0 && i < lane);
-      r1 += g > g1 || (g == g1 && i < lane + 32);
+  {                                // the bar: thread t compares group t / 4 with a quarter of the groups
+    const float g = sh.group_max[tid >> 2];
+    int more = 0, least = 0;       // groups above g, and those and its equals
+#pragma unroll
+    for (int i = 0; i < GROUPS / 4; i += 4) {
+      const float4 y = *(const float4*)(sh.group_max + (tid & 3) * (GROUPS / 4) + i);
+      more += (y.x > g) + (y.y > g) + (y.z > g) + (y.w > g);
+      least += (y.x >= g) + (y.y >= g) + (y.z >= g) + (y.w >= g);
     }
-    if (r0 == n - 1) sh.bar = g0;
-    if (r1 == n - 1) sh.bar = g1;
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) { more += __shfl_xor_sync(0xffffffffu, more, o); least += __shfl_xor_sync(0xffffffffu, least, o); }
+    if (more < n && n <= least) sh.bar = g;      // (the same value, whoever writes it)
   }
   // x - m is exact where it matters, and the constant has two terms: an error of the argument that is the same for all elements would not average out
   float2 sum = make_float2(0.f, 0.f);
@@ -161,7 +167,8 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 3) beam_rows
   keep_packed(x);
   if (mine >= bar && mine > -CUDART_INF_F) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+      if (!(top[k] >= bar)) continue;
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         const float2 a = x[k].pair(i >> 1);
@@ -171,6 +178,7 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 3) beam_rows
           if (at < LIST) sh.list[at] = pair_word(e, (uint32_t)(v0 + (k * BT + tid) * E + i));
         }
       }
+    }
   }
   __syncthreads();
   const int count = (int)sh.count;
@@ -210,29 +218,41 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 3) beam_rows
   }
 }
 
-struct Best { double key; int64_t at; };      // at: w * V + v
-__device__ __forceinline__ bool before(const Best& a, const Best& b) { return a.key > b.key || (a.key == b.key && a.at < b.at); }
+// A candidate of a group.  `order` decides between equal keys: lower beams, then larger logits (keys of theirs may round to the same), then lower tokens first: an order
+// that a beam's slices are sorted by as they are.  0: none.
+struct Best { double key; uint64_t order; };
+constexpr int TOKEN_BITS = 22, FEW = BT;
+__device__ __forceinline__ uint64_t order_of(int w, uint32_t logit, uint32_t v) { return (uint64_t)(63 - w) << (32 + TOKEN_BITS) | (uint64_t)logit << TOKEN_BITS | ((1u << TOKEN_BITS) - 1 - v); }
+__device__ __forceinline__ bool before(const Best& a, const Best& b) { return a.key > b.key || (a.key == b.key && a.order > b.order); }
 __device__ __forceinline__ Best warp_first(Best a) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    const Best u = {__shfl_xor_sync(0xffffffffu, a.key, o), __shfl_xor_sync(0xffffffffu, a.at, o)};
+    const Best u = {__shfl_xor_sync(0xffffffffu, a.key, o), __shfl_xor_sync(0xffffffffu, a.order, o)};
     if (before(u, a)) a = u;
   }
   return a;
 }
 
-// a block per group: a thread holds the heads of some of the sorted lists, one per beam and slice
+__host__ __device__ constexpr int join_items(int n, int lists) { return lists <= FEW && lists > n * n ? lists : n * n; }
+
+// A block per group.  Its n best lie in the n lists (one per beam and slice) whose heads are the best; those lists' elements are ranked by counting, each list being sorted.
+// (Head after head, with a list's next element fetched when its head was taken, took 15 us for 64 groups of 80 lists, 8 to choose.)
 __global__ void __launch_bounds__(BT) beam_join_kernel(const BeamParams p) {
   __shared__ double top[64], rest[64];     // the log-sum-exp of a beam is top / tau + rest
   __shared__ int how[64];           // 0: nothing to choose, 1: slices, 2: finished
-  __shared__ Best first[BWARPS];
-  extern __shared__ unsigned char taken[];     // of every list
+  __shared__ Best first[2][BWARPS];
+  __shared__ int list_of[64];
+  __shared__ Best below[1];         // the last of n heads
+  __shared__ int total;
+  extern __shared__ __align__(16) unsigned char join_smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = p.in.W, n = p.in.n, lists = W * p.slices;
+  Best* const item = (Best*)join_smem;     // [n][n]; the heads of few lists before
+  unsigned char* const taken = join_smem + join_items(n, lists) * sizeof(Best);      // of every list
   const int64_t b = blockIdx.x;
-  const double tau = (double)p.in.temperature;
   wait_for_predecessor();
   launch_dependents();
   for (int i = tid; i < lists; i += BT) taken[i] = 0;
+  if (tid == 0) total = 0;
   for (int w = warp; w < W; w += BWARPS) {
     const int64_t row = b * W + w;
     const float score = p.in.score[row];
@@ -253,7 +273,7 @@ __global__ void __launch_bounds__(BT) beam_join_kernel(const BeamParams p) {
           double sum = 0;
           for (int s = lane; s < p.slices; s += 32) {
             const double2 a = p.part[row * p.slices + s];
-            if (a.x > -CUDART_INF) sum += a.y * exp((a.x - (double)m) / tau);
+            if (a.x > -CUDART_INF) sum += a.y * exp((a.x - (double)m) * p.inv_tau);
           }
           sum = warp_sum(sum);
           if (lane == 0) { top[w] = m; rest[w] = log(sum); }
@@ -267,43 +287,89 @@ __global__ void __launch_bounds__(BT) beam_join_kernel(const BeamParams p) {
     }
   }
   __syncthreads();
-  auto head = [&](int l) -> Best {
-    const int w = l / p.slices, s = l - w * p.slices, k = taken[l];
+  const Best none = {-CUDART_INF, 0};
+  auto element = [&](int l, int k) -> Best {
+    const int w = l / p.slices, s = l - w * p.slices;
     const double score = (double)p.in.score[b * W + w];
-    if (how[w] == 2) return s == 0 && k == 0 ? Best{score, (int64_t)w * p.in.V + p.in.pad} : Best{-CUDART_INF, INT64_MAX};
-    if (how[w] == 0 || k >= n) return {-CUDART_INF, INT64_MAX};
+    if (how[w] == 2) return s == 0 && k == 0 ? Best{score, order_of(w, 0x80000000u, p.in.pad)} : none;
+    if (how[w] == 0) return none;
     const uint64_t c = p.cand[((b * W + w) * p.slices + s) * n + k];
-    if (c == 0) return {-CUDART_INF, INT64_MAX};
-    return {score + (((double)pair_logit(c) - top[w]) / tau - rest[w]), (int64_t)w * p.in.V + pair_token(c)};
+    return c == 0 ? none : Best{score + (((double)pair_logit(c) - top[w]) * p.inv_tau - rest[w]), order_of(w, (uint32_t)(c >> 32), pair_token(c))};
   };
-  Best mine = {-CUDART_INF, INT64_MAX};
+  // the best heads
+  Best mine = none;
   int from = -1;
   auto look = [&] {
-    mine = {-CUDART_INF, INT64_MAX};
-    from = -1;
+    mine = none;
     for (int l = tid; l < lists; l += BT) {
-      const Best h = head(l);
+      const Best h = taken[l] ? none : element(l, 0);
       if (before(h, mine)) { mine = h; from = l; }
     }
   };
-  look();
-  for (int r = 0; r < n; ++r) {
-    Best a = warp_first(mine);
-    if (lane == 0) first[warp] = a;
+  int chosen = 0;
+  Best last = none;
+  if (lists <= FEW) {              // a thread a list: by counting
+    if (tid < lists) item[tid] = mine = element(tid, 0);
+    if (tid == 0) below[0] = none;
     __syncthreads();
-    a = first[0];
+    if (tid < lists && mine.order != 0) {
+      int rank = 0;
+#pragma unroll 4
+      for (int l = 0; l < lists; ++l) rank += before(item[l], mine);
+      if (rank < n) list_of[rank] = tid;
+      if (rank == n - 1) below[0] = mine;
+    }
+    chosen = min(n, __syncthreads_count(mine.order != 0));
+    last = below[0];
+    __syncthreads();
+  } else look();
+#pragma unroll 1
+  for (; lists > FEW && chosen < n; ++chosen) {
+    Best a = warp_first(mine);
+    if (lane == 0) first[chosen & 1][warp] = a;
+    __syncthreads();               // (the other half is written only behind the next)
+    a = first[chosen & 1][0];
 #pragma unroll
     for (int w = 1; w < BWARPS; ++w)
-      if (before(first[w], a)) a = first[w];
-    __syncthreads();
-    const bool none = a.at == INT64_MAX;
-    if (tid == 0) {
-      const int w = none ? -1 : (int)(a.at / p.in.V);
-      p.out.parent[b * n + r] = w;
-      p.out.token[b * n + r] = none ? -1 : (int)(a.at - (int64_t)w * p.in.V);
-      p.out.score[b * n + r] = (float)a.key;
+      if (before(first[chosen & 1][w], a)) a = first[chosen & 1][w];
+    if (a.order == 0) break;
+    if (mine.order == a.order) { list_of[chosen] = from; taken[from] = 1; look(); }
+    last = a;
+  }
+  __syncthreads();
+  int there = 0;
+  for (int i = tid; i < chosen * n; i += BT) {
+    const Best e = element(list_of[i / n], i % n);
+    item[i] = e;
+    there += e.order != 0;
+  }
+  if (there) atomicAdd(&total, there);
+  __syncthreads();
+  for (int i = tid; i < chosen * n; i += BT) {
+    const Best e = item[i];
+    if (e.order == 0 || (chosen == n && before(last, e))) continue;      // (n heads come before it)
+    const int j = i / n;
+    int rank = i - j * n;
+    for (int o = 0; o < chosen && rank < n; ++o) {
+      if (o == j) continue;
+      int lo = 0, hi = n;          // elements of list o before e
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (before(item[o * n + mid], e)) lo = mid + 1;
+        else hi = mid;
+      }
+      rank += lo;
     }
-    if (!none && mine.at == a.at) { ++taken[from]; look(); }
+    if (rank < n) {
+      p.out.parent[b * n + rank] = 63 - (int)(e.order >> (32 + TOKEN_BITS));
+      p.out.token[b * n + rank] = (1 << TOKEN_BITS) - 1 - (int)(e.order & ((1u << TOKEN_BITS) - 1));
+      p.out.score[b * n + rank] = (float)e.key;
+    }
+  }
+  for (int r = total + tid; r < n; r += BT) {
+    p.out.parent[b * n + r] = -1;
+    p.out.token[b * n + r] = -1;
+    p.out.score[b * n + r] = -CUDART_INF_F;
   }
 }
 
@@ -339,6 +405,7 @@ cudaError_t launch_beams(const saki_beam_in& in, const saki_beam_out& out, void*
   BeamParams p = {};
   p.in = in; p.out = out; p.slices = l.slices; p.slice = l.slice; p.flagged = flagged;
   const double c = 1.4426950408889634 / (double)in.temperature;
+  p.inv_tau = 1.0 / (double)in.temperature;
   p.c_hi = (float)c; p.c_lo = (float)(c - (double)p.c_hi);
   p.cand = (uint64_t*)scratch;
   p.part = (double2*)((char*)scratch + round256(rows * l.slices * in.n * 8));
@@ -351,7 +418,9 @@ cudaError_t launch_beams(const saki_beam_in& in, const saki_beam_out& out, void*
   } else
     e = l.nv == 8 ? go(beam_rows_kernel<float, 8>) : l.nv == 4 ? go(beam_rows_kernel<float, 4>) : l.nv == 2 ? go(beam_rows_kernel<float, 2>) : go(beam_rows_kernel<float, 1>);
   if (e != cudaSuccess) return e;
-  return launch_pdl(beam_join_kernel, dim3((unsigned)in.B), BT, (size_t)in.W * l.slices, st, true, p);
+  const size_t bytes = join_items(in.n, in.W * l.slices) * sizeof(Best) + (size_t)in.W * l.slices;      // (64 KB and 64 beams of 512 slices at most)
+  e = cudaFuncSetAttribute(beam_join_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  return e != cudaSuccess ? e : launch_pdl(beam_join_kernel, dim3((unsigned)in.B), BT, bytes, st, true, p);
 }
 
 }  // namespace saki
