@@ -469,14 +469,12 @@ class PageCache:
     """Page tables, lengths and counts of holders of a paged key-value cache (saki_cache), in one int32 tensor `meta` on the GPU:
     `page_table` [B, max_pages], `length` [B] and `ref_count` [n_pages] are views of it.  `PageCache.empty` makes one without
     positions.  The pools that hold keys and values, [n_pages, page_size, H, D] each, are the caller's, a pair per layer."""
-    __slots__ = ("meta", "B", "max_pages", "n_pages", "page_size", "scratch")
+    __slots__ = ("meta", "B", "max_pages", "n_pages", "page_size")
 
     def __init__(self, meta, B, max_pages, n_pages, page_size):
         if meta.dtype != torch.int32 or not meta.is_contiguous() or meta.numel() != B * max_pages + B + n_pages:
             raise ValueError("a cache's tables must be a contiguous int32 tensor of B * max_pages + B + n_pages elements")
         self.meta, self.B, self.max_pages, self.n_pages, self.page_size = meta, B, max_pages, n_pages, page_size
-        # what the integer calls work in: made along with the tables, so that whatever orders a stream behind them covers it
-        self.scratch = torch.empty((_lib or load_library()).saki_cache_scratch_bytes(B, max_pages, n_pages), dtype=torch.uint8, device=meta.device)
 
     @classmethod
     def empty(cls, B, max_pages, n_pages, page_size, device):
@@ -486,15 +484,15 @@ class PageCache:
 
     @property
     def page_table(self):
-        return self.meta[:self.B * self.max_pages].view(self.B, self.max_pages)
+        return self.meta.as_strided((self.B, self.max_pages), (self.max_pages, 1))
 
     @property
     def length(self):
-        return self.meta[self.B * self.max_pages:self.B * (self.max_pages + 1)]
+        return self.meta.as_strided((self.B,), (1,), self.meta.storage_offset() + self.B * self.max_pages)
 
     @property
     def ref_count(self):
-        return self.meta[self.B * (self.max_pages + 1):]
+        return self.meta.as_strided((self.n_pages,), (1,), self.meta.storage_offset() + self.B * (self.max_pages + 1))
 
     def clone(self):
         """Another cache with the same tables, on the same pools."""
@@ -508,7 +506,7 @@ def cache_reserve(cache, n_new, stream=None):
     """saki_cache_reserve: n_new (an int, or an int32 tensor [B]) more positions for every sequence of a PageCache.  Returns
     (copy_src, copy_dst, row_status), int32 [B]: pass the lists to copy_pages before anything is written (where the cache was forked),
     the status to cache_write."""
-    return (_fast or _tensors()).cache_reserve(*cache._args(), cache.scratch, n_new, _handle(stream))
+    return (_fast or _tensors()).cache_reserve(*cache._args(), n_new, _handle(stream))
 
 
 def cache_write(cache, k, v, k_pages, v_pages, row_status=None, n_new=None, stream=None):
@@ -526,13 +524,13 @@ def cache_truncate(cache, keep, of=None, keep_add=0, stream=None):
 def cache_fork(cache, parent, group=None, stream=None):
     """saki_cache_fork: every sequence takes the pages of its parent (int32, B elements), counted within groups of `group`
     sequences (None: all of them).  Returns row_status."""
-    return (_fast or _tensors()).cache_fork(*cache._args(), cache.scratch, parent, max(1, cache.B) if group is None else group, _handle(stream))
+    return (_fast or _tensors()).cache_fork(*cache._args(), parent, max(1, cache.B) if group is None else group, _handle(stream))
 
 
 def cache_compact(cache, stream=None):
     """saki_cache_compact: the used pages move to the lowest ids.  Returns (copy_src, copy_dst, n_moves): pass the lists to
     copy_pages before the cache is used again."""
-    return (_fast or _tensors()).cache_compact(*cache._args(), cache.scratch, _handle(stream))[:3]
+    return (_fast or _tensors()).cache_compact(*cache._args(), _handle(stream))[:3]
 
 
 def copy_pages(pools, copy_src, copy_dst, stream=None):

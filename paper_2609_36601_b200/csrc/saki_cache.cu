@@ -63,7 +63,7 @@ struct ClusterShared {
   long long scan[CWARPS];
   int warp_count[2][CWARPS];
   int count[2];            // of the block, read by the others
-  long long need;          // pages that are dealt out (first block)
+  int need;                // pages that are dealt out (first block)
 };
 
 // The pages are split over the cluster's warps in runs of whole 32s, in order.
@@ -74,10 +74,25 @@ __device__ __forceinline__ Run run_of(int n_pages, int rank) {
   return {(int)min(from, (int64_t)n_pages), (int)min(from + per, (int64_t)n_pages)};
 }
 // pages of a run that `is` says yes to, counted into sh.warp_count[k] and, for the block, sh.count[k] (ends with a barrier)
+// Eight loads are on their way at a time: a run of a few hundred pages costs one wait, not one for every 32.
+constexpr int AHEAD = 8;
+template <typename F, typename G> __device__ __forceinline__ void each_32(Run r, F&& is, G&& take) {      // take(i, is(i), mask of the warp's)
+  const int lane = threadIdx.x & 31;
+  for (int i0 = r.from; i0 < r.to; i0 += 32 * AHEAD) {
+    bool yes[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = i0 + 32 * k + lane;
+      yes[k] = i < r.to && is(i);
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) take(i0 + 32 * k + lane, yes[k], __ballot_sync(0xffffffffu, yes[k]));
+  }
+}
 template <typename F> __device__ __forceinline__ void count_run(ClusterShared& sh, int k, Run r, F&& is) {
   const int lane = threadIdx.x & 31;
   int n = 0;
-  for (int i = r.from; i < r.to; i += 32) n += __popc(__ballot_sync(0xffffffffu, i + lane < r.to && is(i + lane)));
+  each_32(r, is, [&](int, bool, unsigned m) { n += __popc(m); });
   if (lane == 0) sh.warp_count[k][threadIdx.x >> 5] = n;
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -101,12 +116,10 @@ __device__ __forceinline__ int rank_of_run(cg::cluster_group& cl, ClusterShared&
 }
 template <typename F, typename G> __device__ __forceinline__ void each_ranked(Run r, int rank, F&& is, G&& take) {
   const int lane = threadIdx.x & 31;
-  for (int i = r.from; i < r.to; i += 32) {
-    const bool yes = i + lane < r.to && is(i + lane);
-    const unsigned m = __ballot_sync(0xffffffffu, yes);
-    if (yes) take(i + lane, rank + __popc(m & ((1u << lane) - 1u)));
+  each_32(r, is, [&](int i, bool yes, unsigned m) {
+    if (yes) take(i, rank + __popc(m & ((1u << lane) - 1u)));
     rank += __popc(m);
-  }
+  });
 }
 
 // scratch of a reservation: free pages by rank; per shared last page the first sequence that goes on in it, and how many do; per
@@ -130,12 +143,21 @@ __global__ void __launch_bounds__(CT) reserve_kernel(const saki_cache c, const i
   const ReserveScratch w = reserve_scratch(c);
   const Run run = run_of(c.n_pages, rank);
   auto free_page = [&](int id) { return c.ref_count[id] == 0; };
-  count_run(sh, 0, run, free_page);
-  if (rank == 0)
+  // (the first block's plan of the first CT sequences stays in registers)
+  Plan own = {};
+  bool own_shared = false, shared = false;                // goes on in a page with other holders; any sequence does
+  if (rank == 0) {
+    if (tid == 0) sh.need = 0;
     for (int64_t b = tid; b < c.B; b += CT) {
       const Plan p = plan(c, n_new, n_all, b);
-      if (p.last >= 0) { w.first[p.last] = INT_MAX; w.going[p.last] = 0; }
+      const bool parted = p.last >= 0 && c.ref_count[p.last] > 1;
+      if (parted) { w.first[p.last] = INT_MAX; w.going[p.last] = 0; }
+      if (b == tid) { own = p; own_shared = parted; }
+      shared = shared || parted;
     }
+    shared = __syncthreads_or(shared);
+  }
+  count_run(sh, 0, run, free_page);
   cl.sync();
   int n_free = 0;
   const int my_rank = rank_of_run(cl, sh, 0, &n_free);
@@ -143,41 +165,47 @@ __global__ void __launch_bounds__(CT) reserve_kernel(const saki_cache c, const i
     long long carry = 0, total = 0;
     for (int64_t b0 = 0; b0 < c.B; b0 += CT) {
       const int64_t b = b0 + tid;
-      Plan p = {};
-      bool parted = false;
-      if (b < c.B) {
-        p = plan(c, n_new, n_all, b);
-        parted = p.last >= 0 && c.ref_count[p.last] > 1;
+      Plan p = own;
+      bool parted = own_shared;
+      if (b0 > 0) {
+        p = b < c.B ? plan(c, n_new, n_all, b) : Plan{};
+        parted = b < c.B && p.last >= 0 && c.ref_count[p.last] > 1;
       }
       const long long need = b < c.B && !p.status ? p.want - p.have + (parted ? 1 : 0) : 0;
       const long long upto = carry + block_scan(need, sh.scan, total);
       carry += total;
-      if (b < c.B) {
-        const bool ok = !p.status && upto <= n_free;
-        w.seq[b] = ok ? (parted ? 3u : 1u) : 0u;
+      const bool ok = b < c.B && !p.status && upto <= n_free;
+      if (shared) {
+        if (b < c.B) w.seq[b] = ok ? (parted ? 3u : 1u) : 0u;
         if (ok && parted) { atomicMin(w.first + p.last, (int)b); atomicAdd(w.going + p.last, 1); }
+      } else {                     // no page is shared: that is all
+        if (b < c.B) w.seq[b] = ok ? (uint32_t)((upto - need) * 2) : NOT_SERVED;
+        const int most = __reduce_max_sync(0xffffffffu, ok ? (int)upto : 0);
+        if ((tid & 31) == 0) atomicMax(&sh.need, most);
       }
     }
-    __syncthreads();
-    carry = 0;
-    for (int64_t b0 = 0; b0 < c.B; b0 += CT) {
-      const int64_t b = b0 + tid;
-      long long need = 0;
-      uint32_t how = 0;
-      bool copies = false;
-      if (b < c.B && (how = w.seq[b])) {
-        const Plan p = plan(c, n_new, n_all, b);
-        copies = how == 3u && !(w.going[p.last] == c.ref_count[p.last] && w.first[p.last] == (int)b);
-        need = p.want - p.have + (copies ? 1 : 0);
+    if (shared) {
+      __syncthreads();
+      carry = 0;
+      for (int64_t b0 = 0; b0 < c.B; b0 += CT) {
+        const int64_t b = b0 + tid;
+        long long need = 0;
+        uint32_t how = 0;
+        bool copies = false;
+        if (b < c.B && (how = w.seq[b])) {
+          const Plan p = b0 == 0 ? own : plan(c, n_new, n_all, b);
+          copies = how == 3u && !(w.going[p.last] == c.ref_count[p.last] && w.first[p.last] == (int)b);
+          need = p.want - p.have + (copies ? 1 : 0);
+        }
+        const long long upto = carry + block_scan(need, sh.scan, total);
+        carry += total;
+        if (b < c.B) w.seq[b] = how ? (uint32_t)((upto - need) * 2 + (copies ? 1 : 0)) : NOT_SERVED;
       }
-      const long long upto = carry + block_scan(need, sh.scan, total);
-      carry += total;
-      if (b < c.B) w.seq[b] = how ? (uint32_t)((upto - need) * 2 + (copies ? 1 : 0)) : NOT_SERVED;
+      if (tid == 0) sh.need = (int)carry;
     }
-    if (tid == 0) sh.need = carry;
   }
   cl.sync();
-  const long long dealt = cl.map_shared_rank(&sh, 0)->need;
+  const int dealt = cl.map_shared_rank(&sh, 0)->need;
   if (my_rank < dealt)
     each_ranked(run, my_rank, free_page, [&](int id, int r) {
       if (r < dealt) { w.order[r] = id; c.ref_count[id] = 1; }
@@ -385,23 +413,30 @@ template <typename V, int E> __global__ void __launch_bounds__(256) write_kernel
   launch_dependents();
   const int64_t b = blockIdx.x / w.Q;
   const int j = (int)(blockIdx.x - b * w.Q);
-  if (w.row_status && w.row_status[b]) return;
-  const int n = w.n_new ? w.n_new[b] : w.Q;
-  const int64_t L = c.length[b], x = L - n + j;
-  if (n < 0 || n > w.Q || j >= n || x < 0 || !length_ok(c, L)) return;
-  const int id = c.page_table[b * c.ld_table + x / c.page_size], slot = (int)(x % c.page_size);
-  if (!in_pool(id, c.n_pages)) return;
   constexpr int SIZE = (int)sizeof(V) / E;
   const int vecs = w.D / E, half = w.H * vecs;
   const char* const k = (const char*)w.k + (b * w.k_seq + j * w.k_pos) * SIZE;
   const char* const v = (const char*)w.v + (b * w.v_seq + j * w.v_pos) * SIZE;
+  auto from = [&](int i) {
+    const bool second = i >= half;
+    const int r = second ? i - half : i, h = r / vecs, d = (r - h * vecs) * E;
+    return *(const V*)((second ? v + (h * w.v_head + d) * SIZE : k + (h * w.k_head + d) * SIZE));
+  };
+  // (a thread's first piece is on its way while the position is looked up, three reads one behind the other)
+  const V early = from(min((int)threadIdx.x, 2 * half - 1));
+  const uint32_t flag = w.row_status ? w.row_status[b] : 0u;
+  const int n = w.n_new ? w.n_new[b] : w.Q;
+  const int64_t L = c.length[b], x = L - n + j;
+  if (flag || n < 0 || n > w.Q || j >= n || x < 0 || !length_ok(c, L)) return;
+  const int64_t page = x <= INT_MAX ? (unsigned)x / (unsigned)c.page_size : x / c.page_size;
+  const int id = c.page_table[b * c.ld_table + page], slot = (int)(x - page * c.page_size);
+  if (!in_pool(id, c.n_pages)) return;
   char* const kp = (char*)w.k_pages + (id * w.kp_page + slot * w.kp_pos) * SIZE;
   char* const vp = (char*)w.v_pages + (id * w.vp_page + slot * w.vp_pos) * SIZE;
   for (int i = threadIdx.x; i < 2 * half; i += blockDim.x) {
     const bool second = i >= half;
     const int r = second ? i - half : i, h = r / vecs, d = (r - h * vecs) * E;
-    const V e = *(const V*)((second ? v + (h * w.v_head + d) * SIZE : k + (h * w.k_head + d) * SIZE));
-    *(V*)((second ? vp + (h * w.vp_head + d) * SIZE : kp + (h * w.kp_head + d) * SIZE)) = e;
+    *(V*)((second ? vp + (h * w.vp_head + d) * SIZE : kp + (h * w.kp_head + d) * SIZE)) = i == (int)threadIdx.x ? early : from(i);
   }
 }
 

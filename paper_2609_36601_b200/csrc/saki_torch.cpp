@@ -488,28 +488,23 @@ Cache cache_of(PyObject* const* a) {
   c.ref_count = c.length + c.B;
   return k;
 }
-void with_scratch(Cache& k, PyObject* o) {
+void with_scratch(Cache& k) {      // (of the current stream, like the outputs)
   k.c.scratch_bytes = lib.cache_scratch_bytes(k.c.B, k.c.max_pages, k.c.n_pages);
-  if (o == Py_None) k.scratch = empty({k.c.scratch_bytes}, at::kByte, k.dev);
-  else {
-    k.scratch = tensor(o);
-    if (k.scratch.device() != k.dev || !k.scratch.is_contiguous() || (int64_t)(k.scratch.numel() * k.scratch.element_size()) < k.c.scratch_bytes)
-      raise_value("scratch must be a contiguous tensor of " + std::to_string(k.c.scratch_bytes) + " bytes on the cache's device");
-  }
+  k.scratch = empty({k.c.scratch_bytes}, at::kByte, k.dev);
   k.c.scratch = k.scratch.data_ptr();
 }
 
-// cache_reserve(cache..., scratch, n_new, stream) -> (copy_src, copy_dst, row_status)
+// cache_reserve(cache..., n_new, stream) -> (copy_src, copy_dst, row_status)
 PyObject* py_cache_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    n_args(n, CACHE_ARGS + 3);
+    n_args(n, CACHE_ARGS + 2);
     Cache k = cache_of(a);
-    const OnStream on(k.dev, a[7]);
-    with_scratch(k, a[5]);
+    const OnStream on(k.dev, a[6]);
+    with_scratch(k);
     const int32_t* each = nullptr;
     int64_t all = 0;
-    if (THPVariable_Check(a[6])) each = (const int32_t*)packed(a[6], at::kInt, k.c.B, k.dev, "n_new").data_ptr();
-    else if ((all = integer(a[6])) > INT32_MAX || all < INT32_MIN) raise_value("n_new out of range");
+    if (THPVariable_Check(a[5])) each = (const int32_t*)packed(a[5], at::kInt, k.c.B, k.dev, "n_new").data_ptr();
+    else if ((all = integer(a[5])) > INT32_MAX || all < INT32_MIN) raise_value("n_new out of range");
     const at::Tensor src = empty({k.c.B}, at::kInt, k.dev), dst = empty({k.c.B}, at::kInt, k.dev), st = empty({k.c.B}, at::kInt, k.dev);
     check_rc(unlocked([&] { return lib.cache_reserve(&k.c, each, (int32_t)all, (int32_t*)src.data_ptr(), (int32_t*)dst.data_ptr(), (uint32_t*)st.data_ptr(), on.handle); }));
     Owned x(THPVariable_Wrap(src)), y(THPVariable_Wrap(dst)), z(THPVariable_Wrap(st));
@@ -532,28 +527,28 @@ PyObject* py_cache_truncate(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// cache_fork(cache..., scratch, parent, group, stream) -> row_status
+// cache_fork(cache..., parent, group, stream) -> row_status
 PyObject* py_cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    n_args(n, CACHE_ARGS + 4);
+    n_args(n, CACHE_ARGS + 3);
     Cache k = cache_of(a);
-    const OnStream on(k.dev, a[8]);
-    with_scratch(k, a[5]);
-    const int32_t* const parent = (const int32_t*)packed(a[6], at::kInt, k.c.B, k.dev, "parent").data_ptr();
-    const int64_t group = integer(a[7]);
+    const OnStream on(k.dev, a[7]);
+    with_scratch(k);
+    const int32_t* const parent = (const int32_t*)packed(a[5], at::kInt, k.c.B, k.dev, "parent").data_ptr();
+    const int64_t group = integer(a[6]);
     const at::Tensor st = empty({k.c.B}, at::kInt, k.dev);
     check_rc(unlocked([&] { return lib.cache_fork(&k.c, parent, group, (uint32_t*)st.data_ptr(), on.handle); }));
     return THPVariable_Wrap(st);
   });
 }
 
-// cache_compact(cache..., scratch, stream) -> (copy_src, copy_dst, n_moves, row_status)
+// cache_compact(cache..., stream) -> (copy_src, copy_dst, n_moves, row_status)
 PyObject* py_cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    n_args(n, CACHE_ARGS + 2);
+    n_args(n, CACHE_ARGS + 1);
     Cache k = cache_of(a);
-    const OnStream on(k.dev, a[6]);
-    with_scratch(k, a[5]);
+    const OnStream on(k.dev, a[5]);
+    with_scratch(k);
     const int64_t half = k.c.n_pages / 2;
     const at::Tensor src = empty({half}, at::kInt, k.dev), dst = empty({half}, at::kInt, k.dev), moves = empty({}, at::kInt, k.dev), st = empty({k.c.B}, at::kInt, k.dev);
     check_rc(unlocked([&] { return lib.cache_compact(&k.c, (int32_t*)src.data_ptr(), (int32_t*)dst.data_ptr(), (int32_t*)moves.data_ptr(), (uint32_t*)st.data_ptr(), on.handle); }));
