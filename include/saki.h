@@ -442,7 +442,8 @@ SAKI_API int saki_cache_write(const saki_cache* cache, const saki_cache_kv* kv, 
  * see have no influence, whatever they hold; non-finite ones that it sees make its output non-finite.  bf16: products on the tensor cores,
  * sums, maxima and exponentials in float32, the weights in two bf16 terms (16 bits); f32: float32 throughout.  A sequence with a length outside
  * [0, max_pages * page_size], or n outside [0, Q], is flagged BAD_LENGTH, one with an id outside the pool among the pages that its
- * queries see BAD_PAGE, one for which a wait ran out (saki_set_wait_limit) TIMEOUT: out 0, lse -inf.
+ * queries see BAD_PAGE, one for which a wait ran out (saki_set_wait_limit) TIMEOUT: out 0, lse -inf (TIMEOUT:
+ * in the heads that were late).
  * Requirements: Q 1..32, max_pages * page_size below 2^31 - 256, Hq a multiple of H, Hq / H <= 64, D <= 256 and a multiple of 8 (f32: 4); 16-byte aligned pools, and strides
  * of the pools that are multiples of 16 bytes (SAKI_ERR_UNSUPPORTED otherwise).  scratch: saki_paged_attention_scratch_bytes(in) bytes,
  * 256-byte aligned, owned by one call at a time. */
@@ -537,7 +538,7 @@ SAKI_API int saki_solve_evaluations(void* cuda_stream, uint64_t* n_passes);
 
 /* Failure behaviour of the row-per-SM, general and attention kernels (no counterpart in the paper).  A thread block of the first waits for a
  * row's bulk copy from global memory for a bounded number of SM cycles (about two seconds' worth by
- * default).  If the wait runs out the block stops fetching, flags that row (in block verification every position it still
+ * default); the attention kernels wait as long for a tile's copies and products, and what they then have not finished is TIMEOUT.  If the wait runs out the block stops fetching, flags that row (in block verification every position it still
  * takes) SAKI_ROW_TIMEOUT with zero outputs, waits (full limit) for the copy it has in flight, and returns: the
  * kernel always terminates, saki_check() counts the flagged rows and later calls are unaffected.  A block of either kernel, in
  * calls of more rows than are resident at once, waits as long for the answer to its request for a further row; if that wait

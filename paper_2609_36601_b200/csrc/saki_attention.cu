@@ -16,6 +16,7 @@
 // hi.hi + hi.lo + lo.hi: what is dropped is 2^-22 of a product and less.
 #include "saki_attention.cuh"
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <mutex>
 
@@ -88,7 +89,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
   char* const rest = smem + S::WORKERS * (ST * S::STAGE + S::Q_BYTES);
   uint64_t* const full = (uint64_t*)rest + worker * ST;
   LineShared<THREADS>& line = *(LineShared<THREADS>*)(rest + S::WORKERS * ST * 8);
-  int* const late = (int*)(rest + S::WORKERS * ST * 8 + sizeof(LineShared<THREADS>)) + worker;
+  int* const told = (int*)(rest + S::WORKERS * ST * 8 + sizeof(LineShared<THREADS>)) + worker;
   const uint32_t ring_a = smem_addr(ring), q_a = smem_addr(q_s);
   auto together = [&] {            // the worker's warps
     if constexpr (NW == 1) __syncwarp();
@@ -103,7 +104,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
     }
   }
   if (part_of == 0 && lane < ST) mbar_init(full + lane, TMA ? 1 : 32);
-  if (part_of == 0 && lane == 0) *late = 0;
+  if (part_of == 0 && lane == 0) *told = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   wait_for_predecessor();
   launch_dependents();
@@ -112,7 +113,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
   pieces<T, THREADS, S::WORKERS>(p, line, chunk, total);        // (ends with a barrier: the mbarriers are there for all)
   const long long u0 = number * chunk;
   if (u0 >= total) {
-    if (part_of == 0 && lane == 0) p.desc[number] = make_int4(0, 0, 0, 0);
+    if (part_of == 0 && lane == 0) { p.desc[number] = make_int4(0, 0, 0, 0); p.late[number] = make_int2(0, -1); }
     return;
   }
   const int n_tiles = (int)min(chunk, total - u0);
@@ -180,6 +181,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
   Sight sight[2];
   float bad = 0.f;                 // -1: a page outside the pool, -2: a wait ran out (from then on nothing is loaded or waited for)
   bool fresh = true, gave_up = false;
+  int2 late = make_int2(INT_MAX, -1);
   int stage = 0;
   uint32_t parity = 0;
   // what a lane reads: rows of eight by lane & 7, pieces and groups of eight rows by lane >> 3
@@ -240,7 +242,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
     }
     if (gave_up) {
       bad = -2.f;
-      if constexpr (NW > 1) *(volatile int*)late = 1;
+      if constexpr (NW > 1) *(volatile int*)told = 1;
     } else if (bad_tiles >> (i & 31) & 1u) bad = bad == 0.f ? -1.f : bad;
     const uint32_t at_s = ring_a + stage * S::STAGE;
     char* const v_p = ring + stage * S::STAGE + S::HALF;
@@ -348,7 +350,13 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
         const uint4 x = *(const uint4*)(v_p + piece_at<T>(e / PIECES, e % PIECES));
         strange = strange || odd(x.x) || odd(x.y) || odd(x.z) || odd(x.w);
       }
-      if (__any_sync(0xffffffffu, strange)) {        // it goes to the rows that see it by itself, and 0 takes its place
+      if constexpr (NW > 1) {      // one answer for the worker's warps, whatever one that has given up reads: they meet in there
+        uint32_t any;
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                     : "=r"(any) : "r"(strange ? 1u : 0u), "r"(worker + 1), "r"(32 * NW) : "memory");
+        strange = any;
+      } else strange = __any_sync(0xffffffffu, strange);
+      if (strange) {               // it goes to the rows that see it by itself, and 0 takes its place
 #pragma unroll 1
         for (int t = 0; t < T; ++t)
 #pragma unroll
@@ -428,7 +436,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
     if (TMA && wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stage is written by TMA next
     together();                    // the stage may be loaded again
     if constexpr (NW > 1) {        // the warps of a worker give up on the same segment
-      if (*(volatile int*)late) { gave_up = true; bad = -2.f; }
+      if (*(volatile int*)told) { gave_up = true; bad = -2.f; }
     }
     if (now.t + 1 == now.s.nt || i + 1 == n_tiles) {        // the segment ends, or the piece does
       const bool head = i < now.t, tail = now.t + 1 < now.s.nt;      // it goes on from the piece before, or behind
@@ -461,7 +469,8 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
         }
       }
       if (part_of == 0 && lane == 0) {
-        if (!head && !tail && now.hr == 0) put_status(p, now.b, st);
+        if (!head && now.hr == 0) put_status(p, now.b, tail ? now.s.status : st);
+        if (bad == -2.f) { late.x = min(late.x, now.b); late.y = now.b; }
         if (i + 1 == n_tiles) {    // a segment that starts here and goes on: how many pieces behind have a share of it
           const long long end = u0 + i - now.t + now.s.nt;
           p.desc[number] = tail && !head ? make_int4(now.b, now.hr, (int)((end - 1) / chunk) - number, (int)now.s.status) : make_int4(0, 0, 0, 0);
@@ -472,6 +481,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
     now.next(p);
     if (++stage == ST) { stage = 0; parity ^= 1u; }
   }
+  if (part_of == 0 && lane == 0) p.late[number] = late;
   if (gave_up)                     // copies that are still on their way land before the block's shared memory goes to another
     for (int i = max(0, loaded - ST); i < loaded; ++i) mbar_wait_bounded(full + i % ST, (uint32_t)(i / ST) & 1u);
 }
@@ -487,6 +497,11 @@ template <typename E, int ROWS, int DP> __global__ void __launch_bounds__(256) a
   wait_for_predecessor();
   launch_dependents();
   const int4 d = p.desc[blockIdx.x];
+  if (blockIdx.y == 0) {
+    const int2 late = p.late[blockIdx.x];
+    if (late.x <= late.y)
+      for (int b = late.x + (int)threadIdx.x; b <= late.y; b += 256) add_status(p, b, SAKI_ROW_TIMEOUT);
+  }
   if (d.z == 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = d.y / p.RB, row0 = (d.y - h * p.RB) * ROWS;
   const int w0 = warp & ~(share - 1), mine = warp - w0, at_once = 8 / share;
@@ -531,7 +546,7 @@ template <typename E, int ROWS, int DP> __global__ void __launch_bounds__(256) a
       }
       if (mine == 0 && lane == 0) {
         put_lse(p, d.x, h, row0 + rr, top, none ? 0.f : sum);
-        if (rr == 0 && d.y == 0) put_status(p, d.x, st);
+        if (rr == 0 && d.y == 0 && bad) add_status(p, d.x, bad);
       }
     }
     __syncthreads();
@@ -635,7 +650,7 @@ int64_t attention_scratch_bytes(const saki_attn_in& in) {
   const Kernel k = pick(in);
   int64_t most = MAX_WORKERS * 2 * part_floats(k);
   if (on_umma(in)) most = std::max<int64_t>(most, MAX_WORKERS / 8 * 2 * (int64_t)umma_rows(in) * (k.dp + 2));
-  return MAX_WORKERS * 16 + most * 4;
+  return MAX_WORKERS * 24 + most * 4;
 }
 
 cudaError_t launch_attention(const saki_attn_in& in, const saki_attn_out& out, void* scratch, unsigned long long* flagged, long long wait_limit,
@@ -652,7 +667,8 @@ cudaError_t launch_attention(const saki_attn_in& in, const saki_attn_out& out, v
   const int size = in.dtype == SAKI_BF16 ? 2 : 4;
   p.q_vec = ((uintptr_t)in.q | (uintptr_t)(in.q_seq * size) | (uintptr_t)(in.q_pos * size) | (uintptr_t)(in.q_head * size)) % 16 == 0;
   p.desc = (int4*)scratch;
-  p.part = (float*)((char*)scratch + MAX_WORKERS * 16);
+  p.late = (int2*)((char*)scratch + MAX_WORKERS * 16);
+  p.part = (float*)((char*)scratch + MAX_WORKERS * 24);
   Kernel k = pick(in);
   bool umma = on_umma(in);
   // Boxes: as many positions of a page as a tile takes.  A page that is no multiple of eight, or strides that the map does not take

@@ -28,6 +28,7 @@ struct AttnParams {
   float c;                  // |scale| * log2(e), above 0
   int4* desc;               // [workers] the segment that starts in a piece and goes on: (b, head and row block, pieces behind, status)
   float* part;              // [workers][2] partial results: of the segment that goes on from the piece before, of the one that goes on behind
+  int2* late;               // [workers] first and last sequence of those with a segment for which a wait of the worker ran out; (0, -1): none
   unsigned long long* flagged;
   long long wait_limit;
 };
@@ -138,9 +139,14 @@ __device__ __forceinline__ void put_lse(const AttnParams& p, int64_t b, int h, i
   const int j = r / p.G;
   p.out.lse[(b * p.in.Q + j) * p.in.Hq + h * p.G + r - j * p.G] = lse_of(m, l);
 }
+// (by the worker that has the sequence's first tile; what comes to light elsewhere is added by the joining kernel)
 __device__ __forceinline__ void put_status(const AttnParams& p, int64_t b, uint32_t st) {
   if (p.out.row_status) p.out.row_status[b] = st;
   if (st) atomicAdd(p.flagged, 1ull);
+}
+
+__device__ __forceinline__ void add_status(const AttnParams& p, int64_t b, uint32_t st) {
+  if (!p.out.row_status || atomicOr(p.out.row_status + b, st) == 0) atomicAdd(p.flagged, 1ull);
 }
 
 // Segments (sequence, key head, row block) that several workers had a part of: ROWS rows of DP values, then ROWS pairs (m, l); l = -1: a bad

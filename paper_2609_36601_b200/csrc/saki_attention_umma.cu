@@ -127,9 +127,10 @@ template <int C> __device__ __forceinline__ void u_st(uint32_t at, const float* 
 __device__ __forceinline__ void u_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // the 128 threads of group g of warps
 __device__ __forceinline__ void u_sync(int g) { asm volatile("bar.sync %0, 128;" ::"r"(g + 1) : "memory"); }
-__device__ __forceinline__ bool u_any(int g, bool yes) {
+__device__ __forceinline__ bool u_any(int g, bool yes, int threads = 128) {
   uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(yes ? 1u : 0u), "r"(g + 1) : "memory");
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"(yes ? 1u : 0u), "r"(g + 1), "r"(threads) : "memory");
   return r != 0;
 }
 __device__ __forceinline__ float u_warp_max(float x) {
@@ -225,7 +226,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
   const int n_tiles = u0 < total ? (int)min(chunk, total - u0) : 0;
 
   if (n_tiles == 0) {
-    if (tid == 0) p.desc[number] = make_int4(0, 0, 0, 0);
+    if (tid == 0) { p.desc[number] = make_int4(0, 0, 0, 0); p.late[number] = make_int2(0, -1); }
   } else if (warp == 0) {
     // ---- loads, in the order in which the products take them up; load j goes to slot j % SLOTS
     Cursor<UT> look;
@@ -284,8 +285,8 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       }
       if (i > 0 && ok) load(&v_map, before);
     }
-    if (!ok)                                  // copies that are still on their way land before the block leaves
-      for (int done = max(0, j - SLOTS); done < j; ++done) mbar_wait_bounded(r.full + done % SLOTS, (uint32_t)(done / SLOTS) & 1u);
+    // all copies land before the block leaves, also where the others have given up and do not wait for them
+    for (int done = max(0, j - SLOTS); done < j; ++done) mbar_wait_bounded(r.full + done % SLOTS, (uint32_t)(done / SLOTS) & 1u);
   } else if (warp == 1) {
     if (lane == 0) {
       // ---- scores: those of tile i once its keys are there and the weights of tile i - 2 have left their buffer
@@ -311,10 +312,8 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         if (first) { u_commit(r.q_empty + qb); ++seg; }
         u_next(p, at);
       }
-      if (*(volatile int*)&r.abort) {         // nothing of it is under way when tensor memory goes
-        u_commit(r.drain);
-        mbar_wait_bounded(r.drain, 0);
-      }
+      u_commit(r.drain);                      // nothing of it is under way when tensor memory goes (the others may have given up)
+      mbar_wait_bounded(r.drain, 0);
     }
   } else if (warp == 2) {
     if (lane == 0) {
@@ -341,10 +340,8 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         if (first || i + 1 == n_tiles) { u_commit(r.seg_pv + (seg & 1)); ++seg; }
         u_next(p, at);
       }
-      if (*(volatile int*)&r.abort) {
-        u_commit(r.drain + 1);
-        mbar_wait_bounded(r.drain + 1, 0);
-      }
+      u_commit(r.drain + 1);
+      mbar_wait_bounded(r.drain + 1, 0);
     }
   } else if (warp == 3) {
     // ---- queries of the piece's segments
@@ -530,7 +527,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
               }
             const float2 z2 = __bfloat1622float2(__hadd2(__hadd2(z[0], z[1]), __hadd2(z[2], z[3])));
             const bool strange = !(z2.x + z2.y == 0.f);
-            if (u_any(g, strange)) { // it goes to the rows that see it by itself, and 0 takes its place
+            if (u_any(6, strange, 128 * GROUPS)) { // (one answer for all groups, whatever one that has given up reads) it goes to the rows that see it by itself, and 0 takes its place
               if (!fresh) {
                 if (!dead && !u_wait(r.pv_done + ((i - 1) & 1), ((i - 1) >> 1) & 1, r, limit)) dead = true;
               } else if (!dead && !u_wait(r.seg_free + (seg & 1), ((seg >> 1) & 1) ^ 1u, r, limit)) dead = true;
@@ -561,7 +558,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
                 u_st<CW>(o_at, y);
               }
               u_st_wait();
-              asm volatile("bar.sync 7, %0;" ::"n"(128 * GROUPS) : "memory");      // (all groups have found it)
+              asm volatile("bar.sync 7, %0;" ::"n"(128 * GROUPS) : "memory");      // (all groups have it)
               if (partly && g == 0)
 #pragma unroll 1
                 for (int j = 0; j < PIECES; ++j) {
@@ -616,6 +613,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
     u_at(p, at, r.line.b[0], u0 - r.line.before[0]);
     bool dead = false;
     int left = n_tiles, row = 0, j = 0;
+    int2 late = make_int2(INT_MAX, -1);
 #pragma unroll 1
     for (int seg = 0; left > 0; ++seg) {
       const int sb = seg & 1, rest = at.s.nt - at.t;
@@ -632,7 +630,8 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       if (!dead && !u_wait(r.seg_sums + sb, (seg >> 1) & 1, r, limit)) dead = true;
       if (!dead && !u_wait(r.seg_pv + sb, (seg >> 1) & 1, r, limit)) dead = true;
       u_after();
-      const float b = u_any(GROUPS, dead) ? -2.f : r.end_bad[sb] ? -1.f : 0.f;
+      // (a group that gave up goes on without waiting, so the rest may have come from nothing: it said so before)
+      const float b = u_any(GROUPS, dead || *(volatile int*)&r.abort) ? -2.f : r.end_bad[sb] ? -1.f : 0.f;
       const uint32_t st = at.s.status | status_of(b);
       const bool partial = head || tail;
       float* const part = p.part + (number * 2 + (head ? 0 : 1)) * (int64_t)PART<N, DP>;
@@ -666,7 +665,8 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       u_before();
       u_arrive(r.seg_free + sb);
       if (t == 0) {
-        if (!partial && at.hr == 0) put_status(p, at.b, st);
+        if (!head && at.hr == 0) put_status(p, at.b, tail ? at.s.status : st);
+        if (b == -2.f) { late.x = min(late.x, at.b); late.y = at.b; }
         if (left <= rest)          // a segment that starts here and goes on: how many pieces behind have a share of it
           p.desc[number] = tail && !head ? make_int4(at.b, at.hr, (int)((u0 + n_tiles - left - at.t + at.s.nt - 1) / chunk) - number, (int)at.s.status) : make_int4(0, 0, 0, 0);
       }
@@ -675,6 +675,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       u_next(p, at);
       u_sync(GROUPS);              // (row_at and inverse are written again)
     }
+    if (t == 0) p.late[number] = late;
   }
   u_before();
   __syncthreads();
