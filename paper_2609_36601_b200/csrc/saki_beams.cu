@@ -8,6 +8,8 @@
 // by one instead.  A second, small kernel joins the slices of a beam (log-sum-exp in float64) and the beams of a group (float64 keys).
 #include "saki_device.cuh"
 #include <algorithm>
+#include <cmath>
+#include <limits>
 
 namespace saki {
 
@@ -77,7 +79,7 @@ struct BeamShared {
 };
 
 // NV: 16-byte vectors that a thread holds
-template <typename T, int NV> __global__ void __launch_bounds__(BT, 3) beam_rows_kernel(const BeamParams p) {
+template <typename T, int NV> __global__ void __launch_bounds__(BT, 4) beam_rows_kernel(const BeamParams p) {
   constexpr int E = Vec<T>::E;
   __shared__ BeamShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = p.in.V, n = p.in.n;
@@ -94,16 +96,24 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 3) beam_rows
   const int v0 = slice * p.slice;
   if (tid == 0) sh.count = 0;
   Vec<T> x[NV];
+  if (vec && v0 + NV * BT * E <= V) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = v0 + (k * BT + tid) * E;
-    if (vec && v + E <= V) {
-      const uint4 a = __ldg((const uint4*)(s + v));
+    for (int k = 0; k < NV; ++k) {
+      const uint4 a = __ldg((const uint4*)(s + v0) + k * BT + tid);
       x[k].r[0] = a.x; x[k].r[1] = a.y; x[k].r[2] = a.z; x[k].r[3] = a.w;
-    } else {
+    }
+  } else {
 #pragma unroll
-      for (int i = 0; i < E / 2; ++i)
-        x[k].set(i, v + 2 * i < V ? ld_as_float(s, v + 2 * i) : -CUDART_INF_F, v + 2 * i + 1 < V ? ld_as_float(s, v + 2 * i + 1) : -CUDART_INF_F);
+    for (int k = 0; k < NV; ++k) {
+      const int v = v0 + (k * BT + tid) * E;
+      if (vec && v + E <= V) {
+        const uint4 a = __ldg((const uint4*)(s + v));
+        x[k].r[0] = a.x; x[k].r[1] = a.y; x[k].r[2] = a.z; x[k].r[3] = a.w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i)
+          x[k].set(i, v + 2 * i < V ? ld_as_float(s, v + 2 * i) : -CUDART_INF_F, v + 2 * i + 1 < V ? ld_as_float(s, v + 2 * i + 1) : -CUDART_INF_F);
+      }
     }
   }
   float top[NV], mine = -CUDART_INF_F;
@@ -143,18 +153,32 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 3) beam_rows
     for (int o = 1; o < 4; o <<= 1) { more += __shfl_xor_sync(0xffffffffu, more, o); least += __shfl_xor_sync(0xffffffffu, least, o); }
     if (more < n && n <= least) sh.bar = g;      // (the same value, whoever writes it)
   }
-  // x - m is exact where it matters, and the constant has two terms: an error of the argument that is the same for all elements would not average out
+  // 2^(c x - r), r = c m as rounded to float32: what the rounding did is put right once, below.  The constant has two terms, as an error of the argument that is
+  // the same for all elements would not average out; both are above 0, so that -inf stays -inf.
   float2 sum = make_float2(0.f, 0.f);
-  const float2 hi = splat(p.c_hi), lo = splat(p.c_lo), nm = splat(-m);
+  const float2 hi = splat(p.c_hi), lo = splat(p.c_lo);
+  const float r = fmaf(m, p.c_hi, m * p.c_lo);
+  const bool far = !(fabsf(r) < 4096.f);      // the rounding is no small thing, or c x overflows: x - m first (where -inf must not meet the second term)
+  if (!far) {
+    const float2 nr = splat(-r);
 #pragma unroll
-  for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k)
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
-      const float2 d = fadd2(x[k].pair(i), nm);
-      // -inf: 2^-inf = 0 needs an argument without the second term (-inf * lo may be NaN)
-      const float2 a = ffma2(d, hi, fmul2(make_float2(fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f)), lo));
-      sum = fadd2(sum, ex2f2(a));
+      for (int i = 0; i < E / 2; ++i) {
+        const float2 y = x[k].pair(i);
+        sum = fadd2(sum, ex2f2(ffma2(y, lo, ffma2(y, hi, nr))));
+      }
+  } else {
+#pragma unroll 1
+    for (int k = 0; k < NV * E / 2; ++k) {
+      float2 y = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < NV * E / 2; ++i)
+        if (i == k) y = x[i / (E / 2)].pair(i % (E / 2));
+      const float2 d = fadd2(y, splat(-m));
+      sum = fadd2(sum, ex2f2(ffma2(d, hi, fmul2(make_float2(fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f)), lo))));
     }
+  }
   double total = warp_sum((double)sum.x + (double)sum.y);
   if (lane == 0) sh.warp_sum[warp] = total;
   __syncthreads();
@@ -162,6 +186,10 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 3) beam_rows
   if (tid == 0) {
     total = 0;
     for (int w = 0; w < BWARPS; ++w) total += sh.warp_sum[w];
+    if (!far) {                    // r - c m, of terms that are exact in float64
+      const double t = (double)r - (double)m * ((double)p.c_hi + (double)p.c_lo);
+      total *= fabs(t) < 1e-5 ? 1. + t * (0.69314718055994531 + t * 0.24022650695910071) : exp2(t);      // (two terms of the series, 6e-17 off)
+    }
     *part = make_double2(m, total);
   }
   keep_packed(x);
@@ -406,7 +434,9 @@ cudaError_t launch_beams(const saki_beam_in& in, const saki_beam_out& out, void*
   p.in = in; p.out = out; p.slices = l.slices; p.slice = l.slice; p.flagged = flagged;
   const double c = 1.4426950408889634 / (double)in.temperature;
   p.inv_tau = 1.0 / (double)in.temperature;
-  p.c_hi = (float)c; p.c_lo = (float)(c - (double)p.c_hi);
+  p.c_hi = (float)c;
+  if ((double)p.c_hi >= c) p.c_hi = std::nextafter(p.c_hi, 0.f);
+  p.c_lo = std::max((float)(c - (double)p.c_hi), std::numeric_limits<float>::denorm_min());      // above 0
   p.cand = (uint64_t*)scratch;
   p.part = (double2*)((char*)scratch + round256(rows * l.slices * in.n * 8));
   const dim3 grid((unsigned)(rows * l.slices));

@@ -167,3 +167,25 @@ def test_the_binding_refuses():
     for bad in (lambda: P.beam_select(z.half(), s, 2), lambda: P.beam_select(z, s, 2, temperature=0.0), lambda: P.beam_select(z[:, :, :1], s, 2)):
         with pytest.raises(P.SakiError):
             bad()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("tau", [1e-30, 1e-6, 0.25, 2.0, 1e6, 3e38])
+def test_temperatures_of_any_size(dtype, tau):
+    """Sums whose arguments are huge, tiny or denormal, with -inf among the logits and far from 0."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    for shift in (0.0, 1000.0, -3e30, 1e36):
+        z = (torch.randn((2, 3, 5000), generator=g, device=DEV) * (1 + abs(shift) * 2.0 ** -6) + shift).to(dtype)
+        z[:, :, ::7] = -float("inf")
+        score = torch.randn((2, 3), generator=g, device=DEV)
+        out = P.beam_select(z, score, 4, temperature=tau)
+        assert int(out["row_status"].abs().max()) == 0
+        zd, t = z.double(), float(np.float32(tau))
+        top = zd.amax(-1, keepdim=True)
+        keys = score.double()[..., None] + ((zd - top) / t - torch.log(torch.exp((zd - top) / t).sum(-1, keepdim=True)))
+        best = keys.flatten(1).topk(4).values
+        # the terms of test_gpu_beam_select: LSE, the stored score's rounding; a constant of few bits (denormal) is off by up to 2^-149 of what it multiplies
+        tol = LSE + 2.0 ** -24 * best.abs() + 2.0 ** -148 * float((zd[zd > -float("inf")]).abs().max()) * 2
+        fin = best > -3e38
+        assert ((out["score"].double() - best).abs() <= tol)[fin].all(), (tau, shift)
+    P.check()
