@@ -518,9 +518,9 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
           if (p.in.Q > 1) {        // some rows do not see all of the tile: a value that is not finite must not reach those as 0 * inf
             const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
             __nv_bfloat162 z[4] = {zero, zero, zero, zero};      // 0 x, added up: NaN once there is such a value
-            if (partly)
-#pragma unroll 4
-              for (int j = 0; j < PIECES; ++j) {
+            if (partly)            // (each group looks at a share)
+#pragma unroll
+              for (int j = g; j < PIECES; j += GROUPS) {
                 const uint4 y = *(const uint4*)(v_s + piece_of(t, j));
                 z[0] = __hfma2(bf16x2_of(y.x), zero, z[0]); z[1] = __hfma2(bf16x2_of(y.y), zero, z[1]);
                 z[2] = __hfma2(bf16x2_of(y.z), zero, z[2]); z[3] = __hfma2(bf16x2_of(y.w), zero, z[3]);
