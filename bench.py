@@ -271,6 +271,64 @@ def _lm_head(P, dev, stream, steps, rows=0):
                          "traffic": None}}
 
 
+def _rollout(P, dev, stream, peak, steps=20):
+    """What surrounds block verification in a rollout, on its shapes (512 sequences, 6 drafted positions and a bonus; 8 key heads of 128, 4 query
+    heads each, pages of 16 positions): a single token's and a drafted block's attention over the paged cache, the pages' bookkeeping
+    with the write of the new positions (one captured step), and beam selection at the headline's vocabulary."""
+    import torch
+    B, Q, H, G, D, page, n = 512, 7, 8, 4, 128, 16, 1024
+    max_pages, n_pages = n // page + 1, B * (n // page + 1)
+    g = torch.Generator(device=dev).manual_seed(77)
+    k, v = (torch.randn((n_pages, page, H, D), generator=g, device=dev).to(torch.bfloat16) for _ in range(2))
+    cache = P.PageCache.empty(B, max_pages, n_pages, page, dev)
+    P.cache_reserve(cache, n)
+    flush = torch.empty(320 << 20, dtype=torch.uint8, device=dev)
+
+    def timed(call, reps=steps):
+        for _ in range(3):
+            call()
+        total = 0.0
+        for _ in range(reps):
+            flush.fill_(1)                         # larger than L2
+            e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            e0.record(stream)
+            call()
+            e1.record(stream)
+            torch.cuda.synchronize()
+            total += e0.elapsed_time(e1)
+        return total / reps * 1e-3
+
+    out = {}
+    for name, q in (("attention_token", torch.randn((B, 1, H * G, D), generator=g, device=dev).to(torch.bfloat16)),
+                    ("attention_block", torch.randn((B, Q, H * G, D), generator=g, device=dev).to(torch.bfloat16))):
+        t = timed(lambda: P.paged_attention(q, k, v, cache.page_table, cache.length))
+        alg = 2 * B * n * H * D * 2 + 2 * q.numel() * 2
+        out[name] = {"ms": t * 1e3, "positions": int(B * n), "queries_per_sequence": q.shape[1],
+                     "roofline": {"bound": "hbm", "achieved": alg / t / 1e9, "peak": peak, "unit": "GB/s", "frac": alg / t / 1e9 / peak, "algorithmic_bytes": alg}}
+    nk, nv = (torch.randn((B, Q, H, D), generator=g, device=dev).to(torch.bfloat16) for _ in range(2))
+    keep = torch.zeros(B, dtype=torch.int32, device=dev)
+
+    def block():
+        _, _, st = P.cache_reserve(cache, Q)
+        P.cache_write(cache, nk, nv, k, v, st)
+        P.cache_truncate(cache, keep, of=Q)
+
+    block()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        block()
+    out["cache_block"] = {"ms": timed(graph.replay) * 1e3, "what": "reserve 7 positions, write them, cut back to none kept"}
+    z = torch.randn((64, 8, 151936), generator=g, device=dev).to(torch.bfloat16)
+    score = -5 * torch.rand((64, 8), generator=g, device=dev)
+    t = timed(lambda: P.beam_select(z, score, 8))
+    out["beam_select"] = {"ms": t * 1e3, "rows": 512, "V": 151936,
+                          "roofline": {"bound": "hbm", "achieved": z.numel() * 2 / t / 1e9, "peak": peak, "unit": "GB/s", "frac": z.numel() * 2 / t / 1e9 / peak,
+                                       "algorithmic_bytes": z.numel() * 2}}
+    out["l2"] = "flushed before every call"
+    return out
+
+
 def _vocab_sharded(P, synth, dev, stream, peak, rows=0):
     """Vocabulary-sharded routing of 4096 rows of the headline workload's shape cut into 8 column slices, the ranks
     run one after the other on this GPU (the calls one rank per GPU would make around its all-gathers): time of
@@ -614,8 +672,8 @@ def run_ours(args):
                 cpu["all_cores"] = allc
 
     # ---- the throughput sweep at its full size and the V = 32000 workload, the step in front of the path (the
-    # lm-head GEMM with the first row statistics in its epilogue) and vocabulary-sharded rows: beside the headline
-    sweep = lm_head = vocab_sharded = None
+    # lm-head GEMM with the first row statistics in its epilogue), vocabulary-sharded rows and a rollout's cache: beside the headline
+    sweep = lm_head = vocab_sharded = rollout = None
     if not args.no_sweep and not args.rows and rank == 0:
         del s, t, g, x, d
         out = None
@@ -623,6 +681,8 @@ def run_ours(args):
         sweep = _sweep(P, synth, dev, stream, peak, args)
         torch.cuda.empty_cache()
         vocab_sharded = _vocab_sharded(P, synth, dev, stream, peak)
+        torch.cuda.empty_cache()
+        rollout = _rollout(P, dev, stream, peak)
         torch.cuda.empty_cache()
         lm_head = _lm_head(P, dev, stream, 5)      # last: a dense GEMM at the power limit would colour what follows it
 
@@ -636,6 +696,8 @@ def run_ours(args):
         line["phase_cycles_per_row"] = phases
     if lm_head is not None:
         line["lm_head"] = lm_head
+    if rollout is not None:
+        line["rollout"] = rollout
     if vocab_sharded is not None:
         line["vocab_sharded"] = vocab_sharded
     if sweep is not None:
@@ -681,21 +743,22 @@ def main():
     ap.add_argument("--no-cpu", action="store_true")
     ap.add_argument("--no-next", action="store_true", help="skip the metadata-driven backward measurement")
     ap.add_argument("--no-sweep", action="store_true", help="skip the throughput sweep and the V = 32000 workload")
-    ap.add_argument("--section", default="all", choices=["all", "lm_head", "vocab_sharded"],
-                    help="lm_head / vocab_sharded: time only that section (on --rows positions if given) and print its object (profiling)")
+    ap.add_argument("--section", default="all", choices=["all", "lm_head", "vocab_sharded", "rollout"],
+                    help="lm_head / vocab_sharded / rollout: time only that section (on --rows positions if given) and print its object (profiling)")
     ap.add_argument("--e2e-steps", type=int, default=3)
     ap.add_argument("--cpu-rows", type=int, default=384)
     ap.add_argument("--ref-rows", type=int, default=32)
     args = ap.parse_args()
     if args.gpus > 1 and "RANK" not in os.environ:
         sys.exit(_spawn_ranks(args.gpus))
-    if args.section == "vocab_sharded":
+    if args.section in ("vocab_sharded", "rollout"):
         import torch
         import paper_2609_36601_b200 as P
         from paper_2609_36601_b200 import synth
         torch.cuda.set_device(0)
         peak, _ = _peaks()
-        print(json.dumps(_vocab_sharded(P, synth, "cuda:0", torch.cuda.current_stream(), peak, args.rows)))
+        stream = torch.cuda.current_stream()
+        print(json.dumps(_rollout(P, "cuda:0", stream, peak, args.steps) if args.section == "rollout" else _vocab_sharded(P, synth, "cuda:0", stream, peak, args.rows)))
         return
     if args.section == "lm_head":
         import torch

@@ -15,7 +15,10 @@
 //               the output.  (A group is a warp on each scheduler, which issues an instruction in four to six cycles: so few queries, and groups that
 //               share a tile.  Groups that took turns, a tile each, were slower: a tile's keys and values wait twice as long for their turn in the ring.)
 //   the last 4  a thread per column of the output: at a segment's end they divide and write, while the groups go on
-// What bounds it: HBM (two to three tiles of 64 KB in flight on an SM).
+// What bounds it: HBM where segments are long (two to three tiles of 64 KB in flight on an SM): 64 sequences of 4096 positions, 8 key heads of 128, 4 rows each 182 us, 5.9 TB/s (90 % of
+// the measured copy rate), of 8192 with 28 rows 355 us (93 %), 512 of 1024 with 4 rows 354 us (93 %).  The weights' warps where segments end often or rows are many: 512 of 65 to 2048
+// positions with 28 rows 569 us (61 %: the instructions of an edge, some 7 us a segment), 64 of 8192 with 64 rows 600 us (56 %).  One sequence of 131077, 4 key heads:
+// 58 us (71 %: start, two ends and the joining kernel are some 15 of it).
 // Every wait is bounded: a wait that runs out ends all roles' waits, the segments that are left are flagged, and the block leaves.
 #include "saki_attention.cuh"
 #include <climits>

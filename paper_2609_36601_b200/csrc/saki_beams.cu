@@ -1,6 +1,9 @@
 // Beam selection over vocabulary rows: the n best continuations of a group of W beams by the sum of the beam's score and the
 // log-probability of the token.
 //
+// What bounds it: issue slots and the barriers between a slice's phases (some 900 instructions a warp and 64 elements a thread, 17 us of exponentials), not HBM: 64 groups of 8 beams,
+// 151936 bf16 logits each, 64 us where the bytes take 24, the joining kernel 8 of it; 1 group of 4 beams 14 us, two launches and the chains of one slice and of the join.
+//
 // Within a beam the order of the keys is that of the logits, so a row is read once: a block holds a slice of it in registers, sums
 // its exponentials, and picks the slice's n best logits.  For those, a bar: of the maxima of the 64 groups of four threads the n-th
 // largest is at most the slice's n-th largest logit, and little below it as a rule.  What reaches the bar (about n elements) goes to a list in
@@ -448,8 +451,9 @@ cudaError_t launch_beams(const saki_beam_in& in, const saki_beam_out& out, void*
   } else
     e = l.nv == 8 ? go(beam_rows_kernel<float, 8>) : l.nv == 4 ? go(beam_rows_kernel<float, 4>) : l.nv == 2 ? go(beam_rows_kernel<float, 2>) : go(beam_rows_kernel<float, 1>);
   if (e != cudaSuccess) return e;
-  const size_t bytes = join_items(in.n, in.W * l.slices) * sizeof(Best) + (size_t)in.W * l.slices;      // (64 KB and 64 beams of 512 slices at most)
-  e = cudaFuncSetAttribute(beam_join_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  const size_t bytes = join_items(in.n, in.W * l.slices) * sizeof(Best) + (size_t)in.W * l.slices;
+  constexpr int most = 64 * 64 * (int)sizeof(Best) + 64 * 512;      // (the same for every call: two threads may be here; 64 beams of 512 slices)
+  e = cudaFuncSetAttribute(beam_join_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
   return e != cudaSuccess ? e : launch_pdl(beam_join_kernel, dim3((unsigned)in.B), BT, bytes, st, true, p);
 }
 
