@@ -70,7 +70,7 @@ struct ClusterShared {
 // The pages are split over the cluster's warps in runs of whole 32s, in order.
 struct Run { int from, to; };
 __device__ __forceinline__ Run run_of(int n_pages, int rank) {
-  const int per = ((n_pages + CCS * CWARPS - 1) / (CCS * CWARPS) + 31) & ~31;
+  const int per = (int)(((int64_t)n_pages + CCS * CWARPS - 1) / (CCS * CWARPS) + 31) & ~31;
   const int64_t from = (int64_t)(rank * CWARPS + (threadIdx.x >> 5)) * per;
   return {(int)min(from, (int64_t)n_pages), (int)min(from + per, (int64_t)n_pages)};
 }
@@ -79,15 +79,15 @@ __device__ __forceinline__ Run run_of(int n_pages, int rank) {
 constexpr int AHEAD = 8;
 template <typename F, typename G> __device__ __forceinline__ void each_32(Run r, F&& is, G&& take) {      // take(i, is(i), mask of the warp's)
   const int lane = threadIdx.x & 31;
-  for (int i0 = r.from; i0 < r.to; i0 += 32 * AHEAD) {
+  for (unsigned i0 = (unsigned)r.from; i0 < (unsigned)r.to; i0 += 32 * AHEAD) {      // (unsigned: behind the last page may be 2^31)
     bool yes[AHEAD];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const int i = i0 + 32 * k + lane;
-      yes[k] = i < r.to && is(i);
+      const unsigned i = i0 + 32 * k + lane;
+      yes[k] = i < (unsigned)r.to && is((int)i);
     }
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) take(i0 + 32 * k + lane, yes[k], __ballot_sync(0xffffffffu, yes[k]));
+    for (int k = 0; k < AHEAD; ++k) take((int)(i0 + 32 * k + lane), yes[k], __ballot_sync(0xffffffffu, yes[k]));
   }
 }
 template <typename F> __device__ __forceinline__ void count_run(ClusterShared& sh, int k, Run r, F&& is) {

@@ -12,6 +12,12 @@ from test_gpu_paged_attention import BF16, DEV, F32, _check, _make
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def _nothing_flagged():
+    """The count of flagged rows is the library's: what other tests left in it goes first."""
+    P.check()
+
+
 # one token of few rows: heads up to 64, tables up to 256 positions, and one above; more rows, more tokens; heads at the ends of what a kernel takes
 @pytest.mark.parametrize("Q,G,D,page,lengths,extra", [
     (1, 1, 8, 16, [100, 1], 3), (1, 4, 16, 8, [300, 17], 3), (1, 5, 24, 16, [129, 64], 3), (2, 5, 24, 16, [129, 2], 3),

@@ -17,6 +17,12 @@ DEV = "cuda:0"
 BF16, F32 = torch.bfloat16, torch.float32
 
 
+@pytest.fixture(autouse=True)
+def _nothing_flagged():
+    """The count of flagged rows is the library's: what other tests left in it goes first."""
+    P.check()
+
+
 def _make(B, Q, H, G, D, page, lengths, dtype, seed, head_major=False, extra=3, fill=None):
     """q, pools and tables; slots that hold no position are `fill` (default: numbers like the others)."""
     g = torch.Generator(device=DEV).manual_seed(seed)

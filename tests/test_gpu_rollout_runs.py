@@ -15,6 +15,12 @@ DEV = "cuda:0"
 BF16 = torch.bfloat16
 
 
+@pytest.fixture(autouse=True)
+def _nothing_flagged():
+    """The count of flagged rows is the library's: what other tests left in it goes first."""
+    P.check()
+
+
 class _Model:
     """Tables that keys, values, queries and logits come from."""
 
