@@ -71,13 +71,24 @@ template <typename T, int NV> __device__ __forceinline__ void keep_packed(Vec<T>
     for (int i = 0; i < 4; ++i) asm volatile("" : "+r"(x[k].r[i]));
 }
 
+// a vector that is not aligned, or ends behind V: -inf there.  (Out of line: with eight of these in place warps waited for instructions more than for anything else.)
+template <typename T> __device__ __noinline__ Vec<T> one_by_one(const T* s, int v, int V) {
+  Vec<T> x;
+#pragma unroll
+  for (int i = 0; i < Vec<T>::E / 2; ++i)
+    x.set(i, v + 2 * i < V ? ld_as_float(s, v + 2 * i) : -CUDART_INF_F, v + 2 * i + 1 < V ? ld_as_float(s, v + 2 * i + 1) : -CUDART_INF_F);
+  return x;
+}
+
 struct BeamShared {
   alignas(16) float group_max[GROUPS];
   float warp_max[BWARPS];
   double warp_sum[BWARPS];
   uint64_t warp_best[BWARPS];
   float bar;
-  unsigned count;
+  unsigned vectors, count;
+  alignas(16) uint4 vector[LIST];
+  int vector_at[LIST];
   uint64_t list[LIST];
 };
 
@@ -97,7 +108,7 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 4) beam_rows
   const T* const s = (const T*)p.in.logits + b * p.in.ld_seq + (row - b * p.in.W) * p.in.ld_beam;
   const bool vec = ((uintptr_t)s & 15) == 0;
   const int v0 = slice * p.slice;
-  if (tid == 0) sh.count = 0;
+  if (tid == 0) sh.count = sh.vectors = 0;
   Vec<T> x[NV];
   if (vec && v0 + NV * BT * E <= V) {
 #pragma unroll
@@ -112,11 +123,7 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 4) beam_rows
       if (vec && v + E <= V) {
         const uint4 a = __ldg((const uint4*)(s + v));
         x[k].r[0] = a.x; x[k].r[1] = a.y; x[k].r[2] = a.z; x[k].r[3] = a.w;
-      } else {
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i)
-          x[k].set(i, v + 2 * i < V ? ld_as_float(s, v + 2 * i) : -CUDART_INF_F, v + 2 * i + 1 < V ? ld_as_float(s, v + 2 * i + 1) : -CUDART_INF_F);
-      }
+      } else x[k] = one_by_one(s, v, V);
     }
   }
   float top[NV], mine = -CUDART_INF_F;
@@ -196,24 +203,30 @@ template <typename T, int NV> __global__ void __launch_bounds__(BT, 4) beam_rows
     *part = make_double2(m, total);
   }
   keep_packed(x);
+  // vectors with an element that reaches the bar, then their elements, a thread each
   if (mine >= bar && mine > -CUDART_INF_F) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      if (!(top[k] >= bar)) continue;
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const float2 a = x[k].pair(i >> 1);
-        const float e = i & 1 ? a.y : a.x;
-        if (e >= bar && e > -CUDART_INF_F) {
-          const unsigned at = atomicAdd(&sh.count, 1u);
-          if (at < LIST) sh.list[at] = pair_word(e, (uint32_t)(v0 + (k * BT + tid) * E + i));
+    for (int k = 0; k < NV; ++k)
+      if (top[k] >= bar) {
+        const unsigned at = atomicAdd(&sh.vectors, 1u);
+        if (at < LIST) {
+          sh.vector[at] = make_uint4(x[k].r[0], x[k].r[1], x[k].r[2], x[k].r[3]);
+          sh.vector_at[at] = v0 + (k * BT + tid) * E;
         }
       }
+  }
+  __syncthreads();
+  const int vectors = (int)sh.vectors;
+  for (int i = tid; i < min(vectors, LIST) * E; i += BT) {
+    const float e = ld_as_float((const T*)(sh.vector + i / E), i % E);
+    if (e >= bar && e > -CUDART_INF_F) {
+      const unsigned at = atomicAdd(&sh.count, 1u);
+      if (at < LIST) sh.list[at] = pair_word(e, (uint32_t)(sh.vector_at[i / E] + i % E));
     }
   }
   __syncthreads();
   const int count = (int)sh.count;
-  if (count <= LIST) {
+  if (count <= LIST && vectors <= LIST) {
     for (int i = tid; i < count; i += BT) {
       const uint64_t w = sh.list[i];
       int r = 0;
