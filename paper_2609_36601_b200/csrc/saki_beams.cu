@@ -1,8 +1,9 @@
 // Beam selection over vocabulary rows: the n best continuations of a group of W beams by the sum of the beam's score and the
 // log-probability of the token.
 //
-// What bounds it: issue slots and the barriers between a slice's phases (some 900 instructions a warp and 64 elements a thread, 17 us of exponentials), not HBM: 64 groups of 8 beams,
-// 151936 bf16 logits each, 64 us where the bytes take 24, the joining kernel 8 of it; 1 group of 4 beams 14 us, two launches and the chains of one slice and of the join.
+// What bounds it: issue slots (60 % of them filled; some 860 instructions a warp and 64 elements a thread, 17 us of exponentials) and the barriers between a slice's phases, not HBM:
+// 64 groups of 8 beams, 151936 bf16 logits each, a third of the beams finished, 50 us where the bytes take 24, the joining kernel 8 of it (52 and 59 with four and three blocks an SM
+// instead of five); 1 group of 4 beams 14 us, two launches and the chains of one slice and of the join.
 //
 // Within a beam the order of the keys is that of the logits, so a row is read once: a block holds a slice of it in registers, sums
 // its exponentials, and picks the slice's n best logits.  For those, a bar: of the maxima of the 64 groups of four threads the n-th
@@ -93,7 +94,7 @@ struct BeamShared {
 };
 
 // NV: 16-byte vectors that a thread holds
-template <typename T, int NV> __global__ void __launch_bounds__(BT, 4) beam_rows_kernel(const BeamParams p) {
+template <typename T, int NV> __global__ void __launch_bounds__(BT, 5) beam_rows_kernel(const BeamParams p) {
   constexpr int E = Vec<T>::E;
   __shared__ BeamShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = p.in.V, n = p.in.n;
