@@ -144,3 +144,10 @@ def test_two_streams_at_once_and_two_captured_calls():
         torch.cuda.synchronize()
         for i in set(order):
             assert all(torch.equal(x, y) for x, y in zip(outs[i], want[i % 2]))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Q,G,D,page,lengths", [(1, 4, 128, 128, [500, 128]), (3, 4, 128, 256, [300, 700]), (2, 2, 64, 1000, [1500, 2]), (1, 2, 64, 4096, [5000, 4096]),
+                                                (32, 64, 64, 16, [200, 32]), (32, 64, 128, 12, [70, 33])])
+def test_large_pages_and_many_rows(dtype, Q, G, D, page, lengths):
+    _check(*_make(2, Q, 1, G, D, page, lengths, dtype, Q + G + page, extra=1, fill=float("nan")))
