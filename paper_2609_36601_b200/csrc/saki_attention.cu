@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
       for (int k = 0; k < 2; ++k) {
         top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
         top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
-        top[k] = fmaxf(top[k] * p.c, m[k]);          // (c > 0)
+        top[k] = fmaxf(__fmul_rd(top[k], p.c), m[k]);          // (c > 0)
         shift[k] = top[k] == -CUDART_INF_F ? 0.f : top[k];
       }
       if (__any_sync(0xffffffffu, top[0] != m[0] || top[1] != m[1])) {
@@ -341,7 +341,9 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
       for (int e = 0; e < NT; ++e)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          s[e][k] = ex2f(fmaf(s[e][k], p.c, -shift[k >> 1]));
+          // (a score so large that the rounding of c s, downwards, is no small thing: the largest has the weight 1 all the same; NaN stays)
+          const float x = fmaf(s[e][k], p.c, -shift[k >> 1]);
+          s[e][k] = ex2f(x > 0.f ? 0.f : x);
           l[k >> 1] += s[e][k];
         }
     }

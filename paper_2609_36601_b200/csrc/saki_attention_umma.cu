@@ -21,6 +21,7 @@
 // 58 us (71 %: start, two ends and the joining kernel are some 15 of it).
 // Every wait is bounded: a wait that runs out ends all roles' waits, the segments that are left are flagged, and the block leaves.
 #include "saki_attention.cuh"
+#include <cfloat>
 #include <climits>
 
 namespace saki {
@@ -188,7 +189,7 @@ __device__ __forceinline__ void u_next(const AttnParams& p, Cursor<UT>& c) {
   c = to;
 }
 
-constexpr float NOTHING = -1e30f;       // the maximum of a row that has seen nothing so far
+constexpr float NOTHING = -FLT_MAX;     // the maximum of a row that has seen nothing so far
 
 // GROUPED (D = 128): a box brings both slabs of its positions, [8 positions][2 slabs][8 rows of 128 bytes]; else [slab][128 rows of 128 bytes].  (Boxes of a page
 // of 16 positions are 2 KB then, and 32 of them a tile take longer than the bus: 64 sequences of 4096 at 72 % of the copy rate, 88 % with pages of 64.)
@@ -459,10 +460,16 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
           }
         };
         float big = 0.f;
-        auto weights = [&] {
-          by_four(m_s, [&](int n, float m) { w[n] = ex2f(fmaf(w[n], p.c, -m)); big = fmaxf(big, w[n]); });
-        };
         bool exact = fresh && edge;
+        auto weights = [&] {
+          by_four(m_s, [&](int n, float m) { w[n] = fmaf(w[n], p.c, -m); });
+          // (scores so large that the rounding of c s, downwards, is no small thing: the largest has the weight 1 all the same)
+          if (exact)
+#pragma unroll
+            for (int n = 0; n < CW; ++n) w[n] = w[n] > 0.f ? 0.f : w[n];
+#pragma unroll
+          for (int n = 0; n < CW; ++n) { w[n] = ex2f(w[n]); big = fmaxf(big, w[n]); }
+        };
 #pragma unroll 1
         for (;;) {
           scores();
@@ -475,7 +482,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
             u_sync(g);
             if (t < CW) {
               const int n = c0 + t;
-              const float most = fmaxf(fmaxf(r.top[0][n], r.top[1][n]), fmaxf(r.top[2][n], r.top[3][n])), before = m_s[t], m = fmaxf(before, most * p.c);
+              const float most = fmaxf(fmaxf(r.top[0][n], r.top[1][n]), fmaxf(r.top[2][n], r.top[3][n])), before = m_s[t], m = fmaxf(before, __fmul_rd(most, p.c));
               m_s[t] = m;
               factor_s[t] = ex2f(before - m);
             }
@@ -500,7 +507,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
 #pragma unroll
             for (int k = 0; k < CW / 4; ++k) {
               const float top = u_warp_max(q4 == 0 ? w[k] : q4 == 1 ? w[CW / 4 + k] : q4 == 2 ? w[CW / 2 + k] : w[3 * CW / 4 + k]);
-              if (lane == k) m_s[q4 * (CW / 4) + k] = fmaxf(NOTHING, top * p.c);
+              if (lane == k) m_s[q4 * (CW / 4) + k] = fmaxf(NOTHING, __fmul_rd(top, p.c));
             }
             u_sync(g);
           }

@@ -151,3 +151,25 @@ def test_two_streams_at_once_and_two_captured_calls():
                                                 (32, 64, 64, 16, [200, 32]), (32, 64, 128, 12, [70, 33])])
 def test_large_pages_and_many_rows(dtype, Q, G, D, page, lengths):
     _check(*_make(2, Q, 1, G, D, page, lengths, dtype, Q + G + page, extra=1, fill=float("nan")))
+
+
+@pytest.mark.parametrize("dtype,Q,D,page", [(BF16, 2, 128, 16), (BF16, 1, 128, 16), (BF16, 1, 64, 16), (BF16, 3, 64, 5), (F32, 2, 64, 16)])
+@pytest.mark.parametrize("size", [1e10, 1e15, 1e17])
+def test_scores_far_below_zero(dtype, Q, D, page, size):
+    """Scores of -1e21 to -1e35, the same at all positions: the mean of the values, whatever the maximum was taken to be at first."""
+    n = 700
+    q, k, v, table, length = _make(2, Q, 2, 2, D, page, [n, 40], dtype, 5)
+    q.fill_(size)
+    k.fill_(-size)
+    out, lse, st = P.paged_attention(q, k, v, table, length)
+    assert int(st.abs().max()) == 0 and torch.isfinite(lse).all()
+    for b in range(2):
+        pages = table[b, :-(-int(length[b]) // page)].long()
+        vb = v[pages].flatten(0, 1).double()
+        for j in range(Q):
+            m = int(length[b]) - Q + j + 1
+            want = vb[:m].mean(0).repeat_interleave(2, 0)
+            size_v = vb[:m].abs().mean(0).repeat_interleave(2, 0)
+            half = torch.finfo(dtype).eps / 2
+            # equal weights of 1 (exact in two terms), a sum of m values, one division, one rounding
+            assert ((out[b, j].double() - want).abs() <= half * want.abs() + (m + 4) * 2.0 ** -23 * size_v).all()
