@@ -580,8 +580,8 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
             }
           }
         }
-        if (t == 0 && g == 0) *(volatile int*)(r.keep + (i & 1)) = keep;
         if (i >= PB && !dead && !u_wait(r.pv_done + ((i - PB) & 1), ((i - PB) >> 1) & 1, r, limit)) dead = true;      // the buffer's last product
+        if (t == 0 && g == 0) *(volatile int*)(r.keep + (i & 1)) = keep;      // (only now: before that product was issued, tile i - 2's word was still to be read)
         {
           char* const at = p_s + (i % PB) * S::P_BYTES + (t >> 6) * (N * 256) + (t & 7) * 2 + c0 * 128;
           const uint32_t piece = (uint32_t)((t >> 3) & 7) << 4;
