@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
     if (!gave_up) {
       load();
       look_up();
-      gave_up = !mbar_wait_bounded(full + stage, parity, p.wait_limit);
+      gave_up = !__all_sync(0xffffffffu, mbar_wait_bounded(full + stage, parity, p.wait_limit));      // (one answer for the warp: it votes together in load())
     }
     if (gave_up) {
       bad = -2.f;
