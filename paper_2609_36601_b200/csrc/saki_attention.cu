@@ -69,7 +69,7 @@ template <typename E, int DP, int NW_> struct Shape {
   static constexpr int Q_BYTES = Q_REGS ? 0 : ROWS * DP * (int)sizeof(E);            // of a worker
   static constexpr int FIT = (226 * 1024 - WORKERS * Q_BYTES - 1024 - 8 * THREADS) / (WORKERS * (STAGE + 8));
   static constexpr int MOST = NW == 8 ? 24 : 4 * NW, STAGES = FIT < MOST ? FIT : MOST;
-  static constexpr int SMEM = WORKERS * (STAGES * (STAGE + 8) + Q_BYTES + 4) + (int)sizeof(LineShared<THREADS>) + 1024;
+  static constexpr int SMEM = WORKERS * (STAGES * (STAGE + 8) + Q_BYTES) + (int)sizeof(LineShared<THREADS>) + 1024;
   static_assert(STAGES >= 2 && STAGES < 32 && SMEM <= 227 * 1024, "a block's shared memory");
 };
 // 16-byte piece j of row r in a slab layout with `rows` rows a slab: eight pieces of a row are swizzled by the row, as TMA lays them down
@@ -92,11 +92,19 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
   char* const rest = smem + S::WORKERS * (ST * S::STAGE + S::Q_BYTES);
   uint64_t* const full = (uint64_t*)rest + worker * ST;
   LineShared<THREADS>& line = *(LineShared<THREADS>*)(rest + S::WORKERS * ST * 8);
-  int* const told = (int*)(rest + S::WORKERS * ST * 8 + sizeof(LineShared<THREADS>)) + worker;
   const uint32_t ring_a = smem_addr(ring), q_a = smem_addr(q_s);
   auto together = [&] {            // the worker's warps
     if constexpr (NW == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(worker + 1), "r"(32 * NW) : "memory");
+  };
+  auto any_of_us = [&](bool yes) -> bool {      // one answer for all threads of the worker, who meet there
+    if constexpr (NW == 1) return __any_sync(0xffffffffu, yes);
+    else {
+      uint32_t any;
+      asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                   : "=r"(any) : "r"(yes ? 1u : 0u), "r"(worker + 1), "r"(32 * NW) : "memory");
+      return any != 0;
+    }
   };
 
   // columns behind D stay zero (TMA fills a slab that it loads)
@@ -107,7 +115,6 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
     }
   }
   if (part_of == 0 && lane < ST) mbar_init(full + lane, TMA ? 1 : 32);
-  if (part_of == 0 && lane == 0) *told = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   wait_for_predecessor();
   launch_dependents();
@@ -243,10 +250,8 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
       look_up();
       gave_up = !__all_sync(0xffffffffu, mbar_wait_bounded(full + stage, parity, p.wait_limit));      // (one answer for the warp: it votes together in load())
     }
-    if (gave_up) {
-      bad = -2.f;
-      if constexpr (NW > 1) *(volatile int*)told = 1;
-    } else if (bad_tiles >> (i & 31) & 1u) bad = bad == 0.f ? -1.f : bad;
+    if (gave_up) bad = -2.f;
+    else if (bad_tiles >> (i & 31) & 1u) bad = bad == 0.f ? -1.f : bad;
     const uint32_t at_s = ring_a + stage * S::STAGE;
     char* const v_p = ring + stage * S::STAGE + S::HALF;
     const int x0 = tile_start<T>(now.s, now.t);
@@ -355,12 +360,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
         const uint4 x = *(const uint4*)(v_p + piece_at<T>(e / PIECES, e % PIECES));
         strange = strange || odd(x.x) || odd(x.y) || odd(x.z) || odd(x.w);
       }
-      if constexpr (NW > 1) {      // one answer for the worker's warps, whatever one that has given up reads: they meet in there
-        uint32_t any;
-        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                     : "=r"(any) : "r"(strange ? 1u : 0u), "r"(worker + 1), "r"(32 * NW) : "memory");
-        strange = any;
-      } else strange = __any_sync(0xffffffffu, strange);
+      strange = any_of_us(strange);        // (whatever a warp that has given up reads)
       if (strange) {               // it goes to the rows that see it by itself, and 0 takes its place
 #pragma unroll 1
         for (int t = 0; t < T; ++t)
@@ -439,10 +439,10 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
       }
     }
     if (TMA && wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stage is written by TMA next
-    together();                    // the stage may be loaded again
-    if constexpr (NW > 1) {        // the warps of a worker give up on the same segment
-      if (*(volatile int*)told) { gave_up = true; bad = -2.f; }
-    }
+    // the stage may be loaded again; the warps of a worker give up on the same segment (a word in shared memory, read behind the barrier, could be a faster warp's of the tile behind)
+    if constexpr (NW > 1) {
+      if (any_of_us(gave_up)) { gave_up = true; bad = -2.f; }
+    } else together();
     if (now.t + 1 == now.s.nt || i + 1 == n_tiles) {        // the segment ends, or the piece does
       const bool head = i < now.t, tail = now.t + 1 < now.s.nt;      // it goes on from the piece before, or behind
       const uint32_t st = now.s.status | status_of(bad);

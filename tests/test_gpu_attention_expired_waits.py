@@ -1,4 +1,4 @@
-"""Bounded waits of the attention kernels that run out part of the way: every row
+"""Bounded waits of the attention kernels that run out part of the way: the warps that share a worker's tiles give up on the same segment, and every row
 that was given up on is told.  A limit of two to a few thousand cycles runs out although the copies are on their way; nothing is withheld."""
 import numpy as np
 import pytest
@@ -17,8 +17,9 @@ def _nothing_flagged():
     P.check()
 
 
-# a warp a worker; the kernel on tcgen05
-@pytest.mark.parametrize("dtype,Q,G,D,page", [(BF16, 1, 4, 64, 16), (BF16, 1, 2, 256, 16), (F32, 1, 2, 64, 16), (BF16, 7, 4, 128, 16)])
+# one, two, four and eight warps a worker; pages by TMA and by plain loads; the kernel on tcgen05
+@pytest.mark.parametrize("dtype,Q,G,D,page", [(BF16, 1, 4, 64, 16), (BF16, 1, 2, 256, 16), (BF16, 3, 9, 256, 16), (BF16, 8, 8, 256, 16), (BF16, 16, 8, 256, 5),
+                                              (F32, 1, 2, 64, 16), (F32, 4, 6, 80, 16), (F32, 7, 8, 64, 5), (F32, 16, 8, 64, 16), (BF16, 7, 4, 128, 16)])
 def test_rows_given_up_on_are_told(dtype, Q, G, D, page):
     H = 2
     lengths = [Q + (61 * i) % 211 for i in range(160)] + [9000, 5000]      # many segments a worker, and some that several share
