@@ -379,6 +379,7 @@ typedef struct {
   int32_t max_pages;          /* >= 1 */
   int32_t n_pages;            /* 1 .. 2^30 */
   int32_t page_size;          /* >= 1; max_pages * page_size below 2^31 */
+  const uint32_t* row_status; /* [B] or NULL; read by saki_cache_truncate alone */
 } saki_cache;
 SAKI_API int64_t saki_cache_scratch_bytes(int64_t B, int32_t max_pages, int32_t n_pages);
 
@@ -395,7 +396,9 @@ SAKI_API int saki_cache_reserve(const saki_cache* cache, const int32_t* n_new, i
 /* Sequence b keeps the first keep[b] + keep_add of its last `of` positions, or, with of < 0, of all of them; pages behind them are
  * given back and their entries become -1.  With `of` = K + 1, keep = n_accept of saki_spec_verify and keep_add = 1 this commits a
  * verified block (the token in front of the draft and the accepted prefix).  A number to keep outside [0, of], or `of` beyond the
- * length: BAD_LENGTH, unchanged.  An entry given back whose id is outside the pool: BAD_PAGE, and no count changes for it. */
+ * length: BAD_LENGTH, unchanged.  An entry given back whose id is outside the pool: BAD_PAGE, and no count changes for it.
+ * Sequences whose cache->row_status (of saki_cache_reserve) has a flag did not get the positions that are to be cut: they are passed over, and keep that
+ * flag in row_status (not counted once more; the two arrays may be one). */
 SAKI_API int saki_cache_truncate(const saki_cache* cache, const int32_t* keep, int32_t keep_add, int32_t of, uint32_t* row_status,
                                  void* cuda_stream);
 
@@ -444,7 +447,8 @@ SAKI_API int saki_cache_write(const saki_cache* cache, const saki_cache_kv* kv, 
  * float32.  A sequence with a length outside
  * [0, max_pages * page_size], or n outside [0, Q], is flagged BAD_LENGTH, one with an id outside the pool among the pages that its
  * queries see BAD_PAGE, one for which a wait ran out (saki_set_wait_limit) TIMEOUT: out 0, lse -inf (TIMEOUT:
- * in the heads that were late).
+ * in the heads that were late).  A sequence whose in->row_status (of saki_cache_reserve) has a flag, and whose new positions therefore are not there, has out 0, lse -inf and that flag
+ * (not counted once more; out->row_status must be another array).
  * Requirements: Q 1..32, max_pages * page_size below 2^31 - 256, Hq a multiple of H, Hq / H <= 64, D <= 256 and a multiple of 8 (f32: 4); 16-byte aligned pools, and strides
  * of the pools that are multiples of 16 bytes (SAKI_ERR_UNSUPPORTED otherwise).  scratch: saki_paged_attention_scratch_bytes(in) bytes,
  * 256-byte aligned, owned by one call at a time. */
@@ -460,6 +464,7 @@ typedef struct {
   int32_t dtype;                                            /* of q, the pools and out */
   int32_t window, sinks;                                    /* window 0: all positions */
   float scale;
+  const uint32_t* row_status;                               /* [B] or NULL */
 } saki_attn_in;
 typedef struct {
   void* out; int64_t o_seq, o_pos, o_head;                  /* [B, Q, Hq, D] */

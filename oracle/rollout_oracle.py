@@ -67,9 +67,12 @@ class Cache:
             self.length[b] = L + n
         return src, dst, status
 
-    def truncate(self, keep, of=None):
+    def truncate(self, keep, of=None, row_status=None):
         status = [0] * len(self.length)
         for b, k in enumerate(keep):
+            if row_status is not None and row_status[b]:
+                status[b] = row_status[b]
+                continue
             L = self.length[b]
             last = L if of is None else of
             if not self.ok(L) or last > L or not 0 <= k <= last:
@@ -134,13 +137,16 @@ class Cache:
         return src + pad, dst + pad, len(src), status
 
 
-def paged_attention(q, k_pages, v_pages, page_table, length, scale, n_query=None, window=0, sinks=0):
+def paged_attention(q, k_pages, v_pages, page_table, length, scale, n_query=None, window=0, sinks=0, row_status=None):
     """q [B, Q, Hq, D], pools [n_pages, page_size, H, D] (float64) -> out, lse, status."""
     B, Q, Hq, D = q.shape
     n_pages, page, H = k_pages.shape[:3]
     out, lse, status = np.zeros(q.shape), np.full((B, Q, Hq), -np.inf), np.zeros(B, dtype=np.int64)
     for b in range(B):
         n, nq = int(length[b]), Q if n_query is None else int(n_query[b])
+        if row_status is not None and row_status[b]:
+            status[b] = row_status[b]
+            continue
         if not 0 <= n <= page_table.shape[1] * page or not 0 <= nq <= Q:
             status[b] = ST_BAD_LENGTH
             continue

@@ -111,7 +111,7 @@ class SakiSpecOut(C.Structure):
 class SakiCache(C.Structure):
     _fields_ = [("page_table", C.c_void_p), ("ld_table", C.c_int64), ("length", C.c_void_p), ("ref_count", C.c_void_p),
                 ("scratch", C.c_void_p), ("scratch_bytes", C.c_int64), ("B", C.c_int64),
-                ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+                ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("row_status", C.c_void_p)]
 
 
 class SakiCacheKv(C.Structure):
@@ -130,7 +130,7 @@ class SakiAttnIn(C.Structure):
                 ("page_table", C.c_void_p), ("ld_table", C.c_int64), ("length", C.c_void_p), ("n_query", C.c_void_p), ("B", C.c_int64),
                 ("Q", C.c_int32), ("Hq", C.c_int32), ("H", C.c_int32), ("D", C.c_int32), ("page_size", C.c_int32),
                 ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("dtype", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
-                ("scale", C.c_float)]
+                ("scale", C.c_float), ("row_status", C.c_void_p)]
 
 
 class SakiAttnOut(C.Structure):
@@ -515,10 +515,11 @@ def cache_write(cache, k, v, k_pages, v_pages, row_status=None, n_new=None, stre
     (_fast or _tensors()).cache_write(*cache._args(), k, v, k_pages, v_pages, row_status, n_new, _handle(stream))
 
 
-def cache_truncate(cache, keep, of=None, keep_add=0, stream=None):
+def cache_truncate(cache, keep, of=None, keep_add=0, stream=None, row_status=None):
     """saki_cache_truncate: sequence b keeps the first keep[b] + keep_add (int32 [B]) of its last `of` positions, or of all of
-    them (None).  cache_truncate(cache, verdict["n_accept"], of=K + 1, keep_add=1) commits a verified block.  Returns row_status."""
-    return (_fast or _tensors()).cache_truncate(*cache._args(), keep, keep_add, -1 if of is None else of, _handle(stream))
+    them (None).  cache_truncate(cache, verdict["n_accept"], of=K + 1, keep_add=1, row_status=status) commits a verified block: sequences that
+    row_status (of cache_reserve) flags did not get those positions and are passed over.  Returns row_status."""
+    return (_fast or _tensors()).cache_truncate(*cache._args(), keep, keep_add, -1 if of is None else of, row_status, _handle(stream))
 
 
 def cache_fork(cache, parent, group=None, stream=None):
@@ -538,12 +539,12 @@ def copy_pages(pools, copy_src, copy_dst, stream=None):
     (_fast or _tensors()).copy_pages(pools, copy_src, copy_dst, _handle(stream))
 
 
-def paged_attention(q, k_pages, v_pages, page_table, length, scale=None, window=0, sinks=0, n_query=None, out=None, stream=None):
+def paged_attention(q, k_pages, v_pages, page_table, length, scale=None, window=0, sinks=0, n_query=None, out=None, stream=None, row_status=None):
     """saki_paged_attention: attention of the last Q (n_query[b], int32) positions of every sequence over a paged cache.  q [B, Q, Hq, D],
     pools [n_pages, page_size, H, D] of its type, page_table int32 [B, max_pages], length int32 [B] (a PageCache's), scale 1 / sqrt(D)
-    where None; window > 0: only the last `window` positions and the first `sinks` are seen.  Returns (out like q, lse float32
-    [B, Q, Hq], row_status int32 [B])."""
-    return (_fast or _tensors()).attention(q, k_pages, v_pages, page_table, length, scale, window, sinks, n_query, out, _handle(stream))
+    where None; window > 0: only the last `window` positions and the first `sinks` are seen.  Sequences that row_status (of cache_reserve) flags
+    have not got their new positions: out 0, lse -inf.  Returns (out like q, lse float32 [B, Q, Hq], row_status int32 [B])."""
+    return (_fast or _tensors()).attention(q, k_pages, v_pages, page_table, length, scale, window, sinks, n_query, out, row_status, _handle(stream))
 
 
 def check(stream=None) -> int:

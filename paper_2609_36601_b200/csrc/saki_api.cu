@@ -755,6 +755,8 @@ SAKI_API int saki_paged_attention(const saki_attn_in* in, const saki_attn_out* o
   if (in->B == 0) return SAKI_OK;
   if (!in->q || !in->k_pages || !in->v_pages || !in->page_table || !in->length || !out->out || !scratch)
     return fail(SAKI_ERR_INVALID_ARG, "NULL q, k_pages, v_pages, page_table, length, out or scratch pointer");
+  if (in->row_status && out->row_status && (uintptr_t)out->row_status < (uintptr_t)(in->row_status + in->B) && (uintptr_t)in->row_status < (uintptr_t)(out->row_status + in->B))
+    return fail(SAKI_ERR_INVALID_ARG, "the row_status that is read and the one that is written must be two arrays");
   if (scratch_bytes < attention_scratch_bytes(*in)) return fail(SAKI_ERR_INVALID_ARG, "scratch too small: %lld bytes needed", (long long)attention_scratch_bytes(*in));
   const int64_t size = in->dtype == SAKI_BF16 ? 2 : 4;
   bool ok = aligned(in->k_pages, 16) && aligned(in->v_pages, 16) && aligned(scratch, 256);

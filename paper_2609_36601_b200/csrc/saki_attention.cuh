@@ -51,8 +51,9 @@ template <int T> __device__ __forceinline__ Span span_of(const AttnParams& p, in
   Span s;
   s.n = p.in.length[b];
   s.nq = p.in.n_query ? p.in.n_query[b] : p.in.Q;
-  s.status = 0;
-  if (s.n < 0 || (int64_t)s.n > (int64_t)p.in.max_pages * p.in.page_size || s.nq < 0 || s.nq > p.in.Q) { s.status = SAKI_ROW_BAD_LENGTH; s.n = 0; s.nq = 0; }
+  s.status = p.in.row_status ? p.in.row_status[b] : 0u;      // (refused when positions were reserved)
+  if (s.status) s.n = s.nq = 0;
+  else if (s.n < 0 || (int64_t)s.n > (int64_t)p.in.max_pages * p.in.page_size || s.nq < 0 || s.nq > p.in.Q) { s.status = SAKI_ROW_BAD_LENGTH; s.n = 0; s.nq = 0; }
   s.p0 = s.n - s.nq;
   s.lo = p.in.window > 0 ? (int)max((int64_t)0, (int64_t)s.p0 - p.in.window + 1) : 0;
   if (s.nq == 0) s.lo = s.n;
@@ -142,7 +143,7 @@ __device__ __forceinline__ void put_lse(const AttnParams& p, int64_t b, int h, i
 // (by the worker that has the sequence's first tile; what comes to light elsewhere is added by the joining kernel)
 __device__ __forceinline__ void put_status(const AttnParams& p, int64_t b, uint32_t st) {
   if (p.out.row_status) p.out.row_status[b] = st;
-  if (st) atomicAdd(p.flagged, 1ull);
+  if (st && !(p.in.row_status && p.in.row_status[b])) atomicAdd(p.flagged, 1ull);      // (a flag that came with the call is counted already)
 }
 
 __device__ __forceinline__ void add_status(const AttnParams& p, int64_t b, uint32_t st) {

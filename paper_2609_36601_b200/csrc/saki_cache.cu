@@ -246,6 +246,11 @@ __global__ void __launch_bounds__(256) truncate_kernel(const saki_cache c, const
   const int lane = threadIdx.x & 31;
   const int64_t b = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (b >= c.B) return;
+  if (const uint32_t refused = c.row_status ? c.row_status[b] : 0u) {      // what is to be cut is not there
+    __syncwarp();
+    if (lane == 0 && row_status) row_status[b] = refused;
+    return;
+  }
   const int64_t L = c.length[b], k = (int64_t)keep[b] + keep_add, last = of < 0 ? L : of;
   __syncwarp();
   uint32_t st = 0;

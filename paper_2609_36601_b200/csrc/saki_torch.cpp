@@ -512,12 +512,13 @@ PyObject* py_cache_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// cache_truncate(cache..., keep, keep_add, of, stream) -> row_status
+// cache_truncate(cache..., keep, keep_add, of, row_status, stream) -> row_status
 PyObject* py_cache_truncate(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    n_args(n, CACHE_ARGS + 4);
+    n_args(n, CACHE_ARGS + 5);
     Cache k = cache_of(a);
-    const OnStream on(k.dev, a[8]);
+    const OnStream on(k.dev, a[9]);
+    if (a[8] != Py_None) k.c.row_status = (const uint32_t*)packed(a[8], at::kInt, k.c.B, k.dev, "row_status").data_ptr();
     const int32_t* const keep = (const int32_t*)packed(a[5], at::kInt, k.c.B, k.dev, "keep").data_ptr();
     const int64_t add = integer(a[6]), of = integer(a[7]);
     if (add > INT32_MAX || add < INT32_MIN || of > INT32_MAX || of < INT32_MIN) raise_value("keep_add or of out of range");
@@ -638,10 +639,10 @@ PyObject* py_cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// attention(q, k_pages, v_pages, page_table, length, scale, window, sinks, n_query, out, stream) -> (out, lse, row_status)
+// attention(q, k_pages, v_pages, page_table, length, scale, window, sinks, n_query, out, row_status, stream) -> (out, lse, row_status)
 PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    n_args(n, 11);
+    n_args(n, 12);
     const at::Tensor &q = tensor(a[0]), &kp = tensor(a[1]), &vp = tensor(a[2]), &table = tensor(a[3]);
     if (q.dim() != 4 || kp.dim() != 4 || (q.size(3) > 1 && q.stride(3) != 1)) raise_value("q must be [B, Q, Hq, D] with unit stride along D, the pools [n_pages, page_size, H, D]");
     const at::Device dev = q.device();
@@ -654,13 +655,14 @@ PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (s > INT32_MAX) raise_value("sizes out of range");
     saki_attn_in in = {};
     in.dtype = kv_dtype(q);
-    const OnStream on(dev, a[10]);
+    const OnStream on(dev, a[11]);
     in.q = q.data_ptr(); in.q_seq = step_of(q, 0); in.q_pos = step_of(q, 1); in.q_head = step_of(q, 2);
     in.k_pages = kp.data_ptr(); in.kp_page = step_of(kp, 0); in.kp_pos = step_of(kp, 1); in.kp_head = step_of(kp, 2);
     in.v_pages = vp.data_ptr(); in.vp_page = step_of(vp, 0); in.vp_pos = step_of(vp, 1); in.vp_head = step_of(vp, 2);
     in.page_table = (const int32_t*)table.data_ptr(); in.ld_table = B > 1 ? table.stride(0) : table.size(1);
     in.length = (const int32_t*)packed(a[4], at::kInt, B, dev, "length").data_ptr();
     if (a[8] != Py_None) in.n_query = (const int32_t*)packed(a[8], at::kInt, B, dev, "n_query").data_ptr();
+    if (a[10] != Py_None) in.row_status = (const uint32_t*)packed(a[10], at::kInt, B, dev, "row_status").data_ptr();
     in.B = B; in.Q = (int32_t)Q; in.Hq = (int32_t)Hq; in.H = (int32_t)H; in.D = (int32_t)D;
     in.page_size = (int32_t)page; in.max_pages = (int32_t)table.size(1); in.n_pages = (int32_t)pages;
     const int64_t window = integer(a[6]), sinks = integer(a[7]);
