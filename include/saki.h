@@ -544,8 +544,8 @@ SAKI_API int saki_solve_evaluations(void* cuda_stream, uint64_t* n_passes);
 
 /* Failure behaviour of the row-per-SM, general and attention kernels (no counterpart in the paper).  A thread block of the first waits for a
  * row's bulk copy from global memory for a bounded number of SM cycles (about two seconds' worth by
- * default); the attention kernels wait as long for each tile's copies and products, and flag what they then have not
- * finished.  If the wait runs out the block stops fetching, flags that row (in block verification every position it still
+ * default); the attention kernels wait as long for each tile's copies and products (however many tiles a sequence has), and flag
+ * what they then have not finished.  If the wait runs out the block stops fetching, flags that row (in block verification every position it still
  * takes) SAKI_ROW_TIMEOUT with zero outputs, waits (full limit) for the copy it has in flight, and returns: the
  * kernel always terminates, saki_check() counts the flagged rows and later calls are unaffected.  A block of either kernel, in
  * calls of more rows than are resident at once, waits as long for the answer to its request for a further row; if that wait

@@ -19,7 +19,7 @@
 // the measured copy rate), of 8192 with 28 rows 355 us (93 %), 512 of 1024 with 4 rows 354 us (93 %).  The weights' warps where segments end often or rows are many: 512 of 65 to 2048
 // positions with 28 rows 569 us (61 %: the instructions of an edge, some 7 us a segment), 64 of 8192 with 64 rows 600 us (56 %).  One sequence of 131077, 4 key heads:
 // 58 us (71 %: start, two ends and the joining kernel are some 15 of it).
-// Every wait is bounded: a wait that runs out ends all roles' waits, the segments that are left are flagged, and the block leaves.
+// Every wait is bounded (by the time that no tile is finished): a wait that runs out ends all roles' waits, the segments that are left are flagged, and the block leaves.
 #include "saki_attention.cuh"
 #include <cfloat>
 #include <climits>
@@ -58,7 +58,7 @@ template <int THREADS> struct URest {      // of shared memory
   int end_bad[2];
   int bad[8];             // by tile: a page outside the pool
   int keep[2];            // by tile: its sums go on top of what is there although it is the segment's first
-  int abort;
+  int stop[2];            // a wait ran out; tiles that the groups have finished
   uint32_t tmem;
 };
 static_assert(sizeof(URest<768>) <= 7168, "what is left of shared memory");
@@ -69,18 +69,22 @@ __device__ __forceinline__ int load_of_values(int i, int n) { return i + 1 < n ?
 
 // Code that is rarely run, or run from many places, is kept out of line: with all of it in place a kernel had 107 to 139 KB, and its warps, each in a part of its
 // own, waited for instructions more than for anything else.
-static __device__ __noinline__ bool u_wait_long(uint64_t* bar, uint32_t parity, int* abort, long long limit) {
+// The limit is for a tile: some roles wait for a whole segment, so it starts again whenever the groups have finished one (there are so many tiles and no more).
+static __device__ __noinline__ bool u_wait_long(uint64_t* bar, uint32_t parity, int* stop, long long limit) {
   const bool common = limit >= WAIT_LIMIT_CYCLES;
   if (common && mbar_try_wait(bar, parity)) return true;       // (which itself waits for a while)
-  const long long t0 = clock64();
+  long long t0 = clock64();
+  int done = *(volatile int*)(stop + 1);
   for (;;) {
-    if (*(volatile int*)abort) return false;
-    if (clock64() - t0 > limit) { *(volatile int*)abort = 1; return false; }
+    if (*(volatile int*)stop) return false;
+    const int now = *(volatile int*)(stop + 1);
+    if (now != done) { done = now; t0 = clock64(); }
+    else if (clock64() - t0 > limit) { *(volatile int*)stop = 1; return false; }
     if (common ? mbar_try_wait(bar, parity) : mbar_test_wait(bar, parity)) return true;
   }
 }
 template <typename R> __device__ __forceinline__ bool u_wait(uint64_t* bar, uint32_t parity, R& r, long long limit) {
-  return (limit >= WAIT_LIMIT_CYCLES && mbar_try_wait(bar, parity)) || u_wait_long(bar, parity, &r.abort, limit);
+  return (limit >= WAIT_LIMIT_CYCLES && mbar_try_wait(bar, parity)) || u_wait_long(bar, parity, r.stop, limit);
 }
 __device__ __forceinline__ void u_arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
 __device__ __forceinline__ void u_commit(uint64_t* bar) {
@@ -210,7 +214,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
     for (int i = 0; i < SLOTS; ++i) { mbar_init(r.full + i, 1); mbar_init(r.empty + i, 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(r.q_full + i, 1); mbar_init(r.q_empty + i, 1); mbar_init(r.s_full + i, 1); mbar_init(r.p_ready + i, 128 * GROUPS); mbar_init(r.pv_done + i, 1); mbar_init(r.seg_sums + i, 128 * GROUPS); mbar_init(r.seg_pv + i, 1); mbar_init(r.seg_free + i, 128); }
     mbar_init(r.drain, 1); mbar_init(r.drain + 1, 1);
-    r.abort = 0;
+    r.stop[0] = r.stop[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 2) {
@@ -584,7 +588,10 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
           }
         }
         if (i >= PB && !dead && !u_wait(r.pv_done + ((i - PB) & 1), ((i - PB) >> 1) & 1, r, limit)) dead = true;      // the buffer's last product
-        if (t == 0 && g == 0) *(volatile int*)(r.keep + (i & 1)) = keep;      // (only now: before that product was issued, tile i - 2's word was still to be read)
+        if (t == 0 && g == 0) {
+          *(volatile int*)(r.keep + (i & 1)) = keep;      // (only now: before that product was issued, tile i - 2's word was still to be read)
+          *(volatile int*)(r.stop + 1) = i + 1;
+        }
         {
           char* const at = p_s + (i % PB) * S::P_BYTES + (t >> 6) * (N * 256) + (t & 7) * 2 + c0 * 128;
           const uint32_t piece = (uint32_t)((t >> 3) & 7) << 4;
@@ -644,7 +651,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
       if (!dead && !u_wait(r.seg_pv + sb, (seg >> 1) & 1, r, limit)) dead = true;
       u_after();
       // (a group that gave up goes on without waiting, so the rest may have come from nothing: it said so before)
-      const float b = u_any(GROUPS, dead || *(volatile int*)&r.abort) ? -2.f : r.end_bad[sb] ? -1.f : 0.f;
+      const float b = u_any(GROUPS, dead || *(volatile int*)r.stop) ? -2.f : r.end_bad[sb] ? -1.f : 0.f;
       const uint32_t st = at.s.status | status_of(b);
       const bool partial = head || tail;
       float* const part = p.part + (number * 2 + (head ? 0 : 1)) * (int64_t)PART<N, DP>;

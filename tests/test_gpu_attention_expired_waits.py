@@ -53,3 +53,25 @@ def test_rows_given_up_on_are_told(dtype, Q, G, D, page):
     finally:
         P.set_wait_limit(0)
     assert ran_out > 0
+
+
+@pytest.mark.parametrize("dtype,Q,G,D", [(BF16, 1, 4, 128), (BF16, 7, 4, 128), (BF16, 2, 2, 64), (BF16, 1, 2, 64), (F32, 1, 2, 64)])
+def test_the_limit_is_a_tiles_not_a_sequences(dtype, Q, G, D):
+    """Eight sequences of four million positions on pages that they share: a worker has more than a thousand tiles of one, milliseconds of work, under a limit of a
+    quarter of a millisecond, some hundred times what a tile takes."""
+    page, n_pages, n = 128, 64, 1 << 22
+    g = torch.Generator(device=DEV).manual_seed(D)
+    q = torch.randn((8, Q, G, D), generator=g, device=DEV).to(dtype)
+    k, v = (torch.randn((n_pages, page, 1, D), generator=g, device=DEV).to(dtype) for _ in range(2))
+    table = torch.randint(0, n_pages, (8, n // page), generator=g, device=DEV, dtype=torch.int32)
+    length = torch.tensor([n - 5 * b for b in range(8)], dtype=torch.int32, device=DEV)
+    want = P.paged_attention(q, k, v, table, length)
+    assert P.check() == 0
+    try:
+        P.set_wait_limit(500000)
+        got = P.paged_attention(q, k, v, table, length)
+        assert P.set_wait_limit(0) == 500000
+    finally:
+        P.set_wait_limit(0)
+    assert P.check() == 0 and int(got[2].abs().max()) == 0
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
