@@ -71,6 +71,7 @@ template <typename E, int DP, int NW_> struct Shape {
   static constexpr int MOST = NW == 8 ? 24 : 4 * NW, STAGES = FIT < MOST ? FIT : MOST;
   static constexpr int SMEM = WORKERS * (STAGES * (STAGE + 8) + Q_BYTES) + (int)sizeof(LineShared<THREADS>) + 1024;
   static_assert(STAGES >= 2 && STAGES < 32 && SMEM <= 227 * 1024, "a block's shared memory");
+  static_assert(2 * SMEM > 227 * 1024, "one block on each SM");
 };
 // 16-byte piece j of row r in a slab layout with `rows` rows a slab: eight pieces of a row are swizzled by the row, as TMA lays them down
 template <int ROWS> __device__ __forceinline__ uint32_t piece_at(int r, int j) { return (uint32_t)((j >> 3) * (ROWS * 128) + r * 128 + (((j & 7) ^ (r & 7)) << 4)); }
@@ -564,7 +565,7 @@ template <typename E, int ROWS, int DP> __global__ void __launch_bounds__(256) a
   }
 }
 
-constexpr int MAX_WORKERS = 8 * 148;  // of a call
+constexpr int MAX_SMS = 148, MAX_WORKERS = 8 * MAX_SMS;  // of a call
 
 struct Kernel { const void *tma, *plain; int rows, dp, t, smem, workers, threads; };
 template <typename E, int DP, int NW> Kernel kernel() {
@@ -584,7 +585,6 @@ template <typename E> Kernel pick(const saki_attn_in& in) {
   return in.D <= 64 ? pick<E, 64>(R) : in.D <= 128 ? pick<E, 128>(R) : pick<E, 256>(R);
 }
 Kernel pick(const saki_attn_in& in) { return in.dtype == SAKI_BF16 ? pick<__nv_bfloat16>(in) : pick<float>(in); }
-int64_t part_floats(const Kernel& k) { return (int64_t)k.rows * (k.dp + 2); }
 
 template <typename E, int DP> cudaError_t join(const AttnParams& p, int rows, int workers, cudaStream_t st) {
   // a warp for some four partials: as many as a segment of average length has
@@ -658,10 +658,11 @@ static bool on_umma(const saki_attn_in& in) {
 }
 
 int64_t attention_scratch_bytes(const saki_attn_in& in) {
+  // (a block on each SM; where tcgen05 serves the call the other kernel still has to find room, should the tensor maps be refused)
   const Kernel k = pick(in);
-  int64_t most = MAX_WORKERS * 2 * part_floats(k);
-  if (on_umma(in)) most = std::max<int64_t>(most, MAX_WORKERS / 8 * 2 * (int64_t)umma_rows(in) * (k.dp + 2));
-  return MAX_WORKERS * 24 + most * 4;
+  int64_t rows = (int64_t)k.workers * k.rows;      // with partial results, of a block
+  if (on_umma(in)) rows = std::max<int64_t>(rows, umma_rows(in));
+  return MAX_WORKERS * 24 + MAX_SMS * 2 * rows * (k.dp + 2) * 4;
 }
 
 cudaError_t launch_attention(const saki_attn_in& in, const saki_attn_out& out, void* scratch, unsigned long long* flagged, long long wait_limit,
@@ -697,22 +698,22 @@ cudaError_t launch_attention(const saki_attn_in& in, const saki_attn_out& out, v
       k_map = k5; v_map = v5; p.map_mode = mode;
     }
   }
-  int dev = 0, sms = 148, per = 1, workers = 0;
+  int dev = 0, sms = MAX_SMS, workers = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
+  sms = std::min(sms, MAX_SMS);
   if (umma) { k.rows = umma_rows(in); k.t = UMMA_T; }
   p.RB = (p.R + k.rows - 1) / k.rows;
   const int64_t most = in.B * in.H * p.RB * (((int64_t)in.max_pages * in.page_size + k.t - 1) / k.t);      // tiles, if every table were full
   if (umma) {
-    workers = (int)std::min<int64_t>(most, std::min(sms, MAX_WORKERS / 8));
+    workers = (int)std::min<int64_t>(most, sms);
     e = launch_umma(p, k_map, v_map, workers, st);
   } else {
     const void* const fn = tma ? k.tma : k.plain;
     e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, fn, k.threads, k.smem);
     if (e != cudaSuccess) return e;
-    const int blocks = (int)std::min<int64_t>(most, std::min(sms * std::max(per, 1), MAX_WORKERS / k.workers));
+    const int blocks = (int)std::min<int64_t>(most, sms);
     workers = blocks * k.workers;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3((unsigned)k.threads); cfg.dynamicSmemBytes = (size_t)k.smem; cfg.stream = st;
