@@ -343,21 +343,13 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
         l[0] *= a0; l[1] *= a1;
         m[0] = top[0]; m[1] = top[1];
       }
-      if (is_far(shift[0]) || is_far(shift[1])) {
-#pragma unroll
-        for (int e = 0; e < NT; ++e)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) s[e][k] = far_exponent(s[e][k], p.c, shift[k >> 1]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < NT; ++e)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) s[e][k] = fmaf(s[e][k], p.c, -shift[k >> 1]);
-      }
 #pragma unroll
       for (int e = 0; e < NT; ++e)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { s[e][k] = ex2f(s[e][k]); l[k >> 1] += s[e][k]; }
+        for (int k = 0; k < 4; ++k) {
+          s[e][k] = ex2f(cut_exponent(fmaf(s[e][k], p.c, -shift[k >> 1])));
+          l[k >> 1] += s[e][k];
+        }
     }
     // the weights times the values
     if (edge && p.in.Q > 1) {      // some rows do not see all of the tile: a value that is not finite must not reach those as 0 * inf

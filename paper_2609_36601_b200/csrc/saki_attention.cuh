@@ -155,16 +155,11 @@ __device__ __forceinline__ void add_status(const AttnParams& p, int64_t b, uint3
 template <int ROWS, int DP> constexpr int PART = ROWS * (DP + 2);
 __device__ __forceinline__ uint32_t status_of(float l) { return l == -1.f ? SAKI_ROW_BAD_PAGE : l == -2.f ? SAKI_ROW_TIMEOUT : 0u; }
 
-// The exponent of a weight is f(s) - m with an f of the score alone, so that equal scores weigh the same in every tile, whatever the maximum was taken to be by
-// then: f(s) = c s, unrounded (one fused operation), where |c s| < 2^24, and c s rounded downwards beyond, where what the rounding takes away is a unit and more (the scores are no
-// closer than that themselves, and unrounded the largest could pass what a weight may be).  m is rounded downwards: the largest weight is 1 to 2.
-// Where |m| is well below 2^24, scores beyond it weigh 0 by either rule, and nothing has to be compared.
-constexpr float FAR_SCORE = 16777216.f;
-__device__ __forceinline__ bool is_far(float m) { return !(fabsf(m) < FAR_SCORE - 256.f); }
-__device__ __forceinline__ float far_exponent(float s, float c, float m) {
-  const float t = __fmul_rd(s, c);
-  return fabsf(t) < FAR_SCORE ? fmaf(s, c, -m) : t - m;
-}
+// The exponent of a weight is c s - m in one fused operation, whatever tile it is in and whatever the maximum was taken to be by then: equal scores weigh the same.  m is the
+// largest c s rounded downwards, so the largest exponent is what the rounding took away: below 1 for |c s| < 2^24, up to 64 for 2^30, where a step of the score itself is 64 and more.
+// Beyond that it is cut, for the sums' sake: scores that equal the largest still weigh the same, and one a step of float32 below it may weigh as much.  (NaN stays.)
+constexpr float MOST_EXPONENT = 64.f;
+__device__ __forceinline__ float cut_exponent(float x) { return x > MOST_EXPONENT ? MOST_EXPONENT : x; }
 
 // what a row sees: positions up to `to`, from `from` on or below `first`
 struct Sight {

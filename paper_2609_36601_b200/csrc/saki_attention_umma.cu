@@ -420,7 +420,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
     };
     Cursor<UT> now;
     u_at(p, now, r.line.b[0], u0 - r.line.before[0]);
-    bool dead = false, fresh = true, far = false;          // no tile of the segment so far; a maximum is beyond FAR_SCORE: then all tiles are `exact`
+    bool dead = false, fresh = true;          // no tile of the segment so far
     float l[CW], bad = 0.f;
     int seg = 0, my_query = 0;
 #pragma unroll 1
@@ -441,7 +441,6 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
 #pragma unroll
           for (int n = 0; n < CW; ++n) l[n] = 0.f;
           bad = 0.f;
-          far = false;
           u_sync(g);
         }
         if (!dead && !u_wait(r.s_full + (i & 1), (i >> 1) & 1, r, limit)) dead = true;
@@ -465,11 +464,12 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
           }
         };
         float big = 0.f;
-        bool exact = (fresh && edge) || far;
+        bool exact = fresh && edge;
         auto weights = [&] {
-          // (a maximum beyond FAR_SCORE: `exact` from here on, tile by tile.  Without maxima that large the two forms are the same)
-          if (exact) by_four(m_s, [&](int n, float m) { w[n] = far_exponent(w[n], p.c, m); far = far || (is_far(m) && m != NOTHING); });
-          else by_four(m_s, [&](int n, float m) { w[n] = fmaf(w[n], p.c, -m); });
+          by_four(m_s, [&](int n, float m) { w[n] = fmaf(w[n], p.c, -m); });
+          if (exact)               // (elsewhere a weight beyond 2^8 leads here)
+#pragma unroll
+            for (int n = 0; n < CW; ++n) w[n] = cut_exponent(w[n]);
 #pragma unroll
           for (int n = 0; n < CW; ++n) { w[n] = ex2f(w[n]); big = fmaxf(big, w[n]); }
         };
@@ -510,11 +510,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
 #pragma unroll
             for (int k = 0; k < CW / 4; ++k) {
               const float top = u_warp_max(q4 == 0 ? w[k] : q4 == 1 ? w[CW / 4 + k] : q4 == 2 ? w[CW / 2 + k] : w[3 * CW / 4 + k]);
-              if (lane == k) {
-                const float m = fmaxf(NOTHING, __fmul_rd(top, p.c));
-                m_s[q4 * (CW / 4) + k] = m;
-                if (is_far(m)) big = CUDART_INF_F;      // once more, exact
-              }
+              if (lane == k) m_s[q4 * (CW / 4) + k] = fmaxf(NOTHING, __fmul_rd(top, p.c));
             }
             u_sync(g);
           }

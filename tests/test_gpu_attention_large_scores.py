@@ -84,3 +84,39 @@ def test_scores_that_are_close(dtype, Q, D, page, first, second, sign):
             ll = base / 8 + float(torch.logsumexp(s[:m], 0))
             # the constant's rounding and the result's own, of 2^20; what the maximum's rounding took away is in the sum
             assert abs(float(lse[b, j, 0]) - ll) <= 3 * 2.0 ** -24 * abs(ll) + 2.0 ** -3
+
+
+@pytest.mark.parametrize("dtype,Q,D,page", FORMS)
+@pytest.mark.parametrize("scale", [1.0, 2.0, 4.0, 8.0])
+@pytest.mark.parametrize("first,second", [(0, 1), (1, 0)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_a_step_apart(dtype, Q, D, page, scale, first, second, sign):
+    """Scores of some 2^23 that are a unit, their own last place, apart: times 1 to 8 they lie up to 2^26 from 0, where float32 numbers are 8 apart, and weigh 2.7 to 3000 times
+    what the lower ones do."""
+    lengths = [700, 40, 6000, 1025]
+    q, k, v, table, length = _make(4, Q, 2, 2, D, page, lengths, dtype, 7)
+    q.zero_(); k.zero_()
+    q[..., :32], q[..., 32] = 64.0, 1.0
+    k[..., :31], k[..., 31] = sign * 4096.0, sign * 4032.0
+    for b, n in enumerate(lengths):
+        for x in range(n):
+            k[int(table[b, x // page]), x % page, :, 32] = float(second if (x // 200) % 2 else first)
+    base = sign * 64 * (31 * 4096 + 4032)
+    out, lse, st = P.paged_attention(q, k, v, table, length, scale=scale)
+    assert int(st.abs().max()) == 0
+    half = torch.finfo(dtype).eps / 2
+    for b, n in enumerate(lengths):
+        vb = _rows(table, v, b, n, page)
+        s = torch.tensor([float(second if (x // 200) % 2 else first) for x in range(n)], dtype=torch.float64, device=DEV) * scale
+        for j in range(Q):
+            m = n - Q + j + 1
+            w = torch.softmax(s[:m], 0)
+            want = torch.einsum("x,xhd->hd", w, vb[:m]).repeat_interleave(2, 0)
+            size = torch.einsum("x,xhd->hd", w, vb[:m].abs()).repeat_interleave(2, 0)
+            # exponents: 8 log2(e) apart at most, the constant rounded by 2^-24 of itself and each exponent (up to 24: what the maximum's rounding took away is below 8, the lower scores
+            # 12 below) by 2^-24 of itself; powers of two 2^-22; the rest as above
+            share = 2 * (24 * 2.0 ** -23 + 2.0 ** -21 + (2.0 ** -16 if dtype == BF16 else 0)) + 2.0 ** -20 + (m + 4) * 2.0 ** -23
+            err = (out[b, j].double() - want).abs()
+            assert bool((err <= half * (1 + share) * want.abs() + share * size).all()), (b, j, float((err / size).max()))
+            ll = base * scale + float(torch.logsumexp(s[:m], 0))
+            assert abs(float(lse[b, j, 0]) - ll) <= 4 * 2.0 ** -24 * abs(ll)
