@@ -417,7 +417,7 @@ SAKI_API int saki_cache_compact(const saki_cache* cache, int32_t* copy_src, int3
                                 void* cuda_stream);
 
 /* Page src[i] to page dst[i], i < n, in every one of n_pools pools (HOST arrays of device pointers, byte strides between pages
- * and bytes per page; a page is one run of bytes).  Pairs with an id outside [0, n_pages) are passed over.  No page may be
+ * and bytes per page; a page is one run of bytes: where it is several, each of them is a pool here).  Pairs with an id outside [0, n_pages) are passed over.  No page may be
  * both read and written, or written twice (the lists of saki_cache_reserve and saki_cache_compact never do). */
 SAKI_API int saki_cache_copy_pages(void* const* pools, const int64_t* page_stride, const int64_t* page_bytes, int32_t n_pools,
                                    const int32_t* src, const int32_t* dst, int64_t n, int32_t n_pages, void* cuda_stream);

@@ -535,7 +535,8 @@ def cache_compact(cache, stream=None):
 
 
 def copy_pages(pools, copy_src, copy_dst, stream=None):
-    """saki_cache_copy_pages: page copy_src[i] to page copy_dst[i] (int32; -1: none) in every pool of the sequence `pools`."""
+    """saki_cache_copy_pages: page copy_src[i] to page copy_dst[i] (int32; -1: none) in every pool of the sequence `pools`,
+    tensors [n_pages, ...] of any strides.  (64 runs of memory go into a launch: a page is one, unless heads or positions are outermost or its rows lie apart.)"""
     (_fast or _tensors()).copy_pages(pools, copy_src, copy_dst, _handle(stream))
 
 

@@ -558,18 +558,26 @@ PyObject* py_cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// bytes of a page, if a page of the pool is one run of bytes
-int64_t page_bytes(const at::Tensor& t) {
+// The runs of memory that a page of the pool is made of: where each starts within the page, in elements, and the elements of one.  (In most layouts there is one; heads or
+// positions outermost, or rows with something between them, make several.)
+int64_t page_runs(const at::Tensor& t, std::vector<int64_t>& starts) {
   std::vector<std::pair<int64_t, int64_t>> dims;
   for (int64_t d = 1; d < t.dim(); ++d)
     if (t.size(d) != 1) dims.emplace_back(t.stride(d), t.size(d));
   std::sort(dims.begin(), dims.end());
   int64_t run = 1;
-  for (const auto& d : dims) {
-    if (d.first != run) raise_value("a page of a pool must be one run of memory");
-    run *= d.second;
+  size_t k = 0;
+  for (; k < dims.size() && dims[k].first == run; ++k) run *= dims[k].second;
+  starts.assign(1, 0);
+  int64_t upto = run;              // elements that the page spans so far
+  for (; k < dims.size(); ++k) {
+    const int64_t stride = dims[k].first, n = dims[k].second, have = (int64_t)starts.size();
+    if (stride < upto) raise_value("the elements of a pool's page must not overlap");
+    for (int64_t i = 1; i < n; ++i)
+      for (int64_t r = 0; r < have; ++r) starts.push_back(starts[(size_t)r] + i * stride);
+    upto += (n - 1) * stride;
   }
-  return run * (int64_t)t.element_size();
+  return run;
 }
 // copy_pages(pools, copy_src, copy_dst, stream)
 PyObject* py_copy_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -583,20 +591,24 @@ PyObject* py_copy_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const OnStream on(dev, a[3]);
     packed(a[1], at::kInt, src.numel(), dev, "copy_src");
     const at::Tensor& dst = packed(a[2], at::kInt, src.numel(), dev, "copy_dst");
-    std::vector<void*> pool((size_t)m);
-    std::vector<int64_t> step((size_t)m), bytes((size_t)m);
+    std::vector<void*> pool;         // a run of the pages of a pool each
+    std::vector<int64_t> step, bytes, starts;
     int64_t pages = 0;
     for (int i = 0; i < m; ++i) {
       const at::Tensor& t = tensor(PySequence_Fast_GET_ITEM(seq.p, i));
       if (t.device() != dev || t.dim() < 2 || t.numel() == 0) raise_value("a pool must be a tensor [n_pages, ...] on the lists' device");
       if (i == 0) pages = t.size(0);
       if (t.size(0) != pages || pages > INT32_MAX) raise_value("the pools of a call have the same number of pages");
-      pool[(size_t)i] = t.data_ptr();
-      bytes[(size_t)i] = page_bytes(t);
-      step[(size_t)i] = pages > 1 ? t.stride(0) * (int64_t)t.element_size() : bytes[(size_t)i];
+      const int64_t size = (int64_t)t.element_size(), run = page_runs(t, starts) * size;
+      for (int64_t at : starts) {
+        pool.push_back((char*)t.data_ptr() + at * size);
+        bytes.push_back(run);
+        step.push_back(pages > 1 ? t.stride(0) * size : run);
+      }
     }
+    if (pool.size() > (size_t)INT32_MAX) raise_value("too many pools");
     check_rc(unlocked([&] {
-      return lib.cache_copy_pages(pool.data(), step.data(), bytes.data(), m, (const int32_t*)src.data_ptr(), (const int32_t*)dst.data_ptr(), src.numel(), (int32_t)pages, on.handle);
+      return lib.cache_copy_pages(pool.data(), step.data(), bytes.data(), (int32_t)pool.size(), (const int32_t*)src.data_ptr(), (const int32_t*)dst.data_ptr(), src.numel(), (int32_t)pages, on.handle);
     }));
     Py_RETURN_NONE;
   });
