@@ -528,10 +528,11 @@ def cache_fork(cache, parent, group=None, stream=None):
     return (_fast or _tensors()).cache_fork(*cache._args(), parent, max(1, cache.B) if group is None else group, _handle(stream))
 
 
-def cache_compact(cache, stream=None):
-    """saki_cache_compact: the used pages move to the lowest ids.  Returns (copy_src, copy_dst, n_moves): pass the lists to
-    copy_pages before the cache is used again."""
-    return (_fast or _tensors()).cache_compact(*cache._args(), _handle(stream))[:3]
+def cache_compact(cache, stream=None, return_status=False):
+    """saki_cache_compact: the used pages move to the lowest ids.  Returns (copy_src, copy_dst, n_moves), with return_status row_status
+    (int32 [B]) behind them: pass the lists to copy_pages before the cache is used again."""
+    found = (_fast or _tensors()).cache_compact(*cache._args(), _handle(stream))
+    return found if return_status else found[:3]
 
 
 def copy_pages(pools, copy_src, copy_dst, stream=None):
