@@ -443,8 +443,8 @@ SAKI_API int saki_cache_write(const saki_cache* cache, const saki_cache_kv* kv, 
  *     s_x = scale <q, k_x>,  lse = log sum_x exp(s_x),  out = sum_x exp(s_x - lse) v_x
  * A query that sees nothing (p < 0, j >= n), or no score above -inf: out 0, lse -inf.  Keys and values of positions that a query does not
  * see have no influence, whatever they hold; non-finite ones that it sees make its output non-finite.  bf16: products on the tensor cores,
- * sums, maxima and exponentials in float32, the weights in two bf16 terms (16 bits); f32: factors in two tf32 terms (22 bits), all else in
- * float32.  A sequence with a length outside
+ * sums, maxima and exponentials in float32, the weights in two bf16 terms (16 bits); f32: factors in two tf32 terms (22 bits; numbers
+ * from 3.402e38 on may count as infinite where they are seen), all else in float32.  A sequence with a length outside
  * [0, max_pages * page_size], or n outside [0, Q], is flagged BAD_LENGTH, one with an id outside the pool among the pages that its
  * queries see BAD_PAGE, one for which a wait ran out (saki_set_wait_limit) TIMEOUT: out 0, lse -inf (TIMEOUT:
  * in the heads that were late).  A sequence whose in->row_status (of saki_cache_reserve) has a flag, and whose new positions therefore are not there, has out 0, lse -inf and that flag

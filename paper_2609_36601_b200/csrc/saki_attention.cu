@@ -13,7 +13,7 @@
 // This file's kernel runs the products on mma.sync with float32 accumulators, query rows in groups of 16: float32, bf16 heads above 128 and up to 16, pages that are no whole
 // eights, and single tokens of few rows with small heads or little to see (`on_umma`); all other bf16 calls go to saki_attention_umma.cu.  bf16: m16n8k16; the weights go into the second product as two bf16 terms, so that they carry 16 bits: one
 // term would add an error as large as the rounding of the output (2^-9 each).  f32: m16n8k8 on tf32 terms, x = hi + lo with 11 bits each and
-// hi.hi + hi.lo + lo.hi: what is dropped is 2^-22 of a product and less.
+// hi.hi + hi.lo + lo.hi: what is dropped is 2^-21 of a product and less, of either sign.
 // What bounds it: the latency of a tile's chain of small products at two warps a scheduler.  bf16, heads of 64, 96 sequences of 8000 positions, 5 rows: 309 us, 5.1 TB/s (78 %
 // of the measured copy rate); 96 windows of 1024: 59 us.  f32, heads of 80, 24 sequences of 15000 positions, 3 rows: 217 us, 3.2 TB/s (49 %), of up to 3001, 9 rows: 65 us (some
 // 1400 instructions a warp and tile of 16 positions, half of them the splitting into terms and their products; 251 registers, so eight warps).
@@ -52,7 +52,15 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], 
   asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// x as two tf32 terms: the upper 11 bits, and the rest (exact) with half a unit added, as the product cuts it to 11 bits: 22 bits, rounded
+// x as two tf32 terms.  The first factor of a product (queries, weights): the nearest number of 11 bits and the rest, of either sign and at most 2^-11 of x, of which the product keeps 11 bits
+// (2^-23 of x is cut).  Numbers from (2 - 2^-11) 2^127 on become infinite.
+__device__ __forceinline__ void two_nearest(uint32_t x, uint32_t& hi, uint32_t& lo) {
+  hi = (x + 0x1000u) & 0xffffe000u;
+  lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi));
+}
+// The second (keys, values, which may hold the largest numbers where some rows do not look): the upper 11 bits, and the rest (exact, below 2^-10 of x) with half a unit added, as the product cuts
+// it to 11 bits: 2^-22 of x.  With both factors split like this what is dropped, lo.lo, would be up to 2^-20 and always of the product's sign (the error against 64 bits 6.7e-7 where it is 5.4e-7; a
+// plain float32 form has 6.0e-7).
 __device__ __forceinline__ void two_terms(uint32_t x, uint32_t& hi, uint32_t& lo) {
   hi = x & 0xffffe000u;
   lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) + 0x1000u;
@@ -300,7 +308,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
         uint32_t q[4], qh[4], ql[4];
         if constexpr (!S::Q_REGS) ldm4(q, pair_at<S::ROWS>(q_l, k));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) two_terms(S::Q_REGS ? q_r[S::Q_REGS ? k : 0][e] : q[e], qh[e], ql[e]);
+        for (int e = 0; e < 4; ++e) two_nearest(S::Q_REGS ? q_r[S::Q_REGS ? k : 0][e] : q[e], qh[e], ql[e]);
 #pragma unroll
         for (int e = 0; e < NT; ++e) {
           uint32_t kf[2], kh[2], kl[2];
@@ -418,7 +426,7 @@ __global__ void __launch_bounds__(Shape<E, DP, NW>::THREADS) attn_kernel(const _
 #pragma unroll
       for (int e = 0; e < NT; ++e)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) two_terms(__float_as_uint(s[e][(k & 1) * 2 + (k >> 1)]), wh[e][k], wl[e][k]);
+        for (int k = 0; k < 4; ++k) two_nearest(__float_as_uint(s[e][(k & 1) * 2 + (k >> 1)]), wh[e][k], wl[e][k]);
       const uint32_t v_0 = (uint32_t)(t0 * 128 + (((dc >> 2) ^ t0) << 4)), v_1 = (uint32_t)((t0 + 1) * 128 + (((dc >> 2) ^ (t0 + 1)) << 4));
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
