@@ -21,7 +21,6 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
-#include <mutex>
 
 namespace saki {
 
@@ -602,21 +601,9 @@ template <typename E> cudaError_t join(const AttnParams& p, const Kernel& k, int
   return k.dp == 64 ? join<E, 64>(p, k.rows, workers, st) : k.dp == 128 ? join<E, 128>(p, k.rows, workers, st) : join<E, 256>(p, k.rows, workers, st);
 }
 
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeFn encode() {
-  static EncodeFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess) fn = (EncodeFn)f;
-  });
-  return fn;
-}
 // a pool [n_pages, page_size, H, D]: boxes of 128 bytes by `box` positions of one head and page, zeros behind D
 bool pool_map(CUtensorMap* map, const void* pool, int64_t page, int64_t pos, int64_t head, const saki_attn_in& in, int box) {
-  const EncodeFn fn = encode();
+  const EncodeTiledFn fn = encode_fn();
   const int64_t size = in.dtype == SAKI_BF16 ? 2 : 4, row = (in.D * size + 15) & ~15ll;
   auto step = [&](int64_t s, int64_t n) { return (cuuint64_t)(n > 1 ? s * size : row); };      // (of a dimension of one: never used)
   const cuuint64_t dims[4] = {(cuuint64_t)in.D, (cuuint64_t)in.H, (cuuint64_t)in.page_size, (cuuint64_t)in.n_pages};
@@ -628,7 +615,7 @@ bool pool_map(CUtensorMap* map, const void* pool, int64_t page, int64_t pos, int
 
 // ... as `mode` sees it (bf16, D = 128)
 bool eights_map(CUtensorMap* map, const void* pool, int64_t page, int64_t pos, int64_t head, const saki_attn_in& in, int box, int mode) {
-  const EncodeFn fn = encode();
+  const EncodeTiledFn fn = encode_fn();
   const cuuint64_t eights = (cuuint64_t)in.page_size / 8, pages = (cuuint64_t)in.n_pages, H = (cuuint64_t)in.H;
   auto step = [](int64_t s, cuuint64_t n) { return (cuuint64_t)(n > 1 ? s * 2 : 256); };      // (of a dimension of one: never used)
   const cuuint64_t c4 = mode == MAP_HEADS ? pages : mode == MAP_PAGES ? pages * H : H;

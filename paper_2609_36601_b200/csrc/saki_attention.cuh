@@ -1,10 +1,9 @@
 // What the attention kernels share: the line of tiles and its pieces, what a query sees, how results are written or left to be joined.
 #pragma once
 #include "saki_device.cuh"
-#include <cuda.h>
+#include "saki_tensor_map.cuh"
 #include <algorithm>
 #include <cmath>
-#include <mutex>
 
 namespace saki {
 

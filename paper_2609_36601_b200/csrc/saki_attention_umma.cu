@@ -452,8 +452,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
         // in front of some rows, behind others
         const bool partly = edge && !hidden && !(now.s.nq == p.in.Q && x <= now.s.p0 && (p.in.window <= 0 || x > now.s.n - 1 - p.in.window || x < sinks));
         auto scores = [&] {
-#pragma unroll
-          for (int n = 0; n < CW; n += CW) u_ld<CW>(tmem + lanes + (i & 1) * N + c0 + n, w + n);
+          u_ld<CW>(tmem + lanes + (i & 1) * N + c0, w);
           if (hidden) {
 #pragma unroll
             for (int n = 0; n < CW; ++n) w[n] = -CUDART_INF_F;
@@ -546,15 +545,13 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
               } else if (!dead && !u_wait(r.seg_free + (seg & 1), ((seg >> 1) & 1) ^ 1u, r, limit)) dead = true;
               u_after();
               keep = fresh;
-#pragma unroll 1
-              for (int n0 = 0; n0 < CW; n0 += CW) {
-                const uint32_t o_at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + c0 + n0;
+              {
+                const uint32_t o_at = tmem + lanes + 2 * N + (seg & 1) * 2 * N + c0;
                 float y[CW];
                 if (fresh) {
 #pragma unroll
                   for (int e = 0; e < CW; ++e) y[e] = 0.f;
-#pragma unroll
-                  for (int k = 1; k < 2; ++k) u_st<CW>(o_at + k * N, y);
+                  u_st<CW>(o_at + N, y);
                 } else u_ld<CW>(o_at, y);
                 if (t < DP)
 #pragma unroll 1
@@ -566,7 +563,7 @@ template <int DP, int N, bool GROUPED> __global__ void __launch_bounds__(UShape<
                     if (!(fabsf(z) < CUDART_INF_F))
 #pragma unroll
                       for (int e = 0; e < CW; ++e)
-                        if (xx <= to_s[n0 + e] && (xx >= from_s[n0 + e] || xx < sinks)) y[e] += z;
+                        if (xx <= to_s[e] && (xx >= from_s[e] || xx < sinks)) y[e] += z;
                   }
                 u_st<CW>(o_at, y);
               }

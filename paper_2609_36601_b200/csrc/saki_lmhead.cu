@@ -24,7 +24,7 @@
 // Every wait on an mbarrier is bounded; a wait that runs out sets an error byte, and every role then
 // leaves its loop, tensor memory is released and the kernel returns.
 #include "saki_common.cuh"
-#include <cuda.h>
+#include "saki_tensor_map.cuh"
 #include <math_constants.h>
 #include <algorithm>
 #include <mutex>
@@ -343,22 +343,6 @@ __global__ void lmhead_rows_kernel(const LmParams P, float* row_max, float* lse)
 }
 
 // ---------------------------------------------------------------- host side
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
-      fn = (EncodeTiledFn)p;
-  });
-  return fn;
-}
-
 // a [rows, d] bf16 matrix, d contiguous: boxes of 64 x box_rows elements, 128-byte swizzle, zero fill outside
 static bool make_map(CUtensorMap* map, const void* ptr, int64_t rows, int64_t d, int64_t ld, int box_rows) {
   EncodeTiledFn fn = encode_fn();
