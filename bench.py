@@ -311,7 +311,7 @@ def _rollout(P, dev, stream, peak, steps=20):
     def block():
         _, _, st = P.cache_reserve(cache, Q)
         P.cache_write(cache, nk, nv, k, v, st)
-        P.cache_truncate(cache, keep, of=Q)
+        P.cache_truncate(cache, keep, of=Q, row_status=st)
 
     block()
     graph = torch.cuda.CUDAGraph()

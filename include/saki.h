@@ -406,7 +406,7 @@ SAKI_API int saki_cache_truncate(const saki_cache* cache, const int32_t* keep, i
  * are counted within groups of that many sequences, as saki_beam_select gives them).  Nothing is copied: pages are shared until
  * saki_cache_reserve parts them.  parent -1: the sequence is emptied; other ids outside the group: emptied and BAD_ID.  An id
  * outside the pool among the pages that a row had or takes: BAD_PAGE (it is taken as it is, and counted nowhere); a length
- * outside the table: BAD_LENGTH, read as 0. */
+ * outside the table: BAD_LENGTH, read as 0.  A row that is its own parent stays as it is and is not looked at. */
 SAKI_API int saki_cache_fork(const saki_cache* cache, const int32_t* parent, int64_t group, uint32_t* row_status, void* cuda_stream);
 
 /* The used pages move to the lowest ids: with n used pages, page copy_src[i] (id >= n, ascending) goes to page copy_dst[i] (id < n,
@@ -441,7 +441,7 @@ SAKI_API int saki_cache_write(const saki_cache* cache, const saki_cache_kv* kv, 
  * Appendix K).  Query j of sequence b stands at position p = length[b] - n + j, n = n_query[b] or Q, and sees the positions
  * x <= p, with window > 0 of them only x > p - window and x < sinks.  Per head h (key head h / (Hq / H)):
  *     s_x = scale <q, k_x>,  lse = log sum_x exp(s_x),  out = sum_x exp(s_x - lse) v_x
- * A query that sees nothing (p < 0, j >= n), or no score above -inf: out 0, lse -inf.  Keys and values of positions that a query does not
+ * There is no backward pass.  A query that sees nothing (p < 0, j >= n), or no score above -inf: out 0, lse -inf.  Keys and values of positions that a query does not
  * see have no influence, whatever they hold; non-finite ones that it sees make its output non-finite.  bf16: products on the tensor cores,
  * sums, maxima and exponentials in float32, the weights in two bf16 terms (16 bits); f32: factors in two tf32 terms (22 bits; numbers
  * from 3.402e38 on may count as infinite where they are seen), all else in float32.  A sequence with a length outside

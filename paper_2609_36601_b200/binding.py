@@ -460,7 +460,7 @@ def sample_proposal(s, temperature=1.0, seed=0, row_offset=0, stream=None):
 def beam_select(logits, score, n, temperature=1.0, finished=None, pad=0, stream=None):
     """saki_beam_select: the n best continuations of every group of beams.  logits [B, W, V], score float32 [B, W] (sums of
     log-probabilities so far), finished uint8 [B, W] or None: such a beam goes on with the token `pad` and its own score.  Returns
-    a dict of parent, token (int32 [B, n]), score (float32 [B, n]) and row_status (int32 [B, W])."""
+    a dict of parent, token (int32 [B, n]), score (float32 [B, n]) and row_status (int32 [B, W]).  No gradient."""
     parent, token, best, status = (_fast or _tensors()).beams(logits, score, n, temperature, finished, pad, _handle(stream))
     return {"parent": parent, "token": token, "score": best, "row_status": status}
 
@@ -545,7 +545,8 @@ def paged_attention(q, k_pages, v_pages, page_table, length, scale=None, window=
     """saki_paged_attention: attention of the last Q (n_query[b], int32) positions of every sequence over a paged cache.  q [B, Q, Hq, D],
     pools [n_pages, page_size, H, D] of its type, page_table int32 [B, max_pages], length int32 [B] (a PageCache's), scale 1 / sqrt(D)
     where None; window > 0: only the last `window` positions and the first `sinks` are seen.  Sequences that row_status (of cache_reserve) flags
-    have not got their new positions: out 0, lse -inf.  Returns (out like q, lse float32 [B, Q, Hq], row_status int32 [B])."""
+    have not got their new positions: out 0, lse -inf.  No gradient: what it returns is apart from the graph of its inputs.  Returns (out like q, lse float32
+    [B, Q, Hq], row_status int32 [B])."""
     return (_fast or _tensors()).attention(q, k_pages, v_pages, page_table, length, scale, window, sinks, n_query, out, row_status, _handle(stream))
 
 

@@ -1,7 +1,7 @@
 // Attention of a few new tokens per sequence over a paged key-value cache.
 //
-// Every key and value is read once and meets G * Q query rows (G query heads share a key head, Q new tokens), so up to some 60
-// rows the call is bound by HBM.  The work is therefore laid out by what is read: the visible positions of all sequences, key heads and row
+// Every key and value is read once for all G * Q query rows that meet it (G query heads share a key head, Q new tokens), up to 128 of them (64 on tcgen05, and for float32 heads above 128; more rows are
+// further row blocks, which read it again).  The work is therefore laid out by what is read: the visible positions of all sequences, key heads and row
 // blocks, in tiles of T positions, form one line of tiles that is cut into equal pieces, whatever the lengths are (they are known on
 // the device only).  A piece belongs to one worker: a warp (two or four warps where there are more rows than one holds) with a ring of tiles in
 // shared memory of its own, which it fills by TMA ahead of its products, across the ends of sequences.  No worker waits for another; each row's running maximum, sum
@@ -14,9 +14,10 @@
 // eights, and single tokens of few rows with small heads or little to see (`on_umma`); all other bf16 calls go to saki_attention_umma.cu.  bf16: m16n8k16; the weights go into the second product as two bf16 terms, so that they carry 16 bits: one
 // term would add an error as large as the rounding of the output (2^-9 each).  f32: m16n8k8 on tf32 terms, x = hi + lo with 11 bits each and
 // hi.hi + hi.lo + lo.hi: what is dropped is 2^-21 of a product and less, of either sign.
-// What bounds it: the latency of a tile's chain of small products at two warps a scheduler.  bf16, heads of 64, 96 sequences of 8000 positions, 5 rows: 309 us, 5.1 TB/s (78 %
-// of the measured copy rate); 96 windows of 1024: 59 us.  f32, heads of 80, 24 sequences of 15000 positions, 3 rows: 217 us, 3.2 TB/s (49 %), of up to 3001, 9 rows: 65 us (some
-// 1400 instructions a warp and tile of 16 positions, half of them the splitting into terms and their products; 251 registers, so eight warps).
+// What bounds it: the latency of a tile's chain of small products at two warps a scheduler.  bf16, heads of 64, 96 sequences of 8000 positions, 5 rows, pages of 32
+// positions, one head after the other: 311 us, 5.1 TB/s (77 % of the measured copy rate; 406 where the heads of a position lie side by side, 128 bytes each); 96 windows of 1024: 61 us.  Heads of 256, 64
+// sequences of 4096: 4 rows 560 us (59 %), 28 rows 1131 (29 %: tiles of 16 positions, one warp a scheduler).  f32, heads of 80, 24 sequences of 15000 positions, 3 rows: 217 us, 3.2 TB/s (49 %), heads
+// of 128 381 (44 %; tiles of 8 positions); of up to 3001, 9 rows: 65 us (some 1400 instructions a warp and tile of 16 positions, half of them the splitting into terms and their products; 251 registers, so eight warps).
 #include "saki_attention.cuh"
 #include <algorithm>
 #include <climits>
@@ -635,9 +636,12 @@ bool mode_fits(int mode, int64_t page, int64_t pos, int64_t head, const saki_att
 
 }  // namespace
 
-// bf16 heads of up to 128 on pages of whole eights go to the kernel on tcgen05, but for single tokens of few rows where its tiles of 128 positions cost more than they
-// bring: heads of up to 64 (96 sequences of 8000 positions, 5 rows: 309 us here, 384 there; of 1024: 64 and 78; but two tokens of 8 rows, 4000 positions: 261 and 237),
-// and where nothing sees more than 256 positions (512 sequences of 128 positions, heads of 128: 85 and 101 us; of 256: 140 and 155; of 512: 254 and 233).
+// bf16 heads of up to 128 on pages of whole eights go to the kernel on tcgen05, but for single tokens of up to 16 rows where its tiles of 128 positions cost more than they
+// bring.  (us here and there, 8 key heads, pages of 16 positions.)
+//  - Heads of up to 64: 96 sequences of 8000 positions, 5 rows 328 and 420, 16 rows 335 and 421; of 2000 98 and 130, 105 and 133; of 1000 60 and 83, 68 and 85.  (With the heads of a position
+//    side by side the longest are alike: 418 and 418, 432 and 419; of 1000 75 and 85.)  But two tokens of 8 rows, 4000 positions: 261 and 237.
+//  - Where nothing can see more than 256 positions: heads of 128, 512 sequences of 128 positions, 4 rows 83 and 104, 16 rows 111 and 109; of 256 139 and 156, 167 and 161; of 512 251 and 208.
+//    What a query can see goes by the table's width: lengths are known on the device only.  (512 sequences of 128 positions in wide tables take the 104.)
 static bool on_umma(const saki_attn_in& in) {
   if (in.dtype != SAKI_BF16 || in.D <= 16 || in.D > 128 || in.page_size % 8 != 0) return false;
   const int64_t table = (int64_t)in.max_pages * in.page_size, seen = in.window > 0 ? std::min<int64_t>(table, (int64_t)in.window + in.sinks) : table;

@@ -15,10 +15,10 @@
 //               the output.  (A group is a warp on each scheduler, which issues an instruction in four to six cycles: so few queries, and groups that
 //               share a tile.  Groups that took turns, a tile each, were slower: a tile's keys and values wait twice as long for their turn in the ring.)
 //   the last 4  a thread per column of the output: at a segment's end they divide and write, while the groups go on
-// What bounds it: HBM where segments are long (two to three tiles of 64 KB in flight on an SM): 64 sequences of 4096 positions, 8 key heads of 128, 4 rows each 182 us, 5.9 TB/s (90 % of
-// the measured copy rate), of 8192 with 28 rows 355 us (93 %), 512 of 1024 with 4 rows 354 us (93 %).  The weights' warps where segments end often or rows are many: 512 of 65 to 2048
-// positions with 28 rows 569 us (61 %: the instructions of an edge, some 7 us a segment), 64 of 8192 with 64 rows 600 us (56 %).  One sequence of 131077, 4 key heads:
-// 58 us (71 %: start, two ends and the joining kernel are some 15 of it).
+// What bounds it: HBM where segments are long (two to three tiles of 64 KB in flight on an SM): 64 sequences of 4096 positions, 8 key heads of 128, 4 rows each 179 us, 6.0 TB/s (92 % of
+// the measured copy rate), of 8192 with 28 rows 362 us (91 %), 512 of 1024 with 4 rows 353 us (93 %).  The weights' warps where segments end often or rows are many: 512 of 65 to 2048
+// positions with 28 rows 568 to 590 us from run to run (59 to 61 %: the instructions of an edge, some 7 us a segment), 64 of 8192 with 64 rows 608 us (54 %).  More rows are row blocks of 64, which read keys
+// and values once each: 136 rows 1776 us, on 512 of 65 to 2048 positions 2863.  One sequence of 131077, 4 key heads: 57 us (72 %: start, two ends and the joining kernel are some 15 of it).
 // Every wait is bounded (by the time that no tile is finished): a wait that runs out ends all roles' waits, the segments that are left are flagged, and the block leaves.
 #include "saki_attention.cuh"
 #include <cfloat>

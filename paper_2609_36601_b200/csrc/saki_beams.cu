@@ -2,8 +2,8 @@
 // log-probability of the token.
 //
 // What bounds it: issue slots (60 % of them filled; some 860 instructions a warp and 64 elements a thread, 17 us of exponentials) and the barriers between a slice's phases, not HBM:
-// 64 groups of 8 beams, 151936 bf16 logits each, a quarter of the beams finished, 50 us where the bytes take 24, the joining kernel 8 of it (52 and 59 with four and three blocks an SM
-// instead of five); 1 group of 4 beams 14 us, two launches and the chains of one slice and of the join.
+// 64 groups of 8 beams, 151936 bf16 logits each, a quarter of the beams finished, 50 us where the bytes that are read (not those of finished beams) take 18, the joining kernel 8 of it (52 and 59 with four
+// and three blocks an SM instead of five); none finished 58 where they take 24, float32 70 and 84 where they take 36 and 48; 1 group of 4 beams 14 us, two launches and the chains of one slice and of the join.
 //
 // Within a beam the order of the keys is that of the logits, so a row is read once: a block holds a slice of it in registers, sums
 // its exponentials, and picks the slice's n best logits.  For those, a bar: of the maxima of the 64 groups of four threads the n-th

@@ -4,7 +4,8 @@
 // The integer calls are bound by latency, not by what they read.  Which page a sequence gets depends on all sequences before
 // it and on all pages below, so reserving and compacting are a handful of scans: one cluster of blocks does them in one launch,
 // with cluster barriers where a grid would need further launches (2 to 3 us each): a reservation for 512 sequences over 40000 pages takes 15 us, of which the scans, five waits
-// for L2 and three cluster barriers are nearly all; for 8 sequences over 2048 pages 12.  The write of 512 x 7 positions of 8 heads of 128 takes 11.5 us (29 MB: 4.5 at the copy rate), copies run at it.  Every result is a function of the call's inputs
+// for L2 and three cluster barriers are nearly all; for 8 sequences over 2048 pages 12.  The write of 512 x 7 positions of 8 heads of 128 takes 11.5 us (29 MB: 4.5 at the copy rate), copies run at it where pages are runs of whole 16 bytes (others go byte
+// by byte: 1024 pages of 2160 bytes in 4 pools at 3.2 TB/s; rows apart, 128 runs a page of 32 KB and two launches a pool, at 0.5).  Every result is a function of the call's inputs
 // alone: pages are dealt out by rank, and the only atomics are sums and minima of integers.
 #include "saki_common.cuh"
 #include <cooperative_groups.h>
