@@ -318,6 +318,49 @@ SAKI_API int64_t saki_lmhead_scratch_bytes(int64_t N, int32_t V);
 SAKI_API int saki_lmhead_lse(const saki_lmhead_in* in, void* logits, int64_t ld_l, float* row_max, float* lse,
                              void* scratch, int64_t scratch_bytes, void* cuda_stream);
 
+/* The trainer's objective straight from hidden states and the lm-head's weights, without [N,V] logits or gradients in memory
+ * (Section 3.5 and Appendix K fix the objective; the paper computes it from full-vocabulary logits):
+ *     z = hidden weight^T / temperature,  pi = softmax(z),  L_i = -coef_i log pi_i(tok_i)
+ * (coef, tok) is (1, teacher_top1) where corrected, else (advantage, target), as in saki_route_bwd_from_meta; without `corrected` it is
+ * (advantage, target) everywhere, without `advantage` the coefficient is 1: plain cross entropy.  Products of bf16 on the tensor cores with
+ * float32 sums; the logits are not rounded.  Rows that contribute nothing (mask 0: MASKED; rollout_status unusable: NOT_COMPUTED; an advantage
+ * that is not finite: NONFINITE; a supervised token outside [0,V): BAD_ID) get loss 0, log-probability 0 and lse 0, take part in no product and cost
+ * none.  A row whose log-sum-exp or log-probability is not finite is flagged NONFINITE, with loss 0 and lse NaN; TIMEOUT likewise, where a bounded wait ran out.
+ * All pointers are DEVICE pointers.  Requirements: weight 16-byte aligned, ld_w and d multiples of 8; hidden rows may lie anywhere (16-byte aligned
+ * ones are read faster).  V is any size from 2 on.
+ * scratch: saki_linear_ce_scratch_bytes(N, d, V, backward) bytes, 256-byte aligned, owned by one call at a time. */
+typedef struct {
+  const void* hidden; int64_t ld_h;     /* [N,d] bf16, unit stride along d, row stride in elements */
+  const void* weight; int64_t ld_w;     /* [V,d] bf16 */
+  int64_t N;                            /* 0 .. 2^22 */
+  int32_t d, V;                         /* d 8 .. 2^16, V 2 .. 2^22 */
+  const int32_t* target;                /* [N] the supervised token (where corrected is 0). Required */
+  const float* advantage;               /* [N] or NULL: 1 */
+  const uint8_t* corrected;             /* [N] or NULL: 0 */
+  const int32_t* teacher_top1;          /* [N] the supervised token where corrected is not 0. Required with corrected */
+  const uint8_t* mask;                  /* [N] or NULL */
+  const uint32_t* rollout_status;       /* [N] or NULL */
+  float temperature;                    /* finite, > 0 */
+} saki_linear_in;
+typedef struct {
+  float* loss;          /* [N] or NULL */
+  float* logp_tok;      /* [N] or NULL: log pi(tok) */
+  float* lse;           /* [N] log sum_v exp(z_v). Required; saki_linear_ce_bwd reads it */
+  uint32_t* row_status; /* [N] or NULL */
+} saki_linear_out;
+SAKI_API int64_t saki_linear_ce_scratch_bytes(int64_t N, int32_t d, int32_t V, int backward);
+SAKI_API int saki_linear_ce_fwd(const saki_linear_in* in, const saki_linear_out* out, void* scratch, int64_t scratch_bytes, void* cuda_stream);
+
+/* The gradients of sum_i grad_scale L_i: with G_iv = grad_scale coef_i / temperature (pi_iv - [v = tok_i]),
+ *     dhidden = G weight [N,d] bf16,  dweight = G^T hidden [V,d] bf16
+ * (either may be NULL: not wanted; what is given is overwritten).  `in` is that of the forward call, `lse` what it returned: rows without a finite
+ * one, and those that contribute nothing, have zero rows in dhidden and no part in dweight.  The logits are computed once more, in
+ * pieces of the vocabulary; a piece's G / (grad_scale / temperature) is rounded to bf16 (half a step of each element) and its products are summed in float32.
+ * The probabilities are taken with the float32 log-sum-exp: its rounding, 2^-24 |lse|, is a share of each of them.  dhidden, dweight 16-byte aligned,
+ * strides multiples of 8.  Where a bounded wait ran out both are NaN throughout. */
+SAKI_API int saki_linear_ce_bwd(const saki_linear_in* in, const float* lse, void* dhidden, int64_t ld_dh, void* dweight, int64_t ld_dw, float grad_scale,
+                                void* scratch, int64_t scratch_bytes, void* cuda_stream);
+
 /* Block verification (Section 3.5, Appendix I) of B drafted blocks of K tokens. */
 typedef struct {
   const void* student_logits; /* [B,K+1,V]: position j of sequence b at element offset

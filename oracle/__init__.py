@@ -19,3 +19,5 @@ from .saki_oracle import (  # noqa: F401
 from .rollout_oracle import (  # noqa: F401
     ST_BAD_PAGE, ST_BAD_LENGTH, ST_NO_PAGES, Cache, paged_attention, beam_select,
 )
+
+from .trainer_oracle import distill_top, linear_ce, supervised, top_logits  # noqa: F401

@@ -19,7 +19,7 @@ _fast = None          # the module _saki_torch, bound to the library
 _BOUND = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc", "saki_route_bwd_from_meta", "saki_select_tm",
           "saki_spec_verify", "saki_sample_proposal", "saki_vshard_stage", "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate",
           "saki_cache_fork", "saki_cache_compact", "saki_cache_copy_pages", "saki_cache_write", "saki_paged_attention_scratch_bytes", "saki_paged_attention",
-          "saki_beam_scratch_bytes", "saki_beam_select", "saki_last_error")
+          "saki_beam_scratch_bytes", "saki_beam_select", "saki_linear_ce_scratch_bytes", "saki_linear_ce_fwd", "saki_linear_ce_bwd", "saki_last_error")
 
 SAKI_F32, SAKI_BF16 = 0, 1
 ROW_SATURATED, ROW_EPS_ZERO, ROW_MASKED, ROW_NONFINITE, ROW_BAD_ID, ROW_TIMEOUT, ROW_NOT_COMPUTED = 1, 2, 4, 8, 16, 32, 64
@@ -32,6 +32,7 @@ EXPORTS = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc",
            "saki_lmhead_scratch_bytes", "saki_lmhead_lse",
            "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate", "saki_cache_fork", "saki_cache_compact",
            "saki_cache_copy_pages", "saki_cache_write", "saki_paged_attention_scratch_bytes", "saki_paged_attention", "saki_beam_scratch_bytes", "saki_beam_select",
+           "saki_linear_ce_scratch_bytes", "saki_linear_ce_fwd", "saki_linear_ce_bwd",
            "saki_sample_proposal", "saki_check", "saki_set_kernel", "saki_last_kernel", "saki_last_layout", "saki_last_rowsm_layout", "saki_redo_count",
            "saki_set_spec_early_out", "saki_spec_positions_routed", "saki_solve_evaluations", "saki_set_wait_limit", "saki_set_phase_clock", "saki_phase_cycles",
            "saki_launch_count",
@@ -148,6 +149,16 @@ class SakiBeamOut(C.Structure):
     _fields_ = [("parent", C.c_void_p), ("token", C.c_void_p), ("score", C.c_void_p), ("row_status", C.c_void_p)]
 
 
+class SakiLinearIn(C.Structure):
+    _fields_ = [("hidden", C.c_void_p), ("ld_h", C.c_int64), ("weight", C.c_void_p), ("ld_w", C.c_int64), ("N", C.c_int64), ("d", C.c_int32), ("V", C.c_int32),
+                ("target", C.c_void_p), ("advantage", C.c_void_p), ("corrected", C.c_void_p), ("teacher_top1", C.c_void_p), ("mask", C.c_void_p),
+                ("rollout_status", C.c_void_p), ("temperature", C.c_float)]
+
+
+class SakiLinearOut(C.Structure):
+    _fields_ = [("loss", C.c_void_p), ("logp_tok", C.c_void_p), ("lse", C.c_void_p), ("row_status", C.c_void_p)]
+
+
 def load_library(path: str | None = None):
     """Loads libsaki.so (built in-tree by `python -m paper_2609_36601_b200.build`)."""
     global _lib, _fast
@@ -214,6 +225,12 @@ def load_library(path: str | None = None):
     lib.saki_beam_scratch_bytes.restype = C.c_int64
     lib.saki_beam_select.argtypes = [C.POINTER(SakiBeamIn), C.POINTER(SakiBeamOut), C.c_void_p, C.c_int64, C.c_void_p]
     lib.saki_beam_select.restype = C.c_int
+    lib.saki_linear_ce_scratch_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int]
+    lib.saki_linear_ce_scratch_bytes.restype = C.c_int64
+    lib.saki_linear_ce_fwd.argtypes = [C.POINTER(SakiLinearIn), C.POINTER(SakiLinearOut), C.c_void_p, C.c_int64, C.c_void_p]
+    lib.saki_linear_ce_fwd.restype = C.c_int
+    lib.saki_linear_ce_bwd.argtypes = [C.POINTER(SakiLinearIn), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.saki_linear_ce_bwd.restype = C.c_int
     lib.saki_set_wait_limit.argtypes = [C.c_int64]
     lib.saki_set_wait_limit.restype = C.c_int64
     lib.saki_set_phase_clock.argtypes = [C.c_int]
@@ -426,6 +443,24 @@ def lmhead_lse(hidden, weight, temperature=1.0, logits=None, scratch=None, strea
     _raise(lib, lib.saki_lmhead_lse(C.byref(li), logits.data_ptr(), ld_l, row_max.data_ptr(), lse.data_ptr(),
                                     scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream_ptr(stream)))
     return logits, row_max, lse
+
+
+def linear_ce(hidden, weight, target, advantage=None, corrected=None, teacher_top1=None, mask=None, rollout_status=None, temperature=1.0, stream=None):
+    """saki_linear_ce_fwd: the loss -coef log softmax(hidden @ weight.T / temperature)[tok] of every row, without its logits in memory.
+    hidden [N, d], weight [V, d] bf16, target int32 [N].  (coef, tok) is (1, target), with `advantage` (float32) (advantage, target), and where
+    `corrected` (uint8, with `teacher_top1` int32) is set (1, teacher_top1): pass the metadata of a routing call, its proposals as targets.  Rows with mask 0 or
+    an unusable rollout_status contribute nothing and cost nothing.  Returns a dict of loss, logp_tok, lse (float32 [N]) and row_status (int32 [N])."""
+    loss, logp, lse, status = (_fast or _tensors()).linear(hidden, weight, target, advantage, corrected, teacher_top1, mask, rollout_status, temperature, _handle(stream))
+    return {"loss": loss, "logp_tok": logp, "lse": lse, "row_status": status}
+
+
+def linear_ce_bwd(hidden, weight, target, lse, advantage=None, corrected=None, teacher_top1=None, mask=None, rollout_status=None, temperature=1.0,
+                  grad_scale=1.0, dhidden=True, dweight=True, stream=None):
+    """saki_linear_ce_bwd: the gradients of grad_scale times the sum of linear_ce's losses with respect to `hidden` and `weight`, bf16.  `lse` is what
+    linear_ce returned, the other arguments are those of that call.  dhidden, dweight: a tensor to write to, True (a new one) or None (not wanted).
+    Returns (dhidden, dweight)."""
+    return (_fast or _tensors()).linear_bwd(hidden, weight, target, advantage, corrected, teacher_top1, mask, rollout_status, temperature, lse, grad_scale,
+                                            dhidden, dweight, _handle(stream))
 
 
 def route_host(s, t, proposal, eps, temperature=1.0, seed=0, row_offset=0, mask=None, grad_scale=1.0,

@@ -802,6 +802,77 @@ SAKI_API int saki_beam_select(const saki_beam_in* in, const saki_beam_out* out, 
   return launched(launch_beams(*in, *out, scratch, flagged, (cudaStream_t)cuda_stream), 2, "beam selection kernel launch");
 }
 
+// ---- cross entropy from hidden states ----
+static int linear_size_check(int64_t N, int32_t d, int32_t V) {
+  g_err[0] = 0;
+  if (N < 0 || N > (1 << 22)) return fail(SAKI_ERR_INVALID_ARG, "N must be in [0, 2^22] (got %lld)", (long long)N);
+  if (d < 8 || d > (1 << 16)) return fail(SAKI_ERR_INVALID_ARG, "d must be in [8, 2^16] (got %d)", d);
+  if (V < 2 || V > (1 << 22)) return fail(SAKI_ERR_INVALID_ARG, "V must be in [2, 2^22] (got %d)", V);
+  return SAKI_OK;
+}
+static int linear_check(const saki_linear_in* in) {
+  g_err[0] = 0;
+  if (!in) return fail(SAKI_ERR_INVALID_ARG, "NULL argument struct");
+  const int rc = linear_size_check(in->N, in->d, in->V);
+  if (rc) return rc;
+  if (!(in->temperature > 0.f) || std::isinf(in->temperature)) return fail(SAKI_ERR_INVALID_ARG, "temperature must be finite and > 0");
+  if (in->ld_h < in->d || in->ld_w < in->d) return fail(SAKI_ERR_INVALID_ARG, "row stride smaller than the row");
+  if (in->N == 0) return SAKI_OK;
+  if (!in->hidden || !in->weight || !in->target) return fail(SAKI_ERR_INVALID_ARG, "NULL hidden, weight or target pointer");
+  if (in->corrected && !in->teacher_top1) return fail(SAKI_ERR_INVALID_ARG, "teacher_top1 is required with corrected");
+  if (!aligned(in->weight, 16) || in->ld_w % 8 || in->d % 8) return fail(SAKI_ERR_UNSUPPORTED, "weight must be 16-byte aligned, its row stride and d multiples of 8");
+  return SAKI_OK;
+}
+static int linear_scratch(const saki_linear_in* in, const void* scratch, int64_t bytes, bool backward) {
+  const int64_t need = linear_scratch_bytes(in->N, in->d, in->V, backward);
+  if (!scratch || bytes < need) return fail(SAKI_ERR_INVALID_ARG, "scratch too small: %lld bytes needed", (long long)need);
+  if (!aligned(scratch, 256)) return fail(SAKI_ERR_UNSUPPORTED, "scratch must be 256-byte aligned");
+  return SAKI_OK;
+}
+
+SAKI_API int64_t saki_linear_ce_scratch_bytes(int64_t N, int32_t d, int32_t V, int backward) {
+  return linear_size_check(N, d, V) ? 0 : linear_scratch_bytes(N, d, V, backward != 0);
+}
+
+SAKI_API int saki_linear_ce_fwd(const saki_linear_in* in, const saki_linear_out* out, void* scratch, int64_t scratch_bytes, void* cuda_stream) {
+  int rc = linear_check(in);
+  if (rc) return rc;
+  if (!out) return fail(SAKI_ERR_INVALID_ARG, "NULL argument struct");
+  if (in->N == 0) return SAKI_OK;
+  if (!out->lse) return fail(SAKI_ERR_INVALID_ARG, "NULL lse pointer");
+  if ((rc = linear_scratch(in, scratch, scratch_bytes, false))) return rc;
+  unsigned long long* flagged = nullptr;
+  if ((rc = device_ready(&flagged))) return rc;
+  int launches = 0;
+  const cudaError_t e = launch_linear_fwd(*in, *out, scratch, flagged, std::min<long long>(g_wait_limit.load(), 1LL << 61), &launches, (cudaStream_t)cuda_stream);
+  return launched(e, launches, "cross entropy kernel launch");
+}
+
+SAKI_API int saki_linear_ce_bwd(const saki_linear_in* in, const float* lse, void* dhidden, int64_t ld_dh, void* dweight, int64_t ld_dw, float grad_scale,
+                                void* scratch, int64_t scratch_bytes, void* cuda_stream) {
+  int rc = linear_check(in);
+  if (rc) return rc;
+  if (!dhidden && !dweight) return fail(SAKI_ERR_INVALID_ARG, "NULL dhidden and dweight pointers");
+  if ((dhidden && ld_dh < in->d) || (dweight && ld_dw < in->d)) return fail(SAKI_ERR_INVALID_ARG, "row stride smaller than the row");
+  if (!std::isfinite(grad_scale)) return fail(SAKI_ERR_INVALID_ARG, "grad_scale must be finite");
+  if ((dhidden && (!aligned(dhidden, 16) || ld_dh % 8)) || (dweight && (!aligned(dweight, 16) || ld_dw % 8)))
+    return fail(SAKI_ERR_UNSUPPORTED, "dhidden and dweight must be 16-byte aligned, their row strides multiples of 8");
+  unsigned long long* flagged = nullptr;
+  if (in->N == 0) {                   // no rows: no gradient of the weights
+    if (!dweight) return SAKI_OK;
+    if ((rc = device_ready(&flagged))) return rc;
+    const cudaError_t e = cudaMemset2DAsync(dweight, (size_t)ld_dw * 2, 0, (size_t)in->d * 2, (size_t)in->V, (cudaStream_t)cuda_stream);
+    return e == cudaSuccess ? SAKI_OK : cuda_fail(e, "cudaMemset2DAsync");
+  }
+  if (!lse) return fail(SAKI_ERR_INVALID_ARG, "NULL lse pointer");
+  if ((rc = linear_scratch(in, scratch, scratch_bytes, true))) return rc;
+  if ((rc = device_ready(&flagged))) return rc;
+  int launches = 0;
+  const cudaError_t e = launch_linear_bwd(*in, lse, dhidden, ld_dh, dweight, ld_dw, grad_scale, scratch, std::min<long long>(g_wait_limit.load(), 1LL << 61), &launches,
+                                          (cudaStream_t)cuda_stream);
+  return launched(e, launches, "cross entropy gradient kernel launch");
+}
+
 SAKI_API int saki_check(void* cuda_stream, uint64_t* n_flagged) {
   g_err[0] = 0;
   unsigned long long* flagged = nullptr;

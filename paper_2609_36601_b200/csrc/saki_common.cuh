@@ -272,6 +272,11 @@ cudaError_t launch_attention(const saki_attn_in& in, const saki_attn_out& out, v
                              int* n_launches, cudaStream_t st);
 int64_t beam_scratch_bytes(int64_t B, int32_t W, int32_t V, int32_t n);
 cudaError_t launch_beams(const saki_beam_in& in, const saki_beam_out& out, void* scratch, unsigned long long* flagged, cudaStream_t st);
+int64_t linear_scratch_bytes(int64_t N, int32_t d, int32_t V, bool backward);
+cudaError_t launch_linear_fwd(const saki_linear_in& in, const saki_linear_out& out, void* scratch, unsigned long long* flagged, long long wait_limit, int* n_launches,
+                              cudaStream_t st);
+cudaError_t launch_linear_bwd(const saki_linear_in& in, const float* lse, void* dhidden, int64_t ld_dh, void* dweight, int64_t ld_dw, float grad_scale, void* scratch,
+                              long long wait_limit, int* n_launches, cudaStream_t st);
 int vshard_combine_host(const saki_vshard_in& in, int stage, const double* gathered, double* state, const saki_out& out,
                         bool allow_fast);
 

@@ -39,6 +39,9 @@ struct Lib {
   decltype(&saki_paged_attention) paged_attention;
   decltype(&saki_beam_scratch_bytes) beam_scratch_bytes;
   decltype(&saki_beam_select) beam_select;
+  decltype(&saki_linear_ce_scratch_bytes) linear_ce_scratch_bytes;
+  decltype(&saki_linear_ce_fwd) linear_ce_fwd;
+  decltype(&saki_linear_ce_bwd) linear_ce_bwd;
   decltype(&saki_last_error) last_error;
 };
 Lib lib = {};
@@ -721,6 +724,79 @@ PyObject* py_beams(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// the arguments that both calls of the cross entropy from hidden states begin with: hidden, weight, target, advantage, corrected, teacher_top1, mask, rollout_status, temperature
+constexpr Py_ssize_t LINEAR_ARGS = 9;
+saki_linear_in linear_of(PyObject* const* a) {
+  const at::Tensor &h = tensor(a[0]), &w = tensor(a[1]);
+  if (h.dim() != 2 || w.dim() != 2 || h.size(1) != w.size(1) || h.scalar_type() != at::kBFloat16 || w.scalar_type() != at::kBFloat16 || h.device() != w.device() ||
+      (h.size(1) > 1 && (h.stride(1) != 1 || w.stride(1) != 1)))
+    raise_value("hidden [N, d] and weight [V, d] must be bfloat16 tensors of one device with the same d and unit stride along it");
+  const int64_t N = h.size(0), d = h.size(1), V = w.size(0);
+  if (d > INT32_MAX || V > INT32_MAX) raise_value("sizes out of range");
+  const at::Device dev = h.device();
+  saki_linear_in in = {};
+  in.hidden = h.data_ptr(); in.ld_h = row_stride(h); in.weight = w.data_ptr(); in.ld_w = row_stride(w);
+  in.N = N; in.d = (int32_t)d; in.V = (int32_t)V;
+  in.target = (const int32_t*)packed(a[2], at::kInt, N, dev, "target").data_ptr();
+  if (a[3] != Py_None) in.advantage = (const float*)packed(a[3], at::kFloat, N, dev, "advantage").data_ptr();
+  if (a[4] != Py_None) in.corrected = (const uint8_t*)packed(a[4], at::kByte, N, dev, "corrected").data_ptr();
+  if (a[5] != Py_None) in.teacher_top1 = (const int32_t*)packed(a[5], at::kInt, N, dev, "teacher_top1").data_ptr();
+  if (a[6] != Py_None) in.mask = (const uint8_t*)packed(a[6], at::kByte, N, dev, "mask").data_ptr();
+  if (a[7] != Py_None) in.rollout_status = (const uint32_t*)packed(a[7], at::kInt, N, dev, "rollout_status").data_ptr();
+  in.temperature = (float)number(a[8]);
+  return in;
+}
+at::Tensor linear_scratch(const saki_linear_in& in, bool backward, at::Device dev) {
+  const int64_t bytes = lib.linear_ce_scratch_bytes(in.N, in.d, in.V, backward);
+  if (bytes == 0) raise_saki(SAKI_ERR_INVALID_ARG, lib.last_error());
+  return empty({bytes}, at::kByte, dev);
+}
+// linear(the arguments above..., stream) -> (loss, logp_tok, lse, row_status)
+PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, LINEAR_ARGS + 1);
+    const saki_linear_in in = linear_of(a);
+    const at::Device dev = tensor(a[0]).device();
+    const OnStream on(dev, a[9]);
+    const at::Tensor loss = empty({in.N}, at::kFloat, dev), logp = empty({in.N}, at::kFloat, dev), lse = empty({in.N}, at::kFloat, dev), st = empty({in.N}, at::kInt, dev);
+    const saki_linear_out out = {(float*)loss.data_ptr(), (float*)logp.data_ptr(), (float*)lse.data_ptr(), (uint32_t*)st.data_ptr()};
+    const at::Tensor scratch = linear_scratch(in, false, dev);
+    check_rc(unlocked([&] { return lib.linear_ce_fwd(&in, &out, scratch.data_ptr(), scratch.numel(), on.handle); }));
+    Owned x(THPVariable_Wrap(loss)), y(THPVariable_Wrap(logp)), z(THPVariable_Wrap(lse)), w(THPVariable_Wrap(st));
+    return PyTuple_Pack(4, x.p, y.p, z.p, w.p);
+  });
+}
+// a gradient like `t`: given, made (True), or not wanted (None)
+at::Tensor gradient(PyObject* o, const at::Tensor& t, const char* name) {
+  if (o == Py_None) return at::Tensor();
+  if (o == Py_True) return empty(t.sizes(), t.scalar_type(), t.device());
+  const at::Tensor& g = tensor(o);
+  if (!g.sizes().equals(t.sizes()) || g.scalar_type() != t.scalar_type() || g.device() != t.device() || (g.size(1) > 1 && g.stride(1) != 1))
+    raise_value(std::string(name) + " must have the shape, type and device of what it is the gradient of, with unit stride along d");
+  return g;
+}
+PyObject* wrap_or_none(const at::Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None); }
+// linear_bwd(the arguments above..., lse, grad_scale, dhidden, dweight, stream) -> (dhidden, dweight)
+PyObject* py_linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, LINEAR_ARGS + 5);
+    const saki_linear_in in = linear_of(a);
+    const at::Tensor &h = tensor(a[0]), &w = tensor(a[1]);
+    const at::Device dev = h.device();
+    const OnStream on(dev, a[13]);
+    const float* lse = (const float*)packed(a[9], at::kFloat, in.N, dev, "lse").data_ptr();
+    const float scale = (float)number(a[10]);
+    const at::Tensor dh = gradient(a[11], h, "dhidden"), dw = gradient(a[12], w, "dweight");
+    const at::Tensor scratch = linear_scratch(in, true, dev);
+    check_rc(unlocked([&] {
+      return lib.linear_ce_bwd(&in, lse, dh.defined() ? dh.data_ptr() : nullptr, dh.defined() ? row_stride(dh) : 0, dw.defined() ? dw.data_ptr() : nullptr,
+                               dw.defined() ? row_stride(dw) : 0, scale, scratch.data_ptr(), scratch.numel(), on.handle);
+    }));
+    Owned x(wrap_or_none(dh)), y(wrap_or_none(dw));
+    return PyTuple_Pack(2, x.p, y.p);
+  });
+}
+
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))py_bind, METH_FASTCALL, nullptr},
     {"alloc_outputs", (PyCFunction)(void (*)(void))py_alloc_outputs, METH_FASTCALL, nullptr},
@@ -737,6 +813,8 @@ PyMethodDef methods[] = {
     {"cache_write", (PyCFunction)(void (*)(void))py_cache_write, METH_FASTCALL, nullptr},
     {"attention", (PyCFunction)(void (*)(void))py_attention, METH_FASTCALL, nullptr},
     {"beams", (PyCFunction)(void (*)(void))py_beams, METH_FASTCALL, nullptr},
+    {"linear", (PyCFunction)(void (*)(void))py_linear, METH_FASTCALL, nullptr},
+    {"linear_bwd", (PyCFunction)(void (*)(void))py_linear_bwd, METH_FASTCALL, nullptr},
     {"vshard_local", (PyCFunction)(void (*)(void))py_vshard_local, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_saki_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
