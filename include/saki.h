@@ -318,6 +318,41 @@ SAKI_API int64_t saki_lmhead_scratch_bytes(int64_t N, int32_t V);
 SAKI_API int saki_lmhead_lse(const saki_lmhead_in* in, void* logits, int64_t ld_l, float* row_max, float* lse,
                              void* scratch, int64_t scratch_bytes, void* cuda_stream);
 
+/* Distillation from a teacher's top logits (the paper moves full-vocabulary rows between engines, and names that as what an engine is bound by; a list of the
+ * teacher's k largest logits is what can be kept of a row instead).  Row i has a list of tokens and their teacher logits; an entry with token -1, or with logit -inf, is not there.
+ * With pi = softmax(s / temperature) over the whole row, K the tokens that are there, t their logits / temperature:
+ *   teacher_lse given   w_j = exp(t_j - teacher_lse[i]), and what the list leaves out is one event, with the teacher's mass R = max(1 - sum w, 2^-20) and the student's
+ *                       S = sum of pi outside K (where S is below 2^-1000, because K is all or the rest is masked, the event is left out)
+ *   NULL                w = softmax(t): the list is all there is, no such event; forward only
+ *   forward (reverse 0) L = sum_K w log(w / pi) + R log(R / S)          reverse   L = sum_K pi log(pi / w) + S log(S / R)
+ *   dlogits[i,:] = grad_scale dL/ds[i,:] in the logits' dtype (round to nearest even); w, R are constants of differentiation
+ * A logit of -inf is a masked entry: probability 0, gradient 0.  Flags: MASKED (mask 0; nothing else of the row is looked at), BAD_ID (a token below -1 or from V on, or one that
+ * is there twice), NONFINITE (a student logit that is NaN or +inf, a listed one that is -inf, a row with nothing but -inf; a teacher logit that is NaN or +inf, a teacher_lse that is not
+ * finite): loss 0, lse 0, gradient row 0 in all cases.  A list with nothing there, without teacher_lse: loss 0, gradient 0.
+ * Asynchronous on the stream.  scratch: saki_distill_scratch_bytes(N, k) bytes, 256-byte aligned, owned by one call at a time.  Rows may start anywhere; where gradient rows and logit rows
+ * lie alike within 16 bytes they are written in whole vectors. */
+typedef struct {
+  const void* student_logits; int64_t ld_s;   /* [N,V], unit stride along V, row stride in elements */
+  int64_t N;                                  /* 0 .. 2^31 - 1 */
+  int32_t V, dtype;                           /* V 2 .. 2^22 */
+  const int32_t* token;                       /* [N,k], row stride ld_k */
+  const float* logit;                         /* [N,k], row stride ld_k */
+  int64_t ld_k; int32_t k;                    /* k 1 .. 128 */
+  int32_t reverse;
+  const float* teacher_lse;                   /* [N] log-sum-exp of the teacher's whole row / temperature, or NULL */
+  const uint8_t* mask;                        /* [N] or NULL */
+  float temperature;                          /* finite, > 0 */
+} saki_distill_in;
+typedef struct {
+  float* loss;          /* [N] or NULL */
+  float* lse;           /* [N] or NULL: log-sum-exp of the student's row / temperature */
+  uint32_t* row_status; /* [N] or NULL */
+} saki_distill_out;
+SAKI_API int64_t saki_distill_scratch_bytes(int64_t N, int32_t k);
+/* dlogits [N,V], row stride ld_g, or NULL: the loss alone */
+SAKI_API int saki_distill_top(const saki_distill_in* in, const saki_distill_out* out, void* dlogits, int64_t ld_g, float grad_scale, void* scratch, int64_t scratch_bytes,
+                              void* cuda_stream);
+
 /* The trainer's objective straight from hidden states and the lm-head's weights, without [N,V] logits or gradients in memory
  * (Section 3.5 and Appendix K fix the objective; the paper computes it from full-vocabulary logits):
  *     z = hidden weight^T / temperature,  pi = softmax(z),  L_i = -coef_i log pi_i(tok_i)

@@ -98,7 +98,8 @@ def distill_top(s, token, logit, teacher_lse=None, reverse=False, tau=1.0, mask=
             status[i] = ST_BAD_ID
             continue
         t = logit[i][there] / tau
-        if not np.isfinite(s[i]).all() or not np.isfinite(t).all() or (teacher_lse is not None and not np.isfinite(teacher_lse[i])):
+        if (np.isnan(s[i]).any() or np.isposinf(s[i]).any() or np.isneginf(s[i]).all() or np.isneginf(s[i][ids]).any() or not np.isfinite(t).all()
+                or (teacher_lse is not None and not np.isfinite(teacher_lse[i]))):
             status[i] = ST_NONFINITE
             continue
         z = s[i] / tau
@@ -113,13 +114,13 @@ def distill_top(s, token, logit, teacher_lse=None, reverse=False, tau=1.0, mask=
         outside[ids] = False
         W = w.sum()
         R, T, lT = 0.0, 0.0, 0.0
-        if teacher_lse is not None and outside.any():
+        if teacher_lse is not None and outside.any() and _lse(z[outside]) - lse[i] > -1000 * np.log(2):
             R, lT = max(1.0 - W, LEAST_REST), _lse(z[outside]) - lse[i]
             T = np.exp(lT)
         if reverse:
             rest = lT - np.log(R) if R else 0.0
             loss[i] = (p[ids] * (lp[ids] - lw)).sum() + T * rest
-            g = p * (rest - loss[i])
+            g = np.where(p > 0, p * (rest - loss[i]), 0.0)
             g[ids] = p[ids] * (lp[ids] - lw - loss[i])
         else:
             loss[i] = (w * (lw - lp[ids])).sum() + (R * (np.log(R) - lT) if R else 0.0)

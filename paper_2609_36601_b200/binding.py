@@ -19,7 +19,7 @@ _fast = None          # the module _saki_torch, bound to the library
 _BOUND = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc", "saki_route_bwd_from_meta", "saki_select_tm",
           "saki_spec_verify", "saki_sample_proposal", "saki_vshard_stage", "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate",
           "saki_cache_fork", "saki_cache_compact", "saki_cache_copy_pages", "saki_cache_write", "saki_paged_attention_scratch_bytes", "saki_paged_attention",
-          "saki_beam_scratch_bytes", "saki_beam_select", "saki_linear_ce_scratch_bytes", "saki_linear_ce_fwd", "saki_linear_ce_bwd", "saki_last_error")
+          "saki_beam_scratch_bytes", "saki_beam_select", "saki_linear_ce_scratch_bytes", "saki_linear_ce_fwd", "saki_linear_ce_bwd", "saki_distill_scratch_bytes", "saki_distill_top", "saki_last_error")
 
 SAKI_F32, SAKI_BF16 = 0, 1
 ROW_SATURATED, ROW_EPS_ZERO, ROW_MASKED, ROW_NONFINITE, ROW_BAD_ID, ROW_TIMEOUT, ROW_NOT_COMPUTED = 1, 2, 4, 8, 16, 32, 64
@@ -32,7 +32,7 @@ EXPORTS = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc",
            "saki_lmhead_scratch_bytes", "saki_lmhead_lse",
            "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate", "saki_cache_fork", "saki_cache_compact",
            "saki_cache_copy_pages", "saki_cache_write", "saki_paged_attention_scratch_bytes", "saki_paged_attention", "saki_beam_scratch_bytes", "saki_beam_select",
-           "saki_linear_ce_scratch_bytes", "saki_linear_ce_fwd", "saki_linear_ce_bwd",
+           "saki_linear_ce_scratch_bytes", "saki_linear_ce_fwd", "saki_linear_ce_bwd", "saki_distill_scratch_bytes", "saki_distill_top",
            "saki_sample_proposal", "saki_check", "saki_set_kernel", "saki_last_kernel", "saki_last_layout", "saki_last_rowsm_layout", "saki_redo_count",
            "saki_set_spec_early_out", "saki_spec_positions_routed", "saki_solve_evaluations", "saki_set_wait_limit", "saki_set_phase_clock", "saki_phase_cycles",
            "saki_launch_count",
@@ -159,6 +159,16 @@ class SakiLinearOut(C.Structure):
     _fields_ = [("loss", C.c_void_p), ("logp_tok", C.c_void_p), ("lse", C.c_void_p), ("row_status", C.c_void_p)]
 
 
+class SakiDistillIn(C.Structure):
+    _fields_ = [("student_logits", C.c_void_p), ("ld_s", C.c_int64), ("N", C.c_int64), ("V", C.c_int32), ("dtype", C.c_int32), ("token", C.c_void_p),
+                ("logit", C.c_void_p), ("ld_k", C.c_int64), ("k", C.c_int32), ("reverse", C.c_int32), ("teacher_lse", C.c_void_p), ("mask", C.c_void_p),
+                ("temperature", C.c_float)]
+
+
+class SakiDistillOut(C.Structure):
+    _fields_ = [("loss", C.c_void_p), ("lse", C.c_void_p), ("row_status", C.c_void_p)]
+
+
 def load_library(path: str | None = None):
     """Loads libsaki.so (built in-tree by `python -m paper_2609_36601_b200.build`)."""
     global _lib, _fast
@@ -231,6 +241,10 @@ def load_library(path: str | None = None):
     lib.saki_linear_ce_fwd.restype = C.c_int
     lib.saki_linear_ce_bwd.argtypes = [C.POINTER(SakiLinearIn), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]
     lib.saki_linear_ce_bwd.restype = C.c_int
+    lib.saki_distill_scratch_bytes.argtypes = [C.c_int64, C.c_int32]
+    lib.saki_distill_scratch_bytes.restype = C.c_int64
+    lib.saki_distill_top.argtypes = [C.POINTER(SakiDistillIn), C.POINTER(SakiDistillOut), C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.saki_distill_top.restype = C.c_int
     lib.saki_set_wait_limit.argtypes = [C.c_int64]
     lib.saki_set_wait_limit.restype = C.c_int64
     lib.saki_set_phase_clock.argtypes = [C.c_int]
@@ -461,6 +475,15 @@ def linear_ce_bwd(hidden, weight, target, lse, advantage=None, corrected=None, t
     Returns (dhidden, dweight)."""
     return (_fast or _tensors()).linear_bwd(hidden, weight, target, advantage, corrected, teacher_top1, mask, rollout_status, temperature, lse, grad_scale,
                                             dhidden, dweight, _handle(stream))
+
+
+def distill_top(s, token, logit, teacher_lse=None, reverse=False, temperature=1.0, mask=None, grad_scale=1.0, dlogits=True, stream=None):
+    """saki_distill_top: divergence between a teacher of which a list of top logits is known (top_logits' token int32 and logit float32 [N, k], token -1: no
+    entry) and the student's rows s [N, V], with its gradient.  With `teacher_lse` (float32 [N]) the tokens outside the list are one event, without it the list
+    is all there is.  reverse: KL(student || teacher) instead of KL(teacher || student); needs teacher_lse.  dlogits: a tensor to write to, True (a new
+    one) or None (the loss alone).  Returns (dict of loss, lse of the student's rows, row_status; dlogits)."""
+    loss, lse, status, g = (_fast or _tensors()).distill(s, token, logit, teacher_lse, reverse, temperature, mask, grad_scale, dlogits, _handle(stream))
+    return {"loss": loss, "lse": lse, "row_status": status}, g
 
 
 def route_host(s, t, proposal, eps, temperature=1.0, seed=0, row_offset=0, mask=None, grad_scale=1.0,

@@ -802,6 +802,45 @@ SAKI_API int saki_beam_select(const saki_beam_in* in, const saki_beam_out* out, 
   return launched(launch_beams(*in, *out, scratch, flagged, (cudaStream_t)cuda_stream), 2, "beam selection kernel launch");
 }
 
+// ---- distillation from a teacher's top logits ----
+static int list_size_check(int64_t N, int32_t k) {
+  g_err[0] = 0;
+  if (N < 0 || N > INT32_MAX) return fail(SAKI_ERR_INVALID_ARG, "N must be in [0, 2^31) (got %lld)", (long long)N);
+  if (k < 1 || k > 128) return fail(SAKI_ERR_INVALID_ARG, "k must be in [1,128] (got %d)", k);
+  return SAKI_OK;
+}
+
+SAKI_API int64_t saki_distill_scratch_bytes(int64_t N, int32_t k) { return list_size_check(N, k) ? 0 : std::max<int64_t>(256, distill_scratch_bytes(N, k)); }
+
+SAKI_API int saki_distill_top(const saki_distill_in* in, const saki_distill_out* out, void* dlogits, int64_t ld_g, float grad_scale, void* scratch, int64_t scratch_bytes,
+                              void* cuda_stream) {
+  g_err[0] = 0;
+  if (!in || !out) return fail(SAKI_ERR_INVALID_ARG, "NULL argument struct");
+  int rc = list_size_check(in->N, in->k);
+  if (rc) return rc;
+  if (in->V < 2 || in->V > (1 << 22)) return fail(SAKI_ERR_INVALID_ARG, "V must be in [2, 2^22] (got %d)", in->V);
+  if (in->dtype != SAKI_F32 && in->dtype != SAKI_BF16) return fail(SAKI_ERR_INVALID_ARG, "unknown dtype %d", in->dtype);
+  if (!(in->temperature > 0.f) || std::isinf(in->temperature)) return fail(SAKI_ERR_INVALID_ARG, "temperature must be finite and > 0");
+  if (in->ld_s < in->V || in->ld_k < in->k || (dlogits && ld_g < in->V)) return fail(SAKI_ERR_INVALID_ARG, "row stride smaller than the row");
+  if (dlogits && !std::isfinite(grad_scale)) return fail(SAKI_ERR_INVALID_ARG, "grad_scale must be finite");
+  if (in->reverse && !in->teacher_lse) return fail(SAKI_ERR_INVALID_ARG, "reverse needs teacher_lse");
+  if (in->N == 0) return SAKI_OK;
+  if (!in->student_logits || !in->token || !in->logit || !scratch) return fail(SAKI_ERR_INVALID_ARG, "NULL student_logits, token, logit or scratch pointer");
+  if (!out->loss && !out->lse && !out->row_status && !dlogits) return fail(SAKI_ERR_INVALID_ARG, "no output is wanted");
+  if (scratch_bytes < distill_scratch_bytes(in->N, in->k)) return fail(SAKI_ERR_INVALID_ARG, "scratch too small: %lld bytes needed", (long long)distill_scratch_bytes(in->N, in->k));
+  if (!aligned(scratch, 256)) return fail(SAKI_ERR_UNSUPPORTED, "scratch must be 256-byte aligned");
+  const uintptr_t size = in->dtype == SAKI_BF16 ? 2 : 4;
+  if (!aligned(in->student_logits, size) || (dlogits && !aligned(dlogits, size))) return fail(SAKI_ERR_UNSUPPORTED, "logits that do not start at a whole element");
+  unsigned long long* flagged = nullptr;
+  if ((rc = device_ready(&flagged))) return rc;
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const bool stream = g_kernel.load() != 1 && distill_stream_can_serve(*in);
+  int launches = 0;
+  const cudaError_t e = launch_distill(*in, *out, dlogits, ld_g, grad_scale, scratch, stream, flagged, &launches, st);
+  if (e == cudaSuccess) g_last_kernel = stream ? 4 : 1;
+  return launched(e, launches, "distillation kernel launch");
+}
+
 // ---- cross entropy from hidden states ----
 static int linear_size_check(int64_t N, int32_t d, int32_t V) {
   g_err[0] = 0;

@@ -277,6 +277,10 @@ cudaError_t launch_linear_fwd(const saki_linear_in& in, const saki_linear_out& o
                               cudaStream_t st);
 cudaError_t launch_linear_bwd(const saki_linear_in& in, const float* lse, void* dhidden, int64_t ld_dh, void* dweight, int64_t ld_dw, float grad_scale, void* scratch,
                               long long wait_limit, int* n_launches, cudaStream_t st);
+int64_t distill_scratch_bytes(int64_t N, int32_t k);
+bool distill_stream_can_serve(const saki_distill_in& in);
+cudaError_t launch_distill(const saki_distill_in& in, const saki_distill_out& out, void* dlogits, int64_t ld_g, float grad_scale, void* scratch, bool stream,
+                           unsigned long long* flagged, int* n_launches, cudaStream_t st);
 int vshard_combine_host(const saki_vshard_in& in, int stage, const double* gathered, double* state, const saki_out& out,
                         bool allow_fast);
 

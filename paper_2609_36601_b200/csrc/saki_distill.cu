@@ -1,0 +1,706 @@
+// Distillation of a student's rows from a teacher's top logits: loss and gradient (see include/saki.h for the definition).  With pi = softmax(z / tau), K the
+// listed tokens, w_j their teacher's probabilities, W their sum, R the rest of the teacher's mass (0: the list is all there is), S the student's mass outside K:
+//   forward   L = sum_K w (log w - log pi) + R (log R - log S)      dL/dz_v = (W + R) pi_v - w_v in K, (W + R - R / S) pi_v outside
+//   reverse   L = sum_K pi (log pi - log w) + S (log S - log R)     dL/dz_v = pi_v (log pi_v - log w_v - L) in K, pi_v (log S - log R - L) outside
+// so outside K the gradient is one number a row times pi.  S is summed over the elements outside K: 1 - sum_K pi would cancel where the student
+// agrees with its teacher, which is what it is trained to.
+//
+// Three kernels:
+//   distill_lists_kernel    a warp a row: looks through the lists (ranges, a token twice), w and log w from float64 exponentials (R = 1 - W cancels)
+//   distill_stream_kernel   persistent CTAs, a row each: a row is read from HBM once and its gradient written once.  Every lane owns 16-byte slots of shared
+//                           memory that it fills with cp.async; the leading steps of a warp's segment stay there for both passes, the rest goes through a
+//                           ring (its second touch comes from L2); while a row's gradient is written the slots take the next row.  A warp knows from a word of bits
+//                           at which of its steps there are listed tokens, and looks for them only there.
+//   distill_general_kernel  float64, any layout, a block a row: for what the other cannot serve, and the rows that it cannot resolve (row list).
+#include "saki_device.cuh"
+#include <algorithm>
+#include <mutex>
+
+namespace saki {
+
+namespace {
+
+constexpr int KMAX = 128;
+constexpr double LEAST_REST = 0x1p-20;
+constexpr double LEAST_LOG_S = -1000 * LN2;      // a student's mass outside K below 2^-1000 is none: all there is masked, by -inf or by the type's lowest value
+
+// what a row's list comes to
+struct alignas(16) ListRow {
+  double W, R, H, log_R;      // W: sum of w as rounded to float32, R of the exact ones, H: sum of w log w; R 0: there is no rest
+  int n;                      // tokens that are there
+  uint32_t status;            // MASKED, BAD_ID, NONFINITE: the row contributes nothing
+};
+
+struct DistillParams {
+  saki_distill_in in;
+  saki_distill_out out;
+  void* dlogits;
+  int64_t ld_g;
+  float grad_scale;
+  ListRow* rows;              // [N]
+  int* id;                    // [N][k] the tokens that are there, -1 elsewhere
+  float2* w;                  // [N][k] (w, log w)
+  unsigned long long* flagged;
+  int32_t* redo_list;         // [N] rows that the streaming kernel hands to the float64 kernel
+  unsigned int* redo_count;
+  int32_t from_list;
+};
+
+__device__ __forceinline__ void write_result(const DistillParams& P, int64_t row, float loss, float lse, uint32_t status) {
+  if (P.out.loss) P.out.loss[row] = loss;
+  if (P.out.lse) P.out.lse[row] = lse;
+  if (P.out.row_status) P.out.row_status[row] = status;
+  if (status & (SAKI_ROW_NONFINITE | SAKI_ROW_BAD_ID)) atomicAdd(P.flagged, 1ull);
+}
+__device__ __forceinline__ double warp_max(double a) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) a = fmax(a, __shfl_xor_sync(0xffffffffu, a, o));
+  return a;
+}
+
+// ---------------------------------------------------------------- lists
+__global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams P) {
+  __shared__ int ids[8][KMAX];
+  launch_dependents();
+  wait_for_predecessor();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = P.in.k;
+  const int64_t row = (int64_t)blockIdx.x * 8 + warp;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *P.redo_count = 0;
+  if (row >= P.in.N) return;
+  const double rtau = 1.0 / (double)P.in.temperature;
+  uint32_t status = 0;
+  int id[KMAX / 32];
+  double t[KMAX / 32];
+  bool bad_id = false, bad = false;
+  if (P.in.mask && P.in.mask[row] == 0) status = SAKI_ROW_MASKED;
+  int n = 0;
+#pragma unroll
+  for (int r = 0; r < KMAX / 32; ++r) {
+    const int j = r * 32 + lane;
+    id[r] = -1; t[r] = -CUDART_INF;
+    if (j < k && !status) {
+      const int v = P.in.token[row * P.in.ld_k + j];
+      const float x = P.in.logit[row * P.in.ld_k + j];
+      bad_id |= v < -1 || v >= P.in.V;
+      if (v >= 0 && v < P.in.V && x != -CUDART_INF_F) {
+        id[r] = v; t[r] = (double)x * rtau;
+        bad |= !(fabsf(x) < CUDART_INF_F);
+      }
+    }
+    ids[warp][j] = id[r];
+    n += __popc(__ballot_sync(0xffffffffu, id[r] >= 0));
+  }
+  __syncwarp();
+  for (int i = 0; i < k; ++i) {
+    const int v = ids[warp][i];
+#pragma unroll
+    for (int r = 0; r < KMAX / 32; ++r) bad_id |= v >= 0 && id[r] == v && i != r * 32 + lane;
+  }
+  const bool with_rest = P.in.teacher_lse != nullptr;
+  double ref = 0;
+  if (with_rest) {
+    const float l = P.in.teacher_lse[row];
+    ref = (double)l;
+    bad |= !(fabsf(l) < CUDART_INF_F);
+  } else {
+    double m = -CUDART_INF, s = 0;
+#pragma unroll
+    for (int r = 0; r < KMAX / 32; ++r) m = fmax(m, t[r]);
+    m = warp_max(m);
+#pragma unroll
+    for (int r = 0; r < KMAX / 32; ++r)
+      if (id[r] >= 0) s += exp(t[r] - m);
+    ref = n ? m + log(warp_sum(s)) : 0;
+  }
+  if (!status && __any_sync(0xffffffffu, bad_id)) status = SAKI_ROW_BAD_ID;
+  if (!status && __any_sync(0xffffffffu, bad)) status = SAKI_ROW_NONFINITE;
+  double W = 0, W32 = 0, H = 0;      // (the loss takes sums of w z from sums of w times the log-sum-exp: the same w in both, or a large common z would not cancel)
+#pragma unroll
+  for (int r = 0; r < KMAX / 32; ++r) {
+    const int j = r * 32 + lane;
+    float2 w = make_float2(0.f, 0.f);
+    if (id[r] >= 0) {
+      const double lw = t[r] - ref, e = exp(lw);
+      w = make_float2((float)e, (float)lw);
+      W += e; W32 += (double)w.x; H += e > 0 ? e * lw : 0;
+    }
+    if (j < k) {
+      P.id[row * k + j] = status ? -1 : id[r];
+      P.w[row * k + j] = w;
+    }
+  }
+  W = warp_sum(W); W32 = warp_sum(W32); H = warp_sum(H);
+  if (lane == 0) {
+    const bool rest = with_rest && n < P.in.V;
+    const double R = rest ? fmax(1.0 - W, LEAST_REST) : 0;
+    P.rows[row] = ListRow{W32, R, H, rest ? log(R) : 0, n, status};
+  }
+}
+
+// ---------------------------------------------------------------- general kernel (float64)
+constexpr int DG_THREADS = 256;
+struct GeneralShared {
+  double sum[DG_THREADS / 32];
+  int id[KMAX];
+  double lw[KMAX];
+  float w[KMAX];
+  uint32_t bits[128];          // a bit for the low 12 bits of a listed token
+};
+__device__ __forceinline__ double block_fold(double v, double* sh, bool max) {
+  v = max ? warp_max(v) : warp_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+  __syncthreads();
+  double a = sh[0];
+  for (int w = 1; w < DG_THREADS / 32; ++w) a = max ? fmax(a, sh[w]) : a + sh[w];
+  return a;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(DG_THREADS) distill_general_kernel(const DistillParams P) {
+  __shared__ GeneralShared sh;
+  wait_for_predecessor();
+  const int64_t n_items = P.from_list ? (int64_t)*P.redo_count : P.in.N;      // (an empty row list, as a rule)
+  const int V = P.in.V, k = P.in.k;
+  const double rtau = 1.0 / (double)P.in.temperature;
+  for (int64_t item = blockIdx.x; item < n_items; item += gridDim.x) {
+    const int64_t row = P.from_list ? (int64_t)P.redo_list[item] : item;
+    const T* s = (const T*)P.in.student_logits + row * P.in.ld_s;
+    T* g = P.dlogits ? (T*)P.dlogits + row * P.ld_g : nullptr;
+    const ListRow list = P.rows[row];
+    uint32_t status = list.status;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 128; i += DG_THREADS) sh.bits[i] = 0;
+    __syncthreads();
+    for (int j = threadIdx.x; j < k; j += DG_THREADS) {
+      const int v = P.id[row * k + j];
+      const float2 w = P.w[row * k + j];
+      sh.id[j] = v; sh.w[j] = w.x; sh.lw[j] = w.y;
+      if (v >= 0) atomicOr(&sh.bits[(v & 4095) >> 5], 1u << (v & 31));
+    }
+    __syncthreads();
+    auto place = [&](int v) {          // of v in the list, -1: not listed
+      if (!(sh.bits[(v & 4095) >> 5] >> (v & 31) & 1u)) return -1;
+      for (int j = 0; j < k; ++j)
+        if (sh.id[j] == v) return j;
+      return -1;
+    };
+    double in_max = -CUDART_INF, out_max = -CUDART_INF, bad = 0;
+    if (!status) {
+      for (int v = threadIdx.x; v < V; v += DG_THREADS) {
+        const double z = (double)ld_as_float(s, v) * rtau;
+        const bool listed = place(v) >= 0;
+        if (!(z < CUDART_INF) || (listed && !(z > -CUDART_INF))) bad = 1;
+        if (listed) in_max = fmax(in_max, z);
+        else out_max = fmax(out_max, z);
+      }
+      bad = block_fold(bad, sh.sum, true);
+      in_max = block_fold(in_max, sh.sum, true);
+      out_max = block_fold(out_max, sh.sum, true);
+      if (bad != 0 || !(fmax(in_max, out_max) > -CUDART_INF)) status = SAKI_ROW_NONFINITE;
+    }
+    if (status) {
+      if (g) for (int v = threadIdx.x; v < V; v += DG_THREADS) st_from_float(g, v, 0.f);
+      if (threadIdx.x == 0) write_result(P, row, 0.f, 0.f, status);
+      continue;
+    }
+    double in_sum = 0, out_sum = 0;
+    for (int v = threadIdx.x; v < V; v += DG_THREADS) {
+      const double z = (double)ld_as_float(s, v) * rtau;
+      if (place(v) >= 0) in_sum += exp(z - in_max);
+      else if (z > -CUDART_INF) out_sum += exp(z - out_max);
+    }
+    in_sum = block_fold(in_sum, sh.sum, false);
+    out_sum = block_fold(out_sum, sh.sum, false);
+    const double top = fmax(in_max, out_max);
+    const double lse = top + log((in_sum > 0 ? in_sum * exp(in_max - top) : 0) + (out_sum > 0 ? out_sum * exp(out_max - top) : 0));
+    double lS = out_sum > 0 ? out_max + log(out_sum) - lse : -CUDART_INF;
+    const bool rest = list.R > 0 && lS > LEAST_LOG_S;
+    if (!rest) lS = 0;
+    const double S = rest ? exp(lS) : 0;
+    double loss = 0;
+    for (int j = threadIdx.x; j < k; j += DG_THREADS) {
+      const int v = sh.id[j];
+      if (v < 0) continue;
+      const double lp = (double)ld_as_float(s, v) * rtau - lse;
+      loss += P.in.reverse ? exp(lp) * (lp - sh.lw[j]) : (double)sh.w[j] * (sh.lw[j] - lp);
+    }
+    loss = block_fold(loss, sh.sum, false);
+    if (rest) loss += P.in.reverse ? S * (lS - list.log_R) : list.R * (list.log_R - lS);
+    if (threadIdx.x == 0) write_result(P, row, (float)loss, (float)lse, 0u);
+    if (!g) continue;
+    const double kg = (double)P.grad_scale * rtau, Z = list.W + (rest ? list.R : 0);
+    const double outside = P.in.reverse ? (rest ? lS - list.log_R : 0) - loss : Z - (rest ? exp(list.log_R - lS) : 0);
+    for (int v = threadIdx.x; v < V; v += DG_THREADS) {
+      const double lp = (double)ld_as_float(s, v) * rtau - lse, p = exp(lp);
+      const int j = place(v);
+      double x = outside * p;
+      if (j >= 0) x = P.in.reverse ? p * (lp - sh.lw[j] - loss) : Z * p - (double)sh.w[j];
+      st_from_float(g, v, (float)(kg * x));
+    }
+  }
+}
+
+// ---------------------------------------------------------------- streaming kernel
+constexpr int WARPS_FULL = 32, WARPS_HALF = 16;
+constexpr int KEEP = 13, RING = 5, RESIDENT = KEEP - RING;      // 512-byte steps of a warp in shared memory; of them, where a segment does not fit, the ring's
+constexpr int MAX_STEPS = 64;
+constexpr float MARGIN = 60.f;                                  // in base 2: how far a lane's elements may lie above its shift
+
+template <typename T> struct Elem;
+template <> struct Elem<__nv_bfloat16> {
+  static constexpr int E = 8, LOG = 3, STEP_LOG = 8;
+  static constexpr uint32_t FILLER = 0xFF7FFF7Fu;               // two of the most negative finite value: exp -> 0
+  static __device__ __forceinline__ float2 pair(const uint4& w, int i) { return unpack_bf16x2(i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w); }
+  static __device__ __forceinline__ float top(const uint4& w) {
+    const float2 a = unpack_bf16x2(max_bf16x2(max_bf16x2(w.x, w.y), max_bf16x2(w.z, w.w)));
+    return fmaxf(a.x, a.y);
+  }
+  static __device__ __forceinline__ float get(const uint4& w, int e) {
+    const int i = e >> 1;
+    const uint32_t r = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+    return __uint_as_float(e & 1 ? r & 0xffff0000u : r << 16);
+  }
+  static __device__ __forceinline__ void put(uint4& w, int e, float x) {
+    const int i = e >> 1;
+    uint32_t r = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+    const uint32_t h = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x));
+    r = e & 1 ? (r & 0x0000ffffu) | (h << 16) : (r & 0xffff0000u) | h;
+    if (i == 0) w.x = r; else if (i == 1) w.y = r; else if (i == 2) w.z = r; else w.w = r;
+  }
+};
+template <> struct Elem<float> {
+  static constexpr int E = 4, LOG = 2, STEP_LOG = 7;
+  static constexpr uint32_t FILLER = 0xFF7FFFFFu;
+  static __device__ __forceinline__ float2 pair(const uint4& w, int i) { return i == 0 ? make_float2(__uint_as_float(w.x), __uint_as_float(w.y)) : make_float2(__uint_as_float(w.z), __uint_as_float(w.w)); }
+  static __device__ __forceinline__ float top(const uint4& w) { return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w))); }
+  static __device__ __forceinline__ float get(const uint4& w, int e) { return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w); }
+  static __device__ __forceinline__ void put(uint4& w, int e, float x) {
+    const uint32_t r = __float_as_uint(x);
+    if (e == 0) w.x = r; else if (e == 1) w.y = r; else if (e == 2) w.z = r; else w.w = r;
+  }
+};
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t pol) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(__cvta_generic_to_global(src)), "l"(pol) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(__cvta_generic_to_global(src)) : "memory"); }
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(__cvta_generic_to_global(src)) : "memory"); }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t at, const uint4& v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_stream(void* p, const uint4& v, uint64_t pol) {
+  asm volatile("st.global.L2::cache_hint.v4.b32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(__cvta_generic_to_global(p)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "l"(pol) : "memory");
+}
+__device__ __forceinline__ uint64_t policy(bool keep) {
+  uint64_t p;
+  if (keep) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+
+// A row in 16-byte pieces that start on 16-byte boundaries of memory: its first and last piece may hold elements of no row of the call.
+template <typename T> struct View {
+  const char* base;            // of piece 0; NULL: there is no row
+  int head;                    // elements of piece 0 before the row
+  int full0, full;             // pieces full0 .. full0 + full - 1 lie within the row
+  int n;                       // pieces
+};
+template <typename T> __device__ __forceinline__ View<T> view_of(const T* row, int V) {
+  constexpr int E = Elem<T>::E;
+  View<T> v;
+  const uintptr_t a = (uintptr_t)row;
+  v.base = (const char*)(a & ~(uintptr_t)15);
+  v.head = (int)((a & 15) / sizeof(T));
+  v.full0 = v.head ? 1 : 0;
+  v.full = max((V + v.head) / E - v.full0, 0);      // (a row that ends within its first piece has none)
+  v.n = (V + v.head + E - 1) / E;
+  return v;
+}
+// a piece with elements of other rows, or none: the filler there
+template <typename T> __device__ __forceinline__ uint4 odd_piece(const char* base, int head, int V, int c) {
+  constexpr int E = Elem<T>::E;
+  uint4 w = make_uint4(Elem<T>::FILLER, Elem<T>::FILLER, Elem<T>::FILLER, Elem<T>::FILLER);
+  const T* p = (const T*)base + (int64_t)c * E;
+#pragma unroll 1
+  for (int e = 0; e < E; ++e)
+    if (c * E + e >= head && c * E + e < head + V) Elem<T>::put(w, e, ld_as_float(p, e));
+  return w;
+}
+template <typename T> __device__ __forceinline__ void fill(uint32_t slot, const View<T>& v, int V, int c, uint64_t pol) {
+  if ((unsigned)(c - v.full0) < (unsigned)v.full) copy16(slot, v.base + (int64_t)c * 16, pol);
+  else if (v.base) sts128(slot, odd_piece<T>(v.base, v.head, V, c));
+}
+
+struct Segment { int c0, steps, res; };      // of a warp: its first piece, steps of 32 pieces, how many of them stay in shared memory
+
+// Visits the warp's steps in order: body(words, step).  Every step commits one group of copies.  A streamed step, once read, requests the streamed step RING
+// further on: of this pass, or past its end the first streamed steps of the pass that follows, over `wrap` (the same row again, or the next one).
+// With REFILL a resident step, once read, requests the same step of `wrap`.
+template <typename T, bool REFILL, typename Body>
+__device__ __forceinline__ void visit(const Segment& sg, int lane, uint32_t base, int V, const View<T>& cur, const View<T>& wrap, uint64_t pol_cur, uint64_t pol_wrap,
+                                      uint64_t pol_res, uint32_t& ring_slot, Body&& body) {
+  uint32_t slot = base;
+  int c = sg.c0 + lane;
+#pragma unroll 1
+  for (int k = 0; k < sg.steps; ++k, c += 32) {
+    uint4 a;
+    copies_wait<RING - 1>();
+    if (k < sg.res) {
+      a = lds128(slot);
+      if (REFILL) fill<T>(slot, wrap, V, c, pol_res);
+      slot += 512;
+    } else {
+      a = lds128(ring_slot);
+      if (k + RING < sg.steps) fill<T>(ring_slot, cur, V, c + RING * 32, pol_cur);
+      else fill<T>(ring_slot, wrap, V, c + (RING - (sg.steps - sg.res)) * 32, pol_wrap);
+      ring_slot += 512;
+      if (ring_slot == base + KEEP * 512) ring_slot = base + RESIDENT * 512;
+    }
+    copies_commit();
+    body(a, k);
+  }
+}
+
+template <int MW> struct StreamShared {
+  double red[4][MW];           // by warp: the sum outside K, its shift, the sum in K, the sum for the loss
+  // by row parity: a warp may be a pass behind the others (what it reads is written again only behind the next barrier but one)
+  float bc[2][4];
+  double dc[2][4];
+  ListRow list[3];             // of three rows in turn: written while a warp may still read the one before last
+  int id[3][KMAX];
+  float2 w[3][KMAX];
+  float x[KMAX], g[KMAX];      // listed elements and their gradients: of the warp that has them
+};
+template <int MW> constexpr int stream_smem = MW * KEEP * 512 + (int)sizeof(StreamShared<MW>);
+
+// The tokens of the list that lie in step `step` of the warp: body(element's place in the step's pieces, place in the list).  `at`: by lane, where listed elements lie in
+// the warp's segment, in elements (below 0: not there).
+template <int SLOTS, int STEP_LOG, typename Body> __device__ __forceinline__ void each_listed(const int (&at)[SLOTS], int step, Body&& body) {
+#pragma unroll
+  for (int r = 0; r < SLOTS; ++r) {
+    unsigned m = __ballot_sync(0xffffffffu, (at[r] >> STEP_LOG) == step);
+    while (m) {
+      const int src = __ffs(m) - 1;
+      m &= m - 1;
+      body(__shfl_sync(0xffffffffu, at[r], src) & ((1 << STEP_LOG) - 1), r * 32 + src);
+    }
+  }
+}
+
+template <typename T, int MW, int SLOTS, bool BWD>
+__global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kernel(const DistillParams P) {
+  using El = Elem<T>;
+  constexpr int E = El::E;
+  extern __shared__ __align__(128) unsigned char dsm[];
+  StreamShared<MW>& sh = *(StreamShared<MW>*)(dsm + MW * KEEP * 512);
+  launch_dependents();
+  wait_for_predecessor();
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  const int V = P.in.V, k = P.in.k;
+  const int64_t N = P.in.N;
+  // whole steps of 32 pieces, dealt out in order: for a row that starts anywhere
+  const int steps_all = ((V + 2 * E - 2) / E + 31) / 32, steps_q = steps_all / MW, steps_r = steps_all - steps_q * MW;
+  Segment sg;
+  sg.steps = steps_q + (warp < steps_r ? 1 : 0);
+  sg.c0 = 32 * (warp * steps_q + min(warp, steps_r));
+  sg.res = sg.steps <= KEEP ? sg.steps : RESIDENT;
+  const uint32_t base = smem_addr(dsm) + (uint32_t)warp * (KEEP * 512) + (uint32_t)lane * 16;
+  uint32_t ring_slot = base + RESIDENT * 512;
+  const double rtau = 1.0 / (double)P.in.temperature;
+  const float c32 = (float)(INV_LN2 * rtau);
+  const uint64_t pol_last = policy(true), pol_first = policy(false);
+  const bool few_groups = sg.steps - 1 < RING;      // a short segment: its copies are fewer groups back than the waits assume
+  const bool reverse = P.in.reverse != 0;
+  View<T> none = {};
+
+  auto view = [&](int64_t row) { return row < N ? view_of<T>((const T*)P.in.student_logits + row * P.in.ld_s, V) : none; };
+  auto stage_list = [&](int64_t row, int b) {       // a row's list and what it comes to, on their way into shared memory
+    if (row >= N) return;
+    for (int j = tid; j < k; j += MW * 32) {
+      copy4(smem_addr(&sh.id[b][j]), P.id + row * k + j);
+      copy8(smem_addr(&sh.w[b][j]), P.w + row * k + j);
+    }
+    if (tid < (int)sizeof(ListRow) / 8) copy8(smem_addr((char*)&sh.list[b] + tid * 8), (const char*)(P.rows + row) + tid * 8);
+  };
+
+  View<T> cur = view(blockIdx.x);
+  stage_list(blockIdx.x, 0);
+  for (int s = 0; s < sg.res; ++s) { fill<T>(base + s * 512, cur, V, sg.c0 + lane + 32 * s, pol_first); copies_commit(); }
+  if (sg.res < sg.steps)
+    for (int j = 0; j < RING; ++j) { fill<T>(ring_slot + j * 512, cur, V, sg.c0 + lane + 32 * (sg.res + j), pol_last); copies_commit(); }
+  copies_commit();
+  copies_wait<0>();
+  __syncthreads();
+
+  int b = 0, parity = 0;
+  for (int64_t row = blockIdx.x; row < N; row += gridDim.x, parity ^= 1) {
+    const int64_t next_row = row + gridDim.x;
+    const View<T> nxt = view(next_row);
+    const int next_b = b == 2 ? 0 : b + 1;
+    if (few_groups) copies_wait<0>();
+    stage_list(next_row, next_b);      // (goes with the first step's group, and is there before the row's second barrier)
+    const bool live = sh.list[b].status == 0;
+    // where listed elements lie in this warp's segment, and at which steps
+    int at[SLOTS];
+    uint32_t here_lo = 0, here_hi = 0;
+#pragma unroll
+    for (int r = 0; r < SLOTS; ++r) {
+      const int j = r * 32 + lane;
+      const int id = j < k ? sh.id[b][j] : -1;
+      const int place = id + cur.head - sg.c0 * E;
+      const bool mine = id >= 0 && place >= 0 && place < sg.steps * 32 * E;
+      at[r] = mine ? place : -1;
+      const int step = place >> El::STEP_LOG;
+      here_lo |= __reduce_or_sync(0xffffffffu, mine && step < 32 ? 1u << step : 0u);
+      here_hi |= __reduce_or_sync(0xffffffffu, mine && step >= 32 ? 1u << (step - 32) : 0u);
+    }
+    const uint64_t here = (uint64_t)here_hi << 32 | here_lo;
+
+    // ------------------------------------------------ pass 1: the sum outside K of 2^(c x + shift).  A lane's shift comes from the warp's first elements, and moves where
+    // elements lie MARGIN above it (with the first ones masked, say)
+    float shift = 0.f, limit;
+    {
+      copies_wait<RING - 1>();
+      float m0 = sg.steps > 0 ? El::top(lds128(base)) : -CUDART_INF_F;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
+      m0 = fminf(fmaxf(m0, -1e8f), 1e30f);      // (masks, of the lowest value or -inf, stay below it; a NaN is passed over: it comes out of the sum)
+      shift = -ceilf(c32 * m0);
+      limit = (MARGIN - shift) / c32;
+    }
+    float2 S0 = splat(0.f), S1 = splat(0.f);
+    {
+      const float2 cc = splat(c32);
+      const bool ahead = sg.steps == sg.res && nxt.base != nullptr;      // a resident row leaves L2 free: the next one is sent on its way there
+      visit<T, !BWD>(sg, lane, base, V, cur, BWD ? cur : nxt, pol_last, pol_first, pol_first, ring_slot, [&](uint4 w, int step) {
+        if (BWD && ahead && (lane & 7) == 0 && sg.c0 + lane + 32 * step < nxt.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(nxt.base + (int64_t)(sg.c0 + lane + 32 * step) * 16));
+        if (here >> step & 1ull)
+          each_listed<SLOTS, El::STEP_LOG>(at, step, [&](int e, int j) {
+            if (lane == e >> El::LOG) {
+              sh.x[j] = El::get(w, e & (E - 1));
+              El::put(w, e & (E - 1), -CUDART_INF_F);
+            }
+          });
+        const float top = El::top(w);
+        if (top > limit) {
+          const float to = -ceilf(c32 * fminf(top, 1e30f)), f = ex2f(fmaxf(to - shift, -200.f));
+          S0 = fmul2(S0, splat(f)); S1 = fmul2(S1, splat(f));
+          shift = to;
+          limit = (MARGIN - shift) / c32;
+        }
+        const float2 kk = splat(shift);
+#pragma unroll
+        for (int i = 0; i < E / 2; i += 2) {
+          S0 = fadd2(S0, ex2f2(ffma2(El::pair(w, i), cc, kk)));
+          S1 = fadd2(S1, ex2f2(ffma2(El::pair(w, i + 1), cc, kk)));
+        }
+      });
+    }
+    __syncwarp();
+    float warp_shift = shift;
+    if (here) {                       // (a segment may have nothing but listed elements and masked ones)
+#pragma unroll
+      for (int r = 0; r < SLOTS; ++r)
+        if (at[r] >= 0) warp_shift = fminf(warp_shift, -ceilf(c32 * fminf(sh.x[r * 32 + lane], 1e30f)));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) warp_shift = fminf(warp_shift, __shfl_xor_sync(0xffffffffu, warp_shift, o));
+    double outside = (((double)S0.x + (double)S0.y) + ((double)S1.x + (double)S1.y)) * (double)ex2f(fmaxf(warp_shift - shift, -200.f));
+    double inside = 0, cross = 0;
+    if (here) {
+      bool lost = false;
+#pragma unroll
+      for (int r = 0; r < SLOTS; ++r)
+        if (at[r] >= 0) {
+          const int j = r * 32 + lane;
+          const float x = sh.x[j];
+          const float2 w = sh.w[b][j];
+          const float e = ex2f(fmaf(x, c32, warp_shift));
+          lost |= !(fabsf(x) < CUDART_INF_F);
+          inside += (double)e;
+          cross += reverse ? (double)e * ((double)x * rtau - (double)w.y) : (double)w.x * ((double)x * rtau);
+        }
+      if (lost) inside = CUDART_NAN;      // a listed token that the student's row has masked, or not finite: the float64 kernel decides
+      inside = warp_sum(inside);
+      cross = warp_sum(cross);
+    }
+    outside = warp_sum(outside);
+    if (lane == 0) { sh.red[0][warp] = outside; sh.red[1][warp] = (double)warp_shift; sh.red[2][warp] = inside; sh.red[3][warp] = cross; }
+    __syncthreads();
+    if (warp == 0) {
+      const int wl = lane < MW ? lane : 0;
+      const bool part = lane < MW;
+      const double ks = sh.red[1][wl];
+      double kr = part ? ks : 1e300;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) kr = fmin(kr, __shfl_xor_sync(0xffffffffu, kr, o));
+      const double f = part ? pow2_exact((int)fmax(kr - ks, -1000.0)) : 0;
+      const double out = warp_sum(f > 0 ? sh.red[0][wl] * f : 0), in = warp_sum(f > 0 ? sh.red[2][wl] * f : part && sh.red[2][wl] != sh.red[2][wl] ? CUDART_NAN : 0);
+      double sum_cross = part ? sh.red[3][wl] : 0;
+      if (reverse && part) sum_cross *= f;
+      sum_cross = warp_sum(sum_cross);
+      if (lane == 0) {
+        float scale_out = 0.f, Zs = 0.f, kg = 0.f, lse_f = 0.f, loss_f = 0.f, grad_shift = 0.f;
+        const ListRow& list = sh.list[b];
+        if (live) {
+          const double sum = out + in;
+          const bool has_rest = list.R > 0 && out > 0;
+          // not finite (or nothing but masked entries), or a share outside K so small that the sum may have lost terms of it,
+          // or logits of millions, whose shifts are no exact float32: the float64 kernel decides
+          if (!(sum > 0) || !(sum < CUDART_INF) || !(fabs(sum_cross) < CUDART_INF) || (list.R > 0 && out < sum * 0x1p-60) || !(fabs(kr) < 8e6)) {
+            P.redo_list[atomicAdd(P.redo_count, 1u)] = (int32_t)row;
+          } else {
+            // sum of exp(x / tau) = exp(x0 / tau) sum of 2^(c (x - x0)) with x0 = -kr / c, up to what c as a float32 is off over distances from x0
+            const double l2 = log2_fast(sum), lse = LN2 * l2 - kr / (double)c32 * rtau;
+            const double rsum = 1.0 / sum;
+            const double lS = has_rest ? LN2 * (log2_fast(out) - l2) : 0;
+            const double Z = list.W + (has_rest ? list.R : 0);
+            double loss, c_out;
+            if (reverse) {
+              loss = sum_cross * rsum - lse * (in * rsum) + (has_rest ? out * rsum * (lS - list.log_R) : 0);
+              c_out = (has_rest ? lS - list.log_R : 0) - loss;
+            } else {
+              loss = list.H - sum_cross + lse * list.W + (has_rest ? list.R * (list.log_R - lS) : 0);
+              c_out = Z - (has_rest ? list.R * sum / out : 0);
+            }
+            const int e = (int)floor(l2);
+            const double kgd = (double)P.grad_scale * rtau;
+            const double ps = pow2_exact(-abs(e)), unit = e >= 0 ? sum * ps : sum / ps;      // sum 2^-e, 1 to 2
+            grad_shift = (float)(kr - (double)e);
+            scale_out = (float)(kgd * c_out / unit);
+            Zs = (float)(1.0 / unit);
+            kg = (float)kgd;
+            lse_f = (float)lse; loss_f = (float)loss;
+            sh.dc[parity][0] = lse; sh.dc[parity][1] = loss; sh.dc[parity][2] = Z;
+            write_result(P, row, loss_f, lse_f, 0u);
+          }
+        } else write_result(P, row, 0.f, 0.f, list.status);
+        float* const bc = sh.bc[parity];
+        bc[0] = grad_shift; bc[1] = scale_out; bc[2] = Zs; bc[3] = kg;
+      }
+    }
+    if (few_groups) copies_wait<0>();
+    __syncthreads();
+
+    // ------------------------------------------------ pass 2: the gradient
+    if constexpr (BWD) {
+      const float* const bc = sh.bc[parity];
+      const float kr = bc[0], scale = bc[1], unit = bc[2], kg = bc[3];
+      const bool zero = unit == 0.f;      // a row that contributes nothing (or waits for the float64 kernel): zeros, whatever its logits
+      if (here) {
+        const double lse = sh.dc[parity][0], loss = sh.dc[parity][1], Z = sh.dc[parity][2];
+#pragma unroll
+        for (int r = 0; r < SLOTS; ++r)
+          if (at[r] >= 0) {
+            const int j = r * 32 + lane;
+            const float x = sh.x[j];
+            const float2 w = sh.w[b][j];
+            const float p = ex2f(fmaf(x, c32, kr)) * unit;
+            const float v = reverse ? p * (float)((double)x * rtau - lse - (double)w.y - loss) : (float)(Z * (double)p - (double)w.x);
+            sh.g[j] = zero ? 0.f : kg * v;
+          }
+      }
+      __syncwarp();
+      const float2 cc = splat(c32), kk = splat(kr), sc = splat(scale);
+      T* const g_row = (T*)P.dlogits + row * P.ld_g;
+      char* const g_base = (char*)((uintptr_t)g_row & ~(uintptr_t)15);
+      const bool alike = ((uintptr_t)g_row & 15) == cur.head * sizeof(T);      // the gradient's pieces lie like the row's
+      visit<T, true>(sg, lane, base, V, cur, nxt, pol_first, pol_last, pol_first, ring_slot, [&](const uint4& w, int step) {
+        uint4 g = make_uint4(0u, 0u, 0u, 0u);
+        if (!zero) {
+          float2 v[E / 2];
+#pragma unroll
+          for (int i = 0; i < E / 2; ++i) v[i] = fmul2(ex2f2(ffma2(El::pair(w, i), cc, kk)), sc);
+          if constexpr (E == 8) g = make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[1].x, v[1].y), pack_bf16x2(v[2].x, v[2].y), pack_bf16x2(v[3].x, v[3].y));
+          else g = make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
+          if (here >> step & 1ull)
+            each_listed<SLOTS, El::STEP_LOG>(at, step, [&](int e, int j) {
+              if (lane == e >> El::LOG) El::put(g, e & (E - 1), sh.g[j]);
+            });
+        }
+        const int c = sg.c0 + lane + 32 * step;
+        if (alike && (unsigned)(c - cur.full0) < (unsigned)cur.full) st_stream(g_base + (int64_t)c * 16, g, pol_first);
+        else if (c < cur.n)
+          for (int e = 0; e < E; ++e)
+            if ((unsigned)(c * E + e - cur.head) < (unsigned)V) st_from_float(g_row, c * E + e - cur.head, El::get(g, e));
+      });
+    }
+    cur = nxt;
+    b = next_b;
+  }
+  copies_wait<0>();
+}
+
+template <typename T, int MW, int SLOTS, bool BWD> cudaError_t launch_stream_as(const DistillParams& p, cudaStream_t st) {
+  static std::mutex mu;
+  static int known_dev = -1, sms = 0;
+  int dev = 0;
+  cudaGetDevice(&dev);
+  constexpr int smem = stream_smem<MW>;
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    if (known_dev != dev) {
+      cudaError_t e = cudaFuncSetAttribute(distill_stream_kernel<T, MW, SLOTS, BWD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+      if (e != cudaSuccess) return e;
+      known_dev = dev;
+    }
+  }
+  const int grid = (int)std::min<int64_t>(p.in.N, (int64_t)sms * (WARPS_FULL / MW));
+  return launch_pdl(distill_stream_kernel<T, MW, SLOTS, BWD>, dim3((unsigned)grid), MW * 32, smem, st, true, p);
+}
+template <typename T, int MW> cudaError_t launch_stream(const DistillParams& p, cudaStream_t st) {
+  if (p.in.k <= 64) return p.dlogits ? launch_stream_as<T, MW, 2, true>(p, st) : launch_stream_as<T, MW, 2, false>(p, st);
+  return p.dlogits ? launch_stream_as<T, MW, 4, true>(p, st) : launch_stream_as<T, MW, 4, false>(p, st);
+}
+
+int64_t round256(int64_t x) { return (x + 255) & ~(int64_t)255; }
+
+}  // namespace
+
+int64_t distill_scratch_bytes(int64_t N, int32_t k) { return 256 + round256(N * 4) + round256(N * (int64_t)sizeof(ListRow)) + round256(N * k * 4) + round256(N * k * 8); }
+
+// rows of up to 64 steps a warp, in both types
+bool distill_stream_can_serve(const saki_distill_in& in) {
+  const int e = in.dtype == SAKI_BF16 ? 8 : 4;
+  return in.N <= 0x7fffffff && ((int64_t)in.V + 2 * e - 2) / e <= (int64_t)MAX_STEPS * 32 * WARPS_FULL;
+}
+
+cudaError_t launch_distill(const saki_distill_in& in, const saki_distill_out& out, void* dlogits, int64_t ld_g, float grad_scale, void* scratch, bool stream,
+                           unsigned long long* flagged, int* n_launches, cudaStream_t st) {
+  DistillParams p = {};
+  p.in = in; p.out = out; p.dlogits = dlogits; p.ld_g = ld_g; p.grad_scale = grad_scale; p.flagged = flagged;
+  char* s = (char*)scratch;
+  p.redo_count = (unsigned int*)s; s += 256;
+  p.redo_list = (int32_t*)s; s += round256(in.N * 4);
+  p.rows = (ListRow*)s; s += round256(in.N * (int64_t)sizeof(ListRow));
+  p.id = (int*)s; s += round256(in.N * in.k * 4);
+  p.w = (float2*)s;
+  cudaError_t e = launch_pdl(distill_lists_kernel, dim3((unsigned)((in.N + 7) / 8)), 256, 0, st, true, p);
+  ++*n_launches;
+  if (e != cudaSuccess) return e;
+  if (stream) {
+    const bool half = (int64_t)in.V * (in.dtype == SAKI_BF16 ? 2 : 4) <= 196608;
+    if (in.dtype == SAKI_BF16) e = half ? launch_stream<__nv_bfloat16, WARPS_HALF>(p, st) : launch_stream<__nv_bfloat16, WARPS_FULL>(p, st);
+    else e = half ? launch_stream<float, WARPS_HALF>(p, st) : launch_stream<float, WARPS_FULL>(p, st);
+    ++*n_launches;
+    if (e != cudaSuccess) return e;
+    p.from_list = 1;
+  }
+  const int grid = (int)std::min<int64_t>(in.N, p.from_list ? 148 : 1 << 20);
+  ++*n_launches;
+  e = in.dtype == SAKI_BF16 ? launch_pdl(distill_general_kernel<__nv_bfloat16>, dim3((unsigned)grid), DG_THREADS, 0, st, true, p)
+                            : launch_pdl(distill_general_kernel<float>, dim3((unsigned)grid), DG_THREADS, 0, st, true, p);
+  return e;
+}
+
+}  // namespace saki

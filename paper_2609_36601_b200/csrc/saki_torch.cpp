@@ -42,6 +42,8 @@ struct Lib {
   decltype(&saki_linear_ce_scratch_bytes) linear_ce_scratch_bytes;
   decltype(&saki_linear_ce_fwd) linear_ce_fwd;
   decltype(&saki_linear_ce_bwd) linear_ce_bwd;
+  decltype(&saki_distill_scratch_bytes) distill_scratch_bytes;
+  decltype(&saki_distill_top) distill_top;
   decltype(&saki_last_error) last_error;
 };
 Lib lib = {};
@@ -797,6 +799,47 @@ PyObject* py_linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// distill(s, token, logit, teacher_lse, reverse, temperature, mask, grad_scale, dlogits, stream) -> (loss, lse, row_status, dlogits)
+PyObject* py_distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, 10);
+    const at::Tensor &s = tensor(a[0]), &token = tensor(a[1]), &logit = tensor(a[2]);
+    if (s.dim() != 2 || (s.size(1) > 1 && s.stride(1) != 1)) raise_value("logits must be [N, V] with unit stride along V");
+    const at::Device dev = s.device();
+    const int64_t N = s.size(0), V = s.size(1);
+    if (token.dim() != 2 || token.size(0) != N || token.scalar_type() != at::kInt || token.device() != dev || !logit.sizes().equals(token.sizes()) ||
+        logit.scalar_type() != at::kFloat || logit.device() != dev || (token.size(1) > 1 && (token.stride(1) != 1 || logit.stride(1) != 1)) || row_stride(token) != row_stride(logit))
+      raise_value("token (int32) and logit (float32) must be [N, k] tensors on the logits' device, with unit stride along k and the same row stride");
+    if (V > INT32_MAX || token.size(1) > INT32_MAX) raise_value("sizes out of range");
+    saki_distill_in in = {};
+    in.dtype = dtype_code(s);
+    const OnStream on(dev, a[9]);
+    in.student_logits = s.data_ptr(); in.ld_s = row_stride(s); in.N = N; in.V = (int32_t)V;
+    in.token = (const int32_t*)token.data_ptr(); in.logit = (const float*)logit.data_ptr(); in.ld_k = row_stride(token); in.k = (int32_t)token.size(1);
+    if (a[3] != Py_None) in.teacher_lse = (const float*)packed(a[3], at::kFloat, N, dev, "teacher_lse").data_ptr();
+    const int reverse = PyObject_IsTrue(a[4]);
+    if (reverse < 0) throw Raised();
+    in.reverse = reverse; in.temperature = (float)number(a[5]);
+    if (a[6] != Py_None) in.mask = (const uint8_t*)packed(a[6], at::kByte, N, dev, "mask").data_ptr();
+    const float scale = (float)number(a[7]);
+    at::Tensor g;
+    if (a[8] == Py_True) g = at::empty_like(s);
+    else if (a[8] != Py_None) {
+      g = tensor(a[8]);
+      if (!g.sizes().equals(s.sizes()) || g.scalar_type() != s.scalar_type() || g.device() != dev || (V > 1 && g.stride(1) != 1))
+        raise_value("dlogits must have the logits' shape, type and device, with unit stride along V");
+    }
+    const at::Tensor loss = empty({N}, at::kFloat, dev), lse = empty({N}, at::kFloat, dev), st = empty({N}, at::kInt, dev);
+    const saki_distill_out out = {(float*)loss.data_ptr(), (float*)lse.data_ptr(), (uint32_t*)st.data_ptr()};
+    const int64_t bytes = lib.distill_scratch_bytes(N, in.k);
+    if (bytes == 0) raise_saki(SAKI_ERR_INVALID_ARG, lib.last_error());
+    const at::Tensor scratch = empty({bytes}, at::kByte, dev);
+    check_rc(unlocked([&] { return lib.distill_top(&in, &out, g.defined() ? g.data_ptr() : nullptr, g.defined() ? row_stride(g) : 0, scale, scratch.data_ptr(), bytes, on.handle); }));
+    Owned x(THPVariable_Wrap(loss)), y(THPVariable_Wrap(lse)), z(THPVariable_Wrap(st)), w(wrap_or_none(g));
+    return PyTuple_Pack(4, x.p, y.p, z.p, w.p);
+  });
+}
+
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))py_bind, METH_FASTCALL, nullptr},
     {"alloc_outputs", (PyCFunction)(void (*)(void))py_alloc_outputs, METH_FASTCALL, nullptr},
@@ -815,6 +858,7 @@ PyMethodDef methods[] = {
     {"beams", (PyCFunction)(void (*)(void))py_beams, METH_FASTCALL, nullptr},
     {"linear", (PyCFunction)(void (*)(void))py_linear, METH_FASTCALL, nullptr},
     {"linear_bwd", (PyCFunction)(void (*)(void))py_linear_bwd, METH_FASTCALL, nullptr},
+    {"distill", (PyCFunction)(void (*)(void))py_distill, METH_FASTCALL, nullptr},
     {"vshard_local", (PyCFunction)(void (*)(void))py_vshard_local, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_saki_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
