@@ -318,6 +318,27 @@ SAKI_API int64_t saki_lmhead_scratch_bytes(int64_t N, int32_t V);
 SAKI_API int saki_lmhead_lse(const saki_lmhead_in* in, void* logits, int64_t ld_l, float* row_max, float* lse,
                              void* scratch, int64_t scratch_bytes, void* cuda_stream);
 
+/* The k largest logits of every row, largest first (of equal ones the lowest token), and log sum_v exp(logits[i,v] / temperature): what saki_distill_top
+ * wants to know of a teacher's row.  (The paper moves whole rows.)  Logits of -inf are masked entries and not listed: behind the last one that is, token -1 and logit -inf;
+ * a row of nothing else has lse -inf.  A NaN or +inf in a row, or a logit that is +inf once divided
+ * by the temperature: NONFINITE, with tokens -1, logits and lse 0.  Rows may start anywhere (whole elements).
+ * Asynchronous on the stream.  scratch: saki_top_scratch_bytes(N, V, k) bytes, 256-byte aligned, owned by one call at a time. */
+typedef struct {
+  const void* logits; int64_t ld;   /* [N,V], unit stride along V, row stride in elements; 0: every row the same */
+  int64_t N;                        /* 0 .. 2^24 */
+  int32_t V, dtype;                 /* V 2 .. 2^22 */
+  int32_t k;                        /* 1 .. 128, more than V too */
+  float temperature;                /* finite, >= 1e-30 */
+} saki_top_in;
+typedef struct {
+  int32_t* token;       /* [N,k] */
+  float* logit;         /* [N,k] the logits themselves, not divided by the temperature */
+  float* lse;           /* [N] or NULL */
+  uint32_t* row_status; /* [N] or NULL */
+} saki_top_out;
+SAKI_API int64_t saki_top_scratch_bytes(int64_t N, int32_t V, int32_t k);
+SAKI_API int saki_top_logits(const saki_top_in* in, const saki_top_out* out, void* scratch, int64_t scratch_bytes, void* cuda_stream);
+
 /* Distillation from a teacher's top logits (the paper moves full-vocabulary rows between engines, and names that as what an engine is bound by; a list of the
  * teacher's k largest logits is what can be kept of a row instead).  Row i has a list of tokens and their teacher logits; an entry with token -1, or with logit -inf, is not there.
  * With pi = softmax(s / temperature) over the whole row, K the tokens that are there, t their logits / temperature:

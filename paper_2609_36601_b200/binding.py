@@ -19,7 +19,8 @@ _fast = None          # the module _saki_torch, bound to the library
 _BOUND = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc", "saki_route_bwd_from_meta", "saki_select_tm",
           "saki_spec_verify", "saki_sample_proposal", "saki_vshard_stage", "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate",
           "saki_cache_fork", "saki_cache_compact", "saki_cache_copy_pages", "saki_cache_write", "saki_paged_attention_scratch_bytes", "saki_paged_attention",
-          "saki_beam_scratch_bytes", "saki_beam_select", "saki_linear_ce_scratch_bytes", "saki_linear_ce_fwd", "saki_linear_ce_bwd", "saki_distill_scratch_bytes", "saki_distill_top", "saki_last_error")
+          "saki_beam_scratch_bytes", "saki_beam_select", "saki_linear_ce_scratch_bytes", "saki_linear_ce_fwd", "saki_linear_ce_bwd", "saki_distill_scratch_bytes", "saki_distill_top", "saki_top_scratch_bytes", "saki_top_logits",
+          "saki_last_error")
 
 SAKI_F32, SAKI_BF16 = 0, 1
 ROW_SATURATED, ROW_EPS_ZERO, ROW_MASKED, ROW_NONFINITE, ROW_BAD_ID, ROW_TIMEOUT, ROW_NOT_COMPUTED = 1, 2, 4, 8, 16, 32, 64
@@ -32,7 +33,7 @@ EXPORTS = ("saki_route_fwd", "saki_route_fwd_bwd", "saki_route_fwd_bwd_noalloc",
            "saki_lmhead_scratch_bytes", "saki_lmhead_lse",
            "saki_cache_scratch_bytes", "saki_cache_reserve", "saki_cache_truncate", "saki_cache_fork", "saki_cache_compact",
            "saki_cache_copy_pages", "saki_cache_write", "saki_paged_attention_scratch_bytes", "saki_paged_attention", "saki_beam_scratch_bytes", "saki_beam_select",
-           "saki_linear_ce_scratch_bytes", "saki_linear_ce_fwd", "saki_linear_ce_bwd", "saki_distill_scratch_bytes", "saki_distill_top",
+           "saki_linear_ce_scratch_bytes", "saki_linear_ce_fwd", "saki_linear_ce_bwd", "saki_distill_scratch_bytes", "saki_distill_top", "saki_top_scratch_bytes", "saki_top_logits",
            "saki_sample_proposal", "saki_check", "saki_set_kernel", "saki_last_kernel", "saki_last_layout", "saki_last_rowsm_layout", "saki_redo_count",
            "saki_set_spec_early_out", "saki_spec_positions_routed", "saki_solve_evaluations", "saki_set_wait_limit", "saki_set_phase_clock", "saki_phase_cycles",
            "saki_launch_count",
@@ -169,6 +170,14 @@ class SakiDistillOut(C.Structure):
     _fields_ = [("loss", C.c_void_p), ("lse", C.c_void_p), ("row_status", C.c_void_p)]
 
 
+class SakiTopIn(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("ld", C.c_int64), ("N", C.c_int64), ("V", C.c_int32), ("dtype", C.c_int32), ("k", C.c_int32), ("temperature", C.c_float)]
+
+
+class SakiTopOut(C.Structure):
+    _fields_ = [("token", C.c_void_p), ("logit", C.c_void_p), ("lse", C.c_void_p), ("row_status", C.c_void_p)]
+
+
 def load_library(path: str | None = None):
     """Loads libsaki.so (built in-tree by `python -m paper_2609_36601_b200.build`)."""
     global _lib, _fast
@@ -245,6 +254,10 @@ def load_library(path: str | None = None):
     lib.saki_distill_scratch_bytes.restype = C.c_int64
     lib.saki_distill_top.argtypes = [C.POINTER(SakiDistillIn), C.POINTER(SakiDistillOut), C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]
     lib.saki_distill_top.restype = C.c_int
+    lib.saki_top_scratch_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32]
+    lib.saki_top_scratch_bytes.restype = C.c_int64
+    lib.saki_top_logits.argtypes = [C.POINTER(SakiTopIn), C.POINTER(SakiTopOut), C.c_void_p, C.c_int64, C.c_void_p]
+    lib.saki_top_logits.restype = C.c_int
     lib.saki_set_wait_limit.argtypes = [C.c_int64]
     lib.saki_set_wait_limit.restype = C.c_int64
     lib.saki_set_phase_clock.argtypes = [C.c_int]
@@ -475,6 +488,14 @@ def linear_ce_bwd(hidden, weight, target, lse, advantage=None, corrected=None, t
     Returns (dhidden, dweight)."""
     return (_fast or _tensors()).linear_bwd(hidden, weight, target, advantage, corrected, teacher_top1, mask, rollout_status, temperature, lse, grad_scale,
                                             dhidden, dweight, _handle(stream))
+
+
+def top_logits(logits, k, temperature=1.0, stream=None):
+    """saki_top_logits: the k largest logits of every row of `logits` [N, V], largest first, of equal ones the lowest token first.  Returns a dict of token (int32
+    [N, k]; -1: no more that are not masked by -inf), logit (float32 [N, k], -inf there), lse (float32 [N], log sum exp(logits / temperature)) and row_status (int32 [N]):
+    of a teacher's rows, what distill_top takes.  No gradient."""
+    token, logit, lse, status = (_fast or _tensors()).top(logits, k, temperature, _handle(stream))
+    return {"token": token, "logit": logit, "lse": lse, "row_status": status}
 
 
 def distill_top(s, token, logit, teacher_lse=None, reverse=False, temperature=1.0, mask=None, grad_scale=1.0, dlogits=True, stream=None):

@@ -841,6 +841,36 @@ SAKI_API int saki_distill_top(const saki_distill_in* in, const saki_distill_out*
   return launched(e, launches, "distillation kernel launch");
 }
 
+// ---- a row's top logits ----
+static int top_check(int64_t N, int32_t V, int32_t k) {
+  g_err[0] = 0;
+  if (N < 0 || N > (1 << 24)) return fail(SAKI_ERR_INVALID_ARG, "N must be in [0, 2^24] (got %lld)", (long long)N);
+  if (V < 2 || V > (1 << 22)) return fail(SAKI_ERR_INVALID_ARG, "V must be in [2, 2^22] (got %d)", V);
+  if (k < 1 || k > 128) return fail(SAKI_ERR_INVALID_ARG, "k must be in [1,128] (got %d)", k);
+  return SAKI_OK;
+}
+
+SAKI_API int64_t saki_top_scratch_bytes(int64_t N, int32_t V, int32_t k) { return top_check(N, V, k) ? 0 : top_scratch_bytes(N, V, k); }
+
+SAKI_API int saki_top_logits(const saki_top_in* in, const saki_top_out* out, void* scratch, int64_t scratch_bytes, void* cuda_stream) {
+  g_err[0] = 0;
+  if (!in || !out) return fail(SAKI_ERR_INVALID_ARG, "NULL argument struct");
+  int rc = top_check(in->N, in->V, in->k);
+  if (rc) return rc;
+  if (in->dtype != SAKI_F32 && in->dtype != SAKI_BF16) return fail(SAKI_ERR_INVALID_ARG, "unknown dtype %d", in->dtype);
+  if (!(in->temperature >= 1e-30f) || std::isinf(in->temperature)) return fail(SAKI_ERR_INVALID_ARG, "temperature must be finite and >= 1e-30");
+  if (in->ld < 0) return fail(SAKI_ERR_INVALID_ARG, "negative row stride");
+  if (in->N == 0) return SAKI_OK;
+  if (!in->logits || !out->token || !out->logit || !scratch) return fail(SAKI_ERR_INVALID_ARG, "NULL logits, token, logit or scratch pointer");
+  if (scratch_bytes < top_scratch_bytes(in->N, in->V, in->k)) return fail(SAKI_ERR_INVALID_ARG, "scratch too small: %lld bytes needed", (long long)top_scratch_bytes(in->N, in->V, in->k));
+  if (!aligned(scratch, 256) || !aligned(in->logits, in->dtype == SAKI_BF16 ? 2 : 4)) return fail(SAKI_ERR_UNSUPPORTED, "scratch must be 256-byte aligned, logits start at a whole element");
+  unsigned long long* flagged = nullptr;
+  if ((rc = device_ready(&flagged))) return rc;
+  int launches = 0;
+  const cudaError_t e = launch_top(*in, *out, scratch, flagged, &launches, (cudaStream_t)cuda_stream);
+  return launched(e, launches, "top logits kernel launch");
+}
+
 // ---- cross entropy from hidden states ----
 static int linear_size_check(int64_t N, int32_t d, int32_t V) {
   g_err[0] = 0;

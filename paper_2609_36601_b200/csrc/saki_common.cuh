@@ -281,6 +281,8 @@ int64_t distill_scratch_bytes(int64_t N, int32_t k);
 bool distill_stream_can_serve(const saki_distill_in& in);
 cudaError_t launch_distill(const saki_distill_in& in, const saki_distill_out& out, void* dlogits, int64_t ld_g, float grad_scale, void* scratch, bool stream,
                            unsigned long long* flagged, int* n_launches, cudaStream_t st);
+int64_t top_scratch_bytes(int64_t N, int32_t V, int32_t k);
+cudaError_t launch_top(const saki_top_in& in, const saki_top_out& out, void* scratch, unsigned long long* flagged, int* n_launches, cudaStream_t st);
 int vshard_combine_host(const saki_vshard_in& in, int stage, const double* gathered, double* state, const saki_out& out,
                         bool allow_fast);
 

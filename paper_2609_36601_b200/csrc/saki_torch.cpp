@@ -44,6 +44,8 @@ struct Lib {
   decltype(&saki_linear_ce_bwd) linear_ce_bwd;
   decltype(&saki_distill_scratch_bytes) distill_scratch_bytes;
   decltype(&saki_distill_top) distill_top;
+  decltype(&saki_top_scratch_bytes) top_scratch_bytes;
+  decltype(&saki_top_logits) top_logits;
   decltype(&saki_last_error) last_error;
 };
 Lib lib = {};
@@ -840,6 +842,30 @@ PyObject* py_distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// top(logits, k, temperature, stream) -> (token, logit, lse, row_status)
+PyObject* py_top(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    n_args(n, 4);
+    const at::Tensor& x = tensor(a[0]);
+    if (x.dim() != 2 || (x.size(1) > 1 && x.stride(1) != 1)) raise_value("logits must be [N, V] with unit stride along V");
+    const at::Device dev = x.device();
+    const int64_t N = x.size(0), V = x.size(1), k = integer(a[1]);
+    if (V > INT32_MAX || k < 1 || k > 128) raise_value("k must be in [1,128]");
+    saki_top_in in = {};
+    in.dtype = dtype_code(x);
+    const OnStream on(dev, a[3]);
+    in.logits = x.data_ptr(); in.ld = row_stride(x); in.N = N; in.V = (int32_t)V; in.k = (int32_t)k; in.temperature = (float)number(a[2]);
+    const at::Tensor token = empty({N, k}, at::kInt, dev), logit = empty({N, k}, at::kFloat, dev), lse = empty({N}, at::kFloat, dev), st = empty({N}, at::kInt, dev);
+    const saki_top_out out = {(int32_t*)token.data_ptr(), (float*)logit.data_ptr(), (float*)lse.data_ptr(), (uint32_t*)st.data_ptr()};
+    const int64_t bytes = lib.top_scratch_bytes(N, in.V, in.k);
+    if (bytes == 0) raise_saki(SAKI_ERR_INVALID_ARG, lib.last_error());
+    const at::Tensor scratch = empty({bytes}, at::kByte, dev);
+    check_rc(unlocked([&] { return lib.top_logits(&in, &out, scratch.data_ptr(), bytes, on.handle); }));
+    Owned t(THPVariable_Wrap(token)), l(THPVariable_Wrap(logit)), y(THPVariable_Wrap(lse)), z(THPVariable_Wrap(st));
+    return PyTuple_Pack(4, t.p, l.p, y.p, z.p);
+  });
+}
+
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))py_bind, METH_FASTCALL, nullptr},
     {"alloc_outputs", (PyCFunction)(void (*)(void))py_alloc_outputs, METH_FASTCALL, nullptr},
@@ -859,6 +885,7 @@ PyMethodDef methods[] = {
     {"linear", (PyCFunction)(void (*)(void))py_linear, METH_FASTCALL, nullptr},
     {"linear_bwd", (PyCFunction)(void (*)(void))py_linear_bwd, METH_FASTCALL, nullptr},
     {"distill", (PyCFunction)(void (*)(void))py_distill, METH_FASTCALL, nullptr},
+    {"top", (PyCFunction)(void (*)(void))py_top, METH_FASTCALL, nullptr},
     {"vshard_local", (PyCFunction)(void (*)(void))py_vshard_local, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_saki_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
