@@ -8,8 +8,8 @@
 // matrix of their own, in order, whose number of rows the products read from device memory.  (So a masked row costs nothing, and what stands in it,
 // infinities among it, reaches nothing.)
 //   forward    one launch over all tiles of the logits: their sums and the supervised token's logit leave, the logits do not
-//   backward   the vocabulary in pieces: the logits of a piece once more, G of the piece in bf16 into a buffer that stays in L2; in the next
-//              launch, beside the next piece's logits, its two products
+//   backward   the vocabulary in pieces: the logits of a piece once more, G of the piece in bf16 into a buffer; in the next launch, beside the next piece's
+//              logits, its two products
 // All three products are tiles of 256 x 256 on CTA pairs (tcgen05, cta_group::2), K in blocks of 64 through a TMA ring; operands that lie with their
 // K outermost (W and H in the two gradients, G in dW) are read M- or N-major as they are, nothing is transposed.  Tiles are dealt out by tickets: the kinds
 // differ in length.  G is rounded to bf16 (half a step, 2^-8 of an element at the most), as an operand of the tensor cores has to be next to bf16 weights; s is
@@ -31,7 +31,7 @@ namespace lin {
 
 namespace {
 
-constexpr int TILE = 256, HALF = 128, BK = 64, ACC = 2, STAGES = 6, SLOTS = 3;
+constexpr int TILE = 256, HALF = 128, BK = 64, ACC = 2, STAGES = 6, SLOTS = 4;
 constexpr int A_BYTES = HALF * BK * 2, STAGE_BYTES = 2 * A_BYTES;
 constexpr int THREADS = 224;
 constexpr int SMEM = STAGES * STAGE_BYTES + 512 + 1024;      // ring, barriers, alignment
@@ -53,13 +53,14 @@ struct Rows {                         // the call's rows, and what is gathered o
   int* tok;                           // by place
   float* coef;
   float* lse2;                        // log-sum-exp in base 2 (backward)
-  __nv_bfloat16* h;                   // [rows, padded to whole tiles][d]
+  __nv_bfloat16* h;                   // [rows, padded to whole tiles][ld]: rows start on 128-byte boundaries
+  int ld;
   int vec;                            // rows of `hidden` start at 16-byte boundaries
 };
 
 struct Tiles {
   Head* head;
-  int launch;                         // which ticket counter
+  int launch;                         // which ticket counter, -1: tiles of one kind alone, dealt out in turn
   int d, V, d_tiles;
   long long wait_limit;
   // logits of columns [v0, v0 + 256 l_tiles): forward (g NULL) or G
@@ -87,14 +88,19 @@ struct Row { int tok; float coef; uint32_t status; };      // tok -1: the row co
 __device__ __forceinline__ Row row_of(const Rows& P, int64_t row) {
   const saki_linear_in& in = P.in;
   Row m = {-1, 0.f, 0u};
-  if (in.mask && in.mask[row] == 0) { m.status = SAKI_ROW_MASKED; return m; }
-  if (in.rollout_status && (in.rollout_status[row] & (SAKI_ROW_NONFINITE | SAKI_ROW_BAD_ID | SAKI_ROW_TIMEOUT | SAKI_ROW_NOT_COMPUTED))) { m.status = SAKI_ROW_NOT_COMPUTED; return m; }
-  const bool c = in.corrected && in.corrected[row] != 0;
-  const int tok = c ? in.teacher_top1[row] : in.target[row];
-  const float coef = c || !in.advantage ? 1.f : in.advantage[row];
+  // (all loads first: a row's word on whether it counts takes one of them, not six in turn)
+  const bool masked = in.mask && in.mask[row] == 0;
+  const uint32_t rollout = in.rollout_status ? in.rollout_status[row] : 0u;
+  const bool hit = in.corrected && in.corrected[row] != 0;
+  const int target = in.target[row], top1 = in.corrected ? in.teacher_top1[row] : 0;
+  const float advantage = in.advantage ? in.advantage[row] : 1.f, lse = P.lse ? P.lse[row] : 0.f;
+  if (masked) { m.status = SAKI_ROW_MASKED; return m; }
+  if (rollout & (SAKI_ROW_NONFINITE | SAKI_ROW_BAD_ID | SAKI_ROW_TIMEOUT | SAKI_ROW_NOT_COMPUTED)) { m.status = SAKI_ROW_NOT_COMPUTED; return m; }
+  const int tok = hit ? top1 : target;
+  const float coef = hit ? 1.f : advantage;
   if (!(fabsf(coef) < CUDART_INF_F)) { m.status = SAKI_ROW_NONFINITE; return m; }
   if (tok < 0 || tok >= in.V) { m.status = SAKI_ROW_BAD_ID; return m; }
-  if (P.lse && !(fabsf(P.lse[row]) < CUDART_INF_F)) { m.status = SAKI_ROW_NONFINITE; return m; }
+  if (!(fabsf(lse) < CUDART_INF_F)) { m.status = SAKI_ROW_NONFINITE; return m; }
   m.tok = tok; m.coef = coef;
   return m;
 }
@@ -113,6 +119,7 @@ __global__ void __launch_bounds__(GT) gather_kernel(const Rows P, int per_block)
     for (int i = tid; i < MAX_LAUNCHES; i += GT) P.head->ticket[i] = 0;
   }
   int n = 0;
+#pragma unroll 4
   for (int64_t i = tid; i < r0; i += GT) n += row_of(P, i).tok >= 0;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
@@ -146,7 +153,7 @@ __global__ void __launch_bounds__(GT) gather_kernel(const Rows P, int per_block)
     for (int r = warp; r < rows; r += GT / 32) {
       if (place[r] < 0) continue;
       const __nv_bfloat16* s = (const __nv_bfloat16*)P.in.hidden + (c0 + r) * P.in.ld_h;
-      __nv_bfloat16* t = P.h + (int64_t)place[r] * d;
+      __nv_bfloat16* t = P.h + (int64_t)place[r] * P.ld;
       if (P.vec) {
 #pragma unroll 4
         for (int j = lane; j < d / 8; j += 32) ((uint4*)t)[j] = __ldg((const uint4*)s + j);
@@ -155,9 +162,9 @@ __global__ void __launch_bounds__(GT) gather_kernel(const Rows P, int per_block)
     }
     base += total;
   }
-  if (blockIdx.x == gridDim.x - 1) {  // the last rows' tile is filled up with zeros
-    const int64_t zeros = (int64_t)((base + TILE - 1) / TILE * TILE - base) * d / 8;
-    uint4* t = (uint4*)(P.h + (int64_t)base * d);
+  if (blockIdx.x == gridDim.x - 1) {  // the last rows' block of K is filled up with zeros (dW sums over whole blocks)
+    const int64_t zeros = (int64_t)((base + BK - 1) / BK * BK - base) * P.ld / 8;
+    uint4* t = (uint4*)(P.h + (int64_t)base * P.ld);
     for (int64_t j = tid; j < zeros; j += GT) t[j] = make_uint4(0u, 0u, 0u, 0u);
     if (tid == 0) P.head->count = base;
   }
@@ -192,7 +199,7 @@ __global__ void __launch_bounds__(256) loss_kernel(const Rows P, const saki_line
     double s = 0.0;
     for (int t = lane; t < n_tiles; t += 32) {
       const float2 a = pp[t];
-      if (a.x > -CUDART_INF_F) s += (double)a.y * exp2((double)a.x - (double)mx);
+      if (a.x > -CUDART_INF_F) s += (double)(a.y * ex2f(a.x - mx));
     }
     s = warp_sum(s);
     const double l = ((double)mx + log2(s)) * LN2, lp = (double)z_tok[at] * (double)rtau - l;
@@ -225,9 +232,10 @@ __global__ void __launch_bounds__(256) dhidden_kernel(const Rows P, const float*
       uint4 r = make_uint4(0u, 0u, 0u, 0u);
       if (at >= 0) {
         float a[8];
-        const float* s = dh + (int64_t)at * d + j;
+        const float* s = dh + (int64_t)at * d + j;      // (8 parts on their way at a time)
 #pragma unroll
         for (int k = 0; k < 8; ++k) a[k] = 0.f;
+#pragma unroll 8
         for (int p = 0; p < splits; ++p, s += dh_split) {
           const float4 x = *(const float4*)s, y = *(const float4*)(s + 4);
           a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w; a[4] += y.x; a[5] += y.y; a[6] += y.z; a[7] += y.w;
@@ -373,10 +381,15 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
   const Plan plan(P);
   const long long limit = P.wait_limit;
 
-  int slot = 0;
+  int slot = 0, in_turn = (int)blockIdx.x >> 1;
   uint32_t slot_phase = 0;
   auto next_tile = [&](bool whole_warp) -> Tile {      // of a role: waits for the next ticket, reads it, gives the slot back
     Tile x = {-1, 0, 0, 0, 0, 0};
+    if (P.launch < 0) {
+      x = plan.tile(P, in_turn < plan.total ? in_turn : -1);
+      in_turn += (int)gridDim.x >> 1;
+      return x;
+    }
     if (!wait(&s_full[slot], slot_phase, stop, limit)) return x;
     x = plan.tile(P, *(volatile int*)&slot_tile[slot]);
     if (whole_warp) __syncwarp();
@@ -391,11 +404,11 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
-      while (ok) {
-        const Tile x = next_tile(false);
-        if (x.kind < 0) break;
+      for (Tile x = next_tile(false), next = x; ok && x.kind >= 0; x = next) {
+        if (x.k0 == x.k1) next = next_tile(false);
         const int rows = x.m * TILE + (int)rank * HALF, cols = x.n * TILE + (int)rank * HALF;      // this CTA's part of M and of N
         for (int kb = x.k0; kb < x.k1; ++kb) {
+          if (kb == (x.k0 + x.k1) / 2) next = next_tile(false);      // (so that there is no wait between tiles)
           if (!wait(&empty[stage], phase ^ 1u, stop, limit)) { ok = false; break; }
           const uint32_t a = smem_addr(base + stage * STAGE_BYTES), b = a + A_BYTES, bar = at_rank(smem_addr(&full[stage]), 0);
           if (rank == 0) mbar_expect_tx(&full[stage], 2 * STAGE_BYTES);
@@ -422,13 +435,13 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
-      while (ok) {
-        const Tile x = next_tile(false);
-        if (x.kind < 0) break;
+      for (Tile x = next_tile(false), next = x; ok && x.kind >= 0; x = next) {
+        if (x.k0 == x.k1) next = next_tile(false);
         if (!wait(&t_empty[acc], acc_phase ^ 1u, stop, limit)) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + (uint32_t)(acc * TILE);
         for (int kb = x.k0; kb < x.k1; ++kb) {
+          if (kb == (x.k0 + x.k1) / 2) next = next_tile(false);
           if (!wait(&full[stage], phase, stop, limit)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t at = smem_addr(base + stage * STAGE_BYTES);
@@ -444,7 +457,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       }
     }
   } else if (warp == 6) {
-    if (lane == 0 && rank == 0) {     // ---- tickets
+    if (lane == 0 && rank == 0 && P.launch >= 0) {     // ---- tickets
       int s = 0;
       uint32_t phase = 0;
       for (;;) {
@@ -475,7 +488,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
         const int col_tile = P.v0 + x.n * TILE;
         const int tok = there ? P.tok[row] : -1;
         if (!P.g) {
-          float m = -CUDART_INF_F, s = 0.f, z = 0.f;
+          float m = -CUDART_INF_F, s = 0.f, z = 0.f;      // m: of the products, the sum under c m
 #pragma unroll 1
           for (int ch = 0; ch < TILE / 32; ++ch) {
             float y[32];
@@ -487,33 +500,58 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
               for (int i = 0; i < 32; ++i)
                 if (tok - col0 == i) z = y[i];
             }
-            float cm = -CUDART_INF_F;
+            if (col0 + 32 > P.V) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              y[i] = col0 + i < P.V ? y[i] * P.c : -CUDART_INF_F;
-              cm = fmaxf(cm, y[i]);
+              for (int i = 0; i < 32; ++i)
+                if (col0 + i >= P.V) y[i] = -CUDART_INF_F;
             }
-            if (cm > m) { s *= ex2f(m - cm); m = cm; }      // (m = -inf at first: s is 0 and stays 0)
-            float add = 0.f;
-            const float mm = m > -CUDART_INF_F ? m : 0.f;   // nothing but -inf (or NaN) so far
+            float t[4];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) add += ex2f(y[i] - mm);
-            s += add;
+            for (int i = 0; i < 4; ++i) t[i] = fmaxf(y[i], y[i + 4]);
+#pragma unroll
+            for (int i = 8; i < 32; i += 8)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) t[j] = fmaxf(t[j], fmaxf(y[i + j], y[i + j + 4]));
+            const float cm = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+            if (cm > m) { s *= m > -CUDART_INF_F ? ex2f((m - cm) * P.c) : 0.f; m = cm; }
+            const float2 cc = splat(P.c), off = splat(m > -CUDART_INF_F ? -m : 0.f);      // (nothing but -inf, or NaN, so far)
+            float2 a0 = splat(0.f), a1 = splat(0.f);
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              a0 = fadd2(a0, ex2f2(fmul2(fadd2(make_float2(y[i], y[i + 1]), off), cc)));
+              a1 = fadd2(a1, ex2f2(fmul2(fadd2(make_float2(y[i + 2], y[i + 3]), off), cc)));
+            }
+            s += (a0.x + a0.y) + (a1.x + a1.y);
           }
           if (there) {
-            P.part[(int64_t)row * P.n_tiles + x.n] = make_float2(m, s);
+            P.part[(int64_t)row * P.n_tiles + x.n] = make_float2(m * P.c, s);
             if ((unsigned)(tok - col_tile) < (unsigned)TILE) P.z_tok[row] = z;
           }
         } else {
           const float k = there ? P.coef[row] : 0.f, l2 = there ? P.lse2[row] : 0.f;
+          const bool large = __any_sync(0xffffffffu, !(fabsf(l2) < 1024.f));
           __nv_bfloat16* out = P.g + (int64_t)row * P.ld_g + x.n * TILE;
 #pragma unroll 1
           for (int ch = 0; ch < TILE / 32; ++ch) {
             float y[32];
             const int col0 = col_tile + ch * 32;
             ld32(from + ch * 32, y);
+            const float2 cc = splat(P.c), off = splat(-l2), kk = splat(k);
+            if (large) {              // a large log-sum-exp's rounding may leave a logit above it
 #pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] = there && col0 + i < P.V ? k * ex2f(fminf(fmaf(y[i], P.c, -l2), 0.f)) : 0.f;      // (a large log-sum-exp's rounding may leave a logit above it)
+              for (int i = 0; i < 32; ++i) y[i] = k * ex2f(fminf(fmaf(y[i], P.c, -l2), 0.f));
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) {
+                const float2 e = fmul2(ex2f2(ffma2(make_float2(y[i], y[i + 1]), cc, off)), kk);
+                y[i] = e.x; y[i + 1] = e.y;
+              }
+            }
+            if (!there || col0 + 32 > P.V) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (!there || col0 + i >= P.V) y[i] = 0.f;
+            }
             if ((unsigned)(tok - col0) < 32u) {
 #pragma unroll
               for (int i = 0; i < 32; ++i)
@@ -597,7 +635,7 @@ int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 // The pieces of the vocabulary, and where things lie in scratch.
 struct Layout {
   int64_t rows;                       // padded to whole tiles
-  int n_tiles, d_tiles, piece, pieces, splits;      // piece: columns, a multiple of 256
+  int n_tiles, d_tiles, ld, piece, pieces, splits;      // piece: columns, a multiple of 256
   int64_t rank, tok, coef, lse2, h, part, z_tok, g, dh, bytes;
 };
 Layout layout(int64_t N, int d, int V, bool backward) {
@@ -605,8 +643,11 @@ Layout layout(int64_t N, int d, int V, bool backward) {
   l.rows = up(std::max<int64_t>(N, 1), TILE);
   l.n_tiles = (V + TILE - 1) / TILE;
   l.d_tiles = (d + TILE - 1) / TILE;
-  // a piece's G takes about half of the L2 cache; the pieces are about equal
-  const int64_t most = std::max<int64_t>(1, (64LL << 20) / (l.rows * 2 * TILE));
+  l.ld = (int)up(d, 64);
+  // A piece's G takes up to 256 MB (two pieces are there at a time); the pieces are about equal.  Larger pieces mean fewer launches, each of which ends with SMs that have
+  // no tile left, and fewer additions to dH in memory; that G does not stay in L2 costs less.  (2560 features, 151936 entries, backward pass of 8192 rows, with pieces of 32, 64, 128, 256
+  // and 512 MB: 19.4, 16.1, 14.7, 14.3 and 14.1 ms; 4096 rows 8.3, 7.5, 7.3, 7.2, 7.2.)
+  const int64_t most = std::max<int64_t>(1, (256LL << 20) / (l.rows * 2 * TILE));
   l.pieces = (int)std::max<int64_t>((l.n_tiles + most - 1) / most, 1);
   l.pieces = std::min(l.pieces, MAX_LAUNCHES - 1);
   const int tiles = (l.n_tiles + l.pieces - 1) / l.pieces;
@@ -618,7 +659,7 @@ Layout layout(int64_t N, int d, int V, bool backward) {
   int64_t at = up((int64_t)sizeof(Head), 256);
   auto take = [&](int64_t bytes) { const int64_t a = at; at += up(bytes, 256); return a; };
   l.rank = take(N * 4); l.tok = take(l.rows * 4); l.coef = take(l.rows * 4); l.lse2 = take(l.rows * 4);
-  l.h = take(l.rows * d * 2);
+  l.h = take(l.rows * l.ld * 2);
   if (!backward) { l.part = take(l.rows * l.n_tiles * 8); l.z_tok = take(l.rows * 4); }
   else { l.g = take(2 * l.rows * l.piece * 2); l.dh = take(l.splits * l.rows * d * 4); }
   l.bytes = at;
@@ -651,7 +692,7 @@ Rows rows_of(const saki_linear_in& in, const float* lse, char* s, const Layout& 
   Rows r = {};
   r.in = in; r.lse = lse; r.head = (Head*)s;
   r.rank = (int*)(s + l.rank); r.tok = (int*)(s + l.tok); r.coef = (float*)(s + l.coef); r.lse2 = (float*)(s + l.lse2);
-  r.h = (__nv_bfloat16*)(s + l.h);
+  r.h = (__nv_bfloat16*)(s + l.h); r.ld = l.ld;
   r.vec = ((uintptr_t)in.hidden & 15) == 0 && in.ld_h % 8 == 0;
   return r;
 }
@@ -680,11 +721,12 @@ cudaError_t launch_linear_fwd(const saki_linear_in& in, const saki_linear_out& o
   char* const s = (char*)scratch;
   const Rows r = rows_of(in, nullptr, s, l);
   Maps maps = {};
-  if (!make_map(&maps.h_k, r.h, l.rows, in.d, in.d, HALF) || !make_map(&maps.w_k, in.weight, in.V, in.d, in.ld_w, HALF)) return cudaErrorInvalidValue;
+  if (!make_map(&maps.h_k, r.h, l.rows, in.d, l.ld, HALF) || !make_map(&maps.w_k, in.weight, in.V, in.d, in.ld_w, HALF)) return cudaErrorInvalidValue;
   maps.h_mn = maps.w_mn = maps.g_k = maps.g_mn = maps.h_k;
   e = launch_gather(r, sms, st);
   if (e != cudaSuccess) return e;
   Tiles t = tiles_of(r, l, wait_limit);
+  t.launch = -1;
   t.l_tiles = l.n_tiles;
   t.part = (float2*)(s + l.part); t.z_tok = (float*)(s + l.z_tok);
   const int pairs = std::min(sms, MAX_CTAS) / 2;
@@ -708,8 +750,8 @@ cudaError_t launch_linear_bwd(const saki_linear_in& in, const float* lse, void* 
   __nv_bfloat16* const g[2] = {(__nv_bfloat16*)(s + l.g), (__nv_bfloat16*)(s + l.g) + l.rows * l.piece};
   Maps maps[2];
   for (int b = 0; b < 2; ++b)
-    if (!make_map(&maps[b].h_k, r.h, l.rows, in.d, in.d, HALF) || !make_map(&maps[b].w_k, in.weight, in.V, in.d, in.ld_w, HALF) ||
-        !make_map(&maps[b].h_mn, r.h, l.rows, in.d, in.d, BK) || !make_map(&maps[b].w_mn, in.weight, in.V, in.d, in.ld_w, BK) ||
+    if (!make_map(&maps[b].h_k, r.h, l.rows, in.d, l.ld, HALF) || !make_map(&maps[b].w_k, in.weight, in.V, in.d, in.ld_w, HALF) ||
+        !make_map(&maps[b].h_mn, r.h, l.rows, in.d, l.ld, BK) || !make_map(&maps[b].w_mn, in.weight, in.V, in.d, in.ld_w, BK) ||
         !make_map(&maps[b].g_k, g[b], l.rows, l.piece, l.piece, HALF) || !make_map(&maps[b].g_mn, g[b], l.rows, l.piece, l.piece, BK)) return cudaErrorInvalidValue;
   e = launch_gather(r, sms, st);
   if (e != cudaSuccess) return e;
@@ -721,7 +763,7 @@ cudaError_t launch_linear_bwd(const saki_linear_in& in, const float* lse, void* 
   const int pairs = std::min(sms, MAX_CTAS) / 2;
   auto columns = [&](int p) { return std::min(l.piece / TILE, l.n_tiles - p * (l.piece / TILE)); };
   for (int p = 0; p <= l.pieces; ++p) {      // the logits of piece p, the products of piece p - 1
-    t.launch = p;
+    t.launch = p > 0 ? p : -1;
     t.l_tiles = p < l.pieces ? columns(p) : 0; t.v0 = p * l.piece; t.g = g[p & 1];
     t.b_tiles = p > 0 ? columns(p - 1) : 0; t.b0 = (p - 1) * l.piece; t.first = p == 1;
     const int64_t tiles = l.rows / TILE * t.l_tiles + (int64_t)t.b_tiles * l.d_tiles * (t.dw != nullptr) + (t.dh && p > 0 ? l.rows / TILE * l.d_tiles * l.splits : 0);
