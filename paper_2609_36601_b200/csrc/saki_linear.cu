@@ -34,7 +34,8 @@ namespace {
 constexpr int TILE = 256, HALF = 128, BK = 64, ACC = 2, STAGES = 6, SLOTS = 4;
 constexpr int A_BYTES = HALF * BK * 2, STAGE_BYTES = 2 * A_BYTES;
 constexpr int THREADS = 224;
-constexpr int SMEM = STAGES * STAGE_BYTES + 512 + 1024;      // ring, barriers, alignment
+constexpr int OUT_BYTES = 32 * 128;                          // what a warp hands to a store: 32 rows of 128 bytes
+constexpr int SMEM = STAGES * STAGE_BYTES + 4 * 2 * OUT_BYTES + 512 + 1024;      // ring, two stores of each epilogue warp, barriers, alignment
 constexpr int MAX_CTAS = 256, MAX_LAUNCHES = 512;
 enum { KIND_LOGITS = 0, KIND_DH, KIND_DW, KINDS };
 
@@ -63,7 +64,7 @@ struct Tiles {
   int launch;                         // which ticket counter, -1: tiles of one kind alone, dealt out in turn
   int d, V, d_tiles;
   long long wait_limit;
-  // logits of columns [v0, v0 + 256 l_tiles): forward (g NULL) or G
+  // logits of columns [v0, v0 + 256 l_tiles): their sums, or G
   int l_tiles, v0;
   float c;                            // log2(e) / temperature
   float2* part;                       // forward: [rows][n_tiles] (maximum, sum) in base 2
@@ -73,14 +74,11 @@ struct Tiles {
   const float* coef;
   const float* lse2;
   float scale;                        // grad_scale / temperature, of dW's sums
-  __nv_bfloat16* g;                   // [rows][ld_g]
-  int ld_g;
+  int grad;                           // G
   // the products of an earlier piece's G: columns [b0, b0 + 256 b_tiles)
   int b_tiles, b0, splits, first;     // dH: a tile's K in so many parts; first: the sums start here
-  float* dh;                          // [splits][rows_pad][d], NULL: not wanted
-  int64_t dh_split;
-  __nv_bfloat16* dw;                  // [V][ld_dw], NULL: not wanted
-  int64_t ld_dw;
+  int dh, dw;                         // wanted
+  int rows;                           // of a part of dH, [splits][rows][d]
 };
 
 // ---------------------------------------------------------------- rows
@@ -217,33 +215,39 @@ __global__ void __launch_bounds__(256) loss_kernel(const Rows P, const saki_line
   }
 }
 
-// backward: the parts of dH are added and rounded, rows that contribute nothing get zeros; NaN everywhere where a wait ran out
+// backward: the parts of dH are added and rounded, rows that contribute nothing get zeros; NaN everywhere where a wait ran out.  L lanes share the parts of eight elements.
+template <int L>
 __global__ void __launch_bounds__(256) dhidden_kernel(const Rows P, const float* dh, int64_t dh_split, int splits, float scale, __nv_bfloat16* out, int64_t ld_out, __nv_bfloat16* dw, int64_t ld_dw) {
   launch_dependents();
   wait_for_predecessor();
   const bool failed = any_failed(P.head);
-  const int d = P.in.d, d8 = d / 8;
+  const int d = P.in.d, d8 = d / 8, sub = threadIdx.x % L;
   const uint4 nan = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
   if (out) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < P.in.N * d8; i += (int64_t)gridDim.x * 256) {
-      const int64_t row = i / d8;
-      const int j = (int)(i - row * d8) * 8;
+    const int64_t n = P.in.N * d8, step = (int64_t)gridDim.x * 256 / L;
+    for (int64_t i0 = (int64_t)blockIdx.x * 256 / L; i0 < n; i0 += step) {      // (the same for all threads of a block: they exchange)
+      const int64_t i = i0 + threadIdx.x / L, row = min(i, n - 1) / d8;
+      const int j = (int)(min(i, n - 1) - row * d8) * 8;
       const int at = P.rank[row];
-      uint4 r = make_uint4(0u, 0u, 0u, 0u);
-      if (at >= 0) {
-        float a[8];
-        const float* s = dh + (int64_t)at * d + j;      // (8 parts on their way at a time)
+      float a[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) a[k] = 0.f;
-#pragma unroll 8
-        for (int p = 0; p < splits; ++p, s += dh_split) {
+      for (int k = 0; k < 8; ++k) a[k] = 0.f;
+      if (at >= 0) {
+        const float* s = dh + (int64_t)at * d + j + sub * dh_split;
+#pragma unroll 4
+        for (int p = sub; p < splits; p += L, s += L * dh_split) {
           const float4 x = *(const float4*)s, y = *(const float4*)(s + 4);
           a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w; a[4] += y.x; a[5] += y.y; a[6] += y.z; a[7] += y.w;
         }
-        r = make_uint4(pack_bf16x2(a[0] * scale, a[1] * scale), pack_bf16x2(a[2] * scale, a[3] * scale), pack_bf16x2(a[4] * scale, a[5] * scale),
-                       pack_bf16x2(a[6] * scale, a[7] * scale));
       }
-      *(uint4*)(out + row * ld_out + j) = failed ? nan : r;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) a[k] += __shfl_xor_sync(0xffffffffu, a[k], o);
+        a[k] *= scale;
+      }
+      if (i < n && sub == 0)
+        *(uint4*)(out + row * ld_out + j) = failed ? nan : make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(a[4], a[5]), pack_bf16x2(a[6], a[7]));
     }
   }
   if (failed && dw)
@@ -318,32 +322,62 @@ __device__ __forceinline__ void ld32(uint32_t at, float (&x)[32]) {
   for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
 }
 
-struct Maps { CUtensorMap h_k, w_k, h_mn, w_mn, g_k, g_mn; };
+// A warp's 32 rows of 128 bytes to a box of 32 rows: the lanes' words go to shared memory in the box's swizzle, one lane hands them to the copy engine (rows of a warp's own
+// stores would be 32 lines of 16 bytes each).  Two buffers; `add`: to what is there.
+__device__ __forceinline__ uint4 pack8(const float* y) { return make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])); }
+struct Out {
+  uint32_t buf;                       // of the warp
+  int n;                              // stores so far
+  __device__ __forceinline__ void put(const uint4 (&w)[8], const CUtensorMap* map, int x, int y, bool add, int lane) {
+    const uint32_t at = buf + (n & 1) * OUT_BYTES;
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the store before the last has been read
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(w[j].x), "r"(w[j].y), "r"(w[j].z), "r"(w[j].w) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+      if (add) asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(at) : "memory");
+      else asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(at) : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+    ++n;
+  }
+};
+
+struct Maps { CUtensorMap h_k, w_k, h_mn, w_mn, g_k, g_mn, g_out, dw_out, dh_out; };
 
 struct Tile { int kind, m, n, k0, k1, split; };      // kind -1: there is none
-// The tiles of a launch: dW, dH, logits, in that order.
+// The tiles of a launch: of the two gradients the longer ones first, logits last.
 struct Plan {
-  int count, m_tiles, n_dw, n_dh, total;
+  int count, m_tiles, n_dw, n_dh, total, blocks;
+  bool dh_first;
   __device__ __forceinline__ Plan(const Tiles& P) {
     count = *(volatile int*)&P.head->count;
     m_tiles = (count + TILE - 1) / TILE;
     n_dw = P.dw ? P.b_tiles * P.d_tiles : 0;
     n_dh = P.dh && P.b_tiles ? m_tiles * P.d_tiles * P.splits : 0;
+    blocks = (min(P.V - P.b0, P.b_tiles * TILE) + BK - 1) / BK;      // of K, of dH
+    dh_first = (int64_t)blocks * BK > (int64_t)count * P.splits;
     total = n_dw + n_dh + m_tiles * P.l_tiles;
   }
   __device__ __forceinline__ Tile tile(const Tiles& P, int t) const {
     Tile x = {-1, 0, 0, 0, 0, 0};
     if (t < 0) return x;
-    if (t < n_dw) {                   // 256 vocabulary entries, 256 features, all rows
-      x.kind = KIND_DW; x.m = t / P.d_tiles; x.n = t - x.m * P.d_tiles; x.k1 = (count + BK - 1) / BK;
-    } else if ((t -= n_dw) < n_dh) {  // 256 rows, 256 features, a part of the piece's entries
+    const int first = dh_first ? n_dh : n_dw;
+    if (t < n_dw + n_dh && (t < first) == dh_first) {      // 256 rows, 256 features, a part of the piece's entries
+      if (!dh_first) t -= n_dw;
       x.kind = KIND_DH;
-      const int per = P.d_tiles * P.splits, blocks = (min(P.V - P.b0, P.b_tiles * TILE) + BK - 1) / BK;
+      const int per = P.d_tiles * P.splits;
       x.m = t / per; t -= x.m * per;
       x.n = t / P.splits; x.split = t - x.n * P.splits;
       x.k0 = (int)((int64_t)blocks * x.split / P.splits); x.k1 = (int)((int64_t)blocks * (x.split + 1) / P.splits);
+    } else if (t < n_dw + n_dh) {     // 256 vocabulary entries, 256 features, all rows
+      if (dh_first) t -= n_dh;
+      x.kind = KIND_DW; x.m = t / P.d_tiles; x.n = t - x.m * P.d_tiles; x.k1 = (count + BK - 1) / BK;
     } else {                          // 256 rows, 256 vocabulary entries; row tiles innermost: a weight tile is read by neighbours
-      t -= n_dh;
+      t -= n_dw + n_dh;
       x.kind = KIND_LOGITS; x.n = t / m_tiles; x.m = t - x.n * m_tiles; x.k1 = (P.d + BK - 1) / BK;
     }
     return x;
@@ -353,7 +387,8 @@ struct Plan {
 __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant__ Maps maps, const Tiles P) {
   extern __shared__ unsigned char raw[];
   unsigned char* base = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);      // (the same offset in both CTAs)
-  uint64_t* full = (uint64_t*)(base + STAGES * STAGE_BYTES);
+  unsigned char* const out_base = base + STAGES * STAGE_BYTES;
+  uint64_t* full = (uint64_t*)(out_base + 4 * 2 * OUT_BYTES);
   uint64_t *empty = full + STAGES, *t_full = empty + STAGES, *t_empty = t_full + ACC, *s_full = t_empty + ACC, *s_empty = s_full + SLOTS;
   int* slot_tile = (int*)(s_empty + SLOTS);
   uint32_t* tmem_slot = (uint32_t*)(slot_tile + SLOTS);
@@ -476,6 +511,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
     const int q = warp & 3;
     int acc = 0;
     uint32_t acc_phase = 0;
+    Out out = {smem_addr(out_base + q * 2 * OUT_BYTES), 0};
     for (;;) {
       const Tile x = next_tile(true);
       if (x.kind < 0) break;
@@ -487,7 +523,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
         const bool there = row < plan.count;
         const int col_tile = P.v0 + x.n * TILE;
         const int tok = there ? P.tok[row] : -1;
-        if (!P.g) {
+        if (!P.grad) {
           float m = -CUDART_INF_F, s = 0.f, z = 0.f;      // m: of the products, the sum under c m
 #pragma unroll 1
           for (int ch = 0; ch < TILE / 32; ++ch) {
@@ -530,70 +566,73 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
         } else {
           const float k = there ? P.coef[row] : 0.f, l2 = there ? P.lse2[row] : 0.f;
           const bool large = __any_sync(0xffffffffu, !(fabsf(l2) < 1024.f));
-          __nv_bfloat16* out = P.g + (int64_t)row * P.ld_g + x.n * TILE;
+#pragma unroll 1
+          for (int ch = 0; ch < TILE / 64; ++ch) {
+            uint4 w[8];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              float y[32];
+              const int col0 = col_tile + ch * 64 + half * 32;
+              ld32(from + ch * 64 + half * 32, y);
+              const float2 cc = splat(P.c), off = splat(-l2), kk = splat(k);
+              if (large) {            // a large log-sum-exp's rounding may leave a logit above it
+#pragma unroll
+                for (int i = 0; i < 32; ++i) y[i] = k * ex2f(fminf(fmaf(y[i], P.c, -l2), 0.f));
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) {
+                  const float2 e = fmul2(ex2f2(ffma2(make_float2(y[i], y[i + 1]), cc, off)), kk);
+                  y[i] = e.x; y[i + 1] = e.y;
+                }
+              }
+              if (!there || col0 + 32 > P.V) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (!there || col0 + i >= P.V) y[i] = 0.f;
+              }
+              if ((unsigned)(tok - col0) < 32u) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (tok - col0 == i) y[i] -= k;
+              }
+#pragma unroll
+              for (int v = 0; v < 4; ++v) w[half * 4 + v] = pack8(y + 8 * v);
+            }
+            out.put(w, &maps.g_out, x.n * TILE + ch * 64, row - lane, false, lane);
+          }
+        }
+      } else if (x.kind == KIND_DH) {
+        const int y0 = x.split * P.rows + row - lane;
+        if (row - lane < plan.count) {             // (rows of the warp)
 #pragma unroll 1
           for (int ch = 0; ch < TILE / 32; ++ch) {
+            if (x.n * TILE + ch * 32 >= P.d) break;
             float y[32];
-            const int col0 = col_tile + ch * 32;
             ld32(from + ch * 32, y);
-            const float2 cc = splat(P.c), off = splat(-l2), kk = splat(k);
-            if (large) {              // a large log-sum-exp's rounding may leave a logit above it
+            uint4 w[8];
 #pragma unroll
-              for (int i = 0; i < 32; ++i) y[i] = k * ex2f(fminf(fmaf(y[i], P.c, -l2), 0.f));
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; i += 2) {
-                const float2 e = fmul2(ex2f2(ffma2(make_float2(y[i], y[i + 1]), cc, off)), kk);
-                y[i] = e.x; y[i + 1] = e.y;
-              }
-            }
-            if (!there || col0 + 32 > P.V) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (!there || col0 + i >= P.V) y[i] = 0.f;
-            }
-            if ((unsigned)(tok - col0) < 32u) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (tok - col0 == i) y[i] -= k;
-            }
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-              *(uint4*)(out + ch * 32 + v * 8) = make_uint4(pack_bf16x2(y[8 * v], y[8 * v + 1]), pack_bf16x2(y[8 * v + 2], y[8 * v + 3]),
-                                                            pack_bf16x2(y[8 * v + 4], y[8 * v + 5]), pack_bf16x2(y[8 * v + 6], y[8 * v + 7]));
+            for (int v = 0; v < 8; ++v) w[v] = make_uint4(__float_as_uint(y[4 * v]), __float_as_uint(y[4 * v + 1]), __float_as_uint(y[4 * v + 2]), __float_as_uint(y[4 * v + 3]));
+            out.put(w, &maps.dh_out, x.n * TILE + ch * 32, y0, !P.first, lane);
           }
         }
       } else {
-        const int col_tile = x.n * TILE;
-        const bool there = x.kind == KIND_DH ? row < plan.count : P.b0 + row < P.V, none = x.k0 == x.k1;      // no rows at all: nothing was summed
-        float* const sums = P.dh + x.split * P.dh_split + (int64_t)row * P.d;
-        __nv_bfloat16* const out = P.dw + (int64_t)(P.b0 + row) * P.ld_dw;
+        const bool none = x.k0 == x.k1;            // no rows at all: nothing was summed
+        const float k = P.scale;
+        if (P.b0 + row - lane < P.V) {
 #pragma unroll 1
-        for (int ch = 0; ch < TILE / 32; ++ch) {
-          float y[32];
-          const int col0 = col_tile + ch * 32;
-          if (col0 >= P.d) break;
-          ld32(from + ch * 32, y);
-          if (!there) continue;
-          const int have = P.d - col0;               // d is a multiple of 8
-          if (x.kind == KIND_DH) {
+          for (int ch = 0; ch < TILE / 64; ++ch) {
+            if (x.n * TILE + ch * 64 >= P.d) break;
+            uint4 w[8];
 #pragma unroll
-            for (int v = 0; v < 8; ++v)
-              if (v * 4 < have) {
-                float4 o = make_float4(y[4 * v], y[4 * v + 1], y[4 * v + 2], y[4 * v + 3]);
-                float4* const at = (float4*)(sums + col0 + v * 4);
-                if (!P.first) { const float4 b = *at; o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w; }
-                *at = o;
-              }
-          } else {
-            const float k = P.scale;
+            for (int half = 0; half < 2; ++half) {
+              float y[32];
+              ld32(from + ch * 64 + half * 32, y);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] = none ? 0.f : y[i] * k;
+              for (int i = 0; i < 32; ++i) y[i] = none ? 0.f : y[i] * k;
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
-              if (v * 8 < have)
-                *(uint4*)(out + col0 + v * 8) = make_uint4(pack_bf16x2(y[8 * v], y[8 * v + 1]), pack_bf16x2(y[8 * v + 2], y[8 * v + 3]),
-                                                           pack_bf16x2(y[8 * v + 4], y[8 * v + 5]), pack_bf16x2(y[8 * v + 6], y[8 * v + 7]));
+              for (int v = 0; v < 4; ++v) w[half * 4 + v] = pack8(y + 8 * v);
+            }
+            out.put(w, &maps.dw_out, x.n * TILE + ch * 64, P.b0 + row - lane, false, lane);
           }
         }
       }
@@ -602,6 +641,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       if (lane == 0) arrive_at(at_rank(smem_addr(&t_empty[acc]), 0));
       if (++acc == ACC) { acc = 0; acc_phase ^= 1u; }
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
@@ -618,15 +658,15 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
 }
 
 // ---------------------------------------------------------------- host side
-// a row-major bf16 matrix: boxes of 64 elements of box_rows rows, 128-byte swizzle, zeros outside
-bool make_map(CUtensorMap* map, const void* ptr, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+// a row-major matrix of bf16 (or float32): boxes of 128 bytes of box_rows rows, 128-byte swizzle, zeros outside
+bool make_map(CUtensorMap* map, const void* ptr, int64_t rows, int64_t cols, int64_t ld, int box_rows, bool f32 = false) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-  const cuuint32_t box[2] = {64u, (cuuint32_t)box_rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld * (f32 ? 4 : 2)};
+  const cuuint32_t box[2] = {f32 ? 32u : 64u, (cuuint32_t)box_rows};
   const cuuint32_t estr[2] = {1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  return fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -653,9 +693,9 @@ Layout layout(int64_t N, int d, int V, bool backward) {
   const int tiles = (l.n_tiles + l.pieces - 1) / l.pieces;
   l.pieces = (l.n_tiles + tiles - 1) / tiles;
   l.piece = tiles * TILE;
-  // few rows: the sums over the vocabulary are cut so that there is work for every pair of SMs, no part below 16 blocks of K
+  // few rows: the sums over the vocabulary are cut so that there is a tile for every pair of SMs, no part below 16 blocks of K
   const int64_t dh_tiles = l.rows / TILE * l.d_tiles;
-  l.splits = (int)std::max<int64_t>(1, std::min<int64_t>((148 + dh_tiles - 1) / dh_tiles, l.piece / BK / 16));
+  l.splits = (int)std::max<int64_t>(1, std::min<int64_t>((74 + dh_tiles - 1) / dh_tiles, l.piece / BK / 16));
   int64_t at = up((int64_t)sizeof(Head), 256);
   auto take = [&](int64_t bytes) { const int64_t a = at; at += up(bytes, 256); return a; };
   l.rank = take(N * 4); l.tok = take(l.rows * 4); l.coef = take(l.rows * 4); l.lse2 = take(l.rows * 4);
@@ -722,7 +762,7 @@ cudaError_t launch_linear_fwd(const saki_linear_in& in, const saki_linear_out& o
   const Rows r = rows_of(in, nullptr, s, l);
   Maps maps = {};
   if (!make_map(&maps.h_k, r.h, l.rows, in.d, l.ld, HALF) || !make_map(&maps.w_k, in.weight, in.V, in.d, in.ld_w, HALF)) return cudaErrorInvalidValue;
-  maps.h_mn = maps.w_mn = maps.g_k = maps.g_mn = maps.h_k;
+  maps.h_mn = maps.w_mn = maps.g_k = maps.g_mn = maps.g_out = maps.dw_out = maps.dh_out = maps.h_k;      // (not used)
   e = launch_gather(r, sms, st);
   if (e != cudaSuccess) return e;
   Tiles t = tiles_of(r, l, wait_limit);
@@ -752,28 +792,30 @@ cudaError_t launch_linear_bwd(const saki_linear_in& in, const float* lse, void* 
   for (int b = 0; b < 2; ++b)
     if (!make_map(&maps[b].h_k, r.h, l.rows, in.d, l.ld, HALF) || !make_map(&maps[b].w_k, in.weight, in.V, in.d, in.ld_w, HALF) ||
         !make_map(&maps[b].h_mn, r.h, l.rows, in.d, l.ld, BK) || !make_map(&maps[b].w_mn, in.weight, in.V, in.d, in.ld_w, BK) ||
-        !make_map(&maps[b].g_k, g[b], l.rows, l.piece, l.piece, HALF) || !make_map(&maps[b].g_mn, g[b], l.rows, l.piece, l.piece, BK)) return cudaErrorInvalidValue;
+        !make_map(&maps[b].g_k, g[b], l.rows, l.piece, l.piece, HALF) || !make_map(&maps[b].g_mn, g[b], l.rows, l.piece, l.piece, BK) ||
+        !make_map(&maps[b].g_out, g[b ^ 1], l.rows, l.piece, l.piece, 32) || !make_map(&maps[b].dh_out, s + l.dh, l.rows * l.splits, in.d, in.d, 32, true) ||
+        !make_map(&maps[b].dw_out, dweight ? dweight : (void*)g[b], dweight ? in.V : 32, dweight ? in.d : 64, dweight ? ld_dw : 64, 32)) return cudaErrorInvalidValue;
   e = launch_gather(r, sms, st);
   if (e != cudaSuccess) return e;
   Tiles t = tiles_of(r, l, wait_limit);
   t.scale = (float)((double)grad_scale / (double)in.temperature);
-  t.ld_g = l.piece; t.splits = l.splits;
-  t.dh = dhidden ? (float*)(s + l.dh) : nullptr; t.dh_split = l.rows * in.d;
-  t.dw = (__nv_bfloat16*)dweight; t.ld_dw = ld_dw;
+  t.splits = l.splits; t.rows = (int)l.rows; t.grad = 1;
+  t.dh = dhidden != nullptr; t.dw = dweight != nullptr;
   const int pairs = std::min(sms, MAX_CTAS) / 2;
   auto columns = [&](int p) { return std::min(l.piece / TILE, l.n_tiles - p * (l.piece / TILE)); };
   for (int p = 0; p <= l.pieces; ++p) {      // the logits of piece p, the products of piece p - 1
     t.launch = p > 0 ? p : -1;
-    t.l_tiles = p < l.pieces ? columns(p) : 0; t.v0 = p * l.piece; t.g = g[p & 1];
+    t.l_tiles = p < l.pieces ? columns(p) : 0; t.v0 = p * l.piece;
     t.b_tiles = p > 0 ? columns(p - 1) : 0; t.b0 = (p - 1) * l.piece; t.first = p == 1;
-    const int64_t tiles = l.rows / TILE * t.l_tiles + (int64_t)t.b_tiles * l.d_tiles * (t.dw != nullptr) + (t.dh && p > 0 ? l.rows / TILE * l.d_tiles * l.splits : 0);
+    const int64_t tiles = l.rows / TILE * t.l_tiles + (int64_t)t.b_tiles * l.d_tiles * t.dw + (t.dh && p > 0 ? l.rows / TILE * l.d_tiles * l.splits : 0);
     e = launch_pdl_cluster(tiles_kernel, dim3((unsigned)(2 * std::min<int64_t>(pairs, tiles))), THREADS, 2, SMEM, st, maps[(p + 1) & 1], t);
     if (e != cudaSuccess) return e;
   }
   *n_launches = l.pieces + 3;
-  const int64_t vectors = std::max<int64_t>(in.N, 1) * (in.d / 8);
-  return launch_pdl(dhidden_kernel, dim3((unsigned)std::min<int64_t>((vectors + 255) / 256, 8 * sms)), 256, 0, st, true, r, (const float*)(s + l.dh), l.rows * in.d, l.splits, t.scale,
-                    (__nv_bfloat16*)dhidden, ld_dh, (__nv_bfloat16*)dweight, ld_dw);
+  const int lanes = l.splits >= 8 ? 8 : 1;
+  const int64_t threads = in.N * (in.d / 8) * lanes;
+  return launch_pdl(lanes == 8 ? dhidden_kernel<8> : dhidden_kernel<1>, dim3((unsigned)std::min<int64_t>((threads + 255) / 256, 8 * sms)), 256, 0, st, true, r, (const float*)(s + l.dh),
+                    l.rows * in.d, l.splits, t.scale, (__nv_bfloat16*)dhidden, ld_dh, (__nv_bfloat16*)dweight, ld_dw);
 }
 
 }  // namespace saki
