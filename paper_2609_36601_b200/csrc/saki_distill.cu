@@ -256,6 +256,10 @@ template <> struct Elem<__nv_bfloat16> {
     const float2 a = unpack_bf16x2(max_bf16x2(max_bf16x2(w.x, w.y), max_bf16x2(w.z, w.w)));
     return fmaxf(a.x, a.y);
   }
+  // whether an element lies above the limit (a pair of the same bf16, rounded down)
+  using Limit = uint32_t;
+  static __device__ __forceinline__ Limit limit(float x) { const uint32_t h = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rd(x)); return h << 16 | h; }
+  static __device__ __forceinline__ bool above(const uint4& w, Limit l) { return max_bf16x2(max_bf16x2(max_bf16x2(w.x, w.y), max_bf16x2(w.z, w.w)), l) != l; }
   static __device__ __forceinline__ float get(const uint4& w, int e) {
     const int i = e >> 1;
     const uint32_t r = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
@@ -274,6 +278,9 @@ template <> struct Elem<float> {
   static constexpr uint32_t FILLER = 0xFF7FFFFFu;
   static __device__ __forceinline__ float2 pair(const uint4& w, int i) { return i == 0 ? make_float2(__uint_as_float(w.x), __uint_as_float(w.y)) : make_float2(__uint_as_float(w.z), __uint_as_float(w.w)); }
   static __device__ __forceinline__ float top(const uint4& w) { return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w))); }
+  using Limit = float;
+  static __device__ __forceinline__ Limit limit(float x) { return x; }
+  static __device__ __forceinline__ bool above(const uint4& w, Limit l) { return top(w) > l; }
   static __device__ __forceinline__ float get(const uint4& w, int e) { return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w); }
   static __device__ __forceinline__ void put(uint4& w, int e, float x) {
     const uint32_t r = __float_as_uint(x);
@@ -335,7 +342,7 @@ template <typename T> __device__ __forceinline__ uint4 odd_piece(const char* bas
   return w;
 }
 template <typename T> __device__ __forceinline__ void fill(uint32_t slot, const View<T>& v, int V, int c, uint64_t pol) {
-  if ((unsigned)(c - v.full0) < (unsigned)v.full) copy16(slot, v.base + (int64_t)c * 16, pol);
+  if ((unsigned)(c - v.full0) < (unsigned)v.full) copy16(slot, v.base + (uint32_t)c * 16u, pol);      // (a row has less than 2^31 bytes)
   else if (v.base) sts128(slot, odd_piece<T>(v.base, v.head, V, c));
 }
 
@@ -395,6 +402,13 @@ template <int SLOTS, int STEP_LOG, typename Body> __device__ __forceinline__ voi
   }
 }
 
+// 1 / x and 2^e for sums of a row, 2^-126 to 2^126: the first to some 1e-14
+__device__ __forceinline__ double pow2_near(int e) { return __longlong_as_double((long long)(1023 + e) << 52); }
+__device__ __forceinline__ double rcp_near(double x) {
+  const int e = (int)(__double_as_longlong(x) >> 52) - 1023;
+  return rcp_fast(x * pow2_near(-e)) * pow2_near(-e);
+}
+
 template <typename T, int MW, int SLOTS, bool BWD>
 __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kernel(const DistillParams P) {
   using El = Elem<T>;
@@ -416,7 +430,8 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
   const uint32_t base = smem_addr(dsm) + (uint32_t)warp * (KEEP * 512) + (uint32_t)lane * 16;
   uint32_t ring_slot = base + RESIDENT * 512;
   const double rtau = 1.0 / (double)P.in.temperature;
-  const float c32 = (float)(INV_LN2 * rtau);
+  const float c32 = (float)(INV_LN2 * rtau), rc32 = 1.f / c32;
+  const double x0_tau = rtau / (double)c32;      // of a shift, in units of the log-sum-exp
   const uint64_t pol_last = policy(true), pol_first = policy(false);
   const bool few_groups = sg.steps - 1 < RING;      // a short segment: its copies are fewer groups back than the waits assume
   const bool reverse = P.in.reverse != 0;
@@ -467,7 +482,8 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
 
     // ------------------------------------------------ pass 1: the sum outside K of 2^(c x + shift).  A lane's shift comes from the warp's first elements, and moves where
     // elements lie MARGIN above it (with the first ones masked, say)
-    float shift = 0.f, limit;
+    float shift = 0.f;
+    typename El::Limit limit;
     {
       copies_wait<RING - 1>();
       float m0 = sg.steps > 0 ? El::top(lds128(base)) : -CUDART_INF_F;
@@ -475,27 +491,28 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
       for (int o = 16; o > 0; o >>= 1) m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
       m0 = fminf(fmaxf(m0, -1e8f), 1e30f);      // (masks, of the lowest value or -inf, stay below it; a NaN is passed over: it comes out of the sum)
       shift = -ceilf(c32 * m0);
-      limit = (MARGIN - shift) / c32;
+      limit = El::limit((MARGIN - shift) * rc32);
     }
     float2 S0 = splat(0.f), S1 = splat(0.f);
+    uint64_t bits = here;             // of the steps that are left
     {
       const float2 cc = splat(c32);
       const bool ahead = sg.steps == sg.res && nxt.base != nullptr;      // a resident row leaves L2 free: the next one is sent on its way there
       visit<T, !BWD>(sg, lane, base, V, cur, BWD ? cur : nxt, pol_last, pol_first, pol_first, ring_slot, [&](uint4 w, int step) {
         if (BWD && ahead && (lane & 7) == 0 && sg.c0 + lane + 32 * step < nxt.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(nxt.base + (int64_t)(sg.c0 + lane + 32 * step) * 16));
-        if (here >> step & 1ull)
+        if (bits & 1ull)
           each_listed<SLOTS, El::STEP_LOG>(at, step, [&](int e, int j) {
             if (lane == e >> El::LOG) {
               sh.x[j] = El::get(w, e & (E - 1));
               El::put(w, e & (E - 1), -CUDART_INF_F);
             }
           });
-        const float top = El::top(w);
-        if (top > limit) {
-          const float to = -ceilf(c32 * fminf(top, 1e30f)), f = ex2f(fmaxf(to - shift, -200.f));
+        bits >>= 1;
+        if (El::above(w, limit)) {
+          const float to = -ceilf(c32 * fminf(El::top(w), 1e30f)), f = ex2f(fmaxf(to - shift, -200.f));
           S0 = fmul2(S0, splat(f)); S1 = fmul2(S1, splat(f));
           shift = to;
-          limit = (MARGIN - shift) / c32;
+          limit = El::limit((MARGIN - shift) * rc32);
         }
         const float2 kk = splat(shift);
 #pragma unroll
@@ -560,9 +577,9 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
             P.redo_list[atomicAdd(P.redo_count, 1u)] = (int32_t)row;
           } else {
             // sum of exp(x / tau) = exp(x0 / tau) sum of 2^(c (x - x0)) with x0 = -kr / c, up to what c as a float32 is off over distances from x0
-            const double l2 = log2_fast(sum), lse = LN2 * l2 - kr / (double)c32 * rtau;
-            const double rsum = 1.0 / sum;
-            const double lS = has_rest ? LN2 * (log2_fast(out) - l2) : 0;
+            const double l2 = log2_fast(sum), lo2 = has_rest ? log2_fast(out) : l2, lse = LN2 * l2 - kr * x0_tau;
+            const double rsum = rcp_near(sum);
+            const double lS = LN2 * (lo2 - l2);
             const double Z = list.W + (has_rest ? list.R : 0);
             double loss, c_out;
             if (reverse) {
@@ -570,14 +587,14 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
               c_out = (has_rest ? lS - list.log_R : 0) - loss;
             } else {
               loss = list.H - sum_cross + lse * list.W + (has_rest ? list.R * (list.log_R - lS) : 0);
-              c_out = Z - (has_rest ? list.R * sum / out : 0);
+              c_out = Z - (has_rest ? list.R * sum * rcp_near(out) : 0);
             }
             const int e = (int)floor(l2);
             const double kgd = (double)P.grad_scale * rtau;
-            const double ps = pow2_exact(-abs(e)), unit = e >= 0 ? sum * ps : sum / ps;      // sum 2^-e, 1 to 2
+            const double unit = rsum * pow2_near(e);      // 1 over sum 2^-e, which is 1 to 2
             grad_shift = (float)(kr - (double)e);
-            scale_out = (float)(kgd * c_out / unit);
-            Zs = (float)(1.0 / unit);
+            scale_out = (float)(kgd * c_out * unit);
+            Zs = (float)unit;
             kg = (float)kgd;
             lse_f = (float)lse; loss_f = (float)loss;
             sh.dc[parity][0] = lse; sh.dc[parity][1] = loss; sh.dc[parity][2] = Z;
@@ -610,6 +627,7 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
           }
       }
       __syncwarp();
+      bits = here;
       const float2 cc = splat(c32), kk = splat(kr), sc = splat(scale);
       T* const g_row = (T*)P.dlogits + row * P.ld_g;
       char* const g_base = (char*)((uintptr_t)g_row & ~(uintptr_t)15);
@@ -622,13 +640,14 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
           for (int i = 0; i < E / 2; ++i) v[i] = fmul2(ex2f2(ffma2(El::pair(w, i), cc, kk)), sc);
           if constexpr (E == 8) g = make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[1].x, v[1].y), pack_bf16x2(v[2].x, v[2].y), pack_bf16x2(v[3].x, v[3].y));
           else g = make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
-          if (here >> step & 1ull)
+          if (bits & 1ull)
             each_listed<SLOTS, El::STEP_LOG>(at, step, [&](int e, int j) {
               if (lane == e >> El::LOG) El::put(g, e & (E - 1), sh.g[j]);
             });
         }
+        bits >>= 1;
         const int c = sg.c0 + lane + 32 * step;
-        if (alike && (unsigned)(c - cur.full0) < (unsigned)cur.full) st_stream(g_base + (int64_t)c * 16, g, pol_first);
+        if (alike && (unsigned)(c - cur.full0) < (unsigned)cur.full) st_stream(g_base + (uint32_t)c * 16u, g, pol_first);
         else if (c < cur.n)
           for (int e = 0; e < E; ++e)
             if ((unsigned)(c * E + e - cur.head) < (unsigned)V) st_from_float(g_row, c * E + e - cur.head, El::get(g, e));

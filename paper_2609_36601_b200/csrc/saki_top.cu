@@ -16,6 +16,7 @@ namespace {
 
 constexpr int TT = 256, TWARPS = TT / 32, LIST = 512, KMAX = 128;
 constexpr int MAX_ENTRIES = 10240;          // groups of a slice: 20 KB of keys
+static_assert(((1 << 22) / (MAX_ENTRIES * 16) + 2) * KMAX * 8 + LIST * 8 + 64 <= 48 * 1024, "the lists of a row's slices are joined in shared memory");
 constexpr int MIN_SLICES = 16;              // a row is cut in so many at the most, unless it is longer than that
 constexpr float MARGIN = 60.f;
 
@@ -44,7 +45,7 @@ constexpr uint32_t LEAST = 0x0080u;                 // key of the lowest finite 
 
 template <typename T> struct Piece;
 template <> struct Piece<__nv_bfloat16> {
-  static constexpr int E = 8, GROUP = 2;
+  static constexpr int E = 8, GROUP = 2, AHEAD = 1;
   static constexpr uint32_t FILLER = 0xFF80FF80u;   // -inf
   static __device__ __forceinline__ float2 pair(const uint4& w, int i) { return unpack_bf16x2(i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w); }
   static __device__ __forceinline__ float top(const uint4 (&w)[GROUP]) {      // (of a pair with a NaN the other)
@@ -54,7 +55,7 @@ template <> struct Piece<__nv_bfloat16> {
   }
 };
 template <> struct Piece<float> {
-  static constexpr int E = 4, GROUP = 4;
+  static constexpr int E = 4, GROUP = 4, AHEAD = 1;
   static constexpr uint32_t FILLER = 0xFF800000u;
   static __device__ __forceinline__ float2 pair(const uint4& w, int i) { return i == 0 ? make_float2(__uint_as_float(w.x), __uint_as_float(w.y)) : make_float2(__uint_as_float(w.z), __uint_as_float(w.w)); }
   static __device__ __forceinline__ float top(const uint4 (&w)[GROUP]) {
@@ -80,7 +81,7 @@ struct TopShared {
 template <typename T>
 __global__ void __launch_bounds__(TT, 5) top_rows_kernel(const TopParams P) {
   using Pc = Piece<T>;
-  constexpr int E = Pc::E, GROUP = Pc::GROUP;
+  constexpr int E = Pc::E, GROUP = Pc::GROUP, AHEAD = Pc::AHEAD;
   __shared__ TopShared sh;
   launch_dependents();
   wait_for_predecessor();
@@ -113,17 +114,23 @@ __global__ void __launch_bounds__(TT, 5) top_rows_kernel(const TopParams P) {
   float shift = 0.f, limit = -CUDART_INF_F;      // (the first group sets them)
   uint32_t mine = 0;
   const float2 cc = splat(P.c);
-  uint4 next[GROUP];
+  uint4 next[AHEAD][GROUP];             // on their way
 #pragma unroll
-  for (int g = 0; g < GROUP; ++g) next[g] = load(p0 + g * TT + tid);
+  for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+    for (int g = 0; g < GROUP; ++g) next[i][g] = load(p0 + (i * GROUP + g) * TT + tid);
 #pragma unroll 1
   for (int i = 0; i < entries; ++i) {
     uint4 w[GROUP];
 #pragma unroll
-    for (int g = 0; g < GROUP; ++g) w[g] = next[g];
-    if (i + 1 < entries) {
+    for (int g = 0; g < GROUP; ++g) {
+      w[g] = next[0][g];
 #pragma unroll
-      for (int g = 0; g < GROUP; ++g) next[g] = load(p0 + ((i + 1) * GROUP + g) * TT + tid);
+      for (int j = 0; j + 1 < AHEAD; ++j) next[j][g] = next[j + 1][g];
+    }
+    if (i + AHEAD < entries) {
+#pragma unroll
+      for (int g = 0; g < GROUP; ++g) next[AHEAD - 1][g] = load(p0 + ((i + AHEAD) * GROUP + g) * TT + tid);
     }
     const float top = Pc::top(w);
     const uint32_t key = order_of(top) >> 16;
@@ -155,17 +162,20 @@ __global__ void __launch_bounds__(TT, 5) top_rows_kernel(const TopParams P) {
   sh.top[tid] = mine;
   __syncthreads();
   if (warp == 0) {
-    // the k-th largest of the threads' maxima (0: fewer have any)
-    uint32_t x[TT / 32], bar = 0;
+    // the k-th largest of the threads' maxima: bisection between the smallest and the largest of them
+    uint32_t x[TT / 32], lo = ~0u, hi = 0;
 #pragma unroll
-    for (int i = 0; i < TT / 32; ++i) x[i] = sh.top[i * 32 + lane];
+    for (int i = 0; i < TT / 32; ++i) { x[i] = sh.top[i * 32 + lane]; lo = min(lo, x[i]); hi = max(hi, x[i]); }
+    uint32_t bar = __reduce_min_sync(0xffffffffu, lo);      // (k of them reach it: there are more than k threads)
+    hi = __reduce_max_sync(0xffffffffu, hi);
 #pragma unroll 1
-    for (int bit = 15; bit >= 0; --bit) {
-      const uint32_t to = bar | 1u << bit;
+    while (bar < hi) {
+      const uint32_t to = (bar + hi + 1) >> 1;
       int n = 0;
 #pragma unroll
       for (int i = 0; i < TT / 32; ++i) n += x[i] >= to;
       if (__reduce_add_sync(0xffffffffu, n) >= k) bar = to;
+      else hi = to - 1;
     }
     if (lane == 0) sh.bar = max(bar, LEAST);
   } else if (warp == 1) {
@@ -311,15 +321,21 @@ __global__ void __launch_bounds__(TT, 5) top_rows_kernel(const TopParams P) {
   }
 }
 
-// A block a row: the slices' lists, each sorted, become one; an element's rank is the sum of its places in all lists.
+// A block a row: the slices' sorted lists become one.  The least of the lists' ceil(k / slices)-th elements is a bar that k elements reach, and twice as many or so do: those are ranked by counting.
+// Where more of them do than LIST, by their places in all lists.
 __global__ void __launch_bounds__(TT) top_join_kernel(const TopParams P) {
-  __shared__ int total;
+  __shared__ int total, above;
   __shared__ bool bad;
+  __shared__ unsigned long long bar;
+  __shared__ uint64_t list[LIST];
+  extern __shared__ uint64_t c[];      // [slices][k]
   launch_dependents();
   wait_for_predecessor();
   const int tid = threadIdx.x, lane = tid & 31, k = P.in.k, n = P.slices;
   const int64_t row = blockIdx.x;
-  if (tid == 0) total = 0;
+  for (int i = tid; i < n * k; i += TT) c[i] = P.cand[row * n * k + i];
+  if (tid == 0) { total = above = 0; bar = ~0ull; }
+  __syncthreads();
   if (tid < 32) {
     double m = CUDART_INF, s = 0;
     bool nan = false;
@@ -339,33 +355,57 @@ __global__ void __launch_bounds__(TT) top_join_kernel(const TopParams P) {
       if (P.out.row_status) P.out.row_status[row] = nan ? SAKI_ROW_NONFINITE : 0u;
       if (nan) atomicAdd(P.flagged, 1ull);
     }
+  } else if (tid < 64) {
+    unsigned long long b = ~0ull;
+    for (int l = lane; l < n; l += 32) b = min(b, (unsigned long long)c[l * k + (k + n - 1) / n - 1]);
+    atomicMin(&bar, b);
   }
   __syncthreads();
-  const uint64_t* const c = P.cand + row * n * k;
   if (!bad) {
+    const uint64_t least = max((unsigned long long)bar, 1ull);      // (0: a list falls short)
     int there = 0;
     for (int i = tid; i < n * k; i += TT) {
       const uint64_t w = c[i];
-      if (w == 0) continue;
-      ++there;
-      const int own = i / k;
-      int rank = i - own * k;
-      for (int l = 0; l < n && rank < k; ++l) {
-        if (l == own) continue;
-        int lo = 0, hi = k;            // elements of list l before w
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (c[l * k + mid] > w) lo = mid + 1;
-          else hi = mid;
-        }
-        rank += lo;
-      }
-      if (rank < k) {
-        P.out.token[row * k + rank] = pair_token(w);
-        P.out.logit[row * k + rank] = pair_logit(w);
+      there += w != 0;
+      if (w >= least) {
+        const int at = atomicAdd(&above, 1);
+        if (at < LIST) list[at] = w;
       }
     }
     if (there) atomicAdd(&total, there);
+    __syncthreads();
+    const int m = above;
+    auto write = [&](int rank, uint64_t w) {
+      P.out.token[row * k + rank] = pair_token(w);
+      P.out.logit[row * k + rank] = pair_logit(w);
+    };
+    if (m <= LIST) {
+      for (int i = tid; i < m; i += TT) {
+        const uint64_t w = list[i];
+        int rank = 0;
+#pragma unroll 4
+        for (int j = 0; j < m; ++j) rank += list[j] > w;
+        if (rank < k) write(rank, w);
+      }
+    } else {
+      for (int i = tid; i < n * k; i += TT) {
+        const uint64_t w = c[i];
+        if (w < least) continue;
+        const int own = i / k;
+        int rank = i - own * k;
+        for (int l = 0; l < n && rank < k; ++l) {
+          if (l == own) continue;
+          int lo = 0, hi = k;            // elements of list l before w
+          while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (c[l * k + mid] > w) lo = mid + 1;
+            else hi = mid;
+          }
+          rank += lo;
+        }
+        if (rank < k) write(rank, w);
+      }
+    }
   }
   __syncthreads();
   for (int i = (bad ? 0 : total) + tid; i < k; i += TT) {
@@ -414,7 +454,7 @@ cudaError_t launch_top(const saki_top_in& in, const saki_top_out& out, void* scr
   *n_launches = 1;
   if (e != cudaSuccess || c.slices == 1) return e;
   ++*n_launches;
-  return launch_pdl(top_join_kernel, dim3((unsigned)in.N), TT, 0, st, true, p);
+  return launch_pdl(top_join_kernel, dim3((unsigned)in.N), TT, (size_t)c.slices * in.k * 8, st, true, p);
 }
 
 }  // namespace saki
