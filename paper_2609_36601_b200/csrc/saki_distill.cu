@@ -52,6 +52,16 @@ __device__ __forceinline__ void write_result(const DistillParams& P, int64_t row
   if (P.out.row_status) P.out.row_status[row] = status;
   if (status & (SAKI_ROW_NONFINITE | SAKI_ROW_BAD_ID)) atomicAdd(P.flagged, 1ull);
 }
+__device__ __forceinline__ float warp_least(float x) {      // of numbers, over the warp
+  float r;
+  asm volatile("redux.sync.min.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float warp_most(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
 __device__ __forceinline__ double warp_max(double a) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) a = fmax(a, __shfl_xor_sync(0xffffffffu, a, o));
@@ -341,39 +351,53 @@ template <typename T> __device__ __forceinline__ uint4 odd_piece(const char* bas
     if (c * E + e >= head && c * E + e < head + V) Elem<T>::put(w, e, ld_as_float(p, e));
   return w;
 }
-template <typename T> __device__ __forceinline__ void fill(uint32_t slot, const View<T>& v, int V, int c, uint64_t pol) {
+template <typename T> __device__ __forceinline__ void fill_piece(uint32_t slot, const View<T>& v, int V, int c, uint64_t pol) {
   if ((unsigned)(c - v.full0) < (unsigned)v.full) copy16(slot, v.base + (uint32_t)c * 16u, pol);      // (a row has less than 2^31 bytes)
   else if (v.base) sts128(slot, odd_piece<T>(v.base, v.head, V, c));
 }
 
 struct Segment { int c0, steps, res; };      // of a warp: its first piece, steps of 32 pieces, how many of them stay in shared memory
 
+// A lane's pieces of a row, by step.  INNER: the warp's whole segment lies within whole pieces of the row.
+template <typename T, bool INNER> struct Source {
+  View<T> v;
+  int V, c0;                   // the lane's first piece
+  const char* at;              // INNER: where it is
+  __device__ __forceinline__ Source(const View<T>& view, int V_, int c) : v(view), V(V_), c0(c), at(view.base + (int64_t)c * 16) {}
+  __device__ __forceinline__ void fill(uint32_t slot, int step, uint64_t pol) const {
+    if constexpr (INNER) copy16(slot, at + (uint32_t)step * 512u, pol);      // (a row has less than 2^31 bytes)
+    else fill_piece<T>(slot, v, V, c0 + 32 * step, pol);
+  }
+};
+
 // Visits the warp's steps in order: body(words, step).  Every step commits one group of copies.  A streamed step, once read, requests the streamed step RING
 // further on: of this pass, or past its end the first streamed steps of the pass that follows, over `wrap` (the same row again, or the next one).
 // With REFILL a resident step, once read, requests the same step of `wrap`.
-template <typename T, bool REFILL, typename Body>
-__device__ __forceinline__ void visit(const Segment& sg, int lane, uint32_t base, int V, const View<T>& cur, const View<T>& wrap, uint64_t pol_cur, uint64_t pol_wrap,
-                                      uint64_t pol_res, uint32_t& ring_slot, Body&& body) {
+template <bool REFILL, typename S, typename Body>
+__device__ __forceinline__ void visit(const Segment& sg, uint32_t base, const S& cur, const S& wrap, uint64_t pol_cur, uint64_t pol_wrap, uint64_t pol_res, uint32_t& ring_slot,
+                                      Body&& body) {
   uint32_t slot = base;
-  int c = sg.c0 + lane;
 #pragma unroll 1
-  for (int k = 0; k < sg.steps; ++k, c += 32) {
-    uint4 a;
+  for (int k = 0; k < sg.res; ++k, slot += 512) {
     copies_wait<RING - 1>();
-    if (k < sg.res) {
-      a = lds128(slot);
-      if (REFILL) fill<T>(slot, wrap, V, c, pol_res);
-      slot += 512;
-    } else {
-      a = lds128(ring_slot);
-      if (k + RING < sg.steps) fill<T>(ring_slot, cur, V, c + RING * 32, pol_cur);
-      else fill<T>(ring_slot, wrap, V, c + (RING - (sg.steps - sg.res)) * 32, pol_wrap);
-      ring_slot += 512;
-      if (ring_slot == base + KEEP * 512) ring_slot = base + RESIDENT * 512;
-    }
+    const uint4 a = lds128(slot);
+    if constexpr (REFILL) wrap.fill(slot, k, pol_res);
     copies_commit();
     body(a, k);
   }
+  uint32_t ring = ring_slot;
+#pragma unroll 1
+  for (int k = sg.res; k < sg.steps; ++k) {
+    copies_wait<RING - 1>();
+    const uint4 a = lds128(ring);
+    if (k + RING < sg.steps) cur.fill(ring, k + RING, pol_cur);
+    else wrap.fill(ring, k + RING - (sg.steps - sg.res), pol_wrap);
+    copies_commit();
+    ring += 512;
+    if (ring == base + KEEP * 512) ring = base + RESIDENT * 512;
+    body(a, k);
+  }
+  ring_slot = ring;
 }
 
 template <int MW> struct StreamShared {
@@ -449,9 +473,9 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
 
   View<T> cur = view(blockIdx.x);
   stage_list(blockIdx.x, 0);
-  for (int s = 0; s < sg.res; ++s) { fill<T>(base + s * 512, cur, V, sg.c0 + lane + 32 * s, pol_first); copies_commit(); }
+  for (int s = 0; s < sg.res; ++s) { fill_piece<T>(base + s * 512, cur, V, sg.c0 + lane + 32 * s, pol_first); copies_commit(); }
   if (sg.res < sg.steps)
-    for (int j = 0; j < RING; ++j) { fill<T>(ring_slot + j * 512, cur, V, sg.c0 + lane + 32 * (sg.res + j), pol_last); copies_commit(); }
+    for (int j = 0; j < RING; ++j) { fill_piece<T>(ring_slot + j * 512, cur, V, sg.c0 + lane + 32 * (sg.res + j), pol_last); copies_commit(); }
   copies_commit();
   copies_wait<0>();
   __syncthreads();
@@ -479,6 +503,8 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
       here_hi |= __reduce_or_sync(0xffffffffu, mine && step >= 32 ? 1u << (step - 32) : 0u);
     }
     const uint64_t here = (uint64_t)here_hi << 32 | here_lo;
+    // the segment lies within whole pieces of this row and the next
+    const bool inner = nxt.base != nullptr && sg.c0 >= max(cur.full0, nxt.full0) && sg.c0 + 32 * sg.steps <= min(cur.full0 + cur.full, nxt.full0 + nxt.full);
 
     // ------------------------------------------------ pass 1: the sum outside K of 2^(c x + shift).  A lane's shift comes from the warp's first elements, and moves where
     // elements lie MARGIN above it (with the first ones masked, say)
@@ -487,9 +513,7 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
     {
       copies_wait<RING - 1>();
       float m0 = sg.steps > 0 ? El::top(lds128(base)) : -CUDART_INF_F;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
-      m0 = fminf(fmaxf(m0, -1e8f), 1e30f);      // (masks, of the lowest value or -inf, stay below it; a NaN is passed over: it comes out of the sum)
+      m0 = fminf(fmaxf(warp_most(m0), -1e8f), 1e30f);      // (masks, of the lowest value or -inf, stay below it; a NaN is passed over: it comes out of the sum)
       shift = -ceilf(c32 * m0);
       limit = El::limit((MARGIN - shift) * rc32);
     }
@@ -498,7 +522,7 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
     {
       const float2 cc = splat(c32);
       const bool ahead = sg.steps == sg.res && nxt.base != nullptr;      // a resident row leaves L2 free: the next one is sent on its way there
-      visit<T, !BWD>(sg, lane, base, V, cur, BWD ? cur : nxt, pol_last, pol_first, pol_first, ring_slot, [&](uint4 w, int step) {
+      auto sum = [&](uint4 w, int step) {
         if (BWD && ahead && (lane & 7) == 0 && sg.c0 + lane + 32 * step < nxt.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(nxt.base + (int64_t)(sg.c0 + lane + 32 * step) * 16));
         if (bits & 1ull)
           each_listed<SLOTS, El::STEP_LOG>(at, step, [&](int e, int j) {
@@ -520,7 +544,14 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
           S0 = fadd2(S0, ex2f2(ffma2(El::pair(w, i), cc, kk)));
           S1 = fadd2(S1, ex2f2(ffma2(El::pair(w, i + 1), cc, kk)));
         }
-      });
+      };
+      if (inner) {
+        const Source<T, true> c(cur, V, sg.c0 + lane), n(nxt, V, sg.c0 + lane);
+        visit<!BWD>(sg, base, c, BWD ? c : n, pol_last, pol_first, pol_first, ring_slot, sum);
+      } else {
+        const Source<T, false> c(cur, V, sg.c0 + lane), n(nxt, V, sg.c0 + lane);
+        visit<!BWD>(sg, base, c, BWD ? c : n, pol_last, pol_first, pol_first, ring_slot, sum);
+      }
     }
     __syncwarp();
     float warp_shift = shift;
@@ -529,8 +560,7 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
       for (int r = 0; r < SLOTS; ++r)
         if (at[r] >= 0) warp_shift = fminf(warp_shift, -ceilf(c32 * fminf(sh.x[r * 32 + lane], 1e30f)));
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) warp_shift = fminf(warp_shift, __shfl_xor_sync(0xffffffffu, warp_shift, o));
+    warp_shift = warp_least(warp_shift);
     double outside = (((double)S0.x + (double)S0.y) + ((double)S1.x + (double)S1.y)) * (double)ex2f(fmaxf(warp_shift - shift, -200.f));
     double inside = 0, cross = 0;
     if (here) {
@@ -547,24 +577,30 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
           cross += reverse ? (double)e * ((double)x * rtau - (double)w.y) : (double)w.x * ((double)x * rtau);
         }
       if (lost) inside = CUDART_NAN;      // a listed token that the student's row has masked, or not finite: the float64 kernel decides
-      inside = warp_sum(inside);
-      cross = warp_sum(cross);
     }
-    outside = warp_sum(outside);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {      // (three chains side by side)
+      outside += __shfl_xor_sync(0xffffffffu, outside, o);
+      inside += __shfl_xor_sync(0xffffffffu, inside, o);
+      cross += __shfl_xor_sync(0xffffffffu, cross, o);
+    }
     if (lane == 0) { sh.red[0][warp] = outside; sh.red[1][warp] = (double)warp_shift; sh.red[2][warp] = inside; sh.red[3][warp] = cross; }
     __syncthreads();
     if (warp == 0) {
       const int wl = lane < MW ? lane : 0;
       const bool part = lane < MW;
       const double ks = sh.red[1][wl];
-      double kr = part ? ks : 1e300;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) kr = fmin(kr, __shfl_xor_sync(0xffffffffu, kr, o));
+      const double kr = (double)warp_least(part ? (float)ks : CUDART_INF_F);
       const double f = part ? pow2_exact((int)fmax(kr - ks, -1000.0)) : 0;
-      const double out = warp_sum(f > 0 ? sh.red[0][wl] * f : 0), in = warp_sum(f > 0 ? sh.red[2][wl] * f : part && sh.red[2][wl] != sh.red[2][wl] ? CUDART_NAN : 0);
-      double sum_cross = part ? sh.red[3][wl] : 0;
-      if (reverse && part) sum_cross *= f;
-      sum_cross = warp_sum(sum_cross);
+      // (a warp whose share is nothing beside the others' may have an infinite one; a NaN among the listed ones counts everywhere)
+      double out = f > 0 ? sh.red[0][wl] * f : 0, in = f > 0 ? sh.red[2][wl] * f : part && sh.red[2][wl] != sh.red[2][wl] ? CUDART_NAN : 0;
+      double sum_cross = part ? sh.red[3][wl] * (reverse ? f : 1.0) : 0;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        out += __shfl_xor_sync(0xffffffffu, out, o);
+        in += __shfl_xor_sync(0xffffffffu, in, o);
+        sum_cross += __shfl_xor_sync(0xffffffffu, sum_cross, o);
+      }
       if (lane == 0) {
         float scale_out = 0.f, Zs = 0.f, kg = 0.f, lse_f = 0.f, loss_f = 0.f, grad_shift = 0.f;
         const ListRow& list = sh.list[b];
@@ -632,7 +668,7 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
       T* const g_row = (T*)P.dlogits + row * P.ld_g;
       char* const g_base = (char*)((uintptr_t)g_row & ~(uintptr_t)15);
       const bool alike = ((uintptr_t)g_row & 15) == cur.head * sizeof(T);      // the gradient's pieces lie like the row's
-      visit<T, true>(sg, lane, base, V, cur, nxt, pol_first, pol_last, pol_first, ring_slot, [&](const uint4& w, int step) {
+      auto gradient = [&](const uint4& w, int step) -> uint4 {
         uint4 g = make_uint4(0u, 0u, 0u, 0u);
         if (!zero) {
           float2 v[E / 2];
@@ -646,12 +682,23 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
             });
         }
         bits >>= 1;
-        const int c = sg.c0 + lane + 32 * step;
-        if (alike && (unsigned)(c - cur.full0) < (unsigned)cur.full) st_stream(g_base + (uint32_t)c * 16u, g, pol_first);
-        else if (c < cur.n)
-          for (int e = 0; e < E; ++e)
-            if ((unsigned)(c * E + e - cur.head) < (unsigned)V) st_from_float(g_row, c * E + e - cur.head, El::get(g, e));
-      });
+        return g;
+      };
+      if (inner && alike) {
+        const Source<T, true> c(cur, V, sg.c0 + lane), n(nxt, V, sg.c0 + lane);
+        char* const to = g_base + (int64_t)(sg.c0 + lane) * 16;
+        visit<true>(sg, base, c, n, pol_first, pol_last, pol_first, ring_slot, [&](const uint4& w, int step) { st_stream(to + (uint32_t)step * 512u, gradient(w, step), pol_first); });
+      } else {
+        const Source<T, false> c(cur, V, sg.c0 + lane), n(nxt, V, sg.c0 + lane);
+        visit<true>(sg, base, c, n, pol_first, pol_last, pol_first, ring_slot, [&](const uint4& w, int step) {
+          const uint4 g = gradient(w, step);
+          const int c = sg.c0 + lane + 32 * step;
+          if (alike && (unsigned)(c - cur.full0) < (unsigned)cur.full) st_stream(g_base + (uint32_t)c * 16u, g, pol_first);
+          else if (c < cur.n)
+            for (int e = 0; e < E; ++e)
+              if ((unsigned)(c * E + e - cur.head) < (unsigned)V) st_from_float(g_row, c * E + e - cur.head, El::get(g, e));
+        });
+      }
     }
     cur = nxt;
     b = next_b;
