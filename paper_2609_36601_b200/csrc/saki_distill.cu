@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(DG_THREADS) distill_general_kernel(const Disti
 
 // ---------------------------------------------------------------- streaming kernel
 constexpr int WARPS_FULL = 32, WARPS_HALF = 16;
-constexpr int KEEP = 13, RING = 5, RESIDENT = KEEP - RING;      // 512-byte steps of a warp in shared memory; of them, where a segment does not fit, the ring's
+constexpr int KEEP = 12, RING = 4, RESIDENT = KEEP - RING;      // 512-byte steps of a warp in shared memory; of them, where a segment does not fit, the ring's (both even: steps go in pairs)
 constexpr int MAX_STEPS = 64;
 constexpr float MARGIN = 60.f;                                  // in base 2: how far a lane's elements may lie above its shift
 
@@ -269,7 +269,8 @@ template <> struct Elem<__nv_bfloat16> {
   // whether an element lies above the limit (a pair of the same bf16, rounded down)
   using Limit = uint32_t;
   static __device__ __forceinline__ Limit limit(float x) { const uint32_t h = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rd(x)); return h << 16 | h; }
-  static __device__ __forceinline__ bool above(const uint4& w, Limit l) { return max_bf16x2(max_bf16x2(max_bf16x2(w.x, w.y), max_bf16x2(w.z, w.w)), l) != l; }
+  static __device__ __forceinline__ uint32_t pairs(const uint4& w) { return max_bf16x2(max_bf16x2(w.x, w.y), max_bf16x2(w.z, w.w)); }
+  static __device__ __forceinline__ bool above(const uint4& w, const uint4& u, Limit l) { return max_bf16x2(max_bf16x2(pairs(w), pairs(u)), l) != l; }
   static __device__ __forceinline__ float get(const uint4& w, int e) {
     const int i = e >> 1;
     const uint32_t r = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
@@ -290,7 +291,7 @@ template <> struct Elem<float> {
   static __device__ __forceinline__ float top(const uint4& w) { return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w))); }
   using Limit = float;
   static __device__ __forceinline__ Limit limit(float x) { return x; }
-  static __device__ __forceinline__ bool above(const uint4& w, Limit l) { return top(w) > l; }
+  static __device__ __forceinline__ bool above(const uint4& w, const uint4& u, Limit l) { return fmaxf(top(w), top(u)) > l; }
   static __device__ __forceinline__ float get(const uint4& w, int e) { return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w); }
   static __device__ __forceinline__ void put(uint4& w, int e, float x) {
     const uint32_t r = __float_as_uint(x);
@@ -370,32 +371,69 @@ template <typename T, bool INNER> struct Source {
   }
 };
 
-// Visits the warp's steps in order: body(words, step).  Every step commits one group of copies.  A streamed step, once read, requests the streamed step RING
+// Visits the warp's steps in order, two at a time: body(words, words of the next step, step), single(words, step) for one that is left over.  Every visit
+// commits one group of copies; all but the last group are there before words are read.  A streamed step, once read, requests the streamed step RING
 // further on: of this pass, or past its end the first streamed steps of the pass that follows, over `wrap` (the same row again, or the next one).
 // With REFILL a resident step, once read, requests the same step of `wrap`.
-template <bool REFILL, typename S, typename Body>
+template <bool REFILL, typename S, typename Body, typename Single>
 __device__ __forceinline__ void visit(const Segment& sg, uint32_t base, const S& cur, const S& wrap, uint64_t pol_cur, uint64_t pol_wrap, uint64_t pol_res, uint32_t& ring_slot,
-                                      Body&& body) {
+                                      Body&& body, Single&& single) {
   uint32_t slot = base;
+  int k = 0;
 #pragma unroll 1
-  for (int k = 0; k < sg.res; ++k, slot += 512) {
-    copies_wait<RING - 1>();
+  for (; k + 1 < sg.res; k += 2, slot += 1024) {
+    copies_wait<1>();
+    const uint4 a = lds128(slot), b = lds128(slot + 512);
+    if constexpr (REFILL) { wrap.fill(slot, k, pol_res); wrap.fill(slot + 512, k + 1, pol_res); }
+    copies_commit();
+    body(a, b, k);
+  }
+  if (k < sg.res) {
+    copies_wait<1>();
     const uint4 a = lds128(slot);
     if constexpr (REFILL) wrap.fill(slot, k, pol_res);
     copies_commit();
-    body(a, k);
+    single(a, k);
+    return;                    // (steps that stream are there only behind an even number of resident ones)
   }
   uint32_t ring = ring_slot;
-#pragma unroll 1
-  for (int k = sg.res; k < sg.steps; ++k) {
-    copies_wait<RING - 1>();
-    const uint4 a = lds128(ring);
-    if (k + RING < sg.steps) cur.fill(ring, k + RING, pol_cur);
-    else wrap.fill(ring, k + RING - (sg.steps - sg.res), pol_wrap);
-    copies_commit();
+  auto next_slot = [&] {
+    const uint32_t at = ring;
     ring += 512;
     if (ring == base + KEEP * 512) ring = base + RESIDENT * 512;
-    body(a, k);
+    return at;
+  };
+#pragma unroll 1
+  for (; k + 1 + RING < sg.steps; k += 2) {
+    copies_wait<1>();
+    const uint32_t s0 = next_slot(), s1 = next_slot();
+    const uint4 a = lds128(s0), b = lds128(s1);
+    cur.fill(s0, k + RING, pol_cur);
+    cur.fill(s1, k + RING + 1, pol_cur);
+    copies_commit();
+    body(a, b, k);
+  }
+  auto refill = [&](uint32_t at, int step) {
+    if (step + RING < sg.steps) cur.fill(at, step + RING, pol_cur);
+    else wrap.fill(at, step + RING - (sg.steps - sg.res), pol_wrap);
+  };
+#pragma unroll 1
+  for (; k + 1 < sg.steps; k += 2) {
+    copies_wait<1>();
+    const uint32_t s0 = next_slot(), s1 = next_slot();
+    const uint4 a = lds128(s0), b = lds128(s1);
+    refill(s0, k);
+    refill(s1, k + 1);
+    copies_commit();
+    body(a, b, k);
+  }
+  if (k < sg.steps) {
+    copies_wait<1>();
+    const uint32_t s0 = next_slot();
+    const uint4 a = lds128(s0);
+    refill(s0, k);
+    copies_commit();
+    single(a, k);
   }
   ring_slot = ring;
 }
@@ -409,19 +447,21 @@ template <int MW> struct StreamShared {
   int id[3][KMAX];
   float2 w[3][KMAX];
   float x[KMAX], g[KMAX];      // listed elements and their gradients: of the warp that has them
+  uint32_t mine[MW][KMAX];     // by warp: what lies in its segment, place in elements << 8 | place in the list
 };
 template <int MW> constexpr int stream_smem = MW * KEEP * 512 + (int)sizeof(StreamShared<MW>);
 
-// The tokens of the list that lie in step `step` of the warp: body(element's place in the step's pieces, place in the list).  `at`: by lane, where listed elements lie in
-// the warp's segment, in elements (below 0: not there).
-template <int SLOTS, int STEP_LOG, typename Body> __device__ __forceinline__ void each_listed(const int (&at)[SLOTS], int step, Body&& body) {
-#pragma unroll
-  for (int r = 0; r < SLOTS; ++r) {
-    unsigned m = __ballot_sync(0xffffffffu, (at[r] >> STEP_LOG) == step);
+// The listed elements in steps `step` and `step` + 1 (step even) of a warp: body(place within the two steps, place in the list).
+template <int STEP_LOG, typename Body> __device__ __forceinline__ void each_listed(const uint32_t* mine, int n, int step, int lane, Body&& body) {
+#pragma unroll 1
+  for (int q = 0; q < n; q += 32) {
+    const uint32_t entry = q + lane < n ? mine[q + lane] : ~0u;
+    unsigned m = __ballot_sync(0xffffffffu, entry >> (8 + STEP_LOG + 1) == (uint32_t)step >> 1);
     while (m) {
       const int src = __ffs(m) - 1;
       m &= m - 1;
-      body(__shfl_sync(0xffffffffu, at[r], src) & ((1 << STEP_LOG) - 1), r * 32 + src);
+      const uint32_t e = __shfl_sync(0xffffffffu, entry, src);
+      body((int)(e >> 8) & ((2 << STEP_LOG) - 1), (int)(e & 255u));
     }
   }
 }
@@ -433,7 +473,7 @@ __device__ __forceinline__ double rcp_near(double x) {
   return rcp_fast(x * pow2_near(-e)) * pow2_near(-e);
 }
 
-template <typename T, int MW, int SLOTS, bool BWD>
+template <typename T, int MW, bool BWD>
 __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kernel(const DistillParams P) {
   using El = Elem<T>;
   constexpr int E = El::E;
@@ -457,7 +497,7 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
   const float c32 = (float)(INV_LN2 * rtau), rc32 = 1.f / c32;
   const double x0_tau = rtau / (double)c32;      // of a shift, in units of the log-sum-exp
   const uint64_t pol_last = policy(true), pol_first = policy(false);
-  const bool few_groups = sg.steps - 1 < RING;      // a short segment: its copies are fewer groups back than the waits assume
+  const bool few_groups = sg.steps <= 4;      // a short segment: its copies are fewer groups back than the waits assume
   const bool reverse = P.in.reverse != 0;
   View<T> none = {};
 
@@ -488,20 +528,24 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
     if (few_groups) copies_wait<0>();
     stage_list(next_row, next_b);      // (goes with the first step's group, and is there before the row's second barrier)
     const bool live = sh.list[b].status == 0;
-    // where listed elements lie in this warp's segment, and at which steps
-    int at[SLOTS];
+    // what of the list lies in this warp's segment, and at which steps
+    uint32_t* const mine = sh.mine[warp];
+    int n_mine = 0;
     uint32_t here_lo = 0, here_hi = 0;
-#pragma unroll
-    for (int r = 0; r < SLOTS; ++r) {
-      const int j = r * 32 + lane;
-      const int id = j < k ? sh.id[b][j] : -1;
+#pragma unroll 1
+    for (int q = 0; q < k; q += 32) {
+      const int id = q + lane < k ? sh.id[b][q + lane] : -1;
       const int place = id + cur.head - sg.c0 * E;
-      const bool mine = id >= 0 && place >= 0 && place < sg.steps * 32 * E;
-      at[r] = mine ? place : -1;
+      const bool in = id >= 0 && place >= 0 && place < sg.steps * 32 * E;
+      const unsigned m = __ballot_sync(0xffffffffu, in);
+      if (m == 0) continue;
+      if (in) mine[n_mine + __popc(m & ((1u << lane) - 1))] = (uint32_t)place << 8 | (uint32_t)(q + lane);
+      n_mine += __popc(m);
       const int step = place >> El::STEP_LOG;
-      here_lo |= __reduce_or_sync(0xffffffffu, mine && step < 32 ? 1u << step : 0u);
-      here_hi |= __reduce_or_sync(0xffffffffu, mine && step >= 32 ? 1u << (step - 32) : 0u);
+      here_lo |= __reduce_or_sync(0xffffffffu, in && step < 32 ? 1u << step : 0u);
+      here_hi |= __reduce_or_sync(0xffffffffu, in && step >= 32 ? 1u << (step - 32) : 0u);
     }
+    __syncwarp();
     const uint64_t here = (uint64_t)here_hi << 32 | here_lo;
     // the segment lies within whole pieces of this row and the next
     const bool inner = nxt.base != nullptr && sg.c0 >= max(cur.full0, nxt.full0) && sg.c0 + 32 * sg.steps <= min(cur.full0 + cur.full, nxt.full0 + nxt.full);
@@ -511,7 +555,7 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
     float shift = 0.f;
     typename El::Limit limit;
     {
-      copies_wait<RING - 1>();
+      copies_wait<1>();
       float m0 = sg.steps > 0 ? El::top(lds128(base)) : -CUDART_INF_F;
       m0 = fminf(fmaxf(warp_most(m0), -1e8f), 1e30f);      // (masks, of the lowest value or -inf, stay below it; a NaN is passed over: it comes out of the sum)
       shift = -ceilf(c32 * m0);
@@ -522,62 +566,76 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
     {
       const float2 cc = splat(c32);
       const bool ahead = sg.steps == sg.res && nxt.base != nullptr;      // a resident row leaves L2 free: the next one is sent on its way there
-      auto sum = [&](uint4 w, int step) {
+      float2 kk = splat(shift);
+      auto ahead_of = [&](int step) {
         if (BWD && ahead && (lane & 7) == 0 && sg.c0 + lane + 32 * step < nxt.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(nxt.base + (int64_t)(sg.c0 + lane + 32 * step) * 16));
-        if (bits & 1ull)
-          each_listed<SLOTS, El::STEP_LOG>(at, step, [&](int e, int j) {
-            if (lane == e >> El::LOG) {
-              sh.x[j] = El::get(w, e & (E - 1));
-              El::put(w, e & (E - 1), -CUDART_INF_F);
-            }
-          });
-        bits >>= 1;
-        if (El::above(w, limit)) {
-          const float to = -ceilf(c32 * fminf(El::top(w), 1e30f)), f = ex2f(fmaxf(to - shift, -200.f));
-          S0 = fmul2(S0, splat(f)); S1 = fmul2(S1, splat(f));
-          shift = to;
-          limit = El::limit((MARGIN - shift) * rc32);
-        }
-        const float2 kk = splat(shift);
+      };
+      auto leave_out = [&](uint4& w0, uint4& w1, int step) {      // listed elements
+        each_listed<El::STEP_LOG>(mine, n_mine, step, lane, [&](int e, int j) {
+          if (lane == (e >> El::LOG & 31)) {
+            const bool second = e >> El::STEP_LOG;
+            sh.x[j] = El::get(second ? w1 : w0, e & (E - 1));
+            if (second) El::put(w1, e & (E - 1), -CUDART_INF_F);
+            else El::put(w0, e & (E - 1), -CUDART_INF_F);
+          }
+        });
+      };
+      auto move = [&](float top) {                    // a new shift; sums so far go along
+        const float to = -ceilf(c32 * fminf(top, 1e30f)), f = ex2f(fmaxf(to - kk.x, -200.f));
+        S0 = fmul2(S0, splat(f)); S1 = fmul2(S1, splat(f));
+        kk = splat(to);
+        limit = El::limit((MARGIN - to) * rc32);
+      };
+      auto add = [&](const uint4& w) {
 #pragma unroll
         for (int i = 0; i < E / 2; i += 2) {
           S0 = fadd2(S0, ex2f2(ffma2(El::pair(w, i), cc, kk)));
           S1 = fadd2(S1, ex2f2(ffma2(El::pair(w, i + 1), cc, kk)));
         }
       };
+      auto two = [&](uint4 w0, uint4 w1, int step) {
+        ahead_of(step); ahead_of(step + 1);
+        if (bits & 3ull) leave_out(w0, w1, step);
+        bits >>= 2;
+        if (El::above(w0, w1, limit)) move(fmaxf(El::top(w0), El::top(w1)));
+        add(w0); add(w1);
+      };
+      auto one = [&](uint4 w, int step) {
+        ahead_of(step);
+        if (bits & 1ull) leave_out(w, w, step);
+        bits >>= 1;
+        if (El::above(w, w, limit)) move(El::top(w));
+        add(w);
+      };
       if (inner) {
         const Source<T, true> c(cur, V, sg.c0 + lane), n(nxt, V, sg.c0 + lane);
-        visit<!BWD>(sg, base, c, BWD ? c : n, pol_last, pol_first, pol_first, ring_slot, sum);
+        visit<!BWD>(sg, base, c, BWD ? c : n, pol_last, pol_first, pol_first, ring_slot, two, one);
       } else {
         const Source<T, false> c(cur, V, sg.c0 + lane), n(nxt, V, sg.c0 + lane);
-        visit<!BWD>(sg, base, c, BWD ? c : n, pol_last, pol_first, pol_first, ring_slot, sum);
+        visit<!BWD>(sg, base, c, BWD ? c : n, pol_last, pol_first, pol_first, ring_slot, two, one);
       }
+      shift = kk.x;
     }
     __syncwarp();
     float warp_shift = shift;
-    if (here) {                       // (a segment may have nothing but listed elements and masked ones)
-#pragma unroll
-      for (int r = 0; r < SLOTS; ++r)
-        if (at[r] >= 0) warp_shift = fminf(warp_shift, -ceilf(c32 * fminf(sh.x[r * 32 + lane], 1e30f)));
-    }
+#pragma unroll 1
+    for (int i = lane; i < n_mine; i += 32)      // (a segment may have nothing but listed elements and masked ones)
+      warp_shift = fminf(warp_shift, -ceilf(c32 * fminf(sh.x[mine[i] & 255u], 1e30f)));
+    __syncwarp();
     warp_shift = warp_least(warp_shift);
     double outside = (((double)S0.x + (double)S0.y) + ((double)S1.x + (double)S1.y)) * (double)ex2f(fmaxf(warp_shift - shift, -200.f));
     double inside = 0, cross = 0;
-    if (here) {
-      bool lost = false;
-#pragma unroll
-      for (int r = 0; r < SLOTS; ++r)
-        if (at[r] >= 0) {
-          const int j = r * 32 + lane;
-          const float x = sh.x[j];
-          const float2 w = sh.w[b][j];
-          const float e = ex2f(fmaf(x, c32, warp_shift));
-          lost |= !(fabsf(x) < CUDART_INF_F);
-          inside += (double)e;
-          cross += reverse ? (double)e * ((double)x * rtau - (double)w.y) : (double)w.x * ((double)x * rtau);
-        }
-      if (lost) inside = CUDART_NAN;      // a listed token that the student's row has masked, or not finite: the float64 kernel decides
+#pragma unroll 1
+    for (int i = lane; i < n_mine; i += 32) {
+      const int j = (int)(mine[i] & 255u);
+      const float x = sh.x[j];
+      const float2 w = sh.w[b][j];
+      const float e = ex2f(fmaf(x, c32, warp_shift));
+      // (a listed token that the student's row has masked, or not finite: the float64 kernel decides)
+      inside += fabsf(x) < CUDART_INF_F ? (double)e : CUDART_NAN;
+      cross += reverse ? (double)e * ((double)x * rtau - (double)w.y) : (double)w.x * ((double)x * rtau);
     }
+    __syncwarp();
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {      // (three chains side by side)
       outside += __shfl_xor_sync(0xffffffffu, outside, o);
@@ -649,18 +707,17 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
       const float* const bc = sh.bc[parity];
       const float kr = bc[0], scale = bc[1], unit = bc[2], kg = bc[3];
       const bool zero = unit == 0.f;      // a row that contributes nothing (or waits for the float64 kernel): zeros, whatever its logits
-      if (here) {
+      {
         const double lse = sh.dc[parity][0], loss = sh.dc[parity][1], Z = sh.dc[parity][2];
-#pragma unroll
-        for (int r = 0; r < SLOTS; ++r)
-          if (at[r] >= 0) {
-            const int j = r * 32 + lane;
-            const float x = sh.x[j];
-            const float2 w = sh.w[b][j];
-            const float p = ex2f(fmaf(x, c32, kr)) * unit;
-            const float v = reverse ? p * (float)((double)x * rtau - lse - (double)w.y - loss) : (float)(Z * (double)p - (double)w.x);
-            sh.g[j] = zero ? 0.f : kg * v;
-          }
+#pragma unroll 1
+        for (int i = lane; i < n_mine; i += 32) {
+          const int j = (int)(mine[i] & 255u);
+          const float x = sh.x[j];
+          const float2 w = sh.w[b][j];
+          const float p = ex2f(fmaf(x, c32, kr)) * unit;
+          const float v = reverse ? p * (float)((double)x * rtau - lse - (double)w.y - loss) : (float)(Z * (double)p - (double)w.x);
+          sh.g[j] = zero ? 0.f : kg * v;
+        }
       }
       __syncwarp();
       bits = here;
@@ -668,37 +725,54 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
       T* const g_row = (T*)P.dlogits + row * P.ld_g;
       char* const g_base = (char*)((uintptr_t)g_row & ~(uintptr_t)15);
       const bool alike = ((uintptr_t)g_row & 15) == cur.head * sizeof(T);      // the gradient's pieces lie like the row's
-      auto gradient = [&](const uint4& w, int step) -> uint4 {
-        uint4 g = make_uint4(0u, 0u, 0u, 0u);
-        if (!zero) {
-          float2 v[E / 2];
+      auto plain = [&](const uint4& w) -> uint4 {
+        float2 v[E / 2];
 #pragma unroll
-          for (int i = 0; i < E / 2; ++i) v[i] = fmul2(ex2f2(ffma2(El::pair(w, i), cc, kk)), sc);
-          if constexpr (E == 8) g = make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[1].x, v[1].y), pack_bf16x2(v[2].x, v[2].y), pack_bf16x2(v[3].x, v[3].y));
-          else g = make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
-          if (bits & 1ull)
-            each_listed<SLOTS, El::STEP_LOG>(at, step, [&](int e, int j) {
-              if (lane == e >> El::LOG) El::put(g, e & (E - 1), sh.g[j]);
-            });
-        }
-        bits >>= 1;
-        return g;
+        for (int i = 0; i < E / 2; ++i) v[i] = fmul2(ex2f2(ffma2(El::pair(w, i), cc, kk)), sc);
+        if constexpr (E == 8) return make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[1].x, v[1].y), pack_bf16x2(v[2].x, v[2].y), pack_bf16x2(v[3].x, v[3].y));
+        else return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
+      };
+      auto put_listed = [&](uint4& g0, uint4& g1, int step) {
+        each_listed<El::STEP_LOG>(mine, n_mine, step, lane, [&](int e, int j) {
+          if (lane == (e >> El::LOG & 31)) {
+            const float x = sh.g[j];
+            if (e >> El::STEP_LOG) El::put(g1, e & (E - 1), x);
+            else El::put(g0, e & (E - 1), x);
+          }
+        });
+      };
+      auto pass = [&](auto&& store, const auto& c, const auto& n) {
+        visit<true>(sg, base, c, n, pol_first, pol_last, pol_first, ring_slot,
+          [&](const uint4& w0, const uint4& w1, int step) {
+            uint4 g0 = make_uint4(0u, 0u, 0u, 0u), g1 = g0;
+            if (!zero) {
+              g0 = plain(w0); g1 = plain(w1);
+              if (bits & 3ull) put_listed(g0, g1, step);
+            }
+            bits >>= 2;
+            store(g0, step); store(g1, step + 1);
+          },
+          [&](const uint4& w, int step) {
+            uint4 g = make_uint4(0u, 0u, 0u, 0u);
+            if (!zero) {
+              g = plain(w);
+              if (bits & 1ull) put_listed(g, g, step);
+            }
+            bits >>= 1;
+            store(g, step);
+          });
       };
       if (inner && alike) {
-        const Source<T, true> c(cur, V, sg.c0 + lane), n(nxt, V, sg.c0 + lane);
         char* const to = g_base + (int64_t)(sg.c0 + lane) * 16;
-        visit<true>(sg, base, c, n, pol_first, pol_last, pol_first, ring_slot, [&](const uint4& w, int step) { st_stream(to + (uint32_t)step * 512u, gradient(w, step), pol_first); });
-      } else {
-        const Source<T, false> c(cur, V, sg.c0 + lane), n(nxt, V, sg.c0 + lane);
-        visit<true>(sg, base, c, n, pol_first, pol_last, pol_first, ring_slot, [&](const uint4& w, int step) {
-          const uint4 g = gradient(w, step);
+        pass([&](const uint4& g, int step) { st_stream(to + (uint32_t)step * 512u, g, pol_first); }, Source<T, true>(cur, V, sg.c0 + lane), Source<T, true>(nxt, V, sg.c0 + lane));
+      } else
+        pass([&](const uint4& g, int step) {
           const int c = sg.c0 + lane + 32 * step;
           if (alike && (unsigned)(c - cur.full0) < (unsigned)cur.full) st_stream(g_base + (uint32_t)c * 16u, g, pol_first);
           else if (c < cur.n)
             for (int e = 0; e < E; ++e)
               if ((unsigned)(c * E + e - cur.head) < (unsigned)V) st_from_float(g_row, c * E + e - cur.head, El::get(g, e));
-        });
-      }
+        }, Source<T, false>(cur, V, sg.c0 + lane), Source<T, false>(nxt, V, sg.c0 + lane));
     }
     cur = nxt;
     b = next_b;
@@ -706,7 +780,7 @@ __global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kerne
   copies_wait<0>();
 }
 
-template <typename T, int MW, int SLOTS, bool BWD> cudaError_t launch_stream_as(const DistillParams& p, cudaStream_t st) {
+template <typename T, int MW, bool BWD> cudaError_t launch_stream_as(const DistillParams& p, cudaStream_t st) {
   static std::mutex mu;
   static int known_dev = -1, sms = 0;
   int dev = 0;
@@ -715,18 +789,17 @@ template <typename T, int MW, int SLOTS, bool BWD> cudaError_t launch_stream_as(
   {
     std::lock_guard<std::mutex> lock(mu);
     if (known_dev != dev) {
-      cudaError_t e = cudaFuncSetAttribute(distill_stream_kernel<T, MW, SLOTS, BWD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      cudaError_t e = cudaFuncSetAttribute(distill_stream_kernel<T, MW, BWD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
       if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
       if (e != cudaSuccess) return e;
       known_dev = dev;
     }
   }
   const int grid = (int)std::min<int64_t>(p.in.N, (int64_t)sms * (WARPS_FULL / MW));
-  return launch_pdl(distill_stream_kernel<T, MW, SLOTS, BWD>, dim3((unsigned)grid), MW * 32, smem, st, true, p);
+  return launch_pdl(distill_stream_kernel<T, MW, BWD>, dim3((unsigned)grid), MW * 32, smem, st, true, p);
 }
 template <typename T, int MW> cudaError_t launch_stream(const DistillParams& p, cudaStream_t st) {
-  if (p.in.k <= 64) return p.dlogits ? launch_stream_as<T, MW, 2, true>(p, st) : launch_stream_as<T, MW, 2, false>(p, st);
-  return p.dlogits ? launch_stream_as<T, MW, 4, true>(p, st) : launch_stream_as<T, MW, 4, false>(p, st);
+  return p.dlogits ? launch_stream_as<T, MW, true>(p, st) : launch_stream_as<T, MW, false>(p, st);
 }
 
 int64_t round256(int64_t x) { return (x + 255) & ~(int64_t)255; }
