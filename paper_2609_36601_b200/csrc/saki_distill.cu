@@ -70,7 +70,7 @@ __device__ __forceinline__ double warp_max(double a) {
 
 // ---------------------------------------------------------------- lists
 __global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams P) {
-  __shared__ int ids[8][KMAX];
+  __shared__ alignas(16) int ids[8][KMAX];
   launch_dependents();
   wait_for_predecessor();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = P.in.k;
@@ -101,11 +101,15 @@ __global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams 
     n += __popc(__ballot_sync(0xffffffffu, id[r] >= 0));
   }
   __syncwarp();
-  for (int i = 0; i < k; ++i) {
-    const int v = ids[warp][i];
+  int same[KMAX / 32] = {};            // entries with the same token, itself among them
+  for (int i = 0; i < k; i += 4) {
+    const int4 v = *(const int4*)&ids[warp][i];
 #pragma unroll
-    for (int r = 0; r < KMAX / 32; ++r) bad_id |= v >= 0 && id[r] == v && i != r * 32 + lane;
+    for (int r = 0; r < KMAX / 32; ++r)
+      if (r * 32 < k) same[r] += (v.x == id[r]) + (v.y == id[r]) + (v.z == id[r]) + (v.w == id[r]);
   }
+#pragma unroll
+  for (int r = 0; r < KMAX / 32; ++r) bad_id |= id[r] >= 0 && same[r] > 1;
   const bool with_rest = P.in.teacher_lse != nullptr;
   double ref = 0;
   if (with_rest) {
@@ -119,7 +123,7 @@ __global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams 
     m = warp_max(m);
 #pragma unroll
     for (int r = 0; r < KMAX / 32; ++r)
-      if (id[r] >= 0) s += exp(t[r] - m);
+      if (r * 32 < k && id[r] >= 0) s += exp(t[r] - m);
     ref = n ? m + log(warp_sum(s)) : 0;
   }
   if (!status && __any_sync(0xffffffffu, bad_id)) status = SAKI_ROW_BAD_ID;
@@ -129,7 +133,7 @@ __global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams 
   for (int r = 0; r < KMAX / 32; ++r) {
     const int j = r * 32 + lane;
     float2 w = make_float2(0.f, 0.f);
-    if (id[r] >= 0) {
+    if (r * 32 < k && id[r] >= 0) {
       const double lw = t[r] - ref, e = exp(lw);
       w = make_float2((float)e, (float)lw);
       W += e; W32 += (double)w.x; H += e > 0 ? e * lw : 0;
@@ -252,7 +256,6 @@ __global__ void __launch_bounds__(DG_THREADS) distill_general_kernel(const Disti
 }
 
 // ---------------------------------------------------------------- streaming kernel
-constexpr int WARPS_FULL = 32, WARPS_HALF = 16;
 constexpr int KEEP = 12, RING = 4, RESIDENT = KEEP - RING;      // 512-byte steps of a warp in shared memory; of them, where a segment does not fit, the ring's (both even: steps go in pairs)
 constexpr int MAX_STEPS = 64;
 constexpr float MARGIN = 60.f;                                  // in base 2: how far a lane's elements may lie above its shift
@@ -347,8 +350,8 @@ template <typename T> __device__ __forceinline__ uint4 odd_piece(const char* bas
   constexpr int E = Elem<T>::E;
   uint4 w = make_uint4(Elem<T>::FILLER, Elem<T>::FILLER, Elem<T>::FILLER, Elem<T>::FILLER);
   const T* p = (const T*)base + (int64_t)c * E;
-#pragma unroll 1
-  for (int e = 0; e < E; ++e)
+#pragma unroll
+  for (int e = 0; e < E; ++e)      // (all on their way at once)
     if (c * E + e >= head && c * E + e < head + V) Elem<T>::put(w, e, ld_as_float(p, e));
   return w;
 }
@@ -450,6 +453,7 @@ template <int MW> struct StreamShared {
   uint32_t mine[MW][KMAX];     // by warp: what lies in its segment, place in elements << 8 | place in the list
 };
 template <int MW> constexpr int stream_smem = MW * KEEP * 512 + (int)sizeof(StreamShared<MW>);
+template <int MW> constexpr int BLOCKS = std::min(32 / MW, 227 * 1024 / (stream_smem<MW> + 1024));      // on an SM
 
 // The listed elements in steps `step` and `step` + 1 (step even) of a warp: body(place within the two steps, place in the list).
 template <int STEP_LOG, typename Body> __device__ __forceinline__ void each_listed(const uint32_t* mine, int n, int step, int lane, Body&& body) {
@@ -474,7 +478,7 @@ __device__ __forceinline__ double rcp_near(double x) {
 }
 
 template <typename T, int MW, bool BWD>
-__global__ void __launch_bounds__(MW * 32, WARPS_FULL / MW) distill_stream_kernel(const DistillParams P) {
+__global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(const DistillParams P) {
   using El = Elem<T>;
   constexpr int E = El::E;
   extern __shared__ __align__(128) unsigned char dsm[];
@@ -795,11 +799,19 @@ template <typename T, int MW, bool BWD> cudaError_t launch_stream_as(const Disti
       known_dev = dev;
     }
   }
-  const int grid = (int)std::min<int64_t>(p.in.N, (int64_t)sms * (WARPS_FULL / MW));
+  const int grid = (int)std::min<int64_t>(p.in.N, (int64_t)sms * BLOCKS<MW>);
   return launch_pdl(distill_stream_kernel<T, MW, BWD>, dim3((unsigned)grid), MW * 32, smem, st, true, p);
 }
-template <typename T, int MW> cudaError_t launch_stream(const DistillParams& p, cudaStream_t st) {
-  return p.dlogits ? launch_stream_as<T, MW, true>(p, st) : launch_stream_as<T, MW, false>(p, st);
+template <typename T, int MW> cudaError_t launch_with(const DistillParams& p, cudaStream_t st) { return p.dlogits ? launch_stream_as<T, MW, true>(p, st) : launch_stream_as<T, MW, false>(p, st); }
+// Warps to a row: as few as keep it in shared memory (several blocks on an SM: one's barriers under another's passes), all 32 where none do; more where there are no more rows than blocks.
+// (2960 bf16 rows with lists of 32, us: 2048 entries 52 with 4 warps, 70 with 16, 122 with 32; 16384 92 with 8, 100, 125; 32003 156 with 16, 174; 65536, which 16 do not
+// keep, 230 and 198; float32 rows of 32003, which they do not keep either, 214 and 193.)
+template <typename T> cudaError_t launch_stream(const DistillParams& p, cudaStream_t st, int sms) {
+  const int64_t bytes = ((int64_t)p.in.V + 2 * Elem<T>::E) * (int64_t)sizeof(T), N = p.in.N;
+  if (bytes <= 4 * KEEP * 512 && N > sms * BLOCKS<8>) return launch_with<T, 4>(p, st);
+  if (bytes <= 8 * KEEP * 512 && N > sms * BLOCKS<16>) return launch_with<T, 8>(p, st);
+  if (bytes <= 16 * KEEP * 512 && N > sms) return launch_with<T, 16>(p, st);
+  return launch_with<T, 32>(p, st);
 }
 
 int64_t round256(int64_t x) { return (x + 255) & ~(int64_t)255; }
@@ -811,7 +823,7 @@ int64_t distill_scratch_bytes(int64_t N, int32_t k) { return 256 + round256(N * 
 // rows of up to 64 steps a warp, in both types
 bool distill_stream_can_serve(const saki_distill_in& in) {
   const int e = in.dtype == SAKI_BF16 ? 8 : 4;
-  return in.N <= 0x7fffffff && ((int64_t)in.V + 2 * e - 2) / e <= (int64_t)MAX_STEPS * 32 * WARPS_FULL;
+  return in.N <= 0x7fffffff && ((int64_t)in.V + 2 * e - 2) / e <= (int64_t)MAX_STEPS * 32 * 32;
 }
 
 cudaError_t launch_distill(const saki_distill_in& in, const saki_distill_out& out, void* dlogits, int64_t ld_g, float grad_scale, void* scratch, bool stream,
@@ -828,9 +840,9 @@ cudaError_t launch_distill(const saki_distill_in& in, const saki_distill_out& ou
   ++*n_launches;
   if (e != cudaSuccess) return e;
   if (stream) {
-    const bool half = (int64_t)in.V * (in.dtype == SAKI_BF16 ? 2 : 4) <= 196608;
-    if (in.dtype == SAKI_BF16) e = half ? launch_stream<__nv_bfloat16, WARPS_HALF>(p, st) : launch_stream<__nv_bfloat16, WARPS_FULL>(p, st);
-    else e = half ? launch_stream<float, WARPS_HALF>(p, st) : launch_stream<float, WARPS_FULL>(p, st);
+    int dev = 0, sms = 148;
+    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    e = in.dtype == SAKI_BF16 ? launch_stream<__nv_bfloat16>(p, st, sms) : launch_stream<float>(p, st, sms);
     ++*n_launches;
     if (e != cudaSuccess) return e;
     p.from_list = 1;

@@ -425,7 +425,8 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       in_turn += (int)gridDim.x >> 1;
       return x;
     }
-    if (!wait(&s_full[slot], slot_phase, stop, limit)) return x;
+    const bool there = wait(&s_full[slot], slot_phase, stop, limit);
+    if (whole_warp ? !__all_sync(0xffffffffu, there) : !there) return x;      // (a warp gives up as one: each lane has a clock of its own)
     x = plan.tile(P, *(volatile int*)&slot_tile[slot]);
     if (whole_warp) __syncwarp();
     if (!whole_warp || lane == 0) arrive_at(at_rank(smem_addr(&s_empty[slot]), 0));
@@ -515,7 +516,8 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
     for (;;) {
       const Tile x = next_tile(true);
       if (x.kind < 0) break;
-      if (!wait(&t_full[acc], acc_phase, stop, limit)) break;
+      const bool done = wait(&t_full[acc], acc_phase, stop, limit);
+      if (!__all_sync(0xffffffffu, done)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * TILE);
       const int row = x.m * TILE + (int)rank * HALF + q * 32 + lane;      // of H, or the vocabulary entry within the piece
