@@ -3,8 +3,8 @@
 // A row (or a slice of it, where there are few rows) is read once by a block of 256 threads: every thread takes 16-byte pieces 256 apart, sums their exponentials
 // under a shift of its own, and leaves the upper 16 bits of the largest element of each group of its pieces, as an ordered key, in shared memory.  The k-th largest of the threads'
 // maxima is a bar that the slice's k-th largest logit reaches, and that little more than k elements reach: only the groups that reach it are read again (some k of
-// ten thousand), what reaches it in them is ranked by counting.  Where hundreds of elements are equal, or the largest lie in few threads' pieces, the list overflows: the
-// best are then taken one by one, each thread offering its best that is left.
+// ten thousand), what reaches it in them is ranked by counting.  Where the largest lie in few threads' pieces the list overflows, and the bar is found by counting elements; where hundreds
+// of them are equal, too, the best are taken one by one, each thread offering its best that is left.
 // Slices of a row are joined by a second kernel.
 #include "saki_device.cuh"
 #include <algorithm>
@@ -73,6 +73,7 @@ struct TopShared {
   uint64_t warp_best[TWARPS];
   uint32_t top[TT];
   uint32_t bar, most, groups, count;
+  int warp_count[TWARPS];
   double slice_shift, slice_sum;
   int group[LIST];
   uint16_t key[MAX_ENTRIES];
@@ -234,37 +235,77 @@ __global__ void __launch_bounds__(TT, 5) top_rows_kernel(const TopParams P) {
   }
   if (!bad) {
     // ------------------------------------------------ groups that reach the bar, and what reaches it in them
-    if (mine >= bar)
-      for (int i = 0; i < entries; ++i)
-        if (sh.key[i * TT + tid] >= bar) {
-          const unsigned at = atomicAdd(&sh.groups, 1u);
-          if (at < LIST) sh.group[at] = i * TT + tid;
-        }
-    __syncthreads();
-    const int groups = (int)sh.groups;
-    if (groups <= LIST)
-      for (int i = tid; i < groups * GROUP; i += TT) {
-        const int g = sh.group[i / GROUP], at = g / TT, p = p0 + (at * GROUP + i % GROUP) * TT + (g - at * TT);
-        const uint4 w = load(p);
+    auto collect = [&](uint32_t bar) -> bool {      // whether it is all in the list
+      if (mine >= bar)
+        for (int i = 0; i < entries; ++i)
+          if (sh.key[i * TT + tid] >= bar) {
+            const unsigned at = atomicAdd(&sh.groups, 1u);
+            if (at < LIST) sh.group[at] = i * TT + tid;
+          }
+      __syncthreads();
+      const int groups = (int)sh.groups;
+      if (groups <= LIST)
+        for (int i = tid; i < groups * GROUP; i += TT) {
+          const int g = sh.group[i / GROUP], at = g / TT, p = p0 + (at * GROUP + i % GROUP) * TT + (g - at * TT);
+          const uint4 w = load(p);
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-          const float2 a = Pc::pair(w, j >> 1);
-          const float x = j & 1 ? a.y : a.x;
-          if (order_of(x) >> 16 >= bar && x > -CUDART_INF_F) {
-            const unsigned n = atomicAdd(&sh.count, 1u);
-            if (n < LIST) sh.list[n] = pair_word(x, p * E + j - head);
+          for (int j = 0; j < E; ++j) {
+            const float2 a = Pc::pair(w, j >> 1);
+            const float x = j & 1 ? a.y : a.x;
+            if (order_of(x) >> 16 >= bar && x > -CUDART_INF_F) {
+              const unsigned n = atomicAdd(&sh.count, 1u);
+              if (n < LIST) sh.list[n] = pair_word(x, p * E + j - head);
+            }
           }
         }
+      __syncthreads();
+      return groups <= LIST && sh.count <= LIST;
+    };
+    bool all = collect(bar);
+    if (!all) {
+      // the largest lie in few threads' pieces (or there are fewer threads with any than k): the bar goes up to the k-th largest itself, by counting what reaches it
+      uint32_t lo = bar, hi = sh.most;
+#pragma unroll 1
+      while (lo < hi) {
+        const uint32_t to = (lo + hi + 1) >> 1;
+        int n = 0;
+        if (mine >= to)
+#pragma unroll 1
+          for (int i = 0; i < entries; ++i)
+            if (sh.key[i * TT + tid] >= to)
+#pragma unroll
+              for (int g = 0; g < GROUP; ++g) {
+                const uint4 w = load(p0 + (i * GROUP + g) * TT + tid);
+#pragma unroll
+                for (int j = 0; j < E / 2; ++j) { const float2 a = Pc::pair(w, j); n += (order_of(a.x) >> 16 >= to) + (order_of(a.y) >> 16 >= to); }
+              }
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (lane == 0) sh.warp_count[warp] = n;
+        __syncthreads();
+        n = 0;
+#pragma unroll
+        for (int w = 0; w < TWARPS; ++w) n += sh.warp_count[w];
+        __syncthreads();
+        if (n >= k) lo = to;
+        else hi = to - 1;
       }
-    __syncthreads();
+      if (tid == 0) sh.groups = sh.count = 0;
+      __syncthreads();
+      all = collect(lo);
+    }
     const int count = (int)sh.count;
-    if (groups <= LIST && count <= LIST) {
-      for (int i = tid; i < count; i += TT) {
-        const uint64_t w = sh.list[i];
+    if (all) {
+      // ranks by counting, one to four threads an element
+      const int parts = count <= TT / 4 ? 4 : count <= TT / 2 ? 2 : 1, step = TT / parts;
+      for (int i0 = warp * 32 / parts; i0 < count; i0 += step) {      // (the same for all threads of a warp: they exchange)
+        const int i = i0 + lane / parts;
+        const uint64_t w = sh.list[min(i, count - 1)];
         int r = 0;
 #pragma unroll 4
-        for (int j = 0; j < count; ++j) r += sh.list[j] > w;
-        if (r < k) sh.best[r] = w;
+        for (int j = tid % parts; j < count; j += parts) r += sh.list[j] > w;
+        if (parts > 1) r += __shfl_xor_sync(0xffffffffu, r, 1);
+        if (parts > 2) r += __shfl_xor_sync(0xffffffffu, r, 2);
+        if (i < count && r < k && tid % parts == 0) sh.best[r] = w;
       }
       for (int i = count + tid; i < k; i += TT) sh.best[i] = 0;
     } else {
