@@ -45,20 +45,22 @@ constexpr uint32_t LEAST = 0x0080u;                 // key of the lowest finite 
 
 template <typename T> struct Piece;
 template <> struct Piece<__nv_bfloat16> {
-  static constexpr int E = 8, GROUP = 2, AHEAD = 1;
+  static constexpr int E = 8;
   static constexpr uint32_t FILLER = 0xFF80FF80u;   // -inf
   static __device__ __forceinline__ float2 pair(const uint4& w, int i) { return unpack_bf16x2(i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w); }
-  static __device__ __forceinline__ float top(const uint4 (&w)[GROUP]) {      // (of a pair with a NaN the other)
-    const uint32_t a = max_bf16x2(max_bf16x2(max_bf16x2(w[0].x, w[0].y), max_bf16x2(w[0].z, w[0].w)), max_bf16x2(max_bf16x2(w[1].x, w[1].y), max_bf16x2(w[1].z, w[1].w)));
+  template <int GROUP> static __device__ __forceinline__ float top(const uint4 (&w)[GROUP]) {      // (of a pair with a NaN the other)
+    uint32_t a = w[0].x;
+#pragma unroll
+    for (int g = 0; g < GROUP; ++g) a = max_bf16x2(a, max_bf16x2(max_bf16x2(w[g].x, w[g].y), max_bf16x2(w[g].z, w[g].w)));
     const float2 f = unpack_bf16x2(a);
     return fmaxf(f.x, f.y);
   }
 };
 template <> struct Piece<float> {
-  static constexpr int E = 4, GROUP = 4, AHEAD = 1;
+  static constexpr int E = 4;
   static constexpr uint32_t FILLER = 0xFF800000u;
   static __device__ __forceinline__ float2 pair(const uint4& w, int i) { return i == 0 ? make_float2(__uint_as_float(w.x), __uint_as_float(w.y)) : make_float2(__uint_as_float(w.z), __uint_as_float(w.w)); }
-  static __device__ __forceinline__ float top(const uint4 (&w)[GROUP]) {
+  template <int GROUP> static __device__ __forceinline__ float top(const uint4 (&w)[GROUP]) {
     float m = -CUDART_INF_F;
 #pragma unroll
     for (int g = 0; g < GROUP; ++g) m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(w[g].x), __uint_as_float(w[g].y)), fmaxf(__uint_as_float(w[g].z), __uint_as_float(w[g].w))));
@@ -79,10 +81,11 @@ struct TopShared {
   uint16_t key[MAX_ENTRIES];
 };
 
-template <typename T>
-__global__ void __launch_bounds__(TT, 5) top_rows_kernel(const TopParams P) {
+// GROUP: pieces to a key.  (With four of them a thread holds too many for six blocks on an SM.)
+template <typename T, int GROUP>
+__global__ void __launch_bounds__(TT, GROUP == 2 ? 6 : 5) top_rows_kernel(const TopParams P) {
   using Pc = Piece<T>;
-  constexpr int E = Pc::E, GROUP = Pc::GROUP, AHEAD = Pc::AHEAD;
+  constexpr int E = Pc::E;
   __shared__ TopShared sh;
   launch_dependents();
   wait_for_predecessor();
@@ -115,23 +118,17 @@ __global__ void __launch_bounds__(TT, 5) top_rows_kernel(const TopParams P) {
   float shift = 0.f, limit = -CUDART_INF_F;      // (the first group sets them)
   uint32_t mine = 0;
   const float2 cc = splat(P.c);
-  uint4 next[AHEAD][GROUP];             // on their way
+  uint4 next[GROUP];                   // on their way
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i)
-#pragma unroll
-    for (int g = 0; g < GROUP; ++g) next[i][g] = load(p0 + (i * GROUP + g) * TT + tid);
+  for (int g = 0; g < GROUP; ++g) next[g] = load(p0 + g * TT + tid);
 #pragma unroll 1
   for (int i = 0; i < entries; ++i) {
     uint4 w[GROUP];
 #pragma unroll
-    for (int g = 0; g < GROUP; ++g) {
-      w[g] = next[0][g];
+    for (int g = 0; g < GROUP; ++g) w[g] = next[g];
+    if (i + 1 < entries) {
 #pragma unroll
-      for (int j = 0; j + 1 < AHEAD; ++j) next[j][g] = next[j + 1][g];
-    }
-    if (i + AHEAD < entries) {
-#pragma unroll
-      for (int g = 0; g < GROUP; ++g) next[AHEAD - 1][g] = load(p0 + ((i + AHEAD) * GROUP + g) * TT + tid);
+      for (int g = 0; g < GROUP; ++g) next[g] = load(p0 + ((i + 1) * GROUP + g) * TT + tid);
     }
     const float top = Pc::top(w);
     const uint32_t key = order_of(top) >> 16;
@@ -455,17 +452,19 @@ __global__ void __launch_bounds__(TT) top_join_kernel(const TopParams P) {
   }
 }
 
-struct Cut { int slices, pieces; };
+struct Cut { int slices, pieces, group; };
 constexpr int MAX_SMS = 256;
 // Slices as long as the keys' room; shorter ones for few rows, so that there are two blocks for every SM, of 256 pieces (one a thread) at the least and MIN_SLICES at the most.
 Cut cut(int64_t rows, int V, int dtype, int sms) {
-  const int e = dtype == SAKI_BF16 ? 8 : 4, group = dtype == SAKI_BF16 ? Piece<__nv_bfloat16>::GROUP : Piece<float>::GROUP;
-  const int all = (V + 2 * e - 2) / e, longest = MAX_ENTRIES * group;
+  const int e = dtype == SAKI_BF16 ? 8 : 4, all = (V + 2 * e - 2) / e;
+  // float32: four pieces to a key keep more bytes on their way, two leave room for six blocks on an SM (2960 rows, 64 best: of 2048 32 and 27 us, of 16384 54 and 53, of 32003 85 and 88, of
+  // 65536 142 and 159)
+  const int group = dtype == SAKI_BF16 || V <= 20480 ? 2 : 4, longest = MAX_ENTRIES * group;
   const int need = (all + longest - 1) / longest;
   int64_t want = (2 * (int64_t)std::min(sms, MAX_SMS) + rows - 1) / std::max<int64_t>(rows, 1);
   want = std::max<int64_t>(need, std::min<int64_t>({want, (int64_t)std::max(MIN_SLICES, need), (int64_t)std::max(1, all / TT)}));
   const int pieces = (int)((all + want - 1) / want);
-  return {(all + pieces - 1) / pieces, pieces};
+  return {(all + pieces - 1) / pieces, pieces, group};
 }
 int sm_count() {
   int dev = 0, sms = 148;
@@ -491,7 +490,9 @@ cudaError_t launch_top(const saki_top_in& in, const saki_top_out& out, void* scr
   p.cand = (uint64_t*)scratch;
   p.part = (double2*)((char*)scratch + round256(in.N * c.slices * in.k * 8));
   const dim3 grid((unsigned)(in.N * c.slices));
-  cudaError_t e = in.dtype == SAKI_BF16 ? launch_pdl(top_rows_kernel<__nv_bfloat16>, grid, TT, 0, st, true, p) : launch_pdl(top_rows_kernel<float>, grid, TT, 0, st, true, p);
+  cudaError_t e = in.dtype == SAKI_BF16 ? launch_pdl(top_rows_kernel<__nv_bfloat16, 2>, grid, TT, 0, st, true, p)
+                  : c.group == 2    ? launch_pdl(top_rows_kernel<float, 2>, grid, TT, 0, st, true, p)
+                                    : launch_pdl(top_rows_kernel<float, 4>, grid, TT, 0, st, true, p);
   *n_launches = 1;
   if (e != cudaSuccess || c.slices == 1) return e;
   ++*n_launches;
