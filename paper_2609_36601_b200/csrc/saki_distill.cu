@@ -15,6 +15,7 @@
 #include "saki_device.cuh"
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 namespace saki {
 
@@ -362,14 +363,18 @@ template <typename T> __device__ __forceinline__ void fill_piece(uint32_t slot, 
 
 struct Segment { int c0, steps, res; };      // of a warp: its first piece, steps of 32 pieces, how many of them stay in shared memory
 
-// A lane's pieces of a row, by step.  INNER: the warp's whole segment lies within whole pieces of the row.
+// A lane's pieces of a row, by step; at steps lo to hi - 1 those of all lanes lie within the row.  INNER: at all steps of the warp.
 template <typename T, bool INNER> struct Source {
   View<T> v;
-  int V, c0;                   // the lane's first piece
-  const char* at;              // INNER: where it is
-  __device__ __forceinline__ Source(const View<T>& view, int V_, int c) : v(view), V(V_), c0(c), at(view.base + (int64_t)c * 16) {}
+  const char* at;              // the lane's first piece
+  int V, c0, lo, hi;
+  __device__ __forceinline__ Source(const View<T>& view, int V_, int first, int lane) : v(view), at(view.base + (int64_t)(first + lane) * 16), V(V_), c0(first + lane) {
+    lo = max((view.full0 - first + 31) >> 5, 0);
+    hi = max((view.full0 + view.full - first) >> 5, lo);
+  }
+  __device__ __forceinline__ bool whole(int step) const { return INNER || (unsigned)(step - lo) < (unsigned)(hi - lo); }
   __device__ __forceinline__ void fill(uint32_t slot, int step, uint64_t pol) const {
-    if constexpr (INNER) copy16(slot, at + (uint32_t)step * 512u, pol);      // (a row has less than 2^31 bytes)
+    if (whole(step)) copy16(slot, at + (uint32_t)step * 512u, pol);      // (a row has less than 2^31 bytes)
     else fill_piece<T>(slot, v, V, c0 + 32 * step, pol);
   }
 };
@@ -381,65 +386,51 @@ template <typename T, bool INNER> struct Source {
 template <bool REFILL, typename S, typename Body, typename Single>
 __device__ __forceinline__ void visit(const Segment& sg, uint32_t base, const S& cur, const S& wrap, uint64_t pol_cur, uint64_t pol_wrap, uint64_t pol_res, uint32_t& ring_slot,
                                       Body&& body, Single&& single) {
-  uint32_t slot = base;
-  int k = 0;
-#pragma unroll 1
-  for (; k + 1 < sg.res; k += 2, slot += 1024) {
-    copies_wait<1>();
-    const uint4 a = lds128(slot), b = lds128(slot + 512);
-    if constexpr (REFILL) { wrap.fill(slot, k, pol_res); wrap.fill(slot + 512, k + 1, pol_res); }
-    copies_commit();
-    body(a, b, k);
-  }
-  if (k < sg.res) {
-    copies_wait<1>();
-    const uint4 a = lds128(slot);
-    if constexpr (REFILL) wrap.fill(slot, k, pol_res);
-    copies_commit();
-    single(a, k);
-    return;                    // (steps that stream are there only behind an even number of resident ones)
-  }
-  uint32_t ring = ring_slot;
+  uint32_t slot = base, ring = ring_slot;
   auto next_slot = [&] {
     const uint32_t at = ring;
     ring += 512;
     if (ring == base + KEEP * 512) ring = base + RESIDENT * 512;
     return at;
   };
-#pragma unroll 1
-  for (; k + 1 + RING < sg.steps; k += 2) {
-    copies_wait<1>();
-    const uint32_t s0 = next_slot(), s1 = next_slot();
-    const uint4 a = lds128(s0), b = lds128(s1);
-    cur.fill(s0, k + RING, pol_cur);
-    cur.fill(s1, k + RING + 1, pol_cur);
-    copies_commit();
-    body(a, b, k);
-  }
   auto refill = [&](uint32_t at, int step) {
     if (step + RING < sg.steps) cur.fill(at, step + RING, pol_cur);
     else wrap.fill(at, step + RING - (sg.steps - sg.res), pol_wrap);
   };
+  int k = 0;
 #pragma unroll 1
-  for (; k + 1 < sg.steps; k += 2) {
-    copies_wait<1>();
-    const uint32_t s0 = next_slot(), s1 = next_slot();
-    const uint4 a = lds128(s0), b = lds128(s1);
-    refill(s0, k);
-    refill(s1, k + 1);
-    copies_commit();
-    body(a, b, k);
-  }
-  if (k < sg.steps) {
-    copies_wait<1>();
-    const uint32_t s0 = next_slot();
-    const uint4 a = lds128(s0);
-    refill(s0, k);
-    copies_commit();
-    single(a, k);
-  }
+    for (; k + 1 < sg.res; k += 2, slot += 1024) {
+      copies_wait<1>();
+      const uint4 a = lds128(slot), b = lds128(slot + 512);
+      if constexpr (REFILL) { wrap.fill(slot, k, pol_res); wrap.fill(slot + 512, k + 1, pol_res); }
+      copies_commit();
+      body(a, b, k);
+    }
+#pragma unroll 1
+    for (; k >= sg.res && k + 1 < sg.steps; k += 2) {
+      copies_wait<1>();
+      const uint32_t s0 = next_slot(), s1 = next_slot();
+      const uint4 a = lds128(s0), b = lds128(s1);
+      refill(s0, k);
+      refill(s1, k + 1);
+      copies_commit();
+      body(a, b, k);
+    }
+    if (k < sg.steps) {
+      const bool stays = k < sg.res;
+      copies_wait<1>();
+      const uint32_t at = stays ? slot : next_slot();
+      const uint4 a = lds128(at);
+      if (!stays) refill(at, k);
+      else if constexpr (REFILL) wrap.fill(at, k, pol_res);
+      copies_commit();
+      single(a, k);
+    }
   ring_slot = ring;
 }
+
+using One = std::integral_constant<int, 1>;
+using Two = std::integral_constant<int, 2>;
 
 template <int MW> struct StreamShared {
   double red[4][MW];           // by warp: the sum outside K, its shift, the sum in K, the sum for the loss
@@ -455,17 +446,18 @@ template <int MW> struct StreamShared {
 template <int MW> constexpr int stream_smem = MW * KEEP * 512 + (int)sizeof(StreamShared<MW>);
 template <int MW> constexpr int BLOCKS = std::min(32 / MW, 227 * 1024 / (stream_smem<MW> + 1024));      // on an SM
 
-// The listed elements in steps `step` and `step` + 1 (step even) of a warp: body(place within the two steps, place in the list).
-template <int STEP_LOG, typename Body> __device__ __forceinline__ void each_listed(const uint32_t* mine, int n, int step, int lane, Body&& body) {
+// The listed elements in steps `step` to `step` + STEPS - 1 of a warp (STEPS 1 or 2, step a multiple of it): body(place within the steps, place in the list).
+template <int STEPS, int STEP_LOG, typename Body> __device__ __forceinline__ void each_listed(const uint32_t* mine, int n, int step, int lane, Body&& body) {
 #pragma unroll 1
   for (int q = 0; q < n; q += 32) {
     const uint32_t entry = q + lane < n ? mine[q + lane] : ~0u;
-    unsigned m = __ballot_sync(0xffffffffu, entry >> (8 + STEP_LOG + 1) == (uint32_t)step >> 1);
+    unsigned m = __ballot_sync(0xffffffffu, entry >> (7 + STEP_LOG + STEPS) == (uint32_t)step >> (STEPS - 1));
+#pragma unroll 1
     while (m) {
       const int src = __ffs(m) - 1;
       m &= m - 1;
       const uint32_t e = __shfl_sync(0xffffffffu, entry, src);
-      body((int)(e >> 8) & ((2 << STEP_LOG) - 1), (int)(e & 255u));
+      body((int)(e >> 8) & ((STEPS << STEP_LOG) - 1), (int)(e & 255u));
     }
   }
 }
@@ -551,8 +543,10 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
     }
     __syncwarp();
     const uint64_t here = (uint64_t)here_hi << 32 | here_lo;
-    // the segment lies within whole pieces of this row and the next
-    const bool inner = nxt.base != nullptr && sg.c0 >= max(cur.full0, nxt.full0) && sg.c0 + 32 * sg.steps <= min(cur.full0 + cur.full, nxt.full0 + nxt.full);
+    // The segment lies within whole pieces of this row and the next: long rows have loops of their own for that (4096 rows of 151936 567 -> 544 us; for short ones it is code that
+    // has to be fetched: 16 rows of 32000 11 -> 16 us).
+    auto holds = [&](const View<T>& v) { return sg.c0 >= v.full0 && sg.c0 + 32 * sg.steps <= v.full0 + v.full; };
+    const bool inner = MW == 32 && nxt.base && holds(cur) && holds(nxt);
 
     // ------------------------------------------------ pass 1: the sum outside K of 2^(c x + shift).  A lane's shift comes from the warp's first elements, and moves where
     // elements lie MARGIN above it (with the first ones masked, say)
@@ -574,8 +568,8 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
       auto ahead_of = [&](int step) {
         if (BWD && ahead && (lane & 7) == 0 && sg.c0 + lane + 32 * step < nxt.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(nxt.base + (int64_t)(sg.c0 + lane + 32 * step) * 16));
       };
-      auto leave_out = [&](uint4& w0, uint4& w1, int step) {      // listed elements
-        each_listed<El::STEP_LOG>(mine, n_mine, step, lane, [&](int e, int j) {
+      auto leave_out = [&](auto steps, uint4& w0, uint4& w1, int step) {      // listed elements
+        each_listed<steps.value, El::STEP_LOG>(mine, n_mine, step, lane, [&](int e, int j) {
           if (lane == (e >> El::LOG & 31)) {
             const bool second = e >> El::STEP_LOG;
             sh.x[j] = El::get(second ? w1 : w0, e & (E - 1));
@@ -599,25 +593,24 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
       };
       auto two = [&](uint4 w0, uint4 w1, int step) {
         ahead_of(step); ahead_of(step + 1);
-        if (bits & 3ull) leave_out(w0, w1, step);
+        if (bits & 3ull) leave_out(Two{}, w0, w1, step);
         bits >>= 2;
         if (El::above(w0, w1, limit)) move(fmaxf(El::top(w0), El::top(w1)));
         add(w0); add(w1);
       };
       auto one = [&](uint4 w, int step) {
         ahead_of(step);
-        if (bits & 1ull) leave_out(w, w, step);
+        if (bits & 1ull) leave_out(One{}, w, w, step);
         bits >>= 1;
         if (El::above(w, w, limit)) move(El::top(w));
         add(w);
       };
-      if (inner) {
-        const Source<T, true> c(cur, V, sg.c0 + lane), n(nxt, V, sg.c0 + lane);
+      auto pass = [&](auto in) {
+        const Source<T, in.value> c(cur, V, sg.c0, lane), n(nxt, V, sg.c0, lane);
         visit<!BWD>(sg, base, c, BWD ? c : n, pol_last, pol_first, pol_first, ring_slot, two, one);
-      } else {
-        const Source<T, false> c(cur, V, sg.c0 + lane), n(nxt, V, sg.c0 + lane);
-        visit<!BWD>(sg, base, c, BWD ? c : n, pol_last, pol_first, pol_first, ring_slot, two, one);
-      }
+      };
+      if (inner) pass(std::bool_constant<MW == 32>{});
+      else pass(std::false_type{});
       shift = kk.x;
     }
     __syncwarp();
@@ -736,8 +729,8 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
         if constexpr (E == 8) return make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[1].x, v[1].y), pack_bf16x2(v[2].x, v[2].y), pack_bf16x2(v[3].x, v[3].y));
         else return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
       };
-      auto put_listed = [&](uint4& g0, uint4& g1, int step) {
-        each_listed<El::STEP_LOG>(mine, n_mine, step, lane, [&](int e, int j) {
+      auto put_listed = [&](auto steps, uint4& g0, uint4& g1, int step) {
+        each_listed<steps.value, El::STEP_LOG>(mine, n_mine, step, lane, [&](int e, int j) {
           if (lane == (e >> El::LOG & 31)) {
             const float x = sh.g[j];
             if (e >> El::STEP_LOG) El::put(g1, e & (E - 1), x);
@@ -745,13 +738,23 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
           }
         });
       };
-      auto pass = [&](auto&& store, const auto& c, const auto& n) {
+      auto pass = [&](auto in) {
+        const Source<T, in.value> c(cur, V, sg.c0, lane), n(nxt, V, sg.c0, lane);
+        char* const to = g_base + (int64_t)c.c0 * 16;
+        auto store = [&](const uint4& g, int step) {
+          const int p = c.c0 + 32 * step;
+          if (in.value || (alike && (c.whole(step) || (unsigned)(p - cur.full0) < (unsigned)cur.full))) st_stream(to + (uint32_t)step * 512u, g, pol_first);
+          else if (p < cur.n)
+#pragma unroll 1
+            for (int e = 0; e < E; ++e)
+              if ((unsigned)(p * E + e - cur.head) < (unsigned)V) st_from_float(g_row, p * E + e - cur.head, El::get(g, e));
+        };
         visit<true>(sg, base, c, n, pol_first, pol_last, pol_first, ring_slot,
           [&](const uint4& w0, const uint4& w1, int step) {
             uint4 g0 = make_uint4(0u, 0u, 0u, 0u), g1 = g0;
             if (!zero) {
               g0 = plain(w0); g1 = plain(w1);
-              if (bits & 3ull) put_listed(g0, g1, step);
+              if (bits & 3ull) put_listed(Two{}, g0, g1, step);
             }
             bits >>= 2;
             store(g0, step); store(g1, step + 1);
@@ -760,23 +763,14 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
             uint4 g = make_uint4(0u, 0u, 0u, 0u);
             if (!zero) {
               g = plain(w);
-              if (bits & 1ull) put_listed(g, g, step);
+              if (bits & 1ull) put_listed(One{}, g, g, step);
             }
             bits >>= 1;
             store(g, step);
           });
       };
-      if (inner && alike) {
-        char* const to = g_base + (int64_t)(sg.c0 + lane) * 16;
-        pass([&](const uint4& g, int step) { st_stream(to + (uint32_t)step * 512u, g, pol_first); }, Source<T, true>(cur, V, sg.c0 + lane), Source<T, true>(nxt, V, sg.c0 + lane));
-      } else
-        pass([&](const uint4& g, int step) {
-          const int c = sg.c0 + lane + 32 * step;
-          if (alike && (unsigned)(c - cur.full0) < (unsigned)cur.full) st_stream(g_base + (uint32_t)c * 16u, g, pol_first);
-          else if (c < cur.n)
-            for (int e = 0; e < E; ++e)
-              if ((unsigned)(c * E + e - cur.head) < (unsigned)V) st_from_float(g_row, c * E + e - cur.head, El::get(g, e));
-        }, Source<T, false>(cur, V, sg.c0 + lane), Source<T, false>(nxt, V, sg.c0 + lane));
+      if (inner && alike) pass(std::bool_constant<MW == 32>{});
+      else pass(std::false_type{});
     }
     cur = nxt;
     b = next_b;
@@ -803,14 +797,14 @@ template <typename T, int MW, bool BWD> cudaError_t launch_stream_as(const Disti
   return launch_pdl(distill_stream_kernel<T, MW, BWD>, dim3((unsigned)grid), MW * 32, smem, st, true, p);
 }
 template <typename T, int MW> cudaError_t launch_with(const DistillParams& p, cudaStream_t st) { return p.dlogits ? launch_stream_as<T, MW, true>(p, st) : launch_stream_as<T, MW, false>(p, st); }
-// Warps to a row: as few as keep it in shared memory (several blocks on an SM: one's barriers under another's passes), all 32 where none do; more where there are no more rows than blocks.
+// Warps to a row: as few as keep it in shared memory (several blocks on an SM: one's barriers under another's passes), all 32 where none do; 16 where there are no more rows than blocks.
 // (2960 bf16 rows with lists of 32, us: 2048 entries 52 with 4 warps, 70 with 16, 122 with 32; 16384 92 with 8, 100, 125; 32003 156 with 16, 174; 65536, which 16 do not
 // keep, 230 and 198; float32 rows of 32003, which they do not keep either, 214 and 193.)
 template <typename T> cudaError_t launch_stream(const DistillParams& p, cudaStream_t st, int sms) {
   const int64_t bytes = ((int64_t)p.in.V + 2 * Elem<T>::E) * (int64_t)sizeof(T), N = p.in.N;
   if (bytes <= 4 * KEEP * 512 && N > sms * BLOCKS<8>) return launch_with<T, 4>(p, st);
   if (bytes <= 8 * KEEP * 512 && N > sms * BLOCKS<16>) return launch_with<T, 8>(p, st);
-  if (bytes <= 16 * KEEP * 512 && N > sms) return launch_with<T, 16>(p, st);
+  if (bytes <= 16 * KEEP * 512) return launch_with<T, 16>(p, st);
   return launch_with<T, 32>(p, st);
 }
 

@@ -695,9 +695,9 @@ Layout layout(int64_t N, int d, int V, bool backward) {
   const int tiles = (l.n_tiles + l.pieces - 1) / l.pieces;
   l.pieces = (l.n_tiles + tiles - 1) / tiles;
   l.piece = tiles * TILE;
-  // few rows: the sums over the vocabulary are cut so that there is a tile for every pair of SMs, no part below 16 blocks of K
+  // few rows: the sums over the vocabulary are cut so that there is a tile for nearly every pair of SMs and no more, no part below 16 blocks of K
   const int64_t dh_tiles = l.rows / TILE * l.d_tiles;
-  l.splits = (int)std::max<int64_t>(1, std::min<int64_t>((74 + dh_tiles - 1) / dh_tiles, l.piece / BK / 16));
+  l.splits = (int)std::max<int64_t>(1, std::min<int64_t>(74 / dh_tiles, l.piece / BK / 16));
   int64_t at = up((int64_t)sizeof(Head), 256);
   auto take = [&](int64_t bytes) { const int64_t a = at; at += up(bytes, 256); return a; };
   l.rank = take(N * 4); l.tok = take(l.rows * 4); l.coef = take(l.rows * 4); l.lse2 = take(l.rows * 4);
