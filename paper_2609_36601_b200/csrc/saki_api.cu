@@ -889,7 +889,8 @@ static int linear_check(const saki_linear_in* in) {
   if (in->N == 0) return SAKI_OK;
   if (!in->hidden || !in->weight || !in->target) return fail(SAKI_ERR_INVALID_ARG, "NULL hidden, weight or target pointer");
   if (in->corrected && !in->teacher_top1) return fail(SAKI_ERR_INVALID_ARG, "teacher_top1 is required with corrected");
-  if (!aligned(in->weight, 16) || in->ld_w % 8 || in->d % 8) return fail(SAKI_ERR_UNSUPPORTED, "weight must be 16-byte aligned, its row stride and d multiples of 8");
+  if (!aligned(in->weight, 16) || in->ld_w % 8 || in->d % 8 || !aligned(in->hidden, 2))
+    return fail(SAKI_ERR_UNSUPPORTED, "weight must be 16-byte aligned, its row stride and d multiples of 8, hidden start at a whole element");
   return SAKI_OK;
 }
 static int linear_scratch(const saki_linear_in* in, const void* scratch, int64_t bytes, bool backward) {

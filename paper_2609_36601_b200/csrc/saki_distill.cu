@@ -12,6 +12,8 @@
 //                           ring (its second touch comes from L2); while a row's gradient is written the slots take the next row.  A warp knows from a word of bits
 //                           at which of its steps there are listed tokens, and looks for them only there.
 //   distill_general_kernel  float64, any layout, a block a row: for what the other cannot serve, and the rows that it cannot resolve (row list).
+// What bounds it: 4096 bf16 rows of 151936 with lists of 64, 544 us where the bytes take 380 (70 %; lists of 1: 500, of 128: 590): instructions (63 % of the issue slots are filled, 62 % of the
+// special-function pipe) and the two block barriers of a row, at which warps wait a fifth of their time.  float32 rows of 151936 run at 81 % of the copy rate.
 #include "saki_device.cuh"
 #include <algorithm>
 #include <mutex>

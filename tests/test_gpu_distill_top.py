@@ -218,6 +218,13 @@ def test_strides_and_alignment(dtype):
     assert empty["loss"].numel() == 0 and ge.shape == (0, V)
 
 
+@pytest.mark.parametrize("reverse", [False, True])
+def test_rows_too_long_for_the_streaming_kernel(reverse):
+    N, V = 3, 300001
+    s, token, logit, t, _ = _inputs(N, V, 40, F32, 10)
+    _check(s, token, logit, torch.logsumexp(t, 1), reverse, kernel=1)
+
+
 def test_offsets_beyond_32_bits():
     V, N = 151936, 5
     s = torch.empty(4 * 5_000_000_00 + V, dtype=BF16, device=DEV).as_strided((N, V), (500_000_000, 1))

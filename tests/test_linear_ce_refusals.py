@@ -45,7 +45,7 @@ def test_refused_backward(other):
     assert _bwd(**other) == 1 and P.last_error()
 
 
-@pytest.mark.parametrize("other", [dict(weight=ONE + 8), dict(ld_w=68), dict(d=60), dict(scratch=ONE + 128)])
+@pytest.mark.parametrize("other", [dict(weight=ONE + 8), dict(ld_w=68), dict(d=60), dict(hidden=ONE + 1), dict(scratch=ONE + 128)])
 def test_alignment(other):
     assert _fwd(**other) == 2 and P.last_error()
     assert _bwd(**other) == 2 and P.last_error()
