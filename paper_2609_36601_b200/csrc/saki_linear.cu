@@ -71,7 +71,7 @@ struct Tiles {
   // logits of columns [v0, v0 + 256 l_tiles): their sums, or G
   int l_tiles, v0;
   float c;                            // log2(e) / temperature
-  float2* part;                       // forward: [rows][n_tiles] (maximum, sum) in base 2
+  float2* part;                       // forward: [rows][n_tiles] (largest product, sum of 2^(c (product - it)))
   float* z_tok;                       // forward: the supervised token's product
   int n_tiles;
   const int* tok;
@@ -179,7 +179,7 @@ __device__ __forceinline__ bool any_failed(const Head* h) {      // all threads 
 }
 
 // forward, a warp a row: the tiles' sums become the row's log-sum-exp and loss
-__global__ void __launch_bounds__(256) loss_kernel(const Rows P, const saki_linear_out out, const float2* part, const float* z_tok, int n_tiles, float rtau, unsigned long long* flagged) {
+__global__ void __launch_bounds__(256) loss_kernel(const Rows P, const saki_linear_out out, const float2* part, const float* z_tok, int n_tiles, float c, unsigned long long* flagged) {
   launch_dependents();
   wait_for_predecessor();
   const bool failed = any_failed(P.head);
@@ -188,6 +188,7 @@ __global__ void __launch_bounds__(256) loss_kernel(const Rows P, const saki_line
   if (row >= P.in.N) return;
   const Row m = row_of(P, row);
   uint32_t status = m.status;
+  const double rtau = 1.0 / (double)P.in.temperature;
   float loss = 0.f, logp = 0.f, lse = 0.f;
   if (m.tok >= 0) {
     const int64_t at = P.rank[row];
@@ -201,10 +202,11 @@ __global__ void __launch_bounds__(256) loss_kernel(const Rows P, const saki_line
     double s = 0.0;
     for (int t = lane; t < n_tiles; t += 32) {
       const float2 a = pp[t];
-      if (a.x > -CUDART_INF_F) s += (double)(a.y * ex2f(a.x - mx));
+      if (a.x > -CUDART_INF_F) s += (double)(a.y * ex2f((a.x - mx) * c));
     }
     s = warp_sum(s);
-    const double l = ((double)mx + log2(s)) * LN2, lp = (double)z_tok[at] * (double)rtau - l;
+    // (both from the largest product: a log-probability next to 0 is no difference of large numbers)
+    const double ls = log2(s) * LN2, l = (double)mx * rtau + ls, lp = ((double)z_tok[at] - (double)mx) * rtau - ls;
     loss = (float)(-(double)m.coef * lp); logp = (float)lp; lse = (float)l;
     if (failed) status = SAKI_ROW_TIMEOUT;
     else if (nan || !(fabsf(lse) < CUDART_INF_F) || !(fabsf(logp) < CUDART_INF_F)) status = SAKI_ROW_NONFINITE;
@@ -566,7 +568,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
             s += (a0.x + a0.y) + (a1.x + a1.y);
           }
           if (there) {
-            P.part[(int64_t)row * P.n_tiles + x.n] = make_float2(m * P.c, s);
+            P.part[(int64_t)row * P.n_tiles + x.n] = make_float2(m, s);
             if ((unsigned)(tok - col_tile) < (unsigned)TILE) P.z_tok[row] = z;
           }
         } else {
@@ -780,8 +782,7 @@ cudaError_t launch_linear_fwd(const saki_linear_in& in, const saki_linear_out& o
   e = launch_pdl_cluster(tiles_kernel, dim3((unsigned)(2 * std::min<int64_t>(pairs, tiles))), THREADS, 2, SMEM, st, maps, t);
   if (e != cudaSuccess) return e;
   *n_launches = 3;
-  return launch_pdl(loss_kernel, dim3((unsigned)((in.N + 7) / 8)), 256, 0, st, true, r, out, (const float2*)t.part, (const float*)t.z_tok, l.n_tiles,
-                    (float)(1.0 / (double)in.temperature), flagged);
+  return launch_pdl(loss_kernel, dim3((unsigned)((in.N + 7) / 8)), 256, 0, st, true, r, out, (const float2*)t.part, (const float*)t.z_tok, l.n_tiles, t.c, flagged);
 }
 
 cudaError_t launch_linear_bwd(const saki_linear_in& in, const float* lse, void* dhidden, int64_t ld_dh, void* dweight, int64_t ld_dw, float grad_scale, void* scratch,

@@ -168,6 +168,24 @@ def test_pieces_and_parts(N, d, V, rows):
     assert bool(((dw.double() - want).abs() <= (2.0 ** -8 + N * 2.0 ** -23 + 2 * z_err) * mag + 2.0 ** -8 * want.abs()).all())
 
 
+def test_losses_next_to_zero():
+    """Confident rows with logits of hundreds: the loss comes from differences to the largest logit.  What is left is the sum of a row, 1 and little more: at most some 18 additions to
+    the 1 in float32, 2^-24 each, and the exponentials' own share of what the others have."""
+    N, d, V = 300, 64, 5000
+    g = torch.Generator(device=DEV).manual_seed(30)
+    w = (2.0 / d ** 0.5 * torch.randn((V, d), generator=g, device=DEV)).to(BF16)
+    target = torch.randint(0, V, (N,), generator=g, device=DEV, dtype=torch.int32)
+    h = (torch.linspace(5, 100, N, device=DEV)[:, None] * w[target.long()].float()).to(BF16)
+    out = P.linear_ce(h, w, target)
+    z = h.double() @ w.double().t()
+    top = z.gather(1, target.long()[:, None])
+    others = torch.exp(z - top).scatter_(1, target.long()[:, None], 0.0).sum(1)
+    assert float(top.max()) > 300 and bool((z.amax(1, keepdim=True) == top).all())
+    z_err = (d + 4) * 2.0 ** -23 * (h.double().abs() @ w.double().abs().t()).amax(1) + 4e-6
+    want = torch.log1p(others)
+    assert bool(((out["loss"].double() - want).abs() <= 18 * 2.0 ** -24 + 2 * z_err * others).all())
+
+
 def test_the_gradient_against_differences():
     """Central differences of the loss (float64 sum of the float32 losses) in random directions of bf16 steps."""
     N, d, V = 64, 64, 500
