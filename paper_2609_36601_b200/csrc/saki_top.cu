@@ -460,9 +460,11 @@ constexpr int MAX_SMS = 256;
 // Slices as long as the keys' room; shorter ones for few rows, so that there are two blocks for every SM, of 256 pieces (one a thread) at the least and MIN_SLICES at the most.
 Cut cut(int64_t rows, int V, int dtype, int sms) {
   const int e = dtype == SAKI_BF16 ? 8 : 4, all = (V + 2 * e - 2) / e;
-  // float32: four pieces to a key keep more bytes on their way, two leave room for six blocks on an SM (2960 rows, 64 best: of 2048 32 and 27 us, of 16384 54 and 53, of 32003 85 and 88, of
-  // 65536 142 and 159)
-  const int group = dtype == SAKI_BF16 || V <= 20480 ? 2 : 4, longest = MAX_ENTRIES * group;
+  // float32: four pieces to a key keep more bytes on their way, two leave room for six blocks on an SM, not five (2960 rows, 64 best: of 2048 32 and 27 us, of 16384 54 and 53, of 32003 84 and 88, of
+  // 65536 142 and 150).  Rows of up to 65536 take two where that is a round of blocks less (1500 rows of 32003 52 and 48, 760 of 65536 53 and 43, 1700 92 and 85; longer rows gain too
+  // little by it: 1500 of 100000 124 and 132).
+  auto rounds = [&](int blocks) { return (rows + (int64_t)blocks * sms - 1) / ((int64_t)blocks * sms); };
+  const int group = dtype == SAKI_BF16 || V <= 20480 || (V <= 65536 && rounds(6) < rounds(5)) ? 2 : 4, longest = MAX_ENTRIES * group;
   const int need = (all + longest - 1) / longest;
   int64_t want = (2 * (int64_t)std::min(sms, MAX_SMS) + rows - 1) / std::max<int64_t>(rows, 1);
   want = std::max<int64_t>(need, std::min<int64_t>({want, (int64_t)std::max(MIN_SLICES, need), (int64_t)std::max(1, all / TT)}));

@@ -43,6 +43,14 @@ def test_matches_the_oracle(N, V, k, tau, dtype):
     _check(_logits(N, V, dtype, N + V + k), k, tau, rows)
 
 
+@pytest.mark.parametrize("V", [20481, 32003, 65536, 65537])
+@pytest.mark.parametrize("N", [740, 800, 1500])
+def test_float32_rows_about_whole_rounds_of_blocks(N, V):
+    x = _logits(N, V, F32, N + V)
+    x[1], x[2, ::3] = torch.linspace(-8, 8, V, device=DEV), -float("inf")      # all that is best in a stretch; masks
+    _check(x, 100, rows=[0, 1, 2, N // 2, N - 1])
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_many_long_rows(dtype):
     x = _logits(600, 163840, dtype, 1)        # the longest that one block takes whole
