@@ -168,6 +168,50 @@ def test_pieces_and_parts(N, d, V, rows):
     assert bool(((dw.double() - want).abs() <= (2.0 ** -8 + N * 2.0 ** -23 + 2 * z_err) * mag + 2.0 ** -8 * want.abs()).all())
 
 
+@pytest.mark.parametrize("N,d,V", [((1 << 20) + 100, 2112, 300), (40, 2112, (1 << 20) + 77)])
+def test_offsets_beyond_32_bits(N, d, V):
+    """Hidden states, or weights, of more than 2^32 bytes: all of the loss and of both gradients against float64 products on the GPU, in blocks."""
+    h, w, target, g = _inputs(N, d, V, 31)
+    out = P.linear_ce(h, w, target)
+    dh, dw = P.linear_ce_bwd(h, w, target, out["lse"])
+    rows, cols = 1 << 14, 1 << 14
+    z_err = 0.0
+    for i in range(0, N, rows):
+        hi = h[i:i + rows].double()
+        yi = target[i:i + rows].long()
+        lse = torch.full((hi.shape[0],), -float("inf"), dtype=torch.float64, device=DEV)
+        for j in range(0, V, cols):
+            wj = w[j:j + cols].double()
+            lse = torch.logaddexp(lse, torch.logsumexp(hi @ wj.t(), 1))
+            z_err = max(z_err, (d + 4) * 2.0 ** -23 * float((hi.abs() @ wj.abs().t()).max()) + 4e-6)
+        tol = 2 * z_err + 2.0 ** -22 * 2 * float(lse.abs().max())
+        z_tok = (hi * w[yi].double()).sum(1)
+        assert float((out["loss"][i:i + rows].double() - (lse - z_tok)).abs().max()) <= tol
+        want, mag = torch.zeros_like(hi), torch.zeros_like(hi)
+        if i == 0 and N > rows:
+            dw_want, dw_mag = ([torch.zeros((min(cols, V - j), d), dtype=torch.float64, device=DEV) for j in range(0, V, cols)] for _ in range(2))
+        for b, j in enumerate(range(0, V, cols)):
+            wj = w[j:j + cols].double()
+            G = torch.exp(hi @ wj.t() - lse[:, None])
+            here = (yi >= j) & (yi < j + wj.shape[0])
+            p_tok = torch.exp(z_tok - lse)
+            G[here.nonzero()[:, 0], yi[here] - j] -= 1.0
+            a = G.abs()
+            a[here.nonzero()[:, 0], yi[here] - j] += p_tok[here] * 2 * tol / 2.0 ** -8      # (pi - 1 is off by a share of pi)
+            want += G @ wj
+            mag += a @ wj.abs()
+            if N <= rows:                     # (one block of rows: there and then)
+                x, m = G.t() @ hi, a.t() @ hi.abs()
+                assert bool(((dw[j:j + cols].double() - x).abs() <= (2.0 ** -8 + N * 2.0 ** -23 + 2 * tol) * m + 2.0 ** -8 * x.abs() + 1e-30).all()), j
+            else:
+                dw_want[b] += G.t() @ hi
+                dw_mag[b] += a.t() @ hi.abs()
+        assert bool(((dh[i:i + rows].double() - want).abs() <= (2.0 ** -8 + V * 2.0 ** -23 + 2 * tol) * mag + 2.0 ** -8 * want.abs()).all()), i
+    if N > rows:
+        for b, j in enumerate(range(0, V, cols)):
+            assert bool(((dw[j:j + cols].double() - dw_want[b]).abs() <= (2.0 ** -8 + N * 2.0 ** -23 + 2 * tol) * dw_mag[b] + 2.0 ** -8 * dw_want[b].abs()).all())
+
+
 def test_losses_next_to_zero():
     """Confident rows with logits of hundreds: the loss comes from differences to the largest logit.  What is left is the sum of a row, 1 and little more: at most some 18 additions to
     the 1 in float32, 2^-24 each, and the exponentials' own share of what the others have."""
