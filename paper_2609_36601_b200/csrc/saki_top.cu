@@ -7,7 +7,7 @@
 // of them are equal, too, the best are taken one by one, each thread offering its best that is left.
 // Slices of a row are joined by a second kernel.
 //
-// What bounds it: 4096 bf16 rows of 151936, 64 best, 236 us where the bytes take 190 (81 %): the special-function pipe at 60 % in the pass, and a row's tail (bar, second reading, ranks: some 5 us that other
+// What bounds it: 4096 bf16 rows of 151936, 64 best, 234 to 245 us (by card) where the bytes take 190 (80 %): the special-function pipe at 60 % in the pass, and a row's tail (bar, second reading, ranks: some 5 us that other
 // blocks of the SM cover in part).  float32 rows of 151936: 95 %.  2960 rows of 2048: 30 us, all tails.  8 rows: 13 us, two launches and the two tails' chains.
 #include "saki_device.cuh"
 #include <algorithm>
