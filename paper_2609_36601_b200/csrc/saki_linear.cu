@@ -610,7 +610,8 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
         }
       } else if (x.kind == KIND_DH) {
         const int y0 = x.split * P.rows + row - lane;
-        if (row - lane < plan.count) {             // (rows of the warp)
+        // (rows of the warp; a part of a short last piece may be empty: nothing was summed, nothing is added.  The first piece, which stores, has 13 blocks a part at the least)
+        if (x.k0 < x.k1 && row - lane < plan.count) {
 #pragma unroll 1
           for (int ch = 0; ch < TILE / 32; ++ch) {
             if (x.n * TILE + ch * 32 >= P.d) break;
