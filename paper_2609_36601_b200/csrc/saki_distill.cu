@@ -649,8 +649,9 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
       const double ks = sh.red[1][wl];
       const double kr = (double)warp_least(part ? (float)ks : CUDART_INF_F);
       const double f = part ? pow2_exact((int)fmax(kr - ks, -1000.0)) : 0;
-      // (a warp whose share is nothing beside the others' may have an infinite one; a NaN among the listed ones counts everywhere)
-      double out = f > 0 ? sh.red[0][wl] * f : 0, in = f > 0 ? sh.red[2][wl] * f : part && sh.red[2][wl] != sh.red[2][wl] ? CUDART_NAN : 0;
+      // (a warp whose share is nothing beside the others' may have an infinite one; a NaN counts everywhere)
+      auto share = [&](double x) { return f > 0 ? x * f : part && x != x ? CUDART_NAN : 0.0; };
+      double out = share(sh.red[0][wl]), in = share(sh.red[2][wl]);
       double sum_cross = part ? sh.red[3][wl] * (reverse ? f : 1.0) : 0;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) {
