@@ -442,7 +442,7 @@ template <int MW> struct StreamShared {
   ListRow list[3];             // of three rows in turn: written while a warp may still read the one before last
   int id[3][KMAX];
   float2 w[3][KMAX];
-  float x[KMAX], g[KMAX];      // listed elements and their gradients: of the warp that has them
+  float x[2][KMAX], g[KMAX];   // listed elements, by row parity (a warp may write the next row's while another still reads this one's), and their gradients: of the warp that has them
   uint32_t mine[MW][KMAX];     // by warp: what lies in its segment, place in elements << 8 | place in the list
 };
 template <int MW> constexpr int stream_smem = MW * KEEP * 512 + (int)sizeof(StreamShared<MW>);
@@ -574,7 +574,7 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
         each_listed<steps.value, El::STEP_LOG>(mine, n_mine, step, lane, [&](int e, int j) {
           if (lane == (e >> El::LOG & 31)) {
             const bool second = e >> El::STEP_LOG;
-            sh.x[j] = El::get(second ? w1 : w0, e & (E - 1));
+            sh.x[parity][j] = El::get(second ? w1 : w0, e & (E - 1));
             if (second) El::put(w1, e & (E - 1), -CUDART_INF_F);
             else El::put(w0, e & (E - 1), -CUDART_INF_F);
           }
@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
     float warp_shift = shift;
 #pragma unroll 1
     for (int i = lane; i < n_mine; i += 32)      // (a segment may have nothing but listed elements and masked ones)
-      warp_shift = fminf(warp_shift, -ceilf(c32 * fminf(sh.x[mine[i] & 255u], 1e30f)));
+      warp_shift = fminf(warp_shift, -ceilf(c32 * fminf(sh.x[parity][mine[i] & 255u], 1e30f)));
     __syncwarp();
     warp_shift = warp_least(warp_shift);
     double outside = (((double)S0.x + (double)S0.y) + ((double)S1.x + (double)S1.y)) * (double)ex2f(fmaxf(warp_shift - shift, -200.f));
@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
 #pragma unroll 1
     for (int i = lane; i < n_mine; i += 32) {
       const int j = (int)(mine[i] & 255u);
-      const float x = sh.x[j];
+      const float x = sh.x[parity][j];
       const float2 w = sh.w[b][j];
       const float e = ex2f(fmaf(x, c32, warp_shift));
       // (a listed token that the student's row has masked, or not finite: the float64 kernel decides)
@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
 #pragma unroll 1
         for (int i = lane; i < n_mine; i += 32) {
           const int j = (int)(mine[i] & 255u);
-          const float x = sh.x[j];
+          const float x = sh.x[parity][j];
           const float2 w = sh.w[b][j];
           const float p = ex2f(fmaf(x, c32, kr)) * unit;
           const float v = reverse ? p * (float)((double)x * rtau - lse - (double)w.y - loss) : (float)(Z * (double)p - (double)w.x);
