@@ -699,7 +699,10 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
         bc[0] = grad_shift; bc[1] = scale_out; bc[2] = Zs; bc[3] = kg;
       }
     }
-    if (few_groups) copies_wait<0>();
+    if (few_groups) {
+      copies_commit();      // (a warp without a step has made no visit, which would have committed its copies of the next row's list)
+      copies_wait<0>();
+    }
     __syncthreads();
 
     // ------------------------------------------------ pass 2: the gradient
