@@ -289,6 +289,7 @@ __global__ void __launch_bounds__(TT, GROUP == 2 ? 6 : 5) top_rows_kernel(const 
         if (n >= k) lo = to;
         else hi = to - 1;
       }
+      __syncthreads();      // (all have read the counts, also where there was nothing to bisect)
       if (tid == 0) sh.groups = sh.count = 0;
       __syncthreads();
       all = collect(lo);
