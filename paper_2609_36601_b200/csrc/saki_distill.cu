@@ -266,7 +266,7 @@ constexpr float MARGIN = 60.f;                                  // in base 2: ho
 template <typename T> struct Elem;
 template <> struct Elem<__nv_bfloat16> {
   static constexpr int E = 8, LOG = 3, STEP_LOG = 8;
-  static constexpr uint32_t FILLER = 0xFF7FFF7Fu;               // two of the most negative finite value: exp -> 0
+  static constexpr uint32_t FILLER = 0xFF80FF80u;               // two of -inf: nothing at any temperature
   static __device__ __forceinline__ float2 pair(const uint4& w, int i) { return unpack_bf16x2(i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w); }
   static __device__ __forceinline__ float top(const uint4& w) {
     const float2 a = unpack_bf16x2(max_bf16x2(max_bf16x2(w.x, w.y), max_bf16x2(w.z, w.w)));
@@ -292,7 +292,7 @@ template <> struct Elem<__nv_bfloat16> {
 };
 template <> struct Elem<float> {
   static constexpr int E = 4, LOG = 2, STEP_LOG = 7;
-  static constexpr uint32_t FILLER = 0xFF7FFFFFu;
+  static constexpr uint32_t FILLER = 0xFF800000u;
   static __device__ __forceinline__ float2 pair(const uint4& w, int i) { return i == 0 ? make_float2(__uint_as_float(w.x), __uint_as_float(w.y)) : make_float2(__uint_as_float(w.z), __uint_as_float(w.w)); }
   static __device__ __forceinline__ float top(const uint4& w) { return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w))); }
   using Limit = float;
