@@ -924,7 +924,7 @@ SAKI_API int saki_linear_ce_bwd(const saki_linear_in* in, const float* lse, void
   if (rc) return rc;
   if (!dhidden && !dweight && in->N > 0) return fail(SAKI_ERR_INVALID_ARG, "NULL dhidden and dweight pointers");      // (of no rows dhidden has no memory)
   if ((dhidden && ld_dh < in->d) || (dweight && ld_dw < in->d)) return fail(SAKI_ERR_INVALID_ARG, "row stride smaller than the row");
-  if (!std::isfinite(grad_scale)) return fail(SAKI_ERR_INVALID_ARG, "grad_scale must be finite");
+  if (!std::isfinite((float)((double)grad_scale / (double)in->temperature))) return fail(SAKI_ERR_INVALID_ARG, "grad_scale and grad_scale / temperature must be finite");
   if ((dhidden && (!aligned(dhidden, 16) || ld_dh % 8)) || (dweight && (!aligned(dweight, 16) || ld_dw % 8)))
     return fail(SAKI_ERR_UNSUPPORTED, "dhidden and dweight must be 16-byte aligned, their row strides multiples of 8");
   unsigned long long* flagged = nullptr;
