@@ -692,7 +692,10 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
             kg = (float)kgd;
             lse_f = (float)lse; loss_f = (float)loss;
             sh.dc[parity][0] = lse; sh.dc[parity][1] = loss; sh.dc[parity][2] = Z;
-            write_result(P, row, loss_f, lse_f, 0u);
+            if (BWD && !(fabsf(scale_out) < CUDART_INF_F && fabsf(kg) < CUDART_INF_F)) {      // factors beyond float32, of gradients that need not be
+              P.redo_list[atomicAdd(P.redo_count, 1u)] = (int32_t)row;
+              scale_out = Zs = 0.f;
+            } else write_result(P, row, loss_f, lse_f, 0u);
           }
         } else write_result(P, row, 0.f, 0.f, list.status);
         float* const bc = sh.bc[parity];
