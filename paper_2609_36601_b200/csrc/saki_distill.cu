@@ -789,18 +789,19 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
 
 template <typename T, int MW, bool BWD> cudaError_t launch_stream_as(const DistillParams& p, cudaStream_t st) {
   static std::mutex mu;
-  static int known_dev = -1, sms = 0;
-  int dev = 0;
+  static int known_dev = -1, known = 0;
+  int dev = 0, sms = 0;
   cudaGetDevice(&dev);
   constexpr int smem = stream_smem<MW>;
   {
     std::lock_guard<std::mutex> lock(mu);
     if (known_dev != dev) {
       cudaError_t e = cudaFuncSetAttribute(distill_stream_kernel<T, MW, BWD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-      if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+      if (e == cudaSuccess) e = cudaDeviceGetAttribute(&known, cudaDevAttrMultiProcessorCount, dev);
       if (e != cudaSuccess) return e;
       known_dev = dev;
     }
+    sms = known;
   }
   const int grid = (int)std::min<int64_t>(p.in.N, (int64_t)sms * BLOCKS<MW>);
   return launch_pdl(distill_stream_kernel<T, MW, BWD>, dim3((unsigned)grid), MW * 32, smem, st, true, p);
