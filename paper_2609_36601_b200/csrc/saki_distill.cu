@@ -16,6 +16,7 @@
 // special-function pipe) and the two block barriers of a row, at which warps wait a fifth of their time.  float32 rows of 151936 run at 81 % of the copy rate.
 #include "saki_device.cuh"
 #include <algorithm>
+#include <cfloat>
 #include <mutex>
 #include <type_traits>
 
@@ -138,7 +139,7 @@ __global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams 
     float2 w = make_float2(0.f, 0.f);
     if (r * 32 < k && id[r] >= 0) {
       const double lw = t[r] - ref, e = exp(lw);
-      w = make_float2((float)e, (float)lw);
+      w = make_float2((float)e, (float)fmax(lw, -(double)FLT_MAX));      // (finite: a student's probability of 0 times it is 0)
       W += e; W32 += (double)w.x; H += e > 0 ? e * lw : 0;
     }
     if (j < k) {
@@ -721,7 +722,8 @@ __global__ void __launch_bounds__(MW * 32, BLOCKS<MW>) distill_stream_kernel(con
           const float x = sh.x[parity][j];
           const float2 w = sh.w[b][j];
           const float p = ex2f(fmaf(x, c32, kr)) * unit;
-          const float v = reverse ? p * (float)((double)x * rtau - lse - (double)w.y - loss) : (float)(Z * (double)p - (double)w.x);
+          // (p 0: of a token masked by the lowest value, say, whose log-ratio is beyond float32)
+          const float v = !reverse ? (float)(Z * (double)p - (double)w.x) : p > 0.f ? p * (float)((double)x * rtau - lse - (double)w.y - loss) : 0.f;
           sh.g[j] = zero ? 0.f : kg * v;
         }
       }
