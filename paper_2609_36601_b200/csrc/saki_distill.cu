@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams 
   const double rtau = 1.0 / (double)P.in.temperature;
   uint32_t status = 0;
   int id[KMAX / 32];
-  double t[KMAX / 32];
+  double t[KMAX / 32];                 // logits, not divided by the temperature: differences first, which float64 holds however large they are
   bool bad_id = false, bad = false;
   if (P.in.mask && P.in.mask[row] == 0) status = SAKI_ROW_MASKED;
   int n = 0;
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams 
       const float x = P.in.logit[row * P.in.ld_k + j];
       bad_id |= v < -1 || v >= P.in.V;
       if (v >= 0 && v < P.in.V && x != -CUDART_INF_F) {
-        id[r] = v; t[r] = (double)x * rtau;
+        id[r] = v; t[r] = (double)x;
         bad |= !(fabsf(x) < CUDART_INF_F);
       }
     }
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams 
 #pragma unroll
   for (int r = 0; r < KMAX / 32; ++r) bad_id |= id[r] >= 0 && same[r] > 1;
   const bool with_rest = P.in.teacher_lse != nullptr;
-  double ref = 0;
+  double top = 0, ref = 0;             // log w = (t - top) rtau - ref
   if (with_rest) {
     const float l = P.in.teacher_lse[row];
     ref = (double)l;
@@ -127,8 +127,9 @@ __global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams 
     m = warp_max(m);
 #pragma unroll
     for (int r = 0; r < KMAX / 32; ++r)
-      if (r * 32 < k && id[r] >= 0) s += exp(t[r] - m);
-    ref = n ? m + log(warp_sum(s)) : 0;
+      if (r * 32 < k && id[r] >= 0) s += exp((t[r] - m) * rtau);
+    s = warp_sum(s);
+    if (n) { top = m; ref = log(s); }
   }
   if (!status && __any_sync(0xffffffffu, bad_id)) status = SAKI_ROW_BAD_ID;
   if (!status && __any_sync(0xffffffffu, bad)) status = SAKI_ROW_NONFINITE;
@@ -138,7 +139,7 @@ __global__ void __launch_bounds__(256) distill_lists_kernel(const DistillParams 
     const int j = r * 32 + lane;
     float2 w = make_float2(0.f, 0.f);
     if (r * 32 < k && id[r] >= 0) {
-      const double lw = t[r] - ref, e = exp(lw);
+      const double lw = (t[r] - top) * rtau - ref, e = exp(lw);
       w = make_float2((float)e, (float)fmax(lw, -(double)FLT_MAX));      // (finite: a student's probability of 0 times it is 0)
       W += e; W32 += (double)w.x; H += e > 0 ? e * lw : 0;
     }
@@ -203,14 +204,15 @@ __global__ void __launch_bounds__(DG_THREADS) distill_general_kernel(const Disti
         if (sh.id[j] == v) return j;
       return -1;
     };
+    // (largest logits and differences to them before the temperature: log-probabilities of rows of 1e30 or the lowest value, masked throughout, are no differences of their own rounding)
     double in_max = -CUDART_INF, out_max = -CUDART_INF, bad = 0;
     if (!status) {
       for (int v = threadIdx.x; v < V; v += DG_THREADS) {
-        const double z = (double)ld_as_float(s, v) * rtau;
+        const double x = (double)ld_as_float(s, v);
         const bool listed = place(v) >= 0;
-        if (!(z < CUDART_INF) || (listed && !(z > -CUDART_INF))) bad = 1;
-        if (listed) in_max = fmax(in_max, z);
-        else out_max = fmax(out_max, z);
+        if (!(x < CUDART_INF) || (listed && !(x > -CUDART_INF))) bad = 1;
+        if (listed) in_max = fmax(in_max, x);
+        else out_max = fmax(out_max, x);
       }
       bad = block_fold(bad, sh.sum, true);
       in_max = block_fold(in_max, sh.sum, true);
@@ -224,15 +226,16 @@ __global__ void __launch_bounds__(DG_THREADS) distill_general_kernel(const Disti
     }
     double in_sum = 0, out_sum = 0;
     for (int v = threadIdx.x; v < V; v += DG_THREADS) {
-      const double z = (double)ld_as_float(s, v) * rtau;
-      if (place(v) >= 0) in_sum += exp(z - in_max);
-      else if (z > -CUDART_INF) out_sum += exp(z - out_max);
+      const double x = (double)ld_as_float(s, v);
+      if (place(v) >= 0) in_sum += exp((x - in_max) * rtau);
+      else if (x > -CUDART_INF) out_sum += exp((x - out_max) * rtau);
     }
     in_sum = block_fold(in_sum, sh.sum, false);
     out_sum = block_fold(out_sum, sh.sum, false);
     const double top = fmax(in_max, out_max);
-    const double lse = top + log((in_sum > 0 ? in_sum * exp(in_max - top) : 0) + (out_sum > 0 ? out_sum * exp(out_max - top) : 0));
-    double lS = out_sum > 0 ? out_max + log(out_sum) - lse : -CUDART_INF;
+    const double log_sum = log((in_sum > 0 ? in_sum * exp((in_max - top) * rtau) : 0) + (out_sum > 0 ? out_sum * exp((out_max - top) * rtau) : 0)), lse = top * rtau + log_sum;
+    auto log_pi = [&](int v) { return ((double)ld_as_float(s, v) - top) * rtau - log_sum; };
+    double lS = out_sum > 0 ? (out_max - top) * rtau + log(out_sum) - log_sum : -CUDART_INF;
     const bool rest = list.R > 0 && lS > LEAST_LOG_S;
     if (!rest) lS = 0;
     const double S = rest ? exp(lS) : 0;
@@ -240,7 +243,7 @@ __global__ void __launch_bounds__(DG_THREADS) distill_general_kernel(const Disti
     for (int j = threadIdx.x; j < k; j += DG_THREADS) {
       const int v = sh.id[j];
       if (v < 0) continue;
-      const double lp = (double)ld_as_float(s, v) * rtau - lse;
+      const double lp = log_pi(v);
       loss += P.in.reverse ? exp(lp) * (lp - sh.lw[j]) : (double)sh.w[j] * (sh.lw[j] - lp);
     }
     loss = block_fold(loss, sh.sum, false);
@@ -250,7 +253,7 @@ __global__ void __launch_bounds__(DG_THREADS) distill_general_kernel(const Disti
     const double kg = (double)P.grad_scale * rtau, Z = list.W + (rest ? list.R : 0);
     const double outside = P.in.reverse ? (rest ? lS - list.log_R : 0) - loss : Z - (rest ? exp(list.log_R - lS) : 0);
     for (int v = threadIdx.x; v < V; v += DG_THREADS) {
-      const double lp = (double)ld_as_float(s, v) * rtau - lse, p = exp(lp);
+      const double lp = log_pi(v), p = exp(lp);
       const int j = place(v);
       double x = outside * p;
       if (j >= 0) x = P.in.reverse ? p * (lp - sh.lw[j] - loss) : Z * p - (double)sh.w[j];
