@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(TT, GROUP == 2 ? 6 : 5) top_rows_kernel(const 
     sh.key[i * TT + tid] = (uint16_t)key;
     mine = max(mine, key);
     if (top > limit) {                 // a new shift; sums so far go along
-      const float to = -ceilf(fminf(P.c * fmaxf(top, -1e8f), 3e38f)), f = ex2f(fmaxf(to - shift, -200.f));
+      const float to = -ceilf(fminf(fmaxf(P.c * top, -1e8f), 3e38f)), f = ex2f(fmaxf(to - shift, -200.f));
       if (limit > -CUDART_INF_F) { S0 = fmul2(S0, splat(f)); S1 = fmul2(S1, splat(f)); }
       shift = to;
       limit = (MARGIN - shift) / P.c;
