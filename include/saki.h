@@ -412,7 +412,7 @@ SAKI_API int saki_linear_ce_fwd(const saki_linear_in* in, const saki_linear_out*
  * (either may be NULL: not wanted; what is given is overwritten).  `in` is that of the forward call, `lse` what it returned: rows without a finite
  * one, and those that contribute nothing, have zero rows in dhidden and no part in dweight.  The logits are computed once more, in
  * pieces of the vocabulary; a piece's G / (grad_scale / temperature) is rounded to bf16 (half a step of each element) and its products are summed in float32.
- * The probabilities are taken with the float32 log-sum-exp: its rounding, 2^-24 |lse|, is a share of each of them.  dhidden, dweight 16-byte aligned,
+ * The probabilities are taken with the float32 log-sum-exp: its roundings, to float32 and there to base 2, 2^-23 |lse| together at the most, are a share of each of them.  dhidden, dweight 16-byte aligned,
  * strides multiples of 8.  grad_scale / temperature is finite as a float32.  Where a bounded wait ran out both are NaN throughout. */
 SAKI_API int saki_linear_ce_bwd(const saki_linear_in* in, const float* lse, void* dhidden, int64_t ld_dh, void* dweight, int64_t ld_dw, float grad_scale,
                                 void* scratch, int64_t scratch_bytes, void* cuda_stream);

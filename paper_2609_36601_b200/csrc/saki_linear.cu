@@ -58,6 +58,7 @@ struct Rows {                         // the call's rows, and what is gathered o
   int* tok;                           // by place
   float* coef;
   float* lse2;                        // log-sum-exp in base 2 (backward)
+  double to_base2;                    // log2(e), as far as the factor of the products is off as a float32: c product - lse2 is a difference then, of which that is a share
   __nv_bfloat16* h;                   // [rows, padded to whole tiles][ld]: rows start on 128-byte boundaries
   int ld;
   int vec;                            // rows of `hidden` start at 16-byte boundaries
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(GT) gather_kernel(const Rows P, int per_block)
     if (at >= 0) {
       P.tok[at] = m.tok;
       P.coef[at] = m.coef;
-      if (P.lse) P.lse2[at] = (float)((double)P.lse[row] * INV_LN2);
+      if (P.lse) P.lse2[at] = (float)((double)P.lse[row] * P.to_base2);
     }
     __syncthreads();
     const int rows = (int)min((int64_t)GT, r1 - c0);
@@ -736,24 +737,26 @@ cudaError_t launch_gather(const Rows& r, int sms, cudaStream_t st) {
   return launch_pdl(gather_kernel, dim3((unsigned)((r.in.N + per - 1) / per)), GT, 0, st, true, r, per);
 }
 
+// The tensor cores cut where float32 units round: a sum that takes n additions of 16 products ends n 2^-26 of itself nearer to 0, on average.  So it was measured, for sums of dense rows of
+// 256 to 8192 features and logits of 0.5 to 20 (with 0.75 and 1.25 times as much made up for, something is left in all of them); sums that need no rounding, of sparse rows say, come out that much too
+// large, which is what all others would lack.  (Losses of 2560 features against 64 bits: 1.5e-6 without it, 4.3e-7 with; float32 units 4.4e-7.)
+double one_over_tau(const saki_linear_in& in) { return (1.0 + (in.d + 15) / 16 * 0x1p-26) / (double)in.temperature; }
+float factor(const saki_linear_in& in) { return (float)(INV_LN2 * one_over_tau(in)); }      // of the products
+
 Rows rows_of(const saki_linear_in& in, const float* lse, char* s, const Layout& l) {
   Rows r = {};
   r.in = in; r.lse = lse; r.head = (Head*)s;
   r.rank = (int*)(s + l.rank); r.tok = (int*)(s + l.tok); r.coef = (float*)(s + l.coef); r.lse2 = (float*)(s + l.lse2);
   r.h = (__nv_bfloat16*)(s + l.h); r.ld = l.ld;
+  r.to_base2 = (double)factor(in) / one_over_tau(in);
   r.vec = ((uintptr_t)in.hidden & 15) == 0 && in.ld_h % 8 == 0;
   return r;
 }
-// The tensor cores cut where float32 units round: a sum that takes n additions of 16 products ends n 2^-26 of itself nearer to 0, on average.  So it was measured, for sums of dense rows of
-// 256 to 8192 features and logits of 0.5 to 20 (with 0.75 and 1.25 times as much made up for, something is left in all of them); sums that need no rounding, of sparse rows say, come out that much too
-// large, which is what all others would lack.  (Losses of 2560 features against 64 bits: 1.5e-6 without it, 4.3e-7 with; float32 units 4.4e-7.)
-double one_over_tau(const saki_linear_in& in) { return (1.0 + (in.d + 15) / 16 * 0x1p-26) / (double)in.temperature; }
-
 Tiles tiles_of(const Rows& r, const Layout& l, long long wait_limit) {
   Tiles t = {};
   t.head = r.head; t.d = r.in.d; t.V = r.in.V; t.d_tiles = l.d_tiles; t.n_tiles = l.n_tiles;
   t.wait_limit = wait_limit > 0 ? wait_limit : WAIT_LIMIT_CYCLES;
-  t.c = (float)(INV_LN2 * one_over_tau(r.in));
+  t.c = factor(r.in);
   t.tok = r.tok; t.coef = r.coef; t.lse2 = r.lse2;
   return t;
 }
