@@ -379,7 +379,8 @@ SAKI_API int saki_distill_top(const saki_distill_in* in, const saki_distill_out*
  *     z = hidden weight^T / temperature,  pi = softmax(z),  L_i = -coef_i log pi_i(tok_i)
  * (coef, tok) is (1, teacher_top1) where corrected, else (advantage, target), as in saki_route_bwd_from_meta; without `corrected` it is
  * (advantage, target) everywhere, without `advantage` the coefficient is 1: plain cross entropy.  Products of bf16 on the tensor cores with
- * float32 sums; the logits are not rounded (and times 1 + d 2^-30: what the tensor cores' sums lack on average).  Rows that contribute nothing (mask 0: MASKED; rollout_status unusable: NOT_COMPUTED; an advantage
+ * float32 sums; the logits are not rounded (and times 1 + d 2^-30: what the tensor cores' sums of dense rows lack on average; sums that need no
+ * rounding come out larger by it, and saki_lmhead_lse has no such factor).  Rows that contribute nothing (mask 0: MASKED; rollout_status unusable: NOT_COMPUTED; an advantage
  * that is not finite: NONFINITE; a supervised token outside [0,V): BAD_ID) get loss 0, log-probability 0 and lse 0, take part in no product and cost
  * none.  A row whose log-sum-exp or log-probability is not finite is flagged NONFINITE, with loss 0 and lse NaN; TIMEOUT likewise, where a bounded wait ran out.
  * All pointers are DEVICE pointers.  Requirements: weight 16-byte aligned, ld_w and d multiples of 8; hidden rows may lie anywhere (16-byte aligned

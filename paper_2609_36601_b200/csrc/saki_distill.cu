@@ -11,8 +11,9 @@
 //                           memory that it fills with cp.async; the leading steps of a warp's segment stay there for both passes, the rest goes through a
 //                           ring (its second touch comes from L2); while a row's gradient is written the slots take the next row.  A warp knows from a word of bits
 //                           at which of its steps there are listed tokens, and looks for them only there.
-//   distill_general_kernel  float64, any layout, a block a row: for what the other cannot serve, and the rows that it cannot resolve (row list).
-// What bounds it: 4096 bf16 rows of 151936 with lists of 64, 544 us where the bytes take 380 (70 %; lists of 1: 500, of 128: 590): instructions (63 % of the issue slots are filled, 62 % of the
+//   distill_general_kernel  float64, any layout, a block a row: for what the other cannot serve, and the rows that it cannot resolve (row list).  Its exponentials cost 13 ms for 1000 float32 rows of
+//                           262144, the first length that it serves alone, where the other takes 0.51 for 262000
+// What bounds it: 4096 bf16 rows of 151936 with lists of 64, 540 us where the bytes take 380 (70 %; lists of 1: 495, of 128: 580; without the gradient 285, bytes 190): instructions (63 % of the issue slots are filled, 62 % of the
 // special-function pipe) and the two block barriers of a row, at which warps wait a fifth of their time.  float32 rows of 151936 run at 81 % of the copy rate.
 #include "saki_device.cuh"
 #include <algorithm>

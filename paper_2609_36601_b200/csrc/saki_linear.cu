@@ -17,7 +17,7 @@
 // pieces), the log-sum-exp float64 across tiles.
 //
 // What bounds it: the tensor cores at the clock that power leaves them.  4096 x 2560 x 151936, called alone: forward 2.14 ms = 1.49 PFLOP/s (89 % of the measured burst of a cuBLAS
-// product), backward 6.86 ms = 1.39 PFLOP/s over its three products; called in a row forward 2.4, both 9.0.  Few rows: 64 x 1024 x 32000 36 and 96 us, where the weights' bytes alone take 10 and 20: seven launches, and tiles
+// product), backward 6.86 ms = 1.39 PFLOP/s over its three products; called in a row forward 2.5, both 9.2.  Few rows: 64 x 1024 x 32000 111 us for both, where the weights' bytes alone take 10 and 20: seven launches, and tiles
 // of 256 rows of which 192 are padding.  Vocabulary rows that start off 128-byte lines (1096 features) cost 5 % of the forward.
 //
 // Persistent CTAs, one per SM:
@@ -738,8 +738,9 @@ cudaError_t launch_gather(const Rows& r, int sms, cudaStream_t st) {
 }
 
 // The tensor cores cut where float32 units round: a sum that takes n additions of 16 products ends n 2^-26 of itself nearer to 0, on average.  So it was measured, for sums of dense rows of
-// 256 to 8192 features and logits of 0.5 to 20 (with 0.75 and 1.25 times as much made up for, something is left in all of them); sums that need no rounding, of sparse rows say, come out that much too
-// large, which is what all others would lack.  (Losses of 2560 features against 64 bits: 1.5e-6 without it, 4.3e-7 with; float32 units 4.4e-7.)
+// 256 to 8192 features and logits of 0.5 to 20 (with 0.75 and 1.25 times as much made up for, something is left in all of them), and it holds to 8 % up to 65536 features.  What is cut off is between nothing (sums that
+// need no rounding, of sparse rows say: they come out that much too large) and some twice that or more (terms that are all of one sign): the factor is the middle of a fault that goes one way, not its bound.
+// (Losses of 2560 features against 64 bits, as a share: 1.2e-6 without it or with twice as much, 4.6e-7 with; float32 units 4.3e-7.)
 double one_over_tau(const saki_linear_in& in) { return (1.0 + (in.d + 15) / 16 * 0x1p-26) / (double)in.temperature; }
 float factor(const saki_linear_in& in) { return (float)(INV_LN2 * one_over_tau(in)); }      // of the products
 
